@@ -16,6 +16,7 @@
 
 #include "../../include/noble.h"
 #include "common.cuh"
+#include "host.cuh"
 #include "profile.cuh"
 #include "simt.cuh"
 #include "adamw.cuh"
@@ -29,6 +30,7 @@
 namespace noble {
 
 __device__ uint32_t g_device_status = 0;
+uint32_t *status_ptr() { return static_cast<uint32_t *>(symbol_address(g_device_status)); }
 
 // Library-owned scratch for noble_linear_bwd_noalloc (see include/noble.h).
 // Every GPU that loads this library holds it until the process exits.
@@ -36,96 +38,6 @@ constexpr size_t kNoallocScratchBytes = NOBLE_NOALLOC_SCRATCH_BYTES;
 static __device__ __align__(256) unsigned char g_noalloc_scratch[kNoallocScratchBytes];
 
 namespace {
-
-thread_local char g_last_error[512] = "";
-std::atomic<uint64_t> g_launches{0};
-
-noble_status fail(noble_status s, const char *fmt, ...)
-{
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
-    va_end(ap);
-    return s;
-}
-
-noble_status check_launch(const char *what)
-{
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return fail(NOBLE_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-    return NOBLE_OK;
-}
-
-// Kernels launched so far by the current entry-point call on this thread.
-thread_local int g_call_kernels = 0;
-
-// Launch through `f`, bracketed by profiling events when profiling is on.
-template <class F>
-noble_status run(cudaStream_t st, const KernelInfo &ki, F &&f)
-{
-    const int slot = Profiler::get().begin(st);
-    f();
-    Profiler::get().end(slot, st, ki);
-    ++g_call_kernels;
-    return check_launch(ki.name);
-}
-
-// Programmatic dependent launch: a kernel after the first of a call may start
-// while the previous one still runs, on the SMs it leaves free; it waits for it
-// (griddep_wait) before reading anything an earlier kernel of the call wrote,
-// and every such grid waits at least once, so its completion implies its
-// predecessors'.  The first kernel of a call, and the first after a memset, is
-// launched normally and sees all prior work in the stream -- except the CosNet
-// kernels, which wait for their predecessor grid in every thread before any
-// global read, so that their set-up may overlap the previous kernel whatever it
-// is, and let their own dependent start only after that.
-constexpr bool kProgrammaticLaunch = true;
-bool pdl_ok() { return kProgrammaticLaunch && g_call_kernels > 0; }
-
-// On clusters of `cluster` CTAs along x (1: none, or the kernel's own).
-template <class... KArgs, class... Args>
-void launch_cluster(void (*kern)(KArgs...), dim3 grid, int cluster, dim3 block, size_t smem, cudaStream_t st, bool pdl,
-                    Args &&...args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    int n = 0;
-    if (cluster > 1) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = cluster, attr[n].val.clusterDim.y = 1, attr[n++].val.clusterDim.z = 1;
-    }
-    if (pdl) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n++].val.programmaticStreamSerializationAllowed = 1;
-    }
-    cfg.attrs = attr;
-    cfg.numAttrs = n;
-    cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
-}
-template <class... KArgs, class... Args>
-void launch_maybe_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, bool pdl,
-                      Args &&...args)
-{
-    launch_cluster(kern, grid, 1, block, smem, st, pdl, std::forward<Args>(args)...);
-}
-
-// cudaMemsetAsync on the stream; the next kernel is then launched normally.
-cudaError_t memset_async(void *p, int v, size_t n, cudaStream_t st)
-{
-    g_call_kernels = 0;
-    return cudaMemsetAsync(p, v, n, st);
-}
-
-#define NOBLE_TRY(expr)                              \
-    do {                                             \
-        noble_status _s = (expr);                    \
-        if (_s != NOBLE_OK) return _s;               \
-    } while (0)
 
 constexpr uint32_t kFlagSimtOnly = NOBLE_FLAG_SIMT_ONLY;
 constexpr uint32_t kFlagInference = NOBLE_FLAG_INFERENCE;
@@ -196,34 +108,6 @@ noble_status validate_desc(const noble_linear_desc *d)
         return fail(NOBLE_ERR_INVALID_ARG, "NOBLE_FLAG_SIGMA_COS1 and NOBLE_FLAG_SIGMA_IDENTITY together");
     if ((d->flags & kFlagActMask) && (d->flags & kFlagSigmaIdentity))
         return fail(NOBLE_ERR_INVALID_ARG, "NOBLE_FLAG_ACT_* and NOBLE_FLAG_SIGMA_IDENTITY together");
-    return NOBLE_OK;
-}
-
-noble_status check_ptr(const void *p, const char *name, bool nullable)
-{
-    if (!p) return nullable ? NOBLE_OK : fail(NOBLE_ERR_INVALID_ARG, "%s is NULL", name);
-    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(NOBLE_ERR_MISALIGNED, "%s is not 16-byte aligned", name);
-    return NOBLE_OK;
-}
-
-noble_status check_device()
-{
-    static int cached[64];  // 0 unknown, 1 ok, 2 bad
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) {
-        cudaGetLastError();
-        return fail(NOBLE_ERR_NO_DEVICE, "no current CUDA device");
-    }
-    if (dev < 64 && cached[dev] == 1) return NOBLE_OK;
-    int major = 0, minor = 0;
-    cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-    cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
-    cudaGetLastError();
-    if (major != 10 || minor != 3) {
-        if (dev < 64) cached[dev] = 2;
-        return fail(NOBLE_ERR_NO_DEVICE, "device %d is sm_%d%d; this library is built for sm_103a", dev, major, minor);
-    }
-    if (dev < 64) cached[dev] = 1;
     return NOBLE_OK;
 }
 
@@ -541,20 +425,6 @@ __global__ void __launch_bounds__(256) sum_split_kernel(const __grid_constant__ 
     sum_few(J, blockIdx.x, gridDim.x);
 }
 
-int num_sms()
-{
-    static int cache[64];
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev >= 0 && dev < 64 && cache[dev]) return cache[dev];
-    int n = 0;
-    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    cudaGetLastError();
-    if (n <= 0) n = 1;
-    if (dev >= 0 && dev < 64) cache[dev] = n;
-    return n;
-}
-
 // Many partials of short outputs.
 noble_status sum_parts(cudaStream_t st, const SplitJobs &J)
 {
@@ -852,26 +722,6 @@ noble_status bwd_simt(const noble_linear_desc *d, const TIn *dy, const TIn *x, c
 // ------------------------------------------------------------ tensor-core path
 using bf16 = __nv_bfloat16;
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static EncodeTiledFn fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) !=
-                cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<EncodeTiledFn>(p);
-    }();
-    return fn;
-}
-
 // 2-D TMA map over a row-major bf16 matrix [rows][cols]: box of 64 columns
 // (128 bytes) by box_rows rows, 128-byte swizzle, zero fill out of bounds.
 // `pitch` is the row pitch in elements (0: cols, a contiguous matrix).
@@ -964,52 +814,6 @@ noble_status make_rows_map(CUtensorMap *m, void *p, bool fp32, int64_t T, int64_
     return NOBLE_OK;
 }
 
-// The current CUDA context (NULL if none or the driver call is unavailable).
-typedef CUresult (*CtxGetCurrentFn)(CUcontext *);
-CUcontext current_context()
-{
-    static CtxGetCurrentFn fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPointByVersion("cuCtxGetCurrent", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return reinterpret_cast<CtxGetCurrentFn>(p);
-    }();
-    CUcontext c = nullptr;
-    if (!fn || fn(&c) != CUDA_SUCCESS) return nullptr;
-    return c;
-}
-
-// Device address of a __device__ variable in the current context.  The
-// host-side name of a __device__ variable is only a stand-in, so the address
-// is looked up with the device current; it is cached per context (a new
-// context after a device reset loads the module at another address).
-template <class T>
-void *symbol_address(const T &symbol)
-{
-    static std::mutex mu;
-    static std::vector<std::pair<CUcontext, void *>> cache;
-    const CUcontext ctx = current_context();
-    std::lock_guard<std::mutex> g(mu);
-    if (ctx)
-        for (auto &e : cache)
-            if (e.first == ctx) return e.second;
-    void *p = nullptr;
-    if (cudaGetSymbolAddress(&p, symbol) != cudaSuccess || !p) {
-        cudaGetLastError();
-        return nullptr;
-    }
-    // the lookup may have created the primary context: key on it
-    const CUcontext now = ctx ? ctx : current_context();
-    if (now) cache.emplace_back(now, p);
-    return p;
-}
-
-// Device address of this device's status word.
-uint32_t *status_ptr() { return static_cast<uint32_t *>(symbol_address(g_device_status)); }
 
 // One K segment of a tensor-core GEMM; A and B are row-major bf16 matrices
 // ([M][K] / [N][K] when K-major, [K][M] / [K][N] when MN-major).
