@@ -373,6 +373,203 @@ noble_status noble_linear_bwd_noalloc(const noble_linear_desc *desc,
                                       float *dW_up, noble_stream stream);
 
 /*
+ * Attention between a QKV and an output projection
+ * ------------------------------------------------
+ * The paper's models are transformers: what stands between two of their NOBLE
+ * layers is attention over the heads of the QKV projection's output, with
+ * rotary positions (Section 4.1.1).  In training noble_rope_fwd and
+ * noble_attn_fwd run between the two projections and their _bwd counterparts
+ * on the way back; in generation noble_kv_append and noble_attn_paged do.
+ * The conventions above hold, except that tensors of heads have strides:
+ */
+typedef struct {
+    void *p;           /* first feature of head 0 of token 0                   */
+    int64_t row, head; /* elements from one token / one head to the next       */
+} noble_heads;
+/* Token t of head h is the d contiguous elements at p + t * row + h * head, in
+ * the descriptor's dtype.  p and both strides are multiples of 16 bytes; a
+ * stride may be 0 or negative for tensors that are only read.  The elements of
+ * a tensor that is written must not overlap each other.  p may be NULL when
+ * the tensor has no elements. */
+
+/*
+ * Rotary positions with per-head norms.  Each head x of the queries and keys is
+ * first normalised by its root mean square (NOBLE_ROPE_NORM), then its first
+ * `rot` features are rotated in pairs by the angles of its token's position:
+ *     n = gain * x / sqrt(mean(x^2) + eps)          over all d features
+ *     y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin   for the pairs (a, b)
+ * Pair i is the features (i, i + rot/2), or (2i, 2i + 1) with
+ * NOBLE_ROPE_INTERLEAVED.  Features from `rot` on keep n.  Row p of `table`
+ * holds position p's rot/2 cosines, then its rot/2 sines (noble_rope_table, or
+ * the caller's own).
+ */
+#define NOBLE_ROPE_INTERLEAVED 1u
+#define NOBLE_ROPE_NORM 2u
+typedef struct {
+    int64_t T;         /* tokens                                               */
+    int64_t n_q, n_kv; /* heads of the queries, and of the keys (and values)   */
+    int64_t d;         /* head size: a multiple of 8, 8 to 256                 */
+    int64_t rot;       /* leading features that rotate: even, 0 to d           */
+    int64_t positions; /* rows of the table                                    */
+    float eps;         /* >= 0                                                 */
+    int32_t dtype;     /* noble_dtype of the heads                             */
+    uint32_t flags;    /* NOBLE_ROPE_* bits                                    */
+} noble_rope_desc;
+
+/*
+ * Fills table[positions][rot] (fp32, device) for position p and pair i with
+ * amplitude * cos / sin of p * f_i, f_i = base^(-2i/rot), each angle computed
+ * in fp64.  For contexts longer than a model was trained on, frequencies are
+ * scaled down by parts: with turns t_i = original * f_i / (2 pi) over the
+ * original context, f_i is kept where t_i >= high_turns, divided by `factor`
+ * where t_i <= low_turns, and in between
+ *     f_i (g + (1 - g) / factor),  g = (t_i - low_turns) / (high_turns - low_turns).
+ * factor 1 keeps every frequency; low_turns = high_turns = infinity divides
+ * all of them.  `scaling` may be NULL: base 10000, factor 1, amplitude 1.
+ */
+typedef struct {
+    double base;       /* > 0                                                  */
+    double factor;     /* > 0                                                  */
+    double original;   /* positions of the original context, > 0               */
+    double low_turns, high_turns; /* low_turns <= high_turns                   */
+    double amplitude;  /* finite                                               */
+} noble_rope_scaling;
+noble_status noble_rope_table(int64_t positions, int64_t rot, const noble_rope_scaling *scaling,
+                              float *table, noble_stream stream);
+
+/*
+ * Forward: q_out, k_out from q, k (which they may be, with the same strides).
+ *   pos     [T]: each token's position.  One outside [0, positions) is a
+ *           caller's error: its outputs are written as 0 and
+ *           noble_get_device_status() reports it (NOBLE_ERR_CUDA).
+ *   gain_q, gain_k [d] fp32 (NULL: all ones); not read without NOBLE_ROPE_NORM.
+ */
+noble_status noble_rope_fwd(const noble_rope_desc *desc, const noble_heads *q, const noble_heads *k,
+                            const int32_t *pos, const float *table, const float *gain_q, const float *gain_k,
+                            const noble_heads *q_out, const noble_heads *k_out, noble_stream stream);
+
+/*
+ * Backward: with w the rotation of dy by the negative angle and xn = x / rms,
+ *     dgain = sum over tokens and heads of w * xn
+ *     dx    = (gain * w - xn * mean(gain * w * xn)) / rms
+ * (dx = w without NOBLE_ROPE_NORM).  q and k are the forward's inputs (NULL
+ * descriptors allowed without NOBLE_ROPE_NORM); dq_in, dk_in may be dq, dk with
+ * the same strides.  dgain_q, dgain_k [d] fp32, NULL to skip; they are added up
+ * in a fixed order, and not written without NOBLE_ROPE_NORM.
+ */
+size_t noble_rope_bwd_workspace_bytes(const noble_rope_desc *desc);
+noble_status noble_rope_bwd(const noble_rope_desc *desc, const noble_heads *dq, const noble_heads *dk,
+                            const noble_heads *q, const noble_heads *k, const int32_t *pos, const float *table,
+                            const float *gain_q, const float *gain_k, const noble_heads *dq_in,
+                            const noble_heads *dk_in, float *dgain_q, float *dgain_k, void *workspace,
+                            size_t workspace_bytes, noble_stream stream);
+
+/*
+ * A cache of keys and values in pages.  Token `t` of page `n` and head `h` is
+ * the d contiguous elements at n * page + t * row + h * head, in k and in v;
+ * all three strides are multiples of 16 bytes, and 64-bit throughout.
+ */
+typedef struct {
+    void *k, *v;
+    int64_t pages, page_size; /* page_size: tokens of a page, 1 to 2^20        */
+    int64_t page, row, head;  /* strides in elements                           */
+} noble_kv_cache;
+
+/*
+ * noble_rope_fwd on new tokens, with the keys, and the values as they are,
+ * written into the cache: token t goes to slots[t] = page * page_size + place.
+ * A negative slot is not stored (a padding token).  A slot beyond the cache is
+ * a caller's error: it is not stored, and noble_get_device_status() reports
+ * it.  Two tokens of a call must not share a slot.
+ */
+noble_status noble_kv_append(const noble_rope_desc *desc, const noble_heads *q, const noble_heads *k,
+                             const noble_heads *v, const int32_t *pos, const int64_t *slots, const float *table,
+                             const float *gain_q, const float *gain_k, const noble_heads *q_out,
+                             const noble_kv_cache *cache, noble_stream stream);
+
+/*
+ * Attention over packed documents.  The T tokens are documents one behind the
+ * other, document n being the tokens doc_start[n] <= t < doc_start[n + 1].
+ * Query i of head h sees the keys j of its document with
+ *     j <= i, or j < doc_start + prefix[n]    (NOBLE_ATTN_CAUSAL; prefix optional)
+ *     i - j < window, and without NOBLE_ATTN_CAUSAL j - i < window  (window > 0)
+ * of head h / (n_q / n_kv), and
+ *     s_ij = scale q_i.k_j;  s_ij = softcap tanh(s_ij / softcap)    (softcap > 0)
+ *     s_ij = s_ij - slope[h] |i - j|                                (slope optional)
+ *     o_i  = sum_j exp(s_ij - lse_i) v_j,  lse_i = log sum_j exp(s_ij).
+ * A query that sees nothing (a token of no document) has o = 0, lse = -inf and
+ * takes no part in any gradient.
+ * doc_start [n_docs + 1] must ascend within [0, T]; if it does not, results are
+ * undefined, but no access leaves the tensors.
+ * What a query does not see does not change its results, whatever values are
+ * there (infinities and NaN too).
+ *
+ * bf16 runs on the tensor cores, with fp32 scores, softmax and sums; the
+ * probabilities and the scores' gradients are rounded to bf16 for their
+ * products.  fp32 operands run in fp32 FMA, as does bf16 with
+ * NOBLE_ATTN_SIMT_ONLY.  Results do not depend on the order in which a GPU
+ * runs the blocks: repeated calls agree bit by bit.
+ */
+#define NOBLE_ATTN_CAUSAL 1u
+#define NOBLE_ATTN_SIMT_ONLY 2u
+typedef struct {
+    int64_t T;         /* tokens, up to 2^24                                   */
+    int64_t n_docs;    /* documents, up to 2^24                                */
+    int64_t n_q, n_kv; /* heads: n_q a multiple of n_kv                        */
+    int64_t d;         /* head size: a multiple of 8, 8 to 128                 */
+    int64_t window;    /* 0: none                                              */
+    float scale;       /* of the products, usually 1 / sqrt(d)                 */
+    float softcap;     /* 0: none                                              */
+    int32_t dtype;     /* noble_dtype of q, k, v, o and their gradients        */
+    uint32_t flags;    /* NOBLE_ATTN_* bits                                    */
+} noble_attn_desc;
+
+/* lse: fp32 [n_q][T]; prefix [n_docs] and slope [n_q] may be NULL. */
+noble_status noble_attn_fwd(const noble_attn_desc *desc, const noble_heads *q, const noble_heads *k,
+                            const noble_heads *v, const int32_t *doc_start, const int32_t *prefix,
+                            const float *slope, const noble_heads *o, float *lse, noble_stream stream);
+
+/*
+ * Backward: dq, dk, dv of L = sum(o * do), from the forward's inputs and its o
+ * and lse.  The gradients of a key head are summed over the query heads that
+ * share it.  workspace as for noble_linear_bwd.
+ */
+size_t noble_attn_bwd_workspace_bytes(const noble_attn_desc *desc);
+noble_status noble_attn_bwd(const noble_attn_desc *desc, const noble_heads *d_o, const noble_heads *q,
+                            const noble_heads *k, const noble_heads *v, const int32_t *doc_start,
+                            const int32_t *prefix, const float *slope, const noble_heads *o, const float *lse,
+                            const noble_heads *dq, const noble_heads *dk, const noble_heads *dv, void *workspace,
+                            size_t workspace_bytes, noble_stream stream);
+
+/*
+ * Attention of the newest q_len tokens of each sequence over a cache.  Token t
+ * of sequence n (row n * q_len + t of q and o) is at position kv_len[n] - q_len
+ * + t and sees the keys of the positions up to its own, with `window`, scale,
+ * softcap and slope as in noble_attn_fwd.  Position j of sequence n lies in
+ * page page_table[n][j / page_size] of the cache, at place j % page_size.  A
+ * token at a negative position sees nothing: o = 0, lse = -inf.
+ * Only what is seen is read from the cache.  A page number outside the cache,
+ * or a kv_len beyond max_pages * page_size or max_len, is a caller's error: the
+ * keys concerned are left out, and noble_get_device_status() reports it.
+ */
+typedef struct {
+    int64_t n_seq;     /* sequences, up to 65535                               */
+    int64_t q_len;     /* new tokens of each, 1 to 64                          */
+    int64_t n_q, n_kv, d; /* as in noble_attn_desc                             */
+    int64_t max_pages; /* entries of a row of page_table                       */
+    int64_t max_len;   /* no kv_len is longer; it sets how the work is split   */
+    int64_t window;
+    float scale, softcap;
+    int32_t dtype;
+    uint32_t flags;    /* 0                                                    */
+} noble_paged_desc;
+size_t noble_attn_paged_workspace_bytes(const noble_paged_desc *desc);
+noble_status noble_attn_paged(const noble_paged_desc *desc, const noble_heads *q, const noble_kv_cache *cache,
+                              const int32_t *page_table, const int32_t *kv_len, const float *slope,
+                              const noble_heads *o, float *lse /* [n_seq * q_len][n_q], NULL to skip */,
+                              void *workspace, size_t workspace_bytes, noble_stream stream);
+
+/*
  * Synchronises `stream`, then reads and clears the device status word of the
  * current device.  NOBLE_ERR_TIMEOUT if any kernel gave up a bounded wait
  * since the last call, NOBLE_ERR_CUDA if the stream reported an error or a

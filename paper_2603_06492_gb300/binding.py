@@ -90,6 +90,34 @@ class Cos3Grads(ctypes.Structure):
     _fields_ = [("dM2", ctypes.c_void_p), ("domega3", ctypes.c_void_p), ("dphi3", ctypes.c_void_p)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "n_q", "n_kv", "d", "rot", "positions")] + [
+        ("eps", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("base", "factor", "original", "low_turns", "high_turns", "amplitude")]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("pages", "page_size", "page", "row", "head")]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "n_docs", "n_q", "n_kv", "d", "window")] + [
+        ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_seq", "q_len", "n_q", "n_kv", "d", "max_pages", "max_len", "window")] + [
+        ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
 def make_desc(T, d_in, d_out, r, dtype, flags=0) -> Desc:
     if isinstance(dtype, str):
         dtype = {"bf16": NOBLE_BF16, "fp32": NOBLE_FP32}[dtype]
@@ -167,6 +195,22 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.noble_linear_lr_multipliers.restype = ctypes.c_int
         lib.noble_linear_grad_bucket.argtypes = [D, ctypes.POINTER(GradBucket)]
         lib.noble_linear_grad_bucket.restype = ctypes.c_int
+        # the attention operators (attention.py); noble_heads and cache arguments are pointers
+        RD, AD, PD = (ctypes.POINTER(t) for t in (RopeDesc, AttnDesc, PagedDesc))
+        lib.noble_rope_table.argtypes = [i64, i64, ctypes.POINTER(RopeScaling), P, P]
+        lib.noble_rope_fwd.argtypes = [RD] + [P] * 9
+        lib.noble_rope_bwd_workspace_bytes.argtypes = [RD]
+        lib.noble_rope_bwd.argtypes = [RD] + [P] * 13 + [S, P]
+        lib.noble_kv_append.argtypes = [RD] + [P] * 11
+        lib.noble_attn_fwd.argtypes = [AD] + [P] * 9
+        lib.noble_attn_bwd_workspace_bytes.argtypes = [AD]
+        lib.noble_attn_bwd.argtypes = [AD] + [P] * 13 + [S, P]
+        lib.noble_attn_paged_workspace_bytes.argtypes = [PD]
+        lib.noble_attn_paged.argtypes = [PD] + [P] * 8 + [S, P]
+        for n in ("rope_table", "rope_fwd", "rope_bwd", "kv_append", "attn_fwd", "attn_bwd", "attn_paged"):
+            getattr(lib, "noble_" + n).restype = ctypes.c_int
+        for n in ("rope_bwd", "attn_bwd", "attn_paged"):
+            getattr(lib, "noble_" + n + "_workspace_bytes").restype = S
         _lib = lib
         return lib
 

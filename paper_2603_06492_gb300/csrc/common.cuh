@@ -12,6 +12,7 @@ enum : uint32_t {
     kStatusTimeout = 1u,   // a bounded mbarrier / flag wait gave up
     kStatusBadShape = 2u,  // a kernel saw a shape it cannot handle and skipped work
     kStatusCounter = 4u,   // a grouped launch found no tile counter of its call and skipped tiles
+    kStatusBadIndex = 8u,  // a position, slot, page or length beyond its table: left out
 };
 
 // Kernels that can give up a bounded wait receive a pointer to the
