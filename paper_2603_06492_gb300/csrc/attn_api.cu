@@ -4,11 +4,13 @@
 // Host side only: argument checks, workspaces and kernel dispatch.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "host.cuh"
 #include "attn_mask.cuh"
 #include "attn_paged.cuh"
 #include "attn_simt.cuh"
+#include "attn_tc_fwd.cuh"
 #include "rope.cuh"
 
 namespace noble {
@@ -254,6 +256,78 @@ noble_status attn_bwd_simt(const attn::RowArgs<T> &a, float *delta, const int2 *
                   [&] { s::dq_kernel<DP, T><<<dim3(blocks, (unsigned)a.n_q), s::kThreads, smem, st>>>(a, delta); }));
     return run(st, {"attn_dkv_simt", kBoundAlu, 0.0, 0.0},
                [&] { s::dkv_kernel<DP, T><<<dim3(blocks, (unsigned)a.n_kv), s::kThreads, smem, st>>>(a, ranges); });
+}
+
+// TMA map of a bf16 tensor of heads: dimensions (inner first) features, head, token; boxes
+// of 64 features by 128 tokens of one head, 128-byte swizzle, zeros out of bounds.
+bool tma_strides(const noble_heads *x, int64_t T, int64_t n)
+{
+    const int64_t most = int64_t(1) << 38;
+    return (n == 1 || (x->head > 0 && x->head < most)) && (T == 1 || (x->row > 0 && x->row < most));
+}
+noble_status make_heads_map(CUtensorMap *m, const noble_heads *x, int64_t T, int64_t n, int64_t d)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
+    // a stride that nothing is reached by may have any value
+    const cuuint64_t head = (cuuint64_t)(n == 1 ? d : x->head) * 2, row = (cuuint64_t)(T == 1 ? n * d : x->row) * 2;
+    cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)n, (cuuint64_t)T};
+    cuuint64_t strides[2] = {head, row};
+    cuuint32_t box[3] = {64, 1, attn::tc::kRows};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, x->p, dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d): %lld tokens, %lld heads of %lld", (int)r, (long long)T,
+                    (long long)n, (long long)d);
+    return NOBLE_OK;
+}
+
+// Score functions beyond a positive scale take the kernels' general form.
+bool general_scores(const attn::Score &s) { return s.softcap > 0.f || s.slope || !(s.scale > 0.f); }
+
+// The register split of a kernel's warpgroups draws on what it was launched with.
+template <auto KERN>
+bool registers_at_least(int n)
+{
+    static const bool ok = [n] {
+        cudaFuncAttributes a{};
+        return cudaFuncGetAttributes(&a, KERN) == cudaSuccess && a.numRegs >= n;
+    }();
+    return ok;
+}
+
+template <int DP, bool GENERAL>
+noble_status attn_fwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[3], cudaStream_t st)
+{
+    namespace t = attn::tc;
+    using F = t::Fwd<DP>;
+    constexpr auto kern = &t::fwd_kernel<DP, GENERAL>;
+    if (!registers_at_least<kern>(168)) return fail(NOBLE_ERR_CUDA, "attn_fwd: registers");
+    NOBLE_TRY((allow<kern>(F::kDynamic)));
+    t::FwdArgs f{a, (int)ceil_div(a.mask.T, 256), status_ptr()};
+    if (!f.status) return fail(NOBLE_ERR_CUDA, "status word address");
+    if ((int64_t)f.tiles * a.n_q > INT32_MAX) return fail(NOBLE_ERR_UNSUPPORTED, "%d tokens of %d heads", a.mask.T, a.n_q);
+    return run(st, {"attn_fwd", kBoundTensor, 0.0, 0.0},
+               [&] { kern<<<f.tiles * a.n_q, F::kThreads, F::kDynamic, st>>>(maps[0], maps[1], maps[2], f); });
+}
+noble_status attn_fwd_tc(const noble_attn_desc *d, const attn::RowArgs<bf> &a, const noble_heads *q, const noble_heads *k,
+                         const noble_heads *v, cudaStream_t st)
+{
+    CUtensorMap maps[3];
+    NOBLE_TRY(make_heads_map(&maps[0], q, d->T, d->n_q, d->d));
+    NOBLE_TRY(make_heads_map(&maps[1], k, d->T, d->n_kv, d->d));
+    NOBLE_TRY(make_heads_map(&maps[2], v, d->T, d->n_kv, d->d));
+    if (general_scores(a.score)) return d->d <= 64 ? attn_fwd_tc<64, true>(a, maps, st) : attn_fwd_tc<128, true>(a, maps, st);
+    return d->d <= 64 ? attn_fwd_tc<64, false>(a, maps, st) : attn_fwd_tc<128, false>(a, maps, st);
+}
+// bf16 runs on the tensor cores unless asked otherwise or a stride is none that TMA takes.
+bool attn_use_tc(const noble_attn_desc *d, std::initializer_list<std::pair<const noble_heads *, int64_t>> xs)
+{
+    bool ok = d->dtype == NOBLE_BF16 && !(d->flags & NOBLE_ATTN_SIMT_ONLY);
+    for (auto &x : xs) ok = ok && tma_strides(x.first, d->T, x.second);
+    return ok;
 }
 
 template <typename T>
@@ -511,6 +585,9 @@ noble_status noble_attn_fwd(const noble_attn_desc *desc, const noble_heads *q, c
         using T = decltype(zero);
         attn::RowArgs<T> a = attn_args<T>(desc, q, k, v, doc_start, prefix, slope);
         a.out = heads<T>(o), a.lse = lse;
+        if constexpr (std::is_same_v<T, bf>)
+            if (attn_use_tc(desc, {{q, desc->n_q}, {k, desc->n_kv}, {v, desc->n_kv}}))
+                return attn_fwd_tc(desc, a, q, k, v, (cudaStream_t)stream);
         return attn_fwd<T>(a, (cudaStream_t)stream);
     };
     return desc->dtype == NOBLE_BF16 ? go(bf{}) : go(float{});

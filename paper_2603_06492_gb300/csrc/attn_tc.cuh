@@ -1,0 +1,167 @@
+// Attention over documents on the tensor cores: what forward and backward share.
+//
+// Tiles are 128 tokens by 64 features of bf16 with the 128-byte swizzle (16 KB, one
+// TMA box), so the same tile serves as a K-major operand (features contracted) and as
+// an MN-major one (tokens contracted).  Heads of 65 to 128 features take two tiles;
+// TMA fills features past d and tokens past T with zeros.
+//
+// TMEM lanes are rows of a score block: a thread of the four warps of a warpgroup owns
+// one row, so that a softmax needs no exchange between threads.
+#pragma once
+
+#include "attn_mask.cuh"
+#include "sm100_ptx.cuh"
+
+namespace noble {
+namespace attn {
+namespace tc {
+
+constexpr int kRows = 128;                  // rows of a score block, keys of a tile
+constexpr uint32_t kChunk = 128 * 64 * 2;   // bytes of a tile of 64 features
+constexpr int kDocsInSmem = 1024;           // document starts kept in shared memory
+
+// ---------------------------------------------------------------- PTX
+// 3-D tiled load (features, head, token); c0 a multiple of 8 elements.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
+
+// D[tmem] (+)= A[tmem] B[smem]: A holds two bf16 per 32-bit column, K ascending.
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// 32 columns of this thread's TMEM lane; valid only after tmem_wait_ld.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+// Waits for this thread's TMEM loads.  The values loaded pass through pin32 after
+// it, so that no use of them is moved before the wait.
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void pin32(uint32_t *r)
+{
+    asm volatile(""
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+    asm volatile(""
+                 : "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                   "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <int N>
+__device__ __forceinline__ void setmaxnreg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void setmaxnreg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// ---------------------------------------------------------------- work handed out by the launch
+// A block that has finished its piece of work takes over that of a block of the grid
+// that has not started (cluster launch control), so that blocks set up once and
+// pieces of unequal size balance.  One warp asks, ahead of need; everyone reads.
+__device__ __forceinline__ void ask_next(uint32_t slot, uint32_t bar)
+{
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(slot),
+                 "r"(bar)
+                 : "memory");
+}
+// The block's index of the answer in `slot`, or -1 if there was none left.
+__device__ __forceinline__ int read_next(uint32_t slot)
+{
+    int x;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 h;\n\t.reg .b32 y, z, w;\n\t"
+        "ld.shared.b128 h, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+        "mov.b32 %0, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, h;\n\t}\n"
+        : "=r"(x)
+        : "r"(slot)
+        : "memory");
+    return x;
+}
+
+// K-major operand of a token tile: features 16 kk .. of its rows.
+__device__ __forceinline__ uint64_t desc_k(uint32_t tile, int kk)
+{
+    return ptx::smem_desc_sw128(tile + (kk >> 2) * kChunk + (kk & 3) * 32, 16, 1024);
+}
+// MN-major operand: tokens 16 kk .. contracted.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t tile, int kk) { return ptx::smem_desc_sw128(tile + kk * 2048, kChunk, 1024); }
+
+// The document starts (and prefixes) in shared memory where they fit, since every
+// piece of work searches them; call with all threads, before a __syncthreads.
+__device__ __forceinline__ Mask mask_in_smem(const Mask &m, int32_t *sm)
+{
+    Mask r = m;
+    if (m.n_docs >= kDocsInSmem) return r;
+    for (int i = threadIdx.x; i <= m.n_docs; i += blockDim.x) sm[i] = m.doc_start[i];
+    r.doc_start = sm;
+    if (m.prefix) {
+        for (int i = threadIdx.x; i < m.n_docs; i += blockDim.x) sm[kDocsInSmem + i] = m.prefix[i];
+        r.prefix = sm + kDocsInSmem;
+    }
+    return r;
+}
+
+}  // namespace tc
+}  // namespace attn
+}  // namespace noble
