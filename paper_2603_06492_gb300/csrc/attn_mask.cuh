@@ -140,12 +140,13 @@ __device__ __forceinline__ void row_load(float (&x)[4], const T *p, int d, int l
 #pragma unroll
     for (int u = 0; u < 4; ++u) x[u] = lane + 32 * u < d ? load_f(p + lane + 32 * u) : 0.f;
 }
+// features [f0, f1) of a row
 template <typename T>
-__device__ __forceinline__ void row_store(T *p, const float (&x)[4], int d, int lane)
+__device__ __forceinline__ void row_store(T *p, const float (&x)[4], int f1, int lane, int f0 = 0)
 {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-        if (lane + 32 * u < d) store_f(p + lane + 32 * u, x[u]);
+        if (lane + 32 * u >= f0 && lane + 32 * u < f1) store_f(p + lane + 32 * u, x[u]);
 }
 __device__ __forceinline__ float row_dot(const float (&a)[4], const float (&b)[4])
 {
@@ -201,12 +202,13 @@ __device__ __forceinline__ void row_pair(const RowArgs<T> &a, const float (&q)[4
     ds = p * (row_dot(d_o, v) - delta) * g * a.score.scale;
 }
 
+// features [f0, f1) of dq
 template <typename T>
-__device__ __noinline__ void row_dq(const RowArgs<T> &a, int i, int h, int lane)
+__device__ __noinline__ void row_dq(const RowArgs<T> &a, int i, int h, int lane, float delta, int f0, int f1)
 {
     const Range r = visible(a.mask, i);
     const int g = h / (a.n_q / a.n_kv);
-    const float lse = a.lse[(int64_t)h * a.mask.T + i], delta = a.delta[(int64_t)h * a.mask.T + i];
+    const float lse = a.lse[(int64_t)h * a.mask.T + i];
     float q[4], d_o[4], acc[4] = {};
     row_load(q, a.q.at(i, h), a.d, lane);
     row_load(d_o, a.d_o.at(i, h), a.d, lane);
@@ -218,7 +220,7 @@ __device__ __noinline__ void row_dq(const RowArgs<T> &a, int i, int h, int lane)
 #pragma unroll
         for (int u = 0; u < 4; ++u) acc[u] += ds * k[u];
     }
-    row_store(a.dq.at(i, h), acc, a.d, lane);
+    row_store(a.dq.at(i, h), acc, min(f1, a.d), lane, f0);
 }
 
 // First query whose range ends after key j, and first whose range starts after it:
@@ -244,7 +246,7 @@ __device__ __forceinline__ Range seen_by(const Mask &m, int j)
 }
 
 template <typename T>
-__device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane)
+__device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane, bool to_dv, bool to_dk)
 {
     const Range r = seen_by(a.mask, j);
     const int group = a.n_q / a.n_kv;
@@ -262,8 +264,8 @@ __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane
 #pragma unroll
             for (int u = 0; u < 4; ++u) dk[u] += ds * q[u], dv[u] += p * d_o[u];
         }
-    row_store(a.dk.at(j, g), dk, a.d, lane);
-    row_store(a.dv.at(j, g), dv, a.d, lane);
+    if (to_dk) row_store(a.dk.at(j, g), dk, a.d, lane);
+    if (to_dv) row_store(a.dv.at(j, g), dv, a.d, lane);
 }
 
 }  // namespace attn

@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ R
     }
     __syncthreads();
     for (int r = tid / 32; r < kB; r += kThreads / 32)
-        if (redo[r]) row_dkv(a, j0 + r, g, tid % 32);
+        if (redo[r]) row_dkv(a, j0 + r, g, tid % 32, true, true);
 }
 
 // grid as fwd_kernel's.  Where one block of keys is all that the queries see, delta is
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Ro
     }
     __syncthreads();
     for (int r = tid / 32; r < kB; r += kThreads / 32)
-        if (redo[r]) row_dq(a, i0 + r, h, tid % 32);
+        if (redo[r]) row_dq(a, i0 + r, h, tid % 32, delta_out[(int64_t)h * T_ + i0 + r], 0, a.d);
 }
 
 }  // namespace simt

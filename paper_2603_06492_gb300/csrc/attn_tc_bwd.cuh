@@ -1,0 +1,855 @@
+// Backward attention over documents on the tensor cores: two kernels, so that each sum
+// has one block and a fixed order, without atomics or partial sums in memory.  Both form the
+// scores again (seven products of the size of one score block's, where sharing them
+// would take five).
+//
+// dq_kernel, 128 queries of a head over the key tiles that they see:
+//     S = Q K^T, dP = dO V^T;  dS = P (dP - delta);  dQ += dS K
+// dkv_kernel, 128 keys of a key head over the query tiles that see them, of every query
+// head that shares it (rows of the score block are keys):
+//     S = K Q^T, dP = V dO^T;  dV += P dO,  dK += dS Q
+// P and dS are written as bf16 over S and dP in TMEM and read from there as operands.
+// Two warpgroups of 128 rows take half of the columns each.
+//
+// The tensor pipe is never behind one chain of dependent steps.  dq: the next S goes to a
+// second buffer, and the next dP runs as soon as this one is in registers.  dkv:
+// dV and the next S run while dS is formed, dK and the next dP while the next P is.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "attn_tc.cuh"
+
+namespace noble {
+namespace attn {
+namespace tc {
+
+struct BwdArgs {
+    RowArgs<__nv_bfloat16> a;
+    float *delta;        // [n_q][T]
+    const int2 *ranges;  // [T]
+    int tiles;           // of 128 tokens
+    uint32_t *status;
+};
+
+template <int DP>
+struct Bwd {
+    static constexpr int kThreads = 384;
+    static constexpr int kStages = DP == 64 ? 4 : 2;
+    static constexpr uint32_t kTile = kChunk * (DP / 64);
+    // two resident tiles, two streams of kStages, document starts, vectors by stage
+    static constexpr uint32_t kR0 = 0, kR1 = kTile, kX = 2 * kTile, kY = kX + kStages * kTile;
+    static constexpr uint32_t kDocs = kY + kStages * kTile;
+    static constexpr uint32_t kVec = kDocs + 2 * kDocsInSmem * 4;  // lse, delta [128], ranges [128], all visible
+    static constexpr uint32_t kVecBytes = 128 * 16 + 16;
+    static constexpr uint32_t kBars = kVec + kStages * kVecBytes;
+    static constexpr int kNumBars = 6 * kStages + 16;
+    static constexpr uint32_t kWork = kBars + 8 * kNumBars;
+    static constexpr uint32_t kBytes = kWork + 32 + 16;
+    static constexpr uint32_t kDynamic = kBytes + 1024;
+};
+
+// Queries that see any key of [j0, j1): none if lo >= hi.
+__device__ __forceinline__ Range queries_of(const Mask &m, int j0, int j1)
+{
+    const int end = docs_end(m);
+    j1 = min(j1, end);
+    if (j0 >= j1) return {0, 0};
+    auto doc = [&](int j) {  // its document, as one start after another
+        int a = -1, b = m.n_docs + 1;
+        while (b - a > 1) {
+            const int c = (a + b) >> 1;
+            if (m.doc_start[c] <= j) a = c;
+            else b = c;
+        }
+        return a;
+    };
+    Range r;
+    const int a = doc(j0);
+    if (a < 0) {
+        r.lo = clampi(m.doc_start[0], 0, m.T);
+    } else {
+        const int s = clampi(m.doc_start[a], 0, m.T), e = clampi(m.doc_start[a + 1], s, m.T);
+        if (!m.causal) r.lo = m.window ? max(s, j0 - m.window + 1) : s;
+        else r.lo = m.prefix && j0 < s + clampi(m.prefix[a], 0, e - s) ? s : j0;
+    }
+    const int z = doc(j1 - 1);
+    if (z < 0) return {0, 0};
+    const int s = clampi(m.doc_start[z], 0, m.T), e = clampi(m.doc_start[z + 1], s, m.T);
+    r.hi = m.window ? min(e, j1 - 1 + m.window) : e;
+    return r;
+}
+
+// 64 score columns: x holds q.k, out s in units of log 2, g ds / d(scale q.k)
+template <bool GENERAL>
+__device__ __forceinline__ float score2(const Score &sc, float slope, float sl, float x, int far, float &g)
+{
+    if (!GENERAL) return x * sl;
+    float y = x * sc.scale;
+    g = 1.f;
+    if (sc.softcap > 0.f) {
+        const float t = tanh_exp(y * (1.f / sc.softcap));
+        g = fmaf(-t, t, 1.f);
+        y = sc.softcap * t;
+    }
+    return fmaf(-slope, fabsf((float)far), y * kLog2e);
+}
+
+// ---------------------------------------------------------------- dq
+template <int DP, bool GENERAL>
+__global__ void __launch_bounds__(Bwd<DP>::kThreads, 1)
+dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mDO, const __grid_constant__ CUtensorMap mK,
+          const __grid_constant__ CUtensorMap mV, const __grid_constant__ BwdArgs args)
+{
+    using B = Bwd<DP>;
+    constexpr int kStages = B::kStages, kChunks = DP / 64;
+    constexpr uint32_t kS0 = 0, kDP = 128, kS1 = 256, kAcc = 384;  // TMEM columns
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = ptx::smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (base - raw);
+    const uint32_t bars = base + B::kBars;
+    auto k_full = [&](int s) { return bars + 8u * s; };
+    auto k_empty = [&](int s) { return bars + 8u * (kStages + s); };
+    auto v_full = [&](int s) { return bars + 8u * (2 * kStages + s); };
+    auto v_empty = [&](int s) { return bars + 8u * (3 * kStages + s); };
+    const uint32_t one = bars + 8u * (4 * kStages);
+    const uint32_t q_full = one, q_empty = one + 8, dp_full = one + 16, dp_read = one + 24, ds_full = one + 32, acc_full = one + 40,
+                   acc_empty = one + 48, sums = one + 56;
+    auto s_full = [&](int i) { return one + 64 + 8u * (i & 1); };  // by buffer: the next S does not wait for this one's readers
+    auto w_full = [&](int s) { return one + 80 + 8u * s; };
+    auto w_empty = [&](int s) { return one + 96 + 8u * s; };
+    auto w_slot = [&](int s) { return base + B::kWork + 16u * s; };
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + 32);
+    float *part = reinterpret_cast<float *>(smem + B::kVec);  // [2][128]
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint32_t *status = args.status;
+
+    if (warp == 8 && lane == 0) {
+        ptx::tma_prefetch_desc(&mQ);
+        ptx::tma_prefetch_desc(&mDO);
+        ptx::tma_prefetch_desc(&mK);
+        ptx::tma_prefetch_desc(&mV);
+        for (int s = 0; s < kStages; ++s) {
+            ptx::mbar_init(k_full(s), 1);
+            ptx::mbar_init(k_empty(s), 1);
+            ptx::mbar_init(v_full(s), 1);
+            ptx::mbar_init(v_empty(s), 1);
+        }
+        ptx::mbar_init(q_full, 1);
+        ptx::mbar_init(q_empty, 1);
+        ptx::mbar_init(s_full(0), 1);
+        ptx::mbar_init(s_full(1), 1);
+        ptx::mbar_init(dp_full, 1);
+        ptx::mbar_init(dp_read, 8);
+        ptx::mbar_init(ds_full, 8);
+        ptx::mbar_init(acc_full, 1);
+        ptx::mbar_init(acc_empty, 8);
+        ptx::mbar_init(sums, 8);
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(w_full(s), 1);
+            ptx::mbar_init(w_empty(s), 10);
+        }
+        ptx::fence_barrier_init();
+    }
+    if (warp == 9) {
+        ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
+        ptx::tmem_relinquish();
+    }
+    const Mask mask = mask_in_smem(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    int asked = 0;
+    auto next_work = [&](bool &ok) {
+        const int s = asked & 1;
+        ok = ptx::mbar_wait(w_full(s), (asked >> 1) & 1, status);
+        if (warp < 8) ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return -1;
+        const int x = read_next(w_slot(s));
+        ptx::fence_proxy_async_smem();
+        if (warp < 8) __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(w_empty(s));
+        ++asked;
+        return x;
+    };
+    // piece of work: 128 queries from i0 of head h over keys [lo, hi)
+    struct Piece {
+        int i0, h, g, lo, hi, steps;
+    };
+    auto piece = [&](int work) {
+        Piece p;
+        p.h = work % args.a.n_q;
+        p.g = p.h / (args.a.n_q / args.a.n_kv);
+        p.i0 = (args.tiles - 1 - work / args.a.n_q) * kRows;
+        p.lo = visible(mask, p.i0).lo;
+        p.hi = visible(mask, min(p.i0 + kRows, mask.T) - 1).hi;
+        p.steps = (max(p.hi - p.lo, 0) + kRows - 1) / kRows;
+        return p;
+    };
+
+    if (warp >= 8) {
+        setmaxnreg_dec<56>();
+        if (warp == 8 && lane == 0) {
+            // ---------------- loads
+            int n = 0, items = 0, nk = 0;
+            bool ok = true;
+            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+                const Piece p = piece(work);
+                if (!p.steps) continue;
+                ok = ptx::mbar_wait(q_empty, (items & 1) ^ 1, status);
+                if (!ok) break;
+                ptx::mbar_arrive_expect_tx(q_full, 2 * B::kTile);
+                for (int c = 0; c < kChunks; ++c) {
+                    tma_load_3d(base + B::kR0 + c * kChunk, &mQ, q_full, 64 * c, p.h, p.i0);
+                    tma_load_3d(base + B::kR1 + c * kChunk, &mDO, q_full, 64 * c, p.h, p.i0);
+                }
+                ++items;
+                for (int t = 0; t < p.steps; ++t, ++n) {
+                    const int st = n % kStages, j = p.lo + t * kRows;
+                    const uint32_t ph = (n / kStages) & 1;
+                    ok = ptx::mbar_wait(k_empty(st), ph ^ 1, status);
+                    if (!ok) break;
+                    ptx::mbar_arrive_expect_tx(k_full(st), B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + st * B::kTile + c * kChunk, &mK, k_full(st), 64 * c, p.g, j);
+                    ++nk;
+                    ok = ptx::mbar_wait(v_empty(st), ph ^ 1, status);
+                    if (!ok) break;
+                    ptx::mbar_arrive_expect_tx(v_full(st), B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + st * B::kTile + c * kChunk, &mV, v_full(st), 64 * c, p.g, j);
+                }
+            }
+            if (items) ptx::mbar_wait(q_full, (items - 1) & 1, nullptr);
+            for (int i = max(nk - kStages, 0); i < nk; ++i) ptx::mbar_wait(k_full(i % kStages), (i / kStages) & 1, nullptr);
+            for (int i = max(n - kStages, 0); i < n; ++i) ptx::mbar_wait(v_full(i % kStages), (i / kStages) & 1, nullptr);
+        } else if (warp == 9 && lane == 0) {
+            // ---------------- products
+            constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_q = ptx::idesc_bf16(128, DP, false, true);
+            int n = 0, items = 0;
+            bool ok = true;
+            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+                const Piece p = piece(work);
+                if (!p.steps) continue;
+                ok = ptx::mbar_wait(q_full, items & 1, status);
+                if (!ok) break;
+                auto score = [&](int i) {
+                    const uint32_t k = base + B::kX + (i % kStages) * B::kTile;
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk)
+                        ptx::mma_bf16(tmem + (i & 1 ? kS1 : kS0), desc_k(base + B::kR0, kk), desc_k(k, kk), id_s, kk > 0);
+                    ptx::mma_commit(s_full(i));
+                };
+                auto dprob = [&](int i) {
+                    const uint32_t v = base + B::kY + (i % kStages) * B::kTile;
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk)
+                        ptx::mma_bf16(tmem + kDP, desc_k(base + B::kR1, kk), desc_k(v, kk), id_s, kk > 0);
+                    ptx::mma_commit(dp_full);
+                    ptx::mma_commit(v_empty(i % kStages));
+                    if (i == n + p.steps - 1) ptx::mma_commit(q_empty);  // the last use of Q and dO
+                };
+                ok = ptx::mbar_wait(k_full(n % kStages), (n / kStages) & 1, status);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                score(n);
+                // the last dP of the piece before is in registers
+                ok = ptx::mbar_wait(v_full(n % kStages), (n / kStages) & 1, status) &&
+                     (n == 0 || ptx::mbar_wait(dp_read, (n - 1) & 1, status));
+                if (!ok) break;
+                ptx::tc_fence_after();
+                dprob(n);
+                for (int t = 0; t < p.steps; ++t) {
+                    const int i = n + t;
+                    if (t + 1 < p.steps) {
+                        const int st = (i + 1) % kStages;
+                        const uint32_t ph = ((i + 1) / kStages) & 1;
+                        ok = ptx::mbar_wait(k_full(st), ph, status);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+                        score(i + 1);  // over the dS that the product before last has read
+                        ok = ptx::mbar_wait(v_full(st), ph, status) && ptx::mbar_wait(dp_read, i & 1, status);
+                        if (!ok) break;
+                        ptx::tc_fence_after();
+                        dprob(i + 1);
+                    }
+                    ok = ptx::mbar_wait(ds_full, i & 1, status) &&
+                         (t > 0 || ptx::mbar_wait(acc_empty, (items & 1) ^ 1, status));
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+                    const uint32_t k = base + B::kX + (i % kStages) * B::kTile, ds = tmem + (i & 1 ? kS1 : kS0);
+#pragma unroll
+                    for (int kk = 0; kk < kRows / 16; ++kk)
+                        mma_ts(tmem + kAcc, ds + 64 * (kk >> 2) + 8 * (kk & 3), desc_mn(k, kk), id_q, t > 0 || kk > 0);
+                    ptx::mma_commit(k_empty(i % kStages));
+                }
+                ptx::mma_commit(acc_full);
+                n += p.steps;
+                ++items;
+            }
+            // every product has finished before TMEM is released below
+            if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
+        } else if (warp == 10 && lane == 0) {
+            // ---------------- work
+            for (int i = 0;; ++i) {
+                const int s = i & 1;
+                if (!ptx::mbar_wait(w_empty(s), ((i >> 1) & 1) ^ 1, status)) break;
+                ptx::mbar_arrive_expect_tx(w_full(s), 16);
+                ask_next(w_slot(s), w_full(s));
+                if (!ptx::mbar_wait(w_full(s), (i >> 1) & 1, status)) break;
+                if (read_next(w_slot(s)) < 0) break;
+                ptx::fence_proxy_async_smem();
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- dS: thread = row and half of the columns
+        setmaxnreg_inc<224>();
+        const int half = warp / 4, row = threadIdx.x % 128;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const float sl = args.a.score.scale * kLog2e;
+        uint32_t n = 0, items = 0, nsums = 0;
+        bool ok = true;
+        for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+            const Piece p = piece(work);
+            const int i = p.i0 + row;
+            const bool real = i < mask.T;
+            const int64_t at = (int64_t)p.h * mask.T + (real ? i : 0);
+            const Range rg = real ? visible(mask, i) : Range{0, 0};
+            const bool none = rg.lo >= rg.hi;
+            const float lse2 = none ? 0.f : args.a.lse[at] * kLog2e;
+            float delta = none ? 0.f : args.delta[at];
+            const float slope = GENERAL && args.a.score.slope ? args.a.score.slope[p.h] * kLog2e : 0.f;
+            for (int t = 0; t < p.steps; ++t, ++n) {
+                const uint32_t tS = tmem + lanes + (n & 1 ? kS1 : kS0) + 64 * half, tP = tmem + lanes + kDP + 64 * half;
+                const int j0 = p.lo + t * kRows + 64 * half;
+                ok = ptx::mbar_wait(s_full(n), (n >> 1) & 1, status) && ptx::mbar_wait(dp_full, n & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                uint32_t xs[64], xp[64];
+                tmem_ld32(tS, xs);
+                tmem_ld32(tS + 32, xs + 32);
+                tmem_ld32(tP, xp);
+                tmem_ld32(tP + 32, xp + 32);
+                tmem_wait_ld();
+                pin32(xs), pin32(xs + 32), pin32(xp), pin32(xp + 32);
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(dp_read);
+                float *s = reinterpret_cast<float *>(xs), *dp = reinterpret_cast<float *>(xp);
+                const int lo = rg.lo - j0, hi = rg.hi - j0;
+                const bool all = __all_sync(0xffffffffu, lo <= 0 && hi >= 64);
+                // p over s; over dp what multiplies p - with the score's derivative, if it has one
+                if (!GENERAL) {
+                    const uint64_t sl2 = pack2(sl, sl), l2 = pack2(-lse2, -lse2);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        float a, b;
+                        unpack2(fma2(pack2(s[c], s[c + 1]), sl2, l2), a, b);
+                        s[c] = exp2_fast(a), s[c + 1] = exp2_fast(b);
+                    }
+                    if (!all)
+#pragma unroll
+                        for (int c = 0; c < 64; ++c) {
+                            const bool in = c >= lo && c < hi;
+                            s[c] = in ? s[c] : 0.f, dp[c] = in ? dp[c] : 0.f;
+                        }
+                }
+                if (p.steps == 1) {
+                    // all that the row sees is here: delta from p and dp themselves (see simt::dq_kernel)
+                    float sum = 0.f;
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) {
+                        float g, q = s[c];
+                        if (GENERAL) q = c >= lo && c < hi ? exp2_fast(score2<true>(args.a.score, slope, sl, s[c], i - j0 - c, g) - lse2) : 0.f;
+                        sum = GENERAL && q == 0.f ? sum : fmaf(q, dp[c], sum);
+                    }
+                    part[128 * half + row] = sum;
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(sums);
+                    ok = ptx::mbar_wait(sums, nsums & 1, status);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    ++nsums;
+                    delta = part[row] + part[128 + row];
+                    if (half == 0 && !none) args.delta[at] = delta;
+                }
+                if (!GENERAL) {
+                    const uint64_t d2 = pack2(-delta, -delta);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        float a, b;
+                        unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), d2)), a, b);
+                        xs[c / 2] = ptx::pack_bf16x2(a, b);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        float e[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            float g;
+                            const float x = score2<true>(args.a.score, slope, sl, s[c + u], i - j0 - c - u, g);
+                            e[u] = c + u >= lo && c + u < hi ? exp2_fast(x - lse2) * (dp[c + u] - delta) * g : 0.f;
+                        }
+                        xs[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
+                    }
+                }
+                tmem_st32(tS, xs);
+                tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ds_full);
+            }
+            if (!ok) break;
+            // ---------------- dq of this row, half of its features
+            if (p.steps) {
+                ok = ptx::mbar_wait(acc_full, items & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ++items;
+                ptx::tc_fence_after();
+            }
+            uint32_t o[DP / 2];
+            if (p.steps) {
+#pragma unroll
+                for (int c = 0; c < DP / 2; c += 32) tmem_ld32(tmem + lanes + kAcc + half * (DP / 2) + c, o + c);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < DP / 2; c += 32) pin32(o + c);
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(acc_empty);
+            }
+            bool fine = true;
+            __nv_bfloat16 *out = args.a.dq.at(real ? i : 0, p.h);
+#pragma unroll
+            for (int e = 0; e < DP / 2; e += 8) {
+                float f[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    f[u] = none ? 0.f : __uint_as_float(o[e + u]) * args.a.score.scale;
+                    fine = fine && isfinite(f[u]);
+                }
+                const int col = half * (DP / 2) + e;
+                if (real && col < args.a.d)
+                    *reinterpret_cast<uint4 *>(out + col) =
+                        make_uint4(ptx::pack_bf16x2(f[0], f[1]), ptx::pack_bf16x2(f[2], f[3]), ptx::pack_bf16x2(f[4], f[5]),
+                                   ptx::pack_bf16x2(f[6], f[7]));
+            }
+            uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
+            __syncwarp();
+            for (; bad; bad &= bad - 1) {
+                const int r = __ffs(bad) - 1;
+                row_dq(args.a, i - lane + r, p.h, lane, __shfl_sync(0xffffffffu, delta, r), half * (DP / 2), half * (DP / 2) + DP / 2);
+            }
+        }
+    }
+
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+// ---------------------------------------------------------------- dk, dv
+template <int DP, bool GENERAL>
+__global__ void __launch_bounds__(Bwd<DP>::kThreads, 1)
+dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mDO, const __grid_constant__ CUtensorMap mK,
+           const __grid_constant__ CUtensorMap mV, const __grid_constant__ BwdArgs args)
+{
+    using B = Bwd<DP>;
+    constexpr int kStages = B::kStages, kChunks = DP / 64;
+    constexpr uint32_t kS = 0, kDP = 128, kDV = 256, kDK = 256 + DP;  // TMEM columns
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = ptx::smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (base - raw);
+    const uint32_t bars = base + B::kBars;
+    auto q_full = [&](int s) { return bars + 8u * s; };
+    auto q_empty = [&](int s) { return bars + 8u * (kStages + s); };
+    auto o_full = [&](int s) { return bars + 8u * (2 * kStages + s); };
+    auto o_empty = [&](int s) { return bars + 8u * (3 * kStages + s); };
+    auto vec_full = [&](int s) { return bars + 8u * (4 * kStages + s); };
+    auto vec_empty = [&](int s) { return bars + 8u * (5 * kStages + s); };
+    const uint32_t one = bars + 8u * (6 * kStages);
+    const uint32_t kv_full = one, kv_empty = one + 8, s_full = one + 16, dp_full = one + 24, p_full = one + 32, ds_full = one + 40,
+                   acc_full = one + 48, acc_empty = one + 56;
+    auto w_full = [&](int s) { return one + 64 + 8u * s; };
+    auto w_empty = [&](int s) { return one + 80 + 8u * s; };
+    auto w_slot = [&](int s) { return base + B::kWork + 16u * s; };
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + 32);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint32_t *status = args.status;
+
+    if (warp == 8 && lane == 0) {
+        ptx::tma_prefetch_desc(&mQ);
+        ptx::tma_prefetch_desc(&mDO);
+        ptx::tma_prefetch_desc(&mK);
+        ptx::tma_prefetch_desc(&mV);
+        for (int s = 0; s < kStages; ++s) {
+            ptx::mbar_init(q_full(s), 1);
+            ptx::mbar_init(q_empty(s), 1);
+            ptx::mbar_init(o_full(s), 1);
+            ptx::mbar_init(o_empty(s), 1);
+            ptx::mbar_init(vec_full(s), 1);
+            ptx::mbar_init(vec_empty(s), 8);
+        }
+        ptx::mbar_init(kv_full, 1);
+        ptx::mbar_init(kv_empty, 1);
+        ptx::mbar_init(s_full, 1);
+        ptx::mbar_init(dp_full, 1);
+        ptx::mbar_init(p_full, 8);
+        ptx::mbar_init(ds_full, 8);
+        ptx::mbar_init(acc_full, 1);
+        ptx::mbar_init(acc_empty, 8);
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(w_full(s), 1);
+            ptx::mbar_init(w_empty(s), 11);
+        }
+        ptx::fence_barrier_init();
+    }
+    if (warp == 9) {
+        ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
+        ptx::tmem_relinquish();
+    }
+    const Mask mask = mask_in_smem(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int group = args.a.n_q / args.a.n_kv;
+
+    // lane 0 of warps 8 and 9, whole warps 0-7 and 10
+    int asked = 0;
+    auto next_work = [&](bool &ok) {
+        const int s = asked & 1;
+        const bool whole = warp < 8 || warp == 10;
+        ok = ptx::mbar_wait(w_full(s), (asked >> 1) & 1, status);
+        if (whole) ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return -1;
+        const int x = read_next(w_slot(s));
+        ptx::fence_proxy_async_smem();
+        if (whole) __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(w_empty(s));
+        ++asked;
+        return x;
+    };
+    // piece of work: 128 keys from j0 of key head g, over query tiles from lo, `per` of a
+    // head and `steps` in all
+    struct Piece {
+        int j0, g, lo, per, steps;
+    };
+    auto piece = [&](int work) {
+        Piece p;
+        p.g = work % args.a.n_kv;
+        p.j0 = work / args.a.n_kv * kRows;
+        const Range r = queries_of(mask, p.j0, p.j0 + kRows);
+        p.lo = r.lo;
+        p.per = (max(r.hi - r.lo, 0) + kRows - 1) / kRows;
+        p.steps = p.per * group;
+        return p;
+    };
+
+    if (warp >= 8) {
+        setmaxnreg_dec<56>();
+        if (warp == 8 && lane == 0) {
+            // ---------------- loads
+            int n = 0, items = 0, nq = 0;
+            bool ok = true;
+            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+                const Piece p = piece(work);
+                if (!p.steps) continue;
+                ok = ptx::mbar_wait(kv_empty, (items & 1) ^ 1, status);
+                if (!ok) break;
+                ptx::mbar_arrive_expect_tx(kv_full, 2 * B::kTile);
+                for (int c = 0; c < kChunks; ++c) {
+                    tma_load_3d(base + B::kR0 + c * kChunk, &mK, kv_full, 64 * c, p.g, p.j0);
+                    tma_load_3d(base + B::kR1 + c * kChunk, &mV, kv_full, 64 * c, p.g, p.j0);
+                }
+                ++items;
+                for (int t = 0; t < p.steps; ++t, ++n) {
+                    const int st = n % kStages, h = p.g * group + t / p.per, i = p.lo + t % p.per * kRows;
+                    const uint32_t ph = (n / kStages) & 1;
+                    ok = ptx::mbar_wait(q_empty(st), ph ^ 1, status);
+                    if (!ok) break;
+                    ptx::mbar_arrive_expect_tx(q_full(st), B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + st * B::kTile + c * kChunk, &mQ, q_full(st), 64 * c, h, i);
+                    ++nq;
+                    ok = ptx::mbar_wait(o_empty(st), ph ^ 1, status);
+                    if (!ok) break;
+                    ptx::mbar_arrive_expect_tx(o_full(st), B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + st * B::kTile + c * kChunk, &mDO, o_full(st), 64 * c, h, i);
+                }
+            }
+            if (items) ptx::mbar_wait(kv_full, (items - 1) & 1, nullptr);
+            for (int i = max(nq - kStages, 0); i < nq; ++i) ptx::mbar_wait(q_full(i % kStages), (i / kStages) & 1, nullptr);
+            for (int i = max(n - kStages, 0); i < n; ++i) ptx::mbar_wait(o_full(i % kStages), (i / kStages) & 1, nullptr);
+        } else if (warp == 9 && lane == 0) {
+            // ---------------- products
+            constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_d = ptx::idesc_bf16(128, DP, false, true);
+            int n = 0, items = 0;
+            bool ok = true;
+            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+                const Piece p = piece(work);
+                if (!p.steps) continue;
+                auto x = [&](int i) { return base + B::kX + (i % kStages) * B::kTile; };
+                auto y = [&](int i) { return base + B::kY + (i % kStages) * B::kTile; };
+                auto score = [&](int i) {
+                    if (!ptx::mbar_wait(q_full(i % kStages), (i / kStages) & 1, status)) return false;
+                    ptx::tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk)
+                        ptx::mma_bf16(tmem + kS, desc_k(base + B::kR0, kk), desc_k(x(i), kk), id_s, kk > 0);
+                    ptx::mma_commit(s_full);
+                    return true;
+                };
+                auto dprob = [&](int i) {
+                    if (!ptx::mbar_wait(o_full(i % kStages), (i / kStages) & 1, status)) return false;
+                    ptx::tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < DP / 16; ++kk)
+                        ptx::mma_bf16(tmem + kDP, desc_k(base + B::kR1, kk), desc_k(y(i), kk), id_s, kk > 0);
+                    ptx::mma_commit(dp_full);
+                    if (i == n + p.steps - 1) ptx::mma_commit(kv_empty);  // the last use of K and V
+                    return true;
+                };
+                ok = ptx::mbar_wait(kv_full, items & 1, status) && score(n) && dprob(n);
+                for (int t = 0; ok && t < p.steps; ++t) {
+                    const int i = n + t;
+                    ok = ptx::mbar_wait(p_full, i & 1, status) && (t > 0 || ptx::mbar_wait(acc_empty, (items & 1) ^ 1, status));
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < kRows / 16; ++kk)
+                        mma_ts(tmem + kDV, tmem + kS + 64 * (kk >> 2) + 8 * (kk & 3), desc_mn(y(i), kk), id_d, t > 0 || kk > 0);
+                    ptx::mma_commit(o_empty(i % kStages));
+                    if (t + 1 < p.steps) ok = score(i + 1);  // over P, read by then: products run in order
+                    ok = ok && ptx::mbar_wait(ds_full, i & 1, status);
+                    if (!ok) break;
+                    ptx::tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < kRows / 16; ++kk)
+                        mma_ts(tmem + kDK, tmem + kDP + 64 * (kk >> 2) + 8 * (kk & 3), desc_mn(x(i), kk), id_d, t > 0 || kk > 0);
+                    ptx::mma_commit(q_empty(i % kStages));
+                    if (t + 1 < p.steps) ok = dprob(i + 1);  // over dS
+                }
+                if (!ok) break;
+                ptx::mma_commit(acc_full);
+                n += p.steps;
+                ++items;
+            }
+            // every product has finished before TMEM is released below
+            if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
+        } else if (warp == 10) {
+            // ---------------- lse, delta and ranges of the query tiles
+            int n = 0;
+            bool ok = true;
+            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+                const Piece p = piece(work);
+                for (int t = 0; t < p.steps; ++t, ++n) {
+                    const int st = n % kStages, h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows;
+                    ok = ptx::mbar_wait(vec_empty(st), ((n / kStages) & 1) ^ 1, status);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    float *vec = reinterpret_cast<float *>(smem + B::kVec + st * B::kVecBytes);
+                    int2 *rg = reinterpret_cast<int2 *>(vec + 256);
+                    bool all = true;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int e = lane + 32 * u, i = i0 + e;
+                        const int2 r = i < mask.T ? args.ranges[i] : make_int2(0, 0);
+                        const bool sees = r.x < r.y;
+                        vec[e] = sees ? args.a.lse[(int64_t)h * mask.T + i] * kLog2e : 0.f;
+                        vec[128 + e] = sees ? args.delta[(int64_t)h * mask.T + i] : 0.f;
+                        rg[e] = r;
+                        all = all && r.x <= p.j0 && r.y >= p.j0 + kRows;
+                    }
+                    all = __all_sync(0xffffffffu, all);
+                    if (lane == 0) *reinterpret_cast<int *>(vec + 512) = all;
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(vec_full(st));
+                }
+            }
+        } else if (warp == 11 && lane == 0) {
+            // ---------------- work
+            for (int i = 0;; ++i) {
+                const int s = i & 1;
+                if (!ptx::mbar_wait(w_empty(s), ((i >> 1) & 1) ^ 1, status)) break;
+                ptx::mbar_arrive_expect_tx(w_full(s), 16);
+                ask_next(w_slot(s), w_full(s));
+                if (!ptx::mbar_wait(w_full(s), (i >> 1) & 1, status)) break;
+                if (read_next(w_slot(s)) < 0) break;
+                ptx::fence_proxy_async_smem();
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- P and dS: thread = key and half of the queries
+        setmaxnreg_inc<224>();
+        const int half = warp / 4, row = threadIdx.x % 128;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const uint32_t tS = tmem + lanes + kS + 64 * half, tP = tmem + lanes + kDP + 64 * half;
+        const float sl = args.a.score.scale * kLog2e;
+        uint32_t n = 0, items = 0;
+        bool ok = true;
+        for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
+            const Piece p = piece(work);
+            const int j = p.j0 + row;
+            for (int t = 0; t < p.steps; ++t, ++n) {
+                const int st = n % kStages;
+                const float *vec = reinterpret_cast<const float *>(smem + B::kVec + st * B::kVecBytes) + 64 * half;
+                const int2 *rg = reinterpret_cast<const int2 *>(vec - 64 * half + 256) + 64 * half;
+                ok = ptx::mbar_wait(vec_full(st), (n / kStages) & 1, status) && ptx::mbar_wait(s_full, n & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                const bool all = *reinterpret_cast<const int *>(vec - 64 * half + 512) != 0;
+                uint32_t xs[64], xp[64];
+                tmem_ld32(tS, xs);
+                tmem_ld32(tS + 32, xs + 32);
+                tmem_wait_ld();
+                pin32(xs), pin32(xs + 32);
+                float *s = reinterpret_cast<float *>(xs), *dp = reinterpret_cast<float *>(xp);
+                uint32_t in[2] = {0xffffffffu, 0xffffffffu};  // which of the queries see this key
+                if (!all) {
+                    in[0] = in[1] = 0;
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) {
+                        const int2 r = rg[c];
+                        in[c / 32] |= (j >= r.x && j < r.y ? 1u : 0u) << (c % 32);
+                    }
+                }
+                // p over s; with a capped score, dp is to be multiplied by p and g
+                uint32_t gs[GENERAL ? 32 : 1];
+                if (!GENERAL) {
+                    const uint64_t sl2 = pack2(sl, sl);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 4) {
+                        const float4 l = *reinterpret_cast<const float4 *>(vec + c);
+                        float a, b;
+                        unpack2(fma2(pack2(s[c], s[c + 1]), sl2, pack2(-l.x, -l.y)), a, b);
+                        s[c] = exp2_fast(a), s[c + 1] = exp2_fast(b);
+                        unpack2(fma2(pack2(s[c + 2], s[c + 3]), sl2, pack2(-l.z, -l.w)), a, b);
+                        s[c + 2] = exp2_fast(a), s[c + 3] = exp2_fast(b);
+                    }
+                } else {
+                    const int h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows + 64 * half;
+                    const float slope = args.a.score.slope ? args.a.score.slope[h] * kLog2e : 0.f;
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        float g[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            s[c + u] = exp2_fast(score2<true>(args.a.score, slope, sl, s[c + u], i0 + c + u - j, g[u]) - vec[c + u]);
+                        // the derivative to 16 bits of the product that dS is rounded to 8 of
+                        const __half2 hg = __floats2half2_rn(g[0], g[1]);
+                        gs[c / 2] = *reinterpret_cast<const uint32_t *>(&hg);
+                    }
+                }
+                if (!all)
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) s[c] = in[c / 32] >> (c % 32) & 1 ? s[c] : 0.f;
+                uint32_t pk[32];
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) pk[c / 2] = ptx::pack_bf16x2(s[c], s[c + 1]);
+                tmem_st32(tS, pk);
+                tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(p_full);
+
+                ok = ptx::mbar_wait(dp_full, n & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                tmem_ld32(tP, xp);
+                tmem_ld32(tP + 32, xp + 32);
+                tmem_wait_ld();
+                pin32(xp), pin32(xp + 32);
+                if (!all)
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) dp[c] = in[c / 32] >> (c % 32) & 1 ? dp[c] : 0.f;
+#pragma unroll
+                for (int c = 0; c < 64; c += 4) {
+                    const float4 d = *reinterpret_cast<const float4 *>(vec + 128 + c);
+                    float e[4];
+                    unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), pack2(-d.x, -d.y))), e[0], e[1]);
+                    unpack2(mul2(pack2(s[c + 2], s[c + 3]), add2(pack2(dp[c + 2], dp[c + 3]), pack2(-d.z, -d.w))), e[2], e[3]);
+                    if (GENERAL) {
+                        const float2 g0 = __half22float2(*reinterpret_cast<const __half2 *>(&gs[c / 2]));
+                        const float2 g1 = __half22float2(*reinterpret_cast<const __half2 *>(&gs[c / 2 + 1]));
+                        e[0] *= g0.x, e[1] *= g0.y, e[2] *= g1.x, e[3] *= g1.y;
+                    }
+                    pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
+                    pk[c / 2 + 1] = ptx::pack_bf16x2(e[2], e[3]);
+                }
+                tmem_st32(tP, pk);
+                tmem_wait_st();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    ptx::mbar_arrive(ds_full);
+                    ptx::mbar_arrive(vec_empty(st));
+                }
+            }
+            if (!ok) break;
+            // ---------------- dv by the first warpgroup, dk by the second
+            if (p.steps) {
+                ok = ptx::mbar_wait(acc_full, items & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ++items;
+                ptx::tc_fence_after();
+            }
+            const bool real = j < mask.T;
+            const float f = half ? args.a.score.scale : 1.f;
+            __nv_bfloat16 *out = (half ? args.a.dk : args.a.dv).at(real ? j : 0, p.g);
+            bool fine = true;
+            uint32_t o[DP];
+            if (p.steps) {
+#pragma unroll
+                for (int c = 0; c < DP; c += 32) tmem_ld32(tmem + lanes + (half ? kDK : kDV) + c, o + c);
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < DP; c += 32) pin32(o + c);
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(acc_empty);
+            } else {
+#pragma unroll
+                for (int c = 0; c < DP; ++c) o[c] = 0;
+            }
+#pragma unroll
+            for (int e = 0; e < DP; e += 8) {
+                float v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    v[u] = __uint_as_float(o[e + u]) * f;
+                    fine = fine && isfinite(v[u]);
+                }
+                if (real && e < args.a.d)
+                    *reinterpret_cast<uint4 *>(out + e) = make_uint4(ptx::pack_bf16x2(v[0], v[1]), ptx::pack_bf16x2(v[2], v[3]),
+                                                                     ptx::pack_bf16x2(v[4], v[5]), ptx::pack_bf16x2(v[6], v[7]));
+            }
+            uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
+            __syncwarp();
+            for (; bad; bad &= bad - 1) row_dkv(args.a, j - lane + __ffs(bad) - 1, p.g, lane, half == 0, half == 1);
+        }
+    }
+
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace tc
+}  // namespace attn
+}  // namespace noble

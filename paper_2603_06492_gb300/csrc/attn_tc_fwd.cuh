@@ -212,6 +212,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 for (int b = 0; b < 2; ++b)
                     if (in(b, t0)) score(b, t0);
                 free_k(t0);
+                if (t0 + 1 == t1) ptx::mma_commit(q_empty);
                 for (int t = t0; t < t1; ++t) {
                     const int i = n + t - t0, st = i % kStages;
                     if (t + 1 < t1) ok = wait_k(t + 1);
@@ -237,13 +238,13 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     if (!ok) break;
                     ptx::mma_commit(v_empty(st));
                     if (t + 1 < t1) free_k(t + 1);
+                    if (t + 2 == t1) ptx::mma_commit(q_empty);
                 }
-                ptx::mma_commit(q_empty);
                 n += t1 - t0;
             }
             // every product has finished before TMEM is released below: commits complete in
-            // order, and the last of a piece of work is q_empty's
-            if (items) ptx::mbar_wait(q_empty, (items - 1) & 1, nullptr);
+            // order, and the last of a piece of work is that of its last V stage
+            if (n) ptx::mbar_wait(v_empty((n - 1) % kStages), ((n - 1) / kStages) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
             // ---------------- work: one answer ahead; after the first "none left" no more is asked
             for (int i = 0;; ++i) {
