@@ -41,7 +41,9 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_
         : "memory");
 }
 
-// 32 columns of this thread's TMEM lane; valid only after tmem_wait_ld.
+// 32 columns of this thread's TMEM lane; valid only after tmem_wait_ld.  These and the
+// stores below are for whole warps: after code whose lanes may have parted (a wait, a
+// masked score) a __syncwarp comes before them.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r)
 {
     asm volatile(
@@ -80,6 +82,13 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r)
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <int N>
+__device__ __forceinline__ void as_floats(float (&f)[N], const uint32_t (&r)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = __uint_as_float(r[i]);
+}
 
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pack2(float a, float b)

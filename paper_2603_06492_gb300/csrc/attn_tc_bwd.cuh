@@ -329,6 +329,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 if (!ok) break;
                 ptx::tc_fence_after();
                 uint32_t xs[64], xp[64];
+                __syncwarp();
                 tmem_ld32(tS, xs);
                 tmem_ld32(tS + 32, xs + 32);
                 tmem_ld32(tP, xp);
@@ -338,7 +339,10 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 ptx::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(dp_read);
-                float *s = reinterpret_cast<float *>(xs), *dp = reinterpret_cast<float *>(xp);
+                float s[64], dp[64];
+                as_floats(s, xs);
+                as_floats(dp, xp);
+                uint32_t pk[32];
                 const int lo = rg.lo - j0, hi = rg.hi - j0;
                 const bool all = __all_sync(0xffffffffu, lo <= 0 && hi >= 64);
                 // p over s; over dp what multiplies p - with the score's derivative, if it has one
@@ -382,7 +386,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                     for (int c = 0; c < 64; c += 2) {
                         float a, b;
                         unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), d2)), a, b);
-                        xs[c / 2] = ptx::pack_bf16x2(a, b);
+                        pk[c / 2] = ptx::pack_bf16x2(a, b);
                     }
                 } else {
 #pragma unroll
@@ -392,12 +396,14 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                         for (int u = 0; u < 2; ++u) {
                             float g;
                             const float x = score2<true>(args.a.score, slope, sl, s[c + u], i - j0 - c - u, g);
-                            e[u] = c + u >= lo && c + u < hi ? exp2_fast(x - lse2) * (dp[c + u] - delta) * g : 0.f;
+                            const float d = exp2_fast(x - lse2) * (dp[c + u] - delta) * g;
+                            e[u] = c + u >= lo && c + u < hi ? d : 0.f;
                         }
-                        xs[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
+                        pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
                     }
                 }
-                tmem_st32(tS, xs);
+                __syncwarp();
+                tmem_st32(tS, pk);
                 tmem_wait_st();
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -414,6 +420,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             }
             uint32_t o[DP / 2];
             if (p.steps) {
+                __syncwarp();
 #pragma unroll
                 for (int c = 0; c < DP / 2; c += 32) tmem_ld32(tmem + lanes + kAcc + half * (DP / 2) + c, o + c);
                 tmem_wait_ld();
@@ -710,11 +717,13 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 ptx::tc_fence_after();
                 const bool all = *reinterpret_cast<const int *>(vec - 64 * half + 512) != 0;
                 uint32_t xs[64], xp[64];
+                __syncwarp();
                 tmem_ld32(tS, xs);
                 tmem_ld32(tS + 32, xs + 32);
                 tmem_wait_ld();
                 pin32(xs), pin32(xs + 32);
-                float *s = reinterpret_cast<float *>(xs), *dp = reinterpret_cast<float *>(xp);
+                float s[64], dp[64];
+                as_floats(s, xs);
                 uint32_t in[2] = {0xffffffffu, 0xffffffffu};  // which of the queries see this key
                 if (!all) {
                     in[0] = in[1] = 0;
@@ -757,6 +766,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 uint32_t pk[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) pk[c / 2] = ptx::pack_bf16x2(s[c], s[c + 1]);
+                __syncwarp();
                 tmem_st32(tS, pk);
                 tmem_wait_st();
                 ptx::tc_fence_before();
@@ -767,10 +777,12 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ptx::tc_fence_after();
+                __syncwarp();
                 tmem_ld32(tP, xp);
                 tmem_ld32(tP + 32, xp + 32);
                 tmem_wait_ld();
                 pin32(xp), pin32(xp + 32);
+                as_floats(dp, xp);
                 if (!all)
 #pragma unroll
                     for (int c = 0; c < 64; ++c) dp[c] = in[c / 32] >> (c % 32) & 1 ? dp[c] : 0.f;
@@ -788,6 +800,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
                     pk[c / 2 + 1] = ptx::pack_bf16x2(e[2], e[3]);
                 }
+                __syncwarp();
                 tmem_st32(tP, pk);
                 tmem_wait_st();
                 ptx::tc_fence_before();
@@ -812,6 +825,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             bool fine = true;
             uint32_t o[DP];
             if (p.steps) {
+                __syncwarp();
 #pragma unroll
                 for (int c = 0; c < DP; c += 32) tmem_ld32(tmem + lanes + (half ? kDK : kDV) + c, o + c);
                 tmem_wait_ld();

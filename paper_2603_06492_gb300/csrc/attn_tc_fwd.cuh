@@ -280,12 +280,14 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 if (!ok) break;
                 ptx::tc_fence_after();
                 uint32_t x[128];
+                __syncwarp();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, x + 32 * c);
                 tmem_wait_ld();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) pin32(x + 32 * c);
-                float *v = reinterpret_cast<float *>(x);
+                float v[128];
+                as_floats(v, x);
                 if (GENERAL) {
                     // in units of log 2
 #pragma unroll
@@ -318,6 +320,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
 #pragma unroll 1
                     for (int c = 0; c < DP; c += 32) {
                         uint32_t o[32];
+                        __syncwarp();
                         tmem_ld32(tO + c, o);
                         tmem_wait_ld();
                         pin32(o);
@@ -331,6 +334,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 if (grow) m = mt;
                 const float mm = m == -INFINITY ? 0.f : m;
                 uint64_t sum0 = 0, sum1 = 0;
+                uint32_t pk[64];
                 const uint64_t sl2 = pack2(GENERAL ? 1.f : sl, GENERAL ? 1.f : sl), m2 = pack2(-mm, -mm);
 #pragma unroll
                 for (int c = 0; c < 128; c += 4) {
@@ -341,11 +345,12 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     for (int u = 0; u < 4; ++u) e[u] = exp2_fast(e[u]);
                     sum0 = add2(sum0, pack2(e[0], e[1]));
                     sum1 = add2(sum1, pack2(e[2], e[3]));
-                    x[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
-                    x[c / 2 + 1] = ptx::pack_bf16x2(e[2], e[3]);
+                    pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
+                    pk[c / 2 + 1] = ptx::pack_bf16x2(e[2], e[3]);
                 }
-                tmem_st32(tS, x);
-                tmem_st32(tS + 32, x + 32);
+                __syncwarp();
+                tmem_st32(tS, pk);
+                tmem_st32(tS + 32, pk + 32);
                 tmem_wait_st();
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -372,6 +377,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             for (int c = 0; c < DP; c += 32) {
                 uint32_t o[32];
                 if (t1 > t0) {
+                    __syncwarp();
                     tmem_ld32(tO + c, o);
                     tmem_wait_ld();
                     pin32(o);
