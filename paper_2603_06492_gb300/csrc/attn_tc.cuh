@@ -30,15 +30,50 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
         : "memory");
 }
 
-// D[tmem] (+)= A[tmem] B[smem]: A holds two bf16 per 32-bit column, K ascending.
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+// Products of one thread, whose every instruction delays the tensor pipe: descriptors
+// are made of a low word per operand, to which a constant is added per step, and a
+// high word that all share (128-byte swizzle, 1024 bytes between groups of 8 rows).
+constexpr uint32_t kDescHigh = 64u | (1u << 14) | (2u << 29);
+// K-major operand of a token tile (features contracted), MN-major one (tokens contracted)
+__device__ __forceinline__ uint32_t desc_k(uint32_t tile) { return ((tile & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t tile) { return ((tile & 0x3FFFFu) >> 4) | ((kChunk >> 4) << 16); }
+__host__ __device__ constexpr uint32_t step_k(int kk) { return ((kk >> 2) * kChunk + (kk & 3) * 32) >> 4; }
+__host__ __device__ constexpr uint32_t step_mn(int kk) { return kk * 2048 >> 4; }
+
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}\n" ::"r"(d_tmem),
+        "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
         : "memory");
+}
+// A from TMEM, two bf16 per 32-bit column, K ascending.
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}\n" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
+        : "memory");
+}
+// D = A B^T over the features of two token tiles (DP of them)
+template <int DP>
+__device__ __forceinline__ void product_features(uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t idesc)
+{
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; ++kk) mma_ss(d_tmem, a + step_k(kk), b + step_k(kk), idesc, kk > 0);
+}
+// D (+)= A B over 128 tokens, A at two places of 64 tokens each in TMEM
+__device__ __forceinline__ void product_tokens(uint32_t d_tmem, uint32_t a_low, uint32_t a_high, uint32_t b, uint32_t idesc, bool more)
+{
+#pragma unroll
+    for (int kk = 0; kk < kRows / 16; ++kk)
+        mma_ts(d_tmem, (kk < 4 ? a_low : a_high) + 8 * (kk & 3), b + step_mn(kk), idesc, kk > 0 ? 1u : (uint32_t)more);
 }
 
 // 32 columns of this thread's TMEM lane; valid only after tmem_wait_ld.  These and the
@@ -147,14 +182,6 @@ __device__ __forceinline__ int read_next(uint32_t slot)
         : "memory");
     return x;
 }
-
-// K-major operand of a token tile: features 16 kk .. of its rows.
-__device__ __forceinline__ uint64_t desc_k(uint32_t tile, int kk)
-{
-    return ptx::smem_desc_sw128(tile + (kk >> 2) * kChunk + (kk & 3) * 32, 16, 1024);
-}
-// MN-major operand: tokens 16 kk .. contracted.
-__device__ __forceinline__ uint64_t desc_mn(uint32_t tile, int kk) { return ptx::smem_desc_sw128(tile + kk * 2048, kChunk, 1024); }
 
 // The document starts (and prefixes) in shared memory where they fit, since every
 // piece of work searches them; call with all threads, before a __syncthreads.

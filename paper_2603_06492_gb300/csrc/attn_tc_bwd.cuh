@@ -191,7 +191,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     };
 
     if (warp >= 8) {
-        setmaxnreg_dec<56>();
+        setmaxnreg_dec<88>();
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, nk = 0;
@@ -234,18 +234,15 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 if (!p.steps) continue;
                 ok = ptx::mbar_wait(q_full, items & 1, status);
                 if (!ok) break;
+                const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
+                               dy = desc_k(base + B::kY), dm = desc_mn(base + B::kX);
+                constexpr uint32_t kStep = B::kTile >> 4;
                 auto score = [&](int i) {
-                    const uint32_t k = base + B::kX + (i % kStages) * B::kTile;
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk)
-                        ptx::mma_bf16(tmem + (i & 1 ? kS1 : kS0), desc_k(base + B::kR0, kk), desc_k(k, kk), id_s, kk > 0);
+                    product_features<DP>(tmem + (i & 1 ? kS1 : kS0), dr0, dx + (i % kStages) * kStep, id_s);
                     ptx::mma_commit(s_full(i));
                 };
                 auto dprob = [&](int i) {
-                    const uint32_t v = base + B::kY + (i % kStages) * B::kTile;
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk)
-                        ptx::mma_bf16(tmem + kDP, desc_k(base + B::kR1, kk), desc_k(v, kk), id_s, kk > 0);
+                    product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
                     ptx::mma_commit(dp_full);
                     ptx::mma_commit(v_empty(i % kStages));
                     if (i == n + p.steps - 1) ptx::mma_commit(q_empty);  // the last use of Q and dO
@@ -278,10 +275,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                          (t > 0 || ptx::mbar_wait(acc_empty, (items & 1) ^ 1, status));
                     if (!ok) break;
                     ptx::tc_fence_after();
-                    const uint32_t k = base + B::kX + (i % kStages) * B::kTile, ds = tmem + (i & 1 ? kS1 : kS0);
-#pragma unroll
-                    for (int kk = 0; kk < kRows / 16; ++kk)
-                        mma_ts(tmem + kAcc, ds + 64 * (kk >> 2) + 8 * (kk & 3), desc_mn(k, kk), id_q, t > 0 || kk > 0);
+                    const uint32_t ds = tmem + (i & 1 ? kS1 : kS0);
+                    product_tokens(tmem + kAcc, ds, ds + 64, dm + (i % kStages) * kStep, id_q, t > 0);
                     ptx::mma_commit(k_empty(i % kStages));
                 }
                 ptx::mma_commit(acc_full);
@@ -305,7 +300,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         __syncwarp();
     } else {
         // ---------------- dS: thread = row and half of the columns
-        setmaxnreg_inc<224>();
+        setmaxnreg_inc<208>();
         const int half = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const float sl = args.a.score.scale * kLog2e;
@@ -563,7 +558,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     };
 
     if (warp >= 8) {
-        setmaxnreg_dec<56>();
+        setmaxnreg_dec<88>();
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, nq = 0;
@@ -604,23 +599,20 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
                 const Piece p = piece(work);
                 if (!p.steps) continue;
-                auto x = [&](int i) { return base + B::kX + (i % kStages) * B::kTile; };
-                auto y = [&](int i) { return base + B::kY + (i % kStages) * B::kTile; };
+                const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
+                               dy = desc_k(base + B::kY), mx = desc_mn(base + B::kX), my = desc_mn(base + B::kY);
+                constexpr uint32_t kStep = B::kTile >> 4;
                 auto score = [&](int i) {
                     if (!ptx::mbar_wait(q_full(i % kStages), (i / kStages) & 1, status)) return false;
                     ptx::tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk)
-                        ptx::mma_bf16(tmem + kS, desc_k(base + B::kR0, kk), desc_k(x(i), kk), id_s, kk > 0);
+                    product_features<DP>(tmem + kS, dr0, dx + (i % kStages) * kStep, id_s);
                     ptx::mma_commit(s_full);
                     return true;
                 };
                 auto dprob = [&](int i) {
                     if (!ptx::mbar_wait(o_full(i % kStages), (i / kStages) & 1, status)) return false;
                     ptx::tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk)
-                        ptx::mma_bf16(tmem + kDP, desc_k(base + B::kR1, kk), desc_k(y(i), kk), id_s, kk > 0);
+                    product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
                     ptx::mma_commit(dp_full);
                     if (i == n + p.steps - 1) ptx::mma_commit(kv_empty);  // the last use of K and V
                     return true;
@@ -631,17 +623,13 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     ok = ptx::mbar_wait(p_full, i & 1, status) && (t > 0 || ptx::mbar_wait(acc_empty, (items & 1) ^ 1, status));
                     if (!ok) break;
                     ptx::tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < kRows / 16; ++kk)
-                        mma_ts(tmem + kDV, tmem + kS + 64 * (kk >> 2) + 8 * (kk & 3), desc_mn(y(i), kk), id_d, t > 0 || kk > 0);
+                    product_tokens(tmem + kDV, tmem + kS, tmem + kS + 64, my + (i % kStages) * kStep, id_d, t > 0);
                     ptx::mma_commit(o_empty(i % kStages));
                     if (t + 1 < p.steps) ok = score(i + 1);  // over P, read by then: products run in order
                     ok = ok && ptx::mbar_wait(ds_full, i & 1, status);
                     if (!ok) break;
                     ptx::tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < kRows / 16; ++kk)
-                        mma_ts(tmem + kDK, tmem + kDP + 64 * (kk >> 2) + 8 * (kk & 3), desc_mn(x(i), kk), id_d, t > 0 || kk > 0);
+                    product_tokens(tmem + kDK, tmem + kDP, tmem + kDP + 64, mx + (i % kStages) * kStep, id_d, t > 0);
                     ptx::mma_commit(q_empty(i % kStages));
                     if (t + 1 < p.steps) ok = dprob(i + 1);  // over dS
                 }
@@ -697,7 +685,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         __syncwarp();
     } else {
         // ---------------- P and dS: thread = key and half of the queries
-        setmaxnreg_inc<224>();
+        setmaxnreg_inc<208>();
         const int half = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t tS = tmem + lanes + kS + 64 * half, tP = tmem + lanes + kDP + 64 * half;

@@ -145,7 +145,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     };
 
     if (warp >= 8) {
-        setmaxnreg_dec<56>();
+        setmaxnreg_dec<88>();
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, issued_k = 0;
@@ -194,11 +194,9 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 ok = ptx::mbar_wait(q_full, items & 1, status);
                 ++items;
                 auto in = [&](int b, int t) { return b ? t >= s.b0 && t < s.b1 : t >= s.a0 && t < s.a1; };
+                const uint32_t dq = desc_k(base + F::kQ), dk = desc_k(base + F::kK), dv = desc_mn(base + F::kV);
                 auto score = [&](int b, int t) {  // S of row block b and tile t
-                    const uint32_t q = base + F::kQ + b * F::kTile, k = base + F::kK + ((n + t - t0) % kStages) * F::kTile;
-#pragma unroll
-                    for (int kk = 0; kk < DP / 16; ++kk)
-                        ptx::mma_bf16(tmem + F::kS + 128 * b, desc_k(q, kk), desc_k(k, kk), id_s, kk > 0);
+                    product_features<DP>(tmem + F::kS + 128 * b, dq + b * (F::kTile >> 4), dk + ((n + t - t0) % kStages) * (F::kTile >> 4), id_s);
                     ptx::mma_commit(s_full(b));
                 };
                 auto wait_k = [&](int t) {
@@ -223,11 +221,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                             ok = ptx::mbar_wait(p_full(b), np[b] & 1, status);
                             if (!ok) break;
                             ptx::tc_fence_after();
-                            const uint32_t v = base + F::kV + st * F::kTile;
-                            const bool more = t > (b ? s.b0 : s.a0);
-#pragma unroll
-                            for (int kk = 0; kk < kRows / 16; ++kk)
-                                mma_ts(tmem + F::kO + DP * b, tmem + F::kS + 128 * b + 8 * kk, desc_mn(v, kk), id_o, more || kk > 0);
+                            const uint32_t p = tmem + F::kS + 128 * b;
+                            product_tokens(tmem + F::kO + DP * b, p, p + 32, dv + st * (F::kTile >> 4), id_o, t > (b ? s.b0 : s.a0));
                             ptx::mma_commit(pv_done(b));
                             ++np[b];
                         }
@@ -260,7 +255,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         __syncwarp();
     } else {
         // ---------------- softmax: warps 0-3 of A, 4-7 of B; thread = row
-        setmaxnreg_inc<224>();
+        setmaxnreg_inc<208>();
         const int b = warp / 4;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t tS = tmem + lanes + F::kS + 128 * b, tO = tmem + lanes + F::kO + DP * b;
