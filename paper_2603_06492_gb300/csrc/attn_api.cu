@@ -9,6 +9,7 @@
 #include "host.cuh"
 #include "attn_mask.cuh"
 #include "attn_paged.cuh"
+#include "attn_paged_mma.cuh"
 #include "attn_simt.cuh"
 #include "attn_tc_bwd.cuh"
 #include "attn_tc_fwd.cuh"
@@ -440,10 +441,18 @@ noble_status paged_launch(const attn::paged::Args<T> &a, cudaStream_t st)
 {
     namespace p = attn::paged;
     constexpr size_t smem = ((p::kRows + p::kKeys) * attn::simt::kLd<DP> + p::kRows * attn::simt::kPP) * 4;
-    NOBLE_TRY((allow<&p::simt_kernel<DP, T>>(smem)));
     const int64_t rows = (int64_t)(a.n_q / a.n_kv) * a.q_len;
     const dim3 grid((unsigned)(a.chunks * ceil_div(rows, p::kRows)), (unsigned)a.n_kv, (unsigned)a.n_seq);
-    NOBLE_TRY(run(st, {"attn_paged", kBoundHbm, 0.0, 0.0}, [&] { p::simt_kernel<DP, T><<<grid, p::kThreads, smem, st>>>(a); }));
+    if constexpr (std::is_same_v<T, bf>) {
+        NOBLE_TRY(run(st, {"attn_paged", kBoundHbm, 0.0, 0.0}, [&] {
+            if (a.page_size % 16 == 0) p::mma_kernel<DP, true><<<grid, p::kThreads, 0, st>>>(a);
+            else p::mma_kernel<DP, false><<<grid, p::kThreads, 0, st>>>(a);
+        }));
+    } else {
+        NOBLE_TRY((allow<&p::simt_kernel<DP, T>>(smem)));
+        NOBLE_TRY(run(st, {"attn_paged_simt", kBoundHbm, 0.0, 0.0},
+                      [&] { p::simt_kernel<DP, T><<<grid, p::kThreads, smem, st>>>(a); }));
+    }
     if (a.chunks == 1) return NOBLE_OK;
     const unsigned blocks = (unsigned)ceil_div((int64_t)a.n_seq * a.q_len * a.n_q, 4);
     return run(st, {"attn_paged_join", kBoundHbm, 0.0, 0.0}, [&] { p::join_kernel<T><<<blocks, 128, 0, st>>>(a); });
