@@ -100,16 +100,17 @@ int lanes_per_head(int64_t d)
     while (lp * 8 < d) lp *= 2;
     return lp;
 }
+int64_t rope_batches(int64_t heads, int64_t d) { return ceil_div(heads, rope::kPasses * (32 / lanes_per_head(d))); }
 // blocks of the backward: they set how many partial sums there are
 int64_t rope_bwd_blocks(const noble_rope_desc *d)
 {
-    const int64_t per = ceil_div(d->n_q + d->n_kv, rope::kPasses * (32 / lanes_per_head(d->d)));
-    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->T * per, rope::kWarps), 4 * kSms));
+    const int64_t per = std::max(rope_batches(d->n_q, d->d), rope_batches(d->n_kv, d->d));
+    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->T * per, rope::kWarps), 2 * kSms));
 }
 
 template <typename T>
 rope::Args<T> rope_args(const noble_rope_desc *d, const noble_heads *q, const noble_heads *k, const int32_t *pos,
-                        const float *table, const float *gain_q, const float *gain_k, int64_t all_heads)
+                        const float *table, const float *gain_q, const float *gain_k)
 {
     rope::Args<T> a{};
     a.q = heads<const T>(q), a.k = heads<const T>(k);
@@ -119,8 +120,8 @@ rope::Args<T> rope_args(const noble_rope_desc *d, const noble_heads *q, const no
     a.gain_q = a.norm ? gain_q : nullptr, a.gain_k = a.norm ? gain_k : nullptr;
     a.tokens = d->T, a.n_q = (int)d->n_q, a.n_kv = (int)d->n_kv, a.d = (int)d->d, a.rot = (int)d->rot;
     a.positions = (int)d->positions, a.eps = d->eps;
-    a.lp = lanes_per_head(d->d);
-    a.per_token = (int)ceil_div(all_heads, rope::kPasses * (32 / a.lp));
+    a.lp = lanes_per_head(d->d), a.inv_d = 1.f / (float)d->d;
+    a.batches_q = (int)rope_batches(d->n_q, d->d), a.batches_kv = (int)rope_batches(d->n_kv, d->d);
     return a;
 }
 
@@ -129,7 +130,12 @@ noble_status rope_fwd_launch(const noble_rope_desc *d, rope::Args<T> &a, cudaStr
 {
     a.status = status_ptr();
     if (!a.status) return fail(NOBLE_ERR_CUDA, "status word address");
-    const int64_t blocks = ceil_div(a.tokens * a.per_token, rope::kWarps);
+    // one batch a warp while that leaves SMs idle, else all batches of a token, which then
+    // share its cosines and sines
+    const int all = a.batches_q + (APPEND ? 2 : 1) * a.batches_kv;
+    a.take = a.tokens * all <= 24 * kSms ? 1 : all;
+    a.groups = (int)ceil_div(all, a.take);
+    const int64_t blocks = ceil_div(a.tokens * a.groups, rope::kWarps);
     if (blocks > INT32_MAX) return fail(NOBLE_ERR_UNSUPPORTED, "%lld tokens of so many heads", (long long)a.tokens);
     const KernelInfo ki{APPEND ? "kv_append" : "rope_fwd", kBoundHbm, 0.0,
                         2.0 * sizeof(T) * a.tokens * a.d * (a.n_q + (APPEND ? 2 : 1) * a.n_kv)};
@@ -411,17 +417,30 @@ noble_status check_cache(const noble_kv_cache *c, int64_t n_kv, int64_t d, int32
     return NOBLE_OK;
 }
 
-// Keys of a chunk, and chunks of the longest sequence: enough blocks to load every SM
-// several times over, of at least 256 keys, so that joining costs little beside reading.
+// Keys of a chunk, and chunks of the longest sequence.  `one` is the chunk with which the
+// blocks of sequences of that length fill the chip once.  One sequence, or shorter chunks
+// than 1024 keys: that.  Several may differ in length, and more and smaller pieces
+// balance, down to an eighth of it or 1024 keys, beside which a block's start and
+// the joining count.  us with chunks of 512 / 1024 / 2048 / 3456 keys: 64 sequences up to
+// 32768 tokens 450 / 394 / 366 / 365 (one: 728); 16 up to 4096 39 / 35 / 53 / 79; one
+// of 131072 82 / 68 / 61 / 79 (one = 1728: 58).
 struct Split {
     int chunk, chunks;
 };
 Split paged_split(const noble_paged_desc *d)
 {
     const int64_t rows = d->n_q / d->n_kv * d->q_len;
-    const int64_t units = std::max<int64_t>(1, d->n_seq * d->n_kv * ceil_div(rows, attn::paged::kRows));
-    const int64_t want = std::max<int64_t>(1, 8 * kSms / units);
-    const int64_t chunk = std::max<int64_t>(256, ceil_div(ceil_div(d->max_len, want), attn::paged::kKeys) * attn::paged::kKeys);
+    const int64_t units = d->n_seq * d->n_kv * ceil_div(rows, attn::paged::kRows);
+    const int64_t slots = kSms * (d->d <= 64 ? attn::paged::kBlocksPerSm<64> : attn::paged::kBlocksPerSm<128>);
+    const int64_t one = ceil_div(d->max_len * std::max<int64_t>(units, 1), slots);
+    // fp32 is bound by its products, not by reading: pieces enough to balance (24 sequences up
+    // to 1024 tokens, 16 heads of 64: chunks of 384 107 us, of 512 139)
+    int64_t chunk = d->dtype == NOBLE_FP32 ? ceil_div(d->max_len * std::max<int64_t>(units, 1), 8 * kSms)
+                    : d->n_seq <= 1        ? one
+                                           : std::max(one / 8, std::min<int64_t>(one, 1024));
+    chunk = std::max<int64_t>(chunk, 256);
+    const int64_t chunks = std::max<int64_t>(1, ceil_div(d->max_len, chunk));
+    chunk = std::max<int64_t>(1, ceil_div(ceil_div(d->max_len, chunks), attn::paged::kKeys)) * attn::paged::kKeys;
     return {(int)chunk, (int)std::max<int64_t>(1, ceil_div(d->max_len, chunk))};
 }
 struct PagedWork {
@@ -454,8 +473,13 @@ noble_status paged_launch(const attn::paged::Args<T> &a, cudaStream_t st)
                       [&] { p::simt_kernel<DP, T><<<grid, p::kThreads, smem, st>>>(a); }));
     }
     if (a.chunks == 1) return NOBLE_OK;
-    const unsigned blocks = (unsigned)ceil_div((int64_t)a.n_seq * a.q_len * a.n_q, 4);
-    return run(st, {"attn_paged_join", kBoundHbm, 0.0, 0.0}, [&] { p::join_kernel<T><<<blocks, 128, 0, st>>>(a); });
+    // warps per row: about eight chunks each
+    int per_row = 1;
+    while (per_row < 8 && a.chunks > 8 * per_row) per_row *= 2;
+    const unsigned blocks = (unsigned)ceil_div((int64_t)a.n_seq * a.q_len * a.n_q, 8 / per_row);
+    const bool pdl = pdl_ok();
+    return run(st, {"attn_paged_join", kBoundHbm, 0.0, 0.0},
+               [&] { launch_maybe_pdl(p::join_kernel<T>, dim3(blocks), dim3(256), 0, st, pdl, a, per_row); });
 }
 
 template <typename T>
@@ -524,7 +548,7 @@ noble_status noble_rope_fwd(const noble_rope_desc *desc, const noble_heads *q, c
     if (desc->T == 0) return NOBLE_OK;
     auto go = [&](auto zero) {
         using T = decltype(zero);
-        rope::Args<T> a = rope_args<T>(desc, q, k, pos, table, gain_q, gain_k, desc->n_q + desc->n_kv);
+        rope::Args<T> a = rope_args<T>(desc, q, k, pos, table, gain_q, gain_k);
         a.q_out = heads<T>(q_out), a.k_out = heads<T>(k_out);
         return rope_fwd_launch<false, T>(desc, a, (cudaStream_t)stream);
     };
@@ -567,8 +591,7 @@ noble_status noble_rope_bwd(const noble_rope_desc *desc, const noble_heads *dq, 
     if (desc->T == 0 && !sums) return NOBLE_OK;
     auto go = [&](auto zero) {
         using T = decltype(zero);
-        rope::Args<T> a = rope_args<T>(desc, norm ? q : nullptr, norm ? k : nullptr, pos, table, gain_q, gain_k,
-                                       desc->n_q + desc->n_kv);
+        rope::Args<T> a = rope_args<T>(desc, norm ? q : nullptr, norm ? k : nullptr, pos, table, gain_q, gain_k);
         a.dq = heads<const T>(dq), a.dk = heads<const T>(dk);
         a.q_out = heads<T>(dq_in), a.k_out = heads<T>(dk_in);
         a.part = sums ? static_cast<float *>(workspace) : nullptr;
@@ -595,7 +618,7 @@ noble_status noble_kv_append(const noble_rope_desc *desc, const noble_heads *q, 
     if (desc->T == 0) return NOBLE_OK;
     auto go = [&](auto zero) {
         using T = decltype(zero);
-        rope::Args<T> a = rope_args<T>(desc, q, k, pos, table, gain_q, gain_k, desc->n_q + 2 * desc->n_kv);
+        rope::Args<T> a = rope_args<T>(desc, q, k, pos, table, gain_q, gain_k);
         a.v = heads<const T>(v), a.q_out = heads<T>(q_out);
         a.slots = slots, a.k_cache = static_cast<T *>(cache->k), a.v_cache = static_cast<T *>(cache->v);
         a.capacity = cache->pages * cache->page_size, a.page_size = (int)cache->page_size;

@@ -8,6 +8,7 @@
 #pragma once
 
 #include "attn_simt.cuh"
+#include "sm100_ptx.cuh"
 
 namespace noble {
 namespace attn {
@@ -199,34 +200,50 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(const __grid_constant__ 
     }
 }
 
-// A warp per row: the chunks' results, each scaled to the common maximum.
+// The chunks' results of a row, each scaled to the common maximum: `per_row` warps of the
+// block's eight (a power of two) take every per_row-th chunk, the first adds theirs up.
 template <typename T>
-__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ Args<T> a)
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Args<T> a, int per_row)
 {
-    const int64_t u = (int64_t)blockIdx.x * 4 + threadIdx.x / 32, rows = (int64_t)a.n_seq * a.q_len * a.n_q;
-    const int lane = threadIdx.x % 32;
-    if (u >= rows) return;
+    __shared__ float4 sum_o[8][32];
+    __shared__ float sum_l[8];
+    ptx::griddep_wait();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, part = warp % per_row;
+    const int64_t u = (int64_t)blockIdx.x * (8 / per_row) + warp / per_row, rows = (int64_t)a.n_seq * a.q_len * a.n_q;
     const int64_t t = u / a.n_q;
     const int h = (int)(u % a.n_q);
-    const Span sp = span(a, (int)(t / a.q_len));
-    const int c0 = sp.from / a.chunk, c1 = max(sp.len - 1, 0) / a.chunk;
-    if (c0 == c1) return;
-    float m = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[2 * (u * a.chunks + c)]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float base = m == -INFINITY ? 0.f : m;
+    int c0 = 0, c1 = -1;
+    if (u < rows) {
+        const Span sp = span(a, (int)(t / a.q_len));
+        c0 = sp.from / a.chunk, c1 = max(sp.len - 1, 0) / a.chunk;
+    }
+    const bool work = c1 > c0;  // a single chunk has written the result itself
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-        const int64_t p = u * a.chunks + c;
-        const float w = exp2f((a.part_ml[2 * p] - base) * kLog2e);
-        l += w * a.part_ml[2 * p + 1];
-        if (4 * lane < a.d) {
-            const float4 x = load4(a.part_o + p * a.d + 4 * lane);
+    float l = 0.f, m = -INFINITY;
+    if (work) {
+        for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[2 * (u * a.chunks + c)]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
+        for (int c = c0 + part; c <= c1; c += per_row) {
+            const int64_t p = u * a.chunks + c;
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * p);
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (4 * lane < a.d) x = load4(a.part_o + p * a.d + 4 * lane);
+            const float w = exp2f((ml.x - base) * kLog2e);
+            l = fmaf(w, ml.y, l);
             acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
         }
+    }
+    sum_o[warp][lane] = acc;
+    if (lane == 0) sum_l[warp] = l;
+    __syncthreads();
+    if (!work || part) return;
+    for (int i = 1; i < per_row; ++i) {
+        const float4 x = sum_o[warp + i][lane];
+        acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+        l += sum_l[warp + i];
     }
     const bool ok = isfinite(acc.x) && isfinite(acc.y) && isfinite(acc.z) && isfinite(acc.w) && isfinite(l);
     if (!__all_sync(0xffffffffu, ok)) {

@@ -11,8 +11,8 @@
 //                (P's own order) and pairs the keys with byte permutes; column n of
 //                step j is feature 64 u + 8 n + j, so a lane ends up with 16
 //                consecutive features of two rows
-// A warp takes every fourth group of 16 keys of its block's chunk, with a softmax of its
-// own; the four are joined in shared memory at the end.  The next keys load while the
+// The warps of a block take turns at its chunk's groups of 16 keys, each with a softmax of
+// its own; the four are joined in shared memory at the end.  The next keys load while the
 // values' product runs, the next values during the keys'.
 #pragma once
 
@@ -40,17 +40,25 @@ __device__ __forceinline__ uint4 load16(const __nv_bfloat16 *p)
     return v;
 }
 
+// Blocks of an SM, which set the registers of a thread: heads of 128 features need all of
+// two (253; with three they spill, 64 sequences up to 32768 tokens 552 us for 365).
+template <int DP> constexpr int kBlocksPerSm = DP == 64 ? 4 : 2;
+
 // PAGE16: pages of a multiple of 16 tokens, so that a group of 16 keys has one page.
 // grid as simt_kernel's
 template <int DP, bool PAGE16>
-__global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 2) mma_kernel(const __grid_constant__ Args<__nv_bfloat16> a)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm<DP>) mma_kernel(const __grid_constant__ Args<__nv_bfloat16> a)
 {
     constexpr int C = DP / 32, U = DP / 64;
+    constexpr int kStep = 64;  // keys of a block at a time
     __shared__ float join_o[4][16][DP + 4], join_m[4][16], join_l[4][16];
     __shared__ int redo[16];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     const int chunk = blockIdx.x % a.chunks, rb = blockIdx.x / a.chunks, kvh = blockIdx.y, n = blockIdx.z;
     const int group = a.n_q / a.n_kv, rows = group * a.q_len;
+    // the page of the first keys, unless a window moves them, while the length is on its way
+    const int guess = chunk * a.chunk + 16 * warp, guess_j = guess + (PAGE16 ? 0 : lane & 15);
+    const int guessed = guess_j / a.page_size < a.max_pages ? a.page_table[(int64_t)n * a.max_pages + guess_j / a.page_size] : -1;
     const Span sp = span(a, n);
     const int first_chunk = sp.from / a.chunk, last_chunk = max(sp.len - 1, 0) / a.chunk;
     if (chunk < first_chunk || chunk > last_chunk) return;
@@ -79,24 +87,20 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 2) mma_kernel(const _
     const __nv_bfloat16 *kb = a.k + kvh * a.head, *vb = a.v + kvh * a.head;
     uint4 k[2][C], v[4][U];
     bool bad_page = false;
-    // element offset of key j, or -1 where nothing may be read
-    auto where = [&](int j) -> int64_t {
-        if (j < j0 || j >= j1) return -1;
-        const int64_t at = place(a, n, j);
-        bad_page = bad_page || at < 0;
-        return at;
-    };
-    // offsets of a group's keys: of its first key (PAGE16; valid keys by index), or one per lane
-    int64_t at;
-    auto find = [&](int jb) {
-        if (!PAGE16) {
-            at = where(jb + (lane & 15));
-        } else {
-            at = jb < j1 ? place(a, n, jb) : -1;
-            bad_page = bad_page || (jb < j1 && at < 0);
+    // Element offset of a group's first key (PAGE16) or of key lane % 16, -1 where nothing
+    // may be read: found a step before its keys load, which would else wait for it.
+    int64_t at = 0, at_next;
+    auto find = [&](int jb, int known) {
+        const int j = jb + (PAGE16 ? 0 : lane & 15);
+        const bool in = j < j1 && (PAGE16 || j >= j0);
+        at_next = -1;
+        if (in) {
+            const int id = known >= 0 ? known : a.page_table[(int64_t)n * a.max_pages + j / a.page_size];
+            if (id >= 0 && id < a.pages) at_next = id * a.page + j % a.page_size * a.row;
+            else bad_page = true;
         }
     };
-    auto key = [&](int jb, int e) -> int64_t {
+    auto key = [&](int jb, int e) -> int64_t {  // of key e of a group
         if (PAGE16) return at >= 0 && jb + e >= j0 && jb + e < j1 ? at + e * a.row : -1;
         return __shfl_sync(0xffffffffu, at, e);
     };
@@ -125,14 +129,15 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 2) mma_kernel(const _
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[u][j][0] = o[u][j][1] = o[u][j][2] = o[u][j][3] = 0.f;
 
-    const int step = 64;
     int jb = (j0 & ~15) + 16 * warp;
-    find(jb);
+    find(jb, jb == guess ? guessed : -1);
+    at = at_next;
     load_k(jb);
     load_v(jb);
-    for (; jb < j1; jb += step) {
-        const bool valid_all = at >= 0;  // (PAGE16) of this group, before `at` moves on
-        const int64_t at_now = at;
+    find(jb + kStep, -1);
+    for (; jb < j1; jb += kStep) {
+        // keys without a page count for no row
+        const uint32_t ok = PAGE16 ? (at >= 0 ? 0xffffu : 0u) : __ballot_sync(0xffffffffu, at >= 0) & 0xffffu;
         float s[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -143,23 +148,19 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 2) mma_kernel(const _
                 mma16816(s[h], q[0][c][2], q[1][c][2], q[0][c][3], q[1][c][3], k[h][c].z, k[h][c].w);
             }
         }
-        // keys without a page count for no row
-        uint32_t ok = 0xffffu;
-        if (PAGE16) ok = valid_all ? 0xffffu : 0u;
-        else ok = __ballot_sync(0xffffffffu, at_now >= 0) & 0xffffu;
-        find(jb + step);
-        load_k(jb + step);
+        at = at_next;
+        load_k(jb + kStep);
         uint32_t p[2][2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             float x[4], top = m[r];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = 8 * (e >> 1) + 2 * t + (e & 1), j = jb + i;
+                const int w = 8 * (e >> 1) + 2 * t + (e & 1), j = jb + w;
                 float y = s[e >> 1][2 * r + (e & 1)] * a.score.scale;
                 if (a.score.softcap > 0.f) y = a.score.softcap * tanh_exp(y / a.score.softcap);
                 if (a.score.slope) y -= slope[r] * (float)(pos[r] - j);
-                x[e] = j >= lo[r] && j >= j0 && j < hi[r] && (ok >> i & 1) ? y * kLog2e : -INFINITY;
+                x[e] = j >= lo[r] && j >= j0 && j < hi[r] && (ok >> w & 1) ? y * kLog2e : -INFINITY;
                 top = fmaxf(top, x[e]);
             }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -179,10 +180,12 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 2) mma_kernel(const _
             l[r] += (x[0] + x[1]) + (x[2] + x[3]);
             p[r][0] = ptx::pack_bf16x2(x[0], x[1]), p[r][1] = ptx::pack_bf16x2(x[2], x[3]);
         }
+        __syncwarp();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t v0[4] = {v[0][u].x, v[0][u].y, v[0][u].z, v[0][u].w}, v1[4] = {v[1][u].x, v[1][u].y, v[1][u].z, v[1][u].w},
-                           v2[4] = {v[2][u].x, v[2][u].y, v[2][u].z, v[2][u].w}, v3[4] = {v[3][u].x, v[3][u].y, v[3][u].z, v[3][u].w};
+            const uint4 w0 = v[0][u], w1 = v[1][u], w2 = v[2][u], w3 = v[3][u];
+            const uint32_t v0[4] = {w0.x, w0.y, w0.z, w0.w}, v1[4] = {w1.x, w1.y, w1.z, w1.w}, v2[4] = {w2.x, w2.y, w2.z, w2.w},
+                           v3[4] = {w3.x, w3.y, w3.z, w3.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const uint32_t sel = j & 1 ? 0x7632 : 0x5410;
@@ -190,7 +193,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 4 : 2) mma_kernel(const _
                          __byte_perm(v2[j / 2], v3[j / 2], sel));
             }
         }
-        load_v(jb + step);
+        load_v(jb + kStep);
+        find(jb + 2 * kStep, -1);
     }
     if (bad_page) raise_status(a.status, kStatusBadIndex);
 

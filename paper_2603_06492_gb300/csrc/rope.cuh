@@ -4,8 +4,11 @@
 // All of it moves every element once each way and is bound by that.  A lane holds 8
 // consecutive features of a head (16 bytes of bf16), LP lanes a head, so a warp
 // reads whole heads in 16-byte pieces; the sum of a norm is a butterfly over LP
-// lanes.  A warp takes kPasses * 32 / LP heads of one token at a time, whose loads are
-// all issued before the first is used and which share the token's cosines and sines.
+// lanes.  A batch is kPasses * 32 / LP heads of one token and one kind (queries, keys or
+// values), whose loads are all issued before the first is used; they stay packed, and it
+// is the packed words that go to the other lane of a pair.  Gains are multiplied
+// into the cosines and sines once per kind, which leaves two products and a scale
+// per element.
 #pragma once
 
 #include "attn_mask.cuh"
@@ -32,9 +35,10 @@ struct Args {
     float *part;                           // [blocks][2][d]: partial gain gradients, or NULL
     int64_t tokens;
     int n_q, n_kv, d, rot, positions;
-    float eps;
+    float eps, inv_d;
     int norm, interleaved;
-    int lp, per_token;  // lanes per head; units of heads per token
+    int lp, batches_q, batches_kv;  // lanes per head; batches of a token's queries, of its keys or values
+    int take, groups;               // forward: batches of a warp, warps of a token
     uint32_t *status;
     // append
     const int64_t *slots;
@@ -43,92 +47,136 @@ struct Args {
     int page_size;
 };
 
+// 8 elements as they are in memory
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p)
+    {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p);
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    __device__ __forceinline__ void set(const float (&x)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+    }
+    __device__ __forceinline__ Raw from(int lane) const
+    {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = __shfl_sync(0xffffffffu, w[i], lane);
+        return r;
+    }
+};
+template <> struct Raw<float> {
+    float x[8];
+    __device__ __forceinline__ void load(const float *p)
+    {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+    __device__ __forceinline__ void store(float *p) const
+    {
+        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    }
+    __device__ __forceinline__ void get(float (&y)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i];
+    }
+    __device__ __forceinline__ void set(const float (&y)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = y[i];
+    }
+    __device__ __forceinline__ Raw from(int lane) const
+    {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.x[i] = __shfl_sync(0xffffffffu, x[i], lane);
+        return r;
+    }
+};
 __device__ __forceinline__ void load8(float (&x)[8], const float *p)
 {
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
-__device__ __forceinline__ void load8(float (&x)[8], const __nv_bfloat16 *p)
-{
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i]));
-        x[2 * i] = f.x, x[2 * i + 1] = f.y;
-    }
-}
-__device__ __forceinline__ void store8(float *p, const float (&x)[8])
-{
-    *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&x)[8])
-{
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-        w[i] = *reinterpret_cast<uint32_t *>(&b);
-    }
-    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    Raw<float> r;
+    r.load(p);
+    r.get(x);
 }
 
-// Cosines and signed sines of a lane's 8 features: y_f = c x_f + s x_(other of f).
+// Factors of a lane's 8 features: y_f = c x_f + s x_(other of f), s = 0 where f does not
+// rotate; with gains (norm) c holds f's and s its partner's.
 struct Turn {
     float c[8], s[8];
 };
 template <int MODE>
+__device__ __forceinline__ int partner(int e, int rot, int interleaved)
+{
+    const int half = rot / 2;
+    if (MODE == kInterleaved || (MODE == kAny && interleaved)) return e ^ 1;
+    return e < half ? e + half : e - half;
+}
+// `row`: the token's row of the table; SIGN -1 turns back
+template <int MODE, int SIGN>
 __device__ __forceinline__ void load_turn(Turn &t, const float *row, int f, int rot, int interleaved)
 {
     const int half = rot / 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.c[i] = 1.f, t.s[i] = 0.f;
     if (MODE == kHalf) {
         if (f < rot) {
             const bool second = f >= half;
             load8(t.c, row + (second ? f - half : f));
             load8(t.s, row + half + (second ? f - half : f));
-            if (!second)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t.s[i] = -t.s[i];
-            return;
+            for (int i = 0; i < 8; ++i) t.s[i] = (second ? SIGN : -SIGN) * t.s[i];
         }
     } else if (MODE == kInterleaved) {
         if (f < rot) {
             const float4 c = *reinterpret_cast<const float4 *>(row + f / 2), s = *reinterpret_cast<const float4 *>(row + half + f / 2);
             t.c[0] = t.c[1] = c.x, t.c[2] = t.c[3] = c.y, t.c[4] = t.c[5] = c.z, t.c[6] = t.c[7] = c.w;
-            t.s[1] = s.x, t.s[3] = s.y, t.s[5] = s.z, t.s[7] = s.w;
-            t.s[0] = -s.x, t.s[2] = -s.y, t.s[4] = -s.z, t.s[6] = -s.w;
-            return;
+            t.s[1] = SIGN * s.x, t.s[3] = SIGN * s.y, t.s[5] = SIGN * s.z, t.s[7] = SIGN * s.w;
+            t.s[0] = -SIGN * s.x, t.s[2] = -SIGN * s.y, t.s[4] = -SIGN * s.z, t.s[6] = -SIGN * s.w;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = f + i;
-            t.c[i] = 1.f, t.s[i] = 0.f;
             if (e < rot) {
                 const int pair = interleaved ? e / 2 : e < half ? e : e - half;
                 const bool first = interleaved ? e % 2 == 0 : e < half;
                 t.c[i] = row[pair];
-                t.s[i] = first ? -row[half + pair] : row[half + pair];
+                t.s[i] = (first ? -SIGN : SIGN) * row[half + pair];
             }
         }
-        return;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t.c[i] = 1.f, t.s[i] = 0.f;
 }
 
-// Rotates by the angle, or back (SIGN -1).  `buf`: 256 floats of the warp (kAny).
-template <int MODE, int SIGN>
-__device__ __forceinline__ void turn8(float (&x)[8], const Turn &t, int f, int rot, int interleaved, float *buf, int lane)
+// The other features of the pairs of a lane's 8.  `buf`: 256 floats of the warp (kAny).
+template <int MODE, typename T>
+__device__ __forceinline__ void others(float (&y)[8], const Raw<T> &r, const float (&x)[8], int f, int rot, int interleaved,
+                                       float *buf, int lane)
 {
-    float y[8];
-    const int half = rot / 2;
     if (MODE == kHalf) {
-        // lanes of features past `rot` multiply what they get by 0 unless it is not finite: they keep theirs
-        const int other = f < half ? lane + half / 8 : lane - half / 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], other & 31);
+        const int other = f >= rot ? lane : f < rot / 2 ? lane + rot / 16 : lane - rot / 16;
+        r.from(other & 31).get(y);
     } else if (MODE == kInterleaved) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
@@ -138,56 +186,61 @@ __device__ __forceinline__ void turn8(float (&x)[8], const Turn &t, int f, int r
         for (int i = 0; i < 8; ++i) buf[lane * 8 + i] = x[i];
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = f + i, o = interleaved ? e ^ 1 : e < half ? e + half : e - half;
-            y[i] = e < rot ? buf[lane * 8 - f + o] : 0.f;
-        }
+        for (int i = 0; i < 8; ++i) y[i] = f + i < rot ? buf[lane * 8 - f + partner<kAny>(f + i, rot, interleaved)] : 0.f;
     }
+}
+// x turned, in place; features that do not rotate do not meet their neighbours' values
+template <int MODE>
+__device__ __forceinline__ void turn8(float (&x)[8], const float (&y)[8], const Turn &t, int f, int rot)
+{
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (MODE == kAny ? f + i < rot : f < rot) x[i] = x[i] * t.c[i] + (SIGN > 0 ? y[i] : -y[i]) * t.s[i];
+    for (int i = 0; i < 8; ++i) {
+        const float a = x[i] * t.c[i];
+        x[i] = (MODE == kAny ? f + i < rot : f < rot) ? fmaf(y[i], t.s[i], a) : a;
+    }
 }
 
 __device__ __forceinline__ float head_sum(float v, int lp)
 {
-    for (int o = 1; o < lp; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float w = __shfl_xor_sync(0xffffffffu, v, o);
+        v += o < lp ? w : 0.f;
+    }
     return v;
 }
 
-// One unit: heads [first, first + kPasses * 32 / lp) of a token.
+// A warp: `take` batches of a token, the next one's loads in flight while one is worked on.
 template <int MODE, bool APPEND, typename T>
-__global__ void __launch_bounds__(32 * kWarps) fwd_kernel(const __grid_constant__ Args<T> a)
+__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 3 : 2) fwd_kernel(const __grid_constant__ Args<T> a)
 {
     __shared__ float bufs[MODE == kAny ? kWarps : 1][256];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t u = (int64_t)blockIdx.x * kWarps + warp;
-    if (u >= a.tokens * a.per_token) return;
-    const int64_t t = u / a.per_token;
-    const int hp = 32 / a.lp, f = lane % a.lp * 8;
-    const int first = (int)(u % a.per_token) * kPasses * hp + lane / a.lp;
-    const int heads = a.n_q + a.n_kv + (APPEND ? a.n_kv : 0);
+    if (u >= a.tokens * a.groups) return;
+    const int64_t t = u / a.groups;
+    const int hp = 32 / a.lp, f = lane % a.lp * 8, own = lane / a.lp;
     const bool in = f < a.d;
-    float x[kPasses][8];
+    const int all = a.batches_q + (APPEND ? 2 : 1) * a.batches_kv;
+    const int b0 = (int)(u % a.groups) * a.take, b1 = min(b0 + a.take, all);
+    // batch b: heads first + own + p * hp of its kind (0 queries, 1 keys, 2 values)
+    auto kind_of = [&](int b) { return b < a.batches_q ? 0 : b < a.batches_q + a.batches_kv ? 1 : 2; };
+    auto first_of = [&](int b, int kind) { return (b - (kind ? a.batches_q + (kind - 1) * a.batches_kv : 0)) * kPasses * hp + own; };
+    auto load = [&](Raw<T> (&r)[kPasses], int b) {
+        const int kind = kind_of(b), h0 = first_of(b, kind), n = kind ? a.n_kv : a.n_q;
+        const Heads<const T> &x = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int h = first + p * hp;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[p][i] = 0.f;
-        if (in && h < heads)
-            load8(x[p], (h < a.n_q                        ? a.q.at(t, h)
-                         : !APPEND || h < a.n_q + a.n_kv ? a.k.at(t, h - a.n_q)
-                                                          : a.v.at(t, h - a.n_q - a.n_kv)) + f);
-    }
+        for (int p = 0; p < kPasses; ++p) {
+            if (in && b < b1 && h0 + p * hp < n) r[p].load(x.at(t, h0 + p * hp) + f);
+            else r[p].zero();
+        }
+    };
+    Raw<T> r[kPasses];
+    load(r, b0);
     const int pos = a.pos[t];
     const bool known = pos >= 0 && pos < a.positions;
     if (!known && lane == 0) raise_status(a.status, kStatusBadIndex);
-    Turn tn;
-    load_turn<MODE>(tn, a.table + (int64_t)(known ? pos : 0) * a.rot, in ? f : a.rot, a.rot, a.interleaved);
-    float gq[8], gk[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) gq[i] = gk[i] = 1.f;
-    if (in && a.gain_q) load8(gq, a.gain_q + f);
-    if (in && a.gain_k) load8(gk, a.gain_k + f);
+    const float *row = a.table + (int64_t)(known ? pos : 0) * a.rot;
     T *kc = nullptr, *vc = nullptr;
     if (APPEND) {
         const int64_t slot = a.slots[t];
@@ -198,115 +251,148 @@ __global__ void __launch_bounds__(32 * kWarps) fwd_kernel(const __grid_constant_
             kc = a.k_cache + at, vc = a.v_cache + at;
         }
     }
+    Turn tn;
+    int have = -1;  // the kind that tn is for
+    for (int b = b0; b < b1; ++b) {
+        const int kind = kind_of(b), h0 = first_of(b, kind), n = kind ? a.n_kv : a.n_q;
+        Raw<T> next[kPasses];
+        load(next, b + 1);
+        if (APPEND && kind == 2) {
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int h = first + p * hp;
-        const bool is_q = h < a.n_q, is_v = APPEND && h >= a.n_q + a.n_kv;
-        float w[8];
+            for (int p = 0; p < kPasses; ++p)
+                if (in && vc && h0 + p * hp < n) r[p].store(vc + (h0 + p * hp) * a.head + f);
+        } else {
+            const float *gain = kind ? a.gain_k : a.gain_q;
+            if (kind != have) load_turn<MODE, 1>(tn, row, known && in ? f : a.rot, a.rot, a.interleaved);
+            if (kind != have && gain && in) {
+                float g[8];
+                load8(g, gain + f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = x[p][i];
-        if (a.norm) {
-            float s = 0.f;
+                for (int i = 0; i < 8; ++i) {
+                    tn.c[i] *= g[i];
+                    if (MODE == kInterleaved) tn.s[i] *= g[i ^ 1];
+                    if (MODE == kAny && f + i < a.rot) tn.s[i] *= gain[partner<MODE>(f + i, a.rot, a.interleaved)];
+                }
+                if (MODE == kHalf && f < a.rot) {
+                    load8(g, gain + partner<MODE>(f, a.rot, 0));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s = fmaf(w[i], w[i], s);
-            const float r = 1.f / sqrtf(head_sum(s, a.lp) / (float)a.d + a.eps);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] *= r * (is_q ? gq[i] : gk[i]);
-        }
-        turn8<MODE, 1>(w, tn, f, a.rot, a.interleaved, bufs[MODE == kAny ? warp : 0], lane);
-        if (!known)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 0.f;
-        if (!in || h >= heads) continue;
-        if (is_q) store8(a.q_out.at(t, h) + f, w);
-        else if (!APPEND) store8(a.k_out.at(t, h - a.n_q) + f, w);
-        else if (!is_v && kc) store8(kc + (h - a.n_q) * a.head + f, w);
-        else if (is_v && vc) store8(vc + (h - a.n_q - a.n_kv) * a.head + f, x[p]);
-    }
-}
-
-// Persistent over units, so that a lane adds up its features' gain gradients in
-// registers, the block in shared memory; one partial per block.
-template <int MODE, typename T>
-__global__ void __launch_bounds__(32 * kWarps) bwd_kernel(const __grid_constant__ Args<T> a)
-{
-    constexpr int kP = 2;  // passes in flight: x and dy of each
-    __shared__ float bufs[kWarps][256];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int hp = 32 / a.lp, f = lane % a.lp * 8;
-    const int heads = a.n_q + a.n_kv;
-    const bool in = f < a.d;
-    float gq[8], gk[8], sq[8], sk[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) gq[i] = gk[i] = 1.f, sq[i] = sk[i] = 0.f;
-    if (in && a.gain_q) load8(gq, a.gain_q + f);
-    if (in && a.gain_k) load8(gk, a.gain_k + f);
-    for (int64_t u = (int64_t)blockIdx.x * kWarps + warp; u < a.tokens * a.per_token; u += (int64_t)gridDim.x * kWarps) {
-        const int64_t t = u / a.per_token;
-        const int pos = a.pos[t];
-        const bool known = pos >= 0 && pos < a.positions;
-        if (!known && lane == 0) raise_status(a.status, kStatusBadIndex);
-        Turn tn;
-        load_turn<MODE>(tn, a.table + (int64_t)(known ? pos : 0) * a.rot, in ? f : a.rot, a.rot, a.interleaved);
-#pragma unroll 1
-        for (int p0 = 0; p0 < kPasses; p0 += kP) {
-            float x[kP][8], w[kP][8];
-#pragma unroll
-            for (int p = 0; p < kP; ++p) {
-                const int h = (int)(u % a.per_token) * kPasses * hp + lane / a.lp + (p0 + p) * hp;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[p][i] = w[p][i] = 0.f;
-                if (in && h < heads) {
-                    load8(w[p], (h < a.n_q ? a.dq.at(t, h) : a.dk.at(t, h - a.n_q)) + f);
-                    if (a.norm) load8(x[p], (h < a.n_q ? a.q.at(t, h) : a.k.at(t, h - a.n_q)) + f);
+                    for (int i = 0; i < 8; ++i) tn.s[i] *= g[i];
                 }
             }
+            have = kind;
 #pragma unroll
-            for (int p = 0; p < kP; ++p) {
-                const int h = (int)(u % a.per_token) * kPasses * hp + lane / a.lp + (p0 + p) * hp;
-                const bool is_q = h < a.n_q, real = in && h < heads;
-                turn8<MODE, -1>(w[p], tn, f, a.rot, a.interleaved, bufs[warp], lane);
-                if (!known)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[p][i] = 0.f;
+            for (int p = 0; p < kPasses; ++p) {
+                const int h = h0 + p * hp;
+                float x[8], y[8];
+                r[p].get(x);
+                others<MODE>(y, r[p], x, f, a.rot, a.interleaved, bufs[MODE == kAny ? warp : 0], lane);
+                float scale = 1.f;
                 if (a.norm) {
                     float s = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s = fmaf(x[p][i], x[p][i], s);
-                    const float r = 1.f / sqrtf(head_sum(s, a.lp) / (float)a.d + a.eps);
+                    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+                    scale = rsqrtf(fmaf(head_sum(s, a.lp), a.inv_d, a.eps));
+                }
+                turn8<MODE>(x, y, tn, f, a.rot);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = known ? x[i] * scale : 0.f;
+                Raw<T> o;
+                o.set(x);
+                if (!in || h >= n) continue;
+                if (kind == 0) o.store(a.q_out.at(t, h) + f);
+                else if (!APPEND) o.store(a.k_out.at(t, h) + f);
+                else if (kc) o.store(kc + h * a.head + f);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) r[p] = next[p];
+    }
+}
+
+// Persistent over the batches of the queries, then of the keys, so that a lane adds up its
+// features' gain gradients in registers, the block in shared memory: one partial per block.
+template <int MODE, typename T>
+__global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_constant__ Args<T> a)
+{
+    __shared__ float bufs[kWarps][256];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int hp = 32 / a.lp, f = lane % a.lp * 8, own = lane / a.lp;
+    const bool in = f < a.d;
+    for (int kind = 0; kind < 2; ++kind) {
+        const Heads<const T> &xs = kind ? a.k : a.q, &ds = kind ? a.dk : a.dq;
+        const Heads<T> &out = kind ? a.k_out : a.q_out;
+        const float *gain = kind ? a.gain_k : a.gain_q;
+        const int n = kind ? a.n_kv : a.n_q, per = kind ? a.batches_kv : a.batches_q;
+        float g[8], sum[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = 1.f, sum[i] = 0.f;
+        if (gain && in) load8(g, gain + f);
+        const int64_t units = a.tokens * per, stride = (int64_t)gridDim.x * kWarps;
+        const int64_t u0 = (int64_t)blockIdx.x * kWarps + warp;
+        int pos = u0 < units ? a.pos[u0 / per] : 0;
+        for (int64_t u = u0; u < units; u += stride) {
+            const int64_t t = u / per;
+            const int h0 = (int)(u % per) * kPasses * hp + own;
+            Raw<T> rx[kPasses], rd[kPasses];
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p) {
+                rx[p].zero(), rd[p].zero();
+                if (in && h0 + p * hp < n) {
+                    rd[p].load(ds.at(t, h0 + p * hp) + f);
+                    if (a.norm) rx[p].load(xs.at(t, h0 + p * hp) + f);
+                }
+            }
+            const bool known = pos >= 0 && pos < a.positions;
+            if (!known && lane == 0) raise_status(a.status, kStatusBadIndex);
+            Turn tn;
+            load_turn<MODE, -1>(tn, a.table + (int64_t)(known ? pos : 0) * a.rot, known && in ? f : a.rot, a.rot, a.interleaved);
+            if (u + stride < units) pos = a.pos[(u + stride) / per];
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p) {
+                const bool real = in && h0 + p * hp < n;
+                float w[8], y[8];
+                rd[p].get(w);
+                others<MODE>(y, rd[p], w, f, a.rot, a.interleaved, bufs[warp], lane);
+                turn8<MODE>(w, y, tn, f, a.rot);
+                if (!known)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = 0.f;
+                if (a.norm) {
+                    float x[8], s = 0.f;
+                    rx[p].get(x);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+                    const float scale = rsqrtf(fmaf(head_sum(s, a.lp), a.inv_d, a.eps));
                     s = 0.f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        x[p][i] *= r;
-                        const float g = w[p][i] * x[p][i];
-                        if (real && is_q) sq[i] += g;
-                        if (real && !is_q) sk[i] += g;
-                        w[p][i] *= is_q ? gq[i] : gk[i];
-                        s = fmaf(w[p][i], x[p][i], s);
+                        x[i] *= scale;
+                        sum[i] = fmaf(w[i], x[i], sum[i]);  // 0 in lanes without a head
+                        w[i] *= g[i];
+                        s = fmaf(w[i], x[i], s);
                     }
-                    s = head_sum(s, a.lp) / (float)a.d;
+                    s = head_sum(s, a.lp) * a.inv_d;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) w[p][i] = r * (w[p][i] - x[p][i] * s);
+                    for (int i = 0; i < 8; ++i) w[i] = scale * fmaf(-x[i], s, w[i]);
                 }
-                if (!real) continue;
-                if (is_q) store8(a.q_out.at(t, h) + f, w[p]);
-                else store8(a.k_out.at(t, h - a.n_q) + f, w[p]);
+                Raw<T> o;
+                o.set(w);
+                if (real) o.store(out.at(t, h0 + p * hp) + f);
             }
         }
-    }
-    if (!a.part) return;
-    // over the heads side by side in the warp, then over the warps, in order
-    for (int which = 0; which < 2; ++which) {
+        if (!a.part) continue;
+        // over the heads side by side in the warp, then over the warps, in order
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bufs[warp][lane * 8 + i] = which ? sk[i] : sq[i];
+        for (int i = 0; i < 8; ++i) bufs[warp][lane * 8 + i] = sum[i];
         __syncthreads();
         for (int e = threadIdx.x; e < a.d; e += 32 * kWarps) {
             float s = 0.f;
             for (int w = 0; w < kWarps; ++w)
-                for (int g = 0; g < hp; ++g) s += bufs[w][g * a.lp * 8 + e];
-            a.part[((int64_t)blockIdx.x * 2 + which) * a.d + e] = s;
+                for (int j = 0; j < hp; ++j) s += bufs[w][j * a.lp * 8 + e];
+            a.part[((int64_t)blockIdx.x * 2 + kind) * a.d + e] = s;
         }
+        __syncthreads();
     }
 }
 
