@@ -339,7 +339,7 @@ bool attn_use_tc(const noble_attn_desc *d, std::initializer_list<std::pair<const
 }
 
 template <int DP, bool GENERAL>
-noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4], float *delta, const int2 *ranges, cudaStream_t st)
+noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4], float *delta, cudaStream_t st)
 {
     namespace t = attn::tc;
     using B = t::Bwd<DP>;
@@ -347,7 +347,7 @@ noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4
     if (!registers_at_least<dq>(168) || !registers_at_least<dkv>(168)) return fail(NOBLE_ERR_CUDA, "attn_bwd: registers");
     NOBLE_TRY((allow<dq>(B::kDynamic)));
     NOBLE_TRY((allow<dkv>(B::kDynamic)));
-    t::BwdArgs f{a, delta, ranges, (int)ceil_div(a.mask.T, t::kRows), status_ptr()};
+    t::BwdArgs f{a, delta, (int)ceil_div(a.mask.T, t::kRows), status_ptr()};
     if (!f.status) return fail(NOBLE_ERR_CUDA, "status word address");
     if ((int64_t)f.tiles * a.n_q > INT32_MAX) return fail(NOBLE_ERR_UNSUPPORTED, "%d tokens of %d heads", a.mask.T, a.n_q);
     NOBLE_TRY(run(st, {"attn_dq", kBoundTensor, 0.0, 0.0},
@@ -368,17 +368,16 @@ noble_status attn_bwd(const attn::RowArgs<T> &a, float *delta, int2 *ranges, cud
 }
 
 noble_status attn_bwd_tc(const noble_attn_desc *d, const attn::RowArgs<bf> &a, const noble_heads *q, const noble_heads *d_o,
-                         const noble_heads *k, const noble_heads *v, float *delta, int2 *ranges, cudaStream_t st)
+                         const noble_heads *k, const noble_heads *v, float *delta, cudaStream_t st)
 {
     CUtensorMap maps[4];
     NOBLE_TRY(make_heads_map(&maps[0], q, d->T, d->n_q, d->d));
     NOBLE_TRY(make_heads_map(&maps[1], d_o, d->T, d->n_q, d->d));
     NOBLE_TRY(make_heads_map(&maps[2], k, d->T, d->n_kv, d->d));
     NOBLE_TRY(make_heads_map(&maps[3], v, d->T, d->n_kv, d->d));
-    NOBLE_TRY(attn_prep<bf>(a, delta, ranges, st));
     if (general_scores(a.score))
-        return d->d <= 64 ? attn_bwd_tc<64, true>(a, maps, delta, ranges, st) : attn_bwd_tc<128, true>(a, maps, delta, ranges, st);
-    return d->d <= 64 ? attn_bwd_tc<64, false>(a, maps, delta, ranges, st) : attn_bwd_tc<128, false>(a, maps, delta, ranges, st);
+        return d->d <= 64 ? attn_bwd_tc<64, true>(a, maps, delta, st) : attn_bwd_tc<128, true>(a, maps, delta, st);
+    return d->d <= 64 ? attn_bwd_tc<64, false>(a, maps, delta, st) : attn_bwd_tc<128, false>(a, maps, delta, st);
 }
 
 // ---------------------------------------------------------------- attention over the cache
@@ -698,7 +697,7 @@ noble_status noble_attn_bwd(const noble_attn_desc *desc, const noble_heads *d_o,
         int2 *ranges = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + attn_work(desc).ranges);
         if constexpr (std::is_same_v<E, bf>)
             if (attn_use_tc(desc, {{q, desc->n_q}, {d_o, desc->n_q}, {k, desc->n_kv}, {v, desc->n_kv}}))
-                return attn_bwd_tc(desc, a, q, d_o, k, v, delta, ranges, (cudaStream_t)stream);
+                return attn_bwd_tc(desc, a, q, d_o, k, v, delta, (cudaStream_t)stream);
         return attn_bwd<E>(a, delta, ranges, (cudaStream_t)stream);
     };
     return desc->dtype == NOBLE_BF16 ? go(bf{}) : go(float{});

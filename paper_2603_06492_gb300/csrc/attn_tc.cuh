@@ -160,7 +160,9 @@ __device__ __forceinline__ void setmaxnreg_dec() { asm volatile("setmaxnreg.dec.
 // ---------------------------------------------------------------- work handed out by the launch
 // A block that has finished its piece of work takes over that of a block of the grid
 // that has not started (cluster launch control), so that blocks set up once and
-// pieces of unequal size balance.  One warp asks, ahead of need; everyone reads.
+// pieces of unequal size balance.  One thread asks, works out what the piece is and
+// publishes that in one of two slots of shared memory, a piece ahead of its readers:
+// it asks again when the loading thread has taken the last one.
 __device__ __forceinline__ void ask_next(uint32_t slot, uint32_t bar)
 {
     asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(slot),
@@ -182,6 +184,66 @@ __device__ __forceinline__ int read_next(uint32_t slot)
         : "memory");
     return x;
 }
+
+struct Piece {
+    int v[8];  // v[0] < 0: none left
+};
+struct Work {
+    uint32_t mem;  // 6 barriers (answer, taken, full and empty by slot), the answer, two pieces
+    static constexpr uint32_t kBytes = 48 + 16 + 2 * 32;
+    __device__ __forceinline__ uint32_t answered() const { return mem; }
+    __device__ __forceinline__ uint32_t taken() const { return mem + 8; }
+    __device__ __forceinline__ uint32_t full(int s) const { return mem + 16 + 8 * s; }
+    __device__ __forceinline__ uint32_t empty(int s) const { return mem + 32 + 8 * s; }
+    __device__ __forceinline__ uint32_t answer() const { return mem + 48; }
+    __device__ __forceinline__ uint32_t slot(int s) const { return mem + 64 + 32 * s; }
+    __device__ __forceinline__ void init(int readers) const
+    {
+        ptx::mbar_init(answered(), 1);
+        ptx::mbar_init(taken(), 1);
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(full(s), 1);
+            ptx::mbar_init(empty(s), readers);
+        }
+    }
+    // The thread that hands out; describe(index) is the piece of a block.
+    template <class F>
+    __device__ __forceinline__ void hand_out(F &&describe, uint32_t *status) const
+    {
+        int work = blockIdx.x;
+        for (int k = 0;; ++k) {
+            Piece p;
+            if (work >= 0) p = describe(work);
+            else p.v[0] = -1;
+            const uint32_t at = slot(k & 1);
+            if (!ptx::mbar_wait(empty(k & 1), ((k >> 1) & 1) ^ 1, status)) break;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p.v[0]), "r"(p.v[1]), "r"(p.v[2]), "r"(p.v[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16), "r"(p.v[4]), "r"(p.v[5]), "r"(p.v[6]), "r"(p.v[7]) : "memory");
+            ptx::mbar_arrive(full(k & 1));
+            if (work < 0) break;  // no more is asked after the first "none left"
+            if (!ptx::mbar_wait(taken(), k & 1, status)) break;
+            ptx::mbar_arrive_expect_tx(answered(), 16);
+            ask_next(answer(), answered());
+            if (!ptx::mbar_wait(answered(), k & 1, status)) break;
+            work = read_next(answer());
+            ptx::fence_proxy_async_smem();
+        }
+    }
+    // Piece k for a reader, `whole` warps together; false when there is none left.
+    __device__ __forceinline__ bool take(Piece &p, int k, bool whole, bool loader, int lane, uint32_t *status) const
+    {
+        bool ok = ptx::mbar_wait(full(k & 1), (k >> 1) & 1, status);
+        if (whole) ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return false;
+        const uint32_t at = slot(k & 1);
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(p.v[0]), "=r"(p.v[1]), "=r"(p.v[2]), "=r"(p.v[3]) : "r"(at) : "memory");
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(p.v[4]), "=r"(p.v[5]), "=r"(p.v[6]), "=r"(p.v[7]) : "r"(at + 16) : "memory");
+        if (whole) __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(empty(k & 1));
+        if (loader && p.v[0] >= 0) ptx::mbar_arrive(taken());
+        return p.v[0] >= 0;
+    }
+};
 
 // The document starts (and prefixes) in shared memory where they fit, since every
 // piece of work searches them; call with all threads, before a __syncthreads.

@@ -26,9 +26,8 @@ namespace tc {
 
 struct BwdArgs {
     RowArgs<__nv_bfloat16> a;
-    float *delta;        // [n_q][T]
-    const int2 *ranges;  // [T]
-    int tiles;           // of 128 tokens
+    float *delta;  // [n_q][T]: sum of o do, by dq_kernel for dkv_kernel
+    int tiles;     // of 128 tokens
     uint32_t *status;
 };
 
@@ -43,9 +42,9 @@ struct Bwd {
     static constexpr uint32_t kVec = kDocs + 2 * kDocsInSmem * 4;  // lse, delta [128], ranges [128], all visible
     static constexpr uint32_t kVecBytes = 128 * 16 + 16;
     static constexpr uint32_t kBars = kVec + kStages * kVecBytes;
-    static constexpr int kNumBars = 6 * kStages + 16;
+    static constexpr int kNumBars = 6 * kStages + 12;
     static constexpr uint32_t kWork = kBars + 8 * kNumBars;
-    static constexpr uint32_t kBytes = kWork + 32 + 16;
+    static constexpr uint32_t kBytes = kWork + Work::kBytes + 16;
     static constexpr uint32_t kDynamic = kBytes + 1024;
 };
 
@@ -95,6 +94,11 @@ __device__ __forceinline__ float score2(const Score &sc, float slope, float sl, 
     return fmaf(-slope, fabsf((float)far), y * kLog2e);
 }
 
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b)
+{
+    return fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), __uint_as_float(a & 0xffff0000u) * __uint_as_float(b & 0xffff0000u));
+}
+
 // ---------------------------------------------------------------- dq
 template <int DP, bool GENERAL>
 __global__ void __launch_bounds__(Bwd<DP>::kThreads, 1)
@@ -117,10 +121,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     const uint32_t q_full = one, q_empty = one + 8, dp_full = one + 16, dp_read = one + 24, ds_full = one + 32, acc_full = one + 40,
                    acc_empty = one + 48, sums = one + 56;
     auto s_full = [&](int i) { return one + 64 + 8u * (i & 1); };  // by buffer: the next S does not wait for this one's readers
-    auto w_full = [&](int s) { return one + 80 + 8u * s; };
-    auto w_empty = [&](int s) { return one + 96 + 8u * s; };
-    auto w_slot = [&](int s) { return base + B::kWork + 16u * s; };
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + 32);
+    const Work works{base + B::kWork};
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
     float *part = reinterpret_cast<float *>(smem + B::kVec);  // [2][128]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     uint32_t *status = args.status;
@@ -146,10 +148,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         ptx::mbar_init(acc_full, 1);
         ptx::mbar_init(acc_empty, 8);
         ptx::mbar_init(sums, 8);
-        for (int s = 0; s < 2; ++s) {
-            ptx::mbar_init(w_full(s), 1);
-            ptx::mbar_init(w_empty(s), 10);
-        }
+        works.init(10);
         ptx::fence_barrier_init();
     }
     if (warp == 9) {
@@ -162,33 +161,17 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     ptx::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    int asked = 0;
-    auto next_work = [&](bool &ok) {
-        const int s = asked & 1;
-        ok = ptx::mbar_wait(w_full(s), (asked >> 1) & 1, status);
-        if (warp < 8) ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return -1;
-        const int x = read_next(w_slot(s));
-        ptx::fence_proxy_async_smem();
-        if (warp < 8) __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(w_empty(s));
-        ++asked;
-        return x;
+    // piece of work: 128 queries from i0 of head h over keys from lo, `steps` tiles
+    struct Rows {
+        int i0, h, g, lo, steps;
     };
-    // piece of work: 128 queries from i0 of head h over keys [lo, hi)
-    struct Piece {
-        int i0, h, g, lo, hi, steps;
+    auto as_rows = [](const Piece &p) { return Rows{p.v[0], p.v[1], p.v[2], p.v[3], p.v[4]}; };
+    auto describe = [&](int work) {
+        const int h = work % args.a.n_q, i0 = (args.tiles - 1 - work / args.a.n_q) * kRows;
+        const int lo = visible(mask, i0).lo, hi = visible(mask, min(i0 + kRows, mask.T) - 1).hi;
+        return Piece{{i0, h, h / (args.a.n_q / args.a.n_kv), lo, (max(hi - lo, 0) + kRows - 1) / kRows, 0, 0, 0}};
     };
-    auto piece = [&](int work) {
-        Piece p;
-        p.h = work % args.a.n_q;
-        p.g = p.h / (args.a.n_q / args.a.n_kv);
-        p.i0 = (args.tiles - 1 - work / args.a.n_q) * kRows;
-        p.lo = visible(mask, p.i0).lo;
-        p.hi = visible(mask, min(p.i0 + kRows, mask.T) - 1).hi;
-        p.steps = (max(p.hi - p.lo, 0) + kRows - 1) / kRows;
-        return p;
-    };
+    Piece pc;
 
     if (warp >= 8) {
         setmaxnreg_dec<88>();
@@ -196,8 +179,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             // ---------------- loads
             int n = 0, items = 0, nk = 0;
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Piece p = piece(work);
+            for (int w = 0; ok && works.take(pc, w, false, true, 0, status); ++w) {
+                const Rows p = as_rows(pc);
                 if (!p.steps) continue;
                 ok = ptx::mbar_wait(q_empty, (items & 1) ^ 1, status);
                 if (!ok) break;
@@ -229,8 +212,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_q = ptx::idesc_bf16(128, DP, false, true);
             int n = 0, items = 0;
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Piece p = piece(work);
+            for (int w = 0; ok && works.take(pc, w, false, false, 0, status); ++w) {
+                const Rows p = as_rows(pc);
                 if (!p.steps) continue;
                 ok = ptx::mbar_wait(q_full, items & 1, status);
                 if (!ok) break;
@@ -286,16 +269,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             // every product has finished before TMEM is released below
             if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
-            // ---------------- work
-            for (int i = 0;; ++i) {
-                const int s = i & 1;
-                if (!ptx::mbar_wait(w_empty(s), ((i >> 1) & 1) ^ 1, status)) break;
-                ptx::mbar_arrive_expect_tx(w_full(s), 16);
-                ask_next(w_slot(s), w_full(s));
-                if (!ptx::mbar_wait(w_full(s), (i >> 1) & 1, status)) break;
-                if (read_next(w_slot(s)) < 0) break;
-                ptx::fence_proxy_async_smem();
-            }
+            works.hand_out(describe, status);
         }
         __syncwarp();
     } else {
@@ -306,15 +280,45 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         const float sl = args.a.score.scale * kLog2e;
         uint32_t n = 0, items = 0, nsums = 0;
         bool ok = true;
-        for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-            const Piece p = piece(work);
+        for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
+            const Rows p = as_rows(pc);
             const int i = p.i0 + row;
             const bool real = i < mask.T;
             const int64_t at = (int64_t)p.h * mask.T + (real ? i : 0);
             const Range rg = real ? visible(mask, i) : Range{0, 0};
             const bool none = rg.lo >= rg.hi;
             const float lse2 = none ? 0.f : args.a.lse[at] * kLog2e;
-            float delta = none ? 0.f : args.delta[at];
+            // delta: half of its features by each thread of a row, exchanged as below
+            float delta = 0.f;
+            if (real) {
+                const __nv_bfloat16 *o = args.a.o.at(i, p.h) + half * (DP / 2), *d_o = args.a.d_o.at(i, p.h) + half * (DP / 2);
+#pragma unroll
+                for (int f = 0; f < DP / 2; f += 8) {
+                    if (half * (DP / 2) + f >= args.a.d) break;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(o + f), y = *reinterpret_cast<const uint4 *>(d_o + f);
+                    delta += dot2(x.x, y.x) + dot2(x.y, y.y) + dot2(x.z, y.z) + dot2(x.w, y.w);
+                }
+            }
+            auto exchange = [&](float v) {  // the sum over both threads of a row
+                part[128 * half + row] = v;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(sums);
+                ok = ptx::mbar_wait(sums, nsums & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                ++nsums;
+                const float total = part[row] + part[128 + row];
+                // both have read it before either writes the next
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(sums);
+                ok = ok && ptx::mbar_wait(sums, nsums & 1, status);
+                ok = __all_sync(0xffffffffu, ok);
+                ++nsums;
+                return total;
+            };
+            delta = exchange(delta);
+            if (!ok) break;
+            if (none) delta = 0.f;
+            if (half == 0 && real) args.delta[at] = delta;
             const float slope = GENERAL && args.a.score.slope ? args.a.score.slope[p.h] * kLog2e : 0.f;
             for (int t = 0; t < p.steps; ++t, ++n) {
                 const uint32_t tS = tmem + lanes + (n & 1 ? kS1 : kS0) + 64 * half, tP = tmem + lanes + kDP + 64 * half;
@@ -365,14 +369,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                         if (GENERAL) q = c >= lo && c < hi ? exp2_fast(score2<true>(args.a.score, slope, sl, s[c], i - j0 - c, g) - lse2) : 0.f;
                         sum = GENERAL && q == 0.f ? sum : fmaf(q, dp[c], sum);
                     }
-                    part[128 * half + row] = sum;
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(sums);
-                    ok = ptx::mbar_wait(sums, nsums & 1, status);
-                    ok = __all_sync(0xffffffffu, ok);
+                    delta = exchange(sum);
                     if (!ok) break;
-                    ++nsums;
-                    delta = part[row] + part[128 + row];
                     if (half == 0 && !none) args.delta[at] = delta;
                 }
                 if (!GENERAL) {
@@ -481,10 +479,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     const uint32_t one = bars + 8u * (6 * kStages);
     const uint32_t kv_full = one, kv_empty = one + 8, s_full = one + 16, dp_full = one + 24, p_full = one + 32, ds_full = one + 40,
                    acc_full = one + 48, acc_empty = one + 56;
-    auto w_full = [&](int s) { return one + 64 + 8u * s; };
-    auto w_empty = [&](int s) { return one + 80 + 8u * s; };
-    auto w_slot = [&](int s) { return base + B::kWork + 16u * s; };
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + 32);
+    const Work works{base + B::kWork};
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
@@ -509,10 +505,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         ptx::mbar_init(ds_full, 8);
         ptx::mbar_init(acc_full, 1);
         ptx::mbar_init(acc_empty, 8);
-        for (int s = 0; s < 2; ++s) {
-            ptx::mbar_init(w_full(s), 1);
-            ptx::mbar_init(w_empty(s), 11);
-        }
+        works.init(11);
         ptx::fence_barrier_init();
     }
     if (warp == 9) {
@@ -526,36 +519,19 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     const uint32_t tmem = *tmem_slot;
     const int group = args.a.n_q / args.a.n_kv;
 
-    // lane 0 of warps 8 and 9, whole warps 0-7 and 10
-    int asked = 0;
-    auto next_work = [&](bool &ok) {
-        const int s = asked & 1;
-        const bool whole = warp < 8 || warp == 10;
-        ok = ptx::mbar_wait(w_full(s), (asked >> 1) & 1, status);
-        if (whole) ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return -1;
-        const int x = read_next(w_slot(s));
-        ptx::fence_proxy_async_smem();
-        if (whole) __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(w_empty(s));
-        ++asked;
-        return x;
-    };
     // piece of work: 128 keys from j0 of key head g, over query tiles from lo, `per` of a
     // head and `steps` in all
-    struct Piece {
+    struct Keys {
         int j0, g, lo, per, steps;
     };
-    auto piece = [&](int work) {
-        Piece p;
-        p.g = work % args.a.n_kv;
-        p.j0 = work / args.a.n_kv * kRows;
-        const Range r = queries_of(mask, p.j0, p.j0 + kRows);
-        p.lo = r.lo;
-        p.per = (max(r.hi - r.lo, 0) + kRows - 1) / kRows;
-        p.steps = p.per * group;
-        return p;
+    auto as_keys = [](const Piece &p) { return Keys{p.v[0], p.v[1], p.v[2], p.v[3], p.v[4]}; };
+    auto describe = [&](int work) {
+        const int g = work % args.a.n_kv, j0 = work / args.a.n_kv * kRows;
+        const Range r = queries_of(mask, j0, j0 + kRows);
+        const int per = (max(r.hi - r.lo, 0) + kRows - 1) / kRows;
+        return Piece{{j0, g, r.lo, per, per * group, 0, 0, 0}};
     };
+    Piece pc;
 
     if (warp >= 8) {
         setmaxnreg_dec<88>();
@@ -563,8 +539,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             // ---------------- loads
             int n = 0, items = 0, nq = 0;
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Piece p = piece(work);
+            for (int w = 0; ok && works.take(pc, w, false, true, 0, status); ++w) {
+                const Keys p = as_keys(pc);
                 if (!p.steps) continue;
                 ok = ptx::mbar_wait(kv_empty, (items & 1) ^ 1, status);
                 if (!ok) break;
@@ -596,8 +572,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_d = ptx::idesc_bf16(128, DP, false, true);
             int n = 0, items = 0;
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Piece p = piece(work);
+            for (int w = 0; ok && works.take(pc, w, false, false, 0, status); ++w) {
+                const Keys p = as_keys(pc);
                 if (!p.steps) continue;
                 const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
                                dy = desc_k(base + B::kY), mx = desc_mn(base + B::kX), my = desc_mn(base + B::kY);
@@ -644,43 +620,51 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             // ---------------- lse, delta and ranges of the query tiles
             int n = 0;
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Piece p = piece(work);
+            for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
+                const Keys p = as_keys(pc);
+                // a step's values are on their way while the stage before is waited for
+                float lse[4], delta[4];
+                bool all = false;
+                auto fetch = [&](int t) {
+                    const int h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows;
+                    // by the order of the ranges: whether every query of the tile sees every key
+                    all = i0 + kRows <= mask.T && visible(mask, i0).hi >= p.j0 + kRows && visible(mask, i0 + kRows - 1).lo <= p.j0;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int i = i0 + lane + 32 * u;
+                        const int64_t at = (int64_t)h * mask.T + i;
+                        lse[u] = i < mask.T ? args.a.lse[at] : 0.f;
+                        delta[u] = i < mask.T ? args.delta[at] : 0.f;
+                    }
+                };
+                if (p.steps) fetch(0);
                 for (int t = 0; t < p.steps; ++t, ++n) {
-                    const int st = n % kStages, h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows;
+                    const int st = n % kStages, i0 = p.lo + t % p.per * kRows;
                     ok = ptx::mbar_wait(vec_empty(st), ((n / kStages) & 1) ^ 1, status);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     float *vec = reinterpret_cast<float *>(smem + B::kVec + st * B::kVecBytes);
                     int2 *rg = reinterpret_cast<int2 *>(vec + 256);
-                    bool all = true;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         const int e = lane + 32 * u, i = i0 + e;
-                        const int2 r = i < mask.T ? args.ranges[i] : make_int2(0, 0);
-                        const bool sees = r.x < r.y;
-                        vec[e] = sees ? args.a.lse[(int64_t)h * mask.T + i] * kLog2e : 0.f;
-                        vec[128 + e] = sees ? args.delta[(int64_t)h * mask.T + i] : 0.f;
-                        rg[e] = r;
-                        all = all && r.x <= p.j0 && r.y >= p.j0 + kRows;
+                        bool sees = all;
+                        if (!all) {
+                            const Range r = i < mask.T ? visible(mask, i) : Range{0, 0};
+                            rg[e] = make_int2(r.lo, r.hi);
+                            sees = r.lo < r.hi;
+                        }
+                        vec[e] = sees ? lse[u] * kLog2e : 0.f;
+                        vec[128 + e] = sees ? delta[u] : 0.f;
                     }
-                    all = __all_sync(0xffffffffu, all);
                     if (lane == 0) *reinterpret_cast<int *>(vec + 512) = all;
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(vec_full(st));
+                    if (t + 1 < p.steps) fetch(t + 1);
                 }
             }
         } else if (warp == 11 && lane == 0) {
-            // ---------------- work
-            for (int i = 0;; ++i) {
-                const int s = i & 1;
-                if (!ptx::mbar_wait(w_empty(s), ((i >> 1) & 1) ^ 1, status)) break;
-                ptx::mbar_arrive_expect_tx(w_full(s), 16);
-                ask_next(w_slot(s), w_full(s));
-                if (!ptx::mbar_wait(w_full(s), (i >> 1) & 1, status)) break;
-                if (read_next(w_slot(s)) < 0) break;
-                ptx::fence_proxy_async_smem();
-            }
+            works.hand_out(describe, status);
         }
         __syncwarp();
     } else {
@@ -692,8 +676,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         const float sl = args.a.score.scale * kLog2e;
         uint32_t n = 0, items = 0;
         bool ok = true;
-        for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-            const Piece p = piece(work);
+        for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
+            const Keys p = as_keys(pc);
             const int j = p.j0 + row;
             for (int t = 0; t < p.steps; ++t, ++n) {
                 const int st = n % kStages;

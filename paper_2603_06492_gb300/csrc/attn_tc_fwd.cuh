@@ -7,7 +7,9 @@
 //     O += P V         P from TMEM, V MN-major in shared memory
 // Row blocks alternate on the tensor pipe: while one's warps compute P the pipe works on
 // the other's products, and each key tile is read from L2 once for 256 queries (32 bytes
-// per clock and SM at the full rate).  O stays in TMEM; it is scaled down only when a row's
+// per clock and SM at the full rate).  Score blocks go to as many buffers as TMEM has room
+// for beside O, three with heads of 64 features, so that S is there before its warps are.
+// O stays in TMEM; it is scaled down only when a row's
 // maximum has grown by more than 2^8 since the last time, which after the first tiles
 // happens rarely.  Sums and maxima are fp32; P is rounded to bf16 for the product (each
 // to 2^-9 of itself), its sum is that of the unrounded values.
@@ -21,17 +23,19 @@ namespace tc {
 
 template <int DP>
 struct Fwd {
-    static constexpr int kThreads = 384;  // two softmax warpgroups; TMA, MMA, work and a spare warp
+    static constexpr int kThreads = 384;  // two softmax warpgroups; loading, product and work threads, a spare warp
     static constexpr int kStages = DP == 64 ? 4 : 2;
+    static constexpr int kBuffers = DP == 64 ? 3 : 2;  // of 128 TMEM columns for S
     static constexpr uint32_t kTile = kChunk * (DP / 64);
     static constexpr uint32_t kQ = 0, kK = 2 * kTile, kV = kK + kStages * kTile, kDocs = kV + kStages * kTile;
-    static constexpr uint32_t kBars = kDocs + 2 * kDocsInSmem * 4;
-    // barriers: q full/empty, k and v full/empty by stage, s full, p full, pv done by row block, work full/empty
-    static constexpr int kNumBars = 2 + 4 * kStages + 6 + 4;
-    static constexpr uint32_t kWork = kBars + 8 * ((kNumBars + 1) & ~1);  // two 16-byte answers
-    static constexpr uint32_t kBytes = kWork + 32 + 16;
+    static constexpr uint32_t kWork = kDocs + 2 * kDocsInSmem * 4, kBars = kWork + Work::kBytes;
+    // q full/empty; k and v full/empty by stage; s full by row block and its own count of
+    // score blocks (a phase of another's would be taken for one of its own); p full by
+    // buffer; pv done by row block
+    static constexpr int kNumBars = 2 + 4 * kStages + 3 * kBuffers + 2;
+    static constexpr uint32_t kBytes = kBars + 8 * kNumBars + 16;
     static constexpr uint32_t kDynamic = kBytes + 1024;
-    static constexpr uint32_t kS = 0, kO = 256;  // TMEM columns: S of A and B, then O of A and B
+    static constexpr uint32_t kO = 128 * kBuffers;  // TMEM column of O
 };
 
 struct FwdArgs {
@@ -40,33 +44,29 @@ struct FwdArgs {
     uint32_t *status;
 };
 
-// Key tiles of a row block, counted from the first key that its piece of work sees.
+// Key tiles of a row block, counted from the first key that its piece of work sees: A
+// has the tiles [0, a1), B [b0, b1), with none in between that neither has.
 struct Span {
-    int i0, h, g, first, a0, a1, b0, b1;  // first key; tiles [a0, a1) of A, [b0, b1) of B
-    __device__ __forceinline__ int begin() const { return a0; }
+    int i0, h, g, first, a1, b0, b1;
     __device__ __forceinline__ int end() const { return max(a1, b1); }
+    __device__ __forceinline__ bool in(int b, int t) const { return b ? t >= b0 && t < b1 : t < a1; }
+    // score blocks before that of (t, b), in the order A, B of a tile
+    __device__ __forceinline__ int before(int t, int b) const { return min(t + b, a1) + clampi(t, b0, b1) - b0; }
 };
+__device__ __forceinline__ Span as_span(const Piece &p) { return {p.v[0], p.v[1], p.v[2], p.v[3], p.v[4], p.v[5], p.v[6]}; }
 
-__device__ __forceinline__ Span fwd_span(const Mask &m, const FwdArgs &f, int work)
+__device__ __forceinline__ Piece fwd_piece(const Mask &m, const FwdArgs &f, int work)
 {
-    Span s;
-    s.h = work % f.a.n_q;
-    s.g = s.h / (f.a.n_q / f.a.n_kv);
-    s.i0 = (f.tiles - 1 - work / f.a.n_q) * 256;
-    const int iA = min(s.i0 + 127, m.T - 1), iB = min(s.i0 + 255, m.T - 1);
-    const Range r0 = visible(m, s.i0), rA = visible(m, iA);
-    s.first = r0.lo;
-    s.a0 = 0;
-    s.a1 = (max(rA.hi - s.first, 0) + kRows - 1) / kRows;
-    if (s.i0 + 128 < m.T) {
-        const Range q0 = visible(m, s.i0 + 128), qB = visible(m, iB);
-        s.b0 = (q0.lo - s.first) / kRows;
-        s.b1 = (max(qB.hi - s.first, 0) + kRows - 1) / kRows;
-        if (s.b1 < s.b0) s.b1 = s.b0;
-    } else {
-        s.b0 = s.b1 = s.a1;
+    const int h = work % f.a.n_q, i0 = (f.tiles - 1 - work / f.a.n_q) * 256;
+    const int first = visible(m, i0).lo;
+    int a1 = (max(visible(m, min(i0 + 127, m.T - 1)).hi - first, 0) + kRows - 1) / kRows, b0 = a1, b1 = a1;
+    if (i0 + 128 < m.T) {
+        b0 = (visible(m, i0 + 128).lo - first) / kRows;
+        b1 = (max(visible(m, min(i0 + 255, m.T - 1)).hi - first, 0) + kRows - 1) / kRows;
+        if (b1 <= b0) b0 = b1 = a1;
+        else a1 = max(a1, b0);
     }
-    return s;
+    return {{i0, h, h / (f.a.n_q / f.a.n_kv), first, a1, b0, b1, 0}};
 }
 
 // GENERAL: capped or biased scores, or a scale that is not positive.
@@ -87,13 +87,11 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     auto k_empty = [&](int s) { return bars + 8u * (2 + kStages + s); };
     auto v_full = [&](int s) { return bars + 8u * (2 + 2 * kStages + s); };
     auto v_empty = [&](int s) { return bars + 8u * (2 + 3 * kStages + s); };
-    auto s_full = [&](int b) { return bars + 8u * (2 + 4 * kStages + b); };
-    auto p_full = [&](int b) { return bars + 8u * (4 + 4 * kStages + b); };
-    auto pv_done = [&](int b) { return bars + 8u * (6 + 4 * kStages + b); };
-    auto w_full = [&](int s) { return bars + 8u * (8 + 4 * kStages + s); };
-    auto w_empty = [&](int s) { return bars + 8u * (10 + 4 * kStages + s); };
-    auto w_slot = [&](int s) { return base + F::kWork + 16u * s; };
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + F::kWork + 32);
+    auto s_full = [&](int b, int i) { return bars + 8u * (2 + 4 * kStages + b * F::kBuffers + i); };
+    auto p_full = [&](int i) { return bars + 8u * (2 + 4 * kStages + 2 * F::kBuffers + i); };
+    auto pv_done = [&](int b) { return bars + 8u * (2 + 4 * kStages + 3 * F::kBuffers + b); };
+    const Work works{base + F::kWork};
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + F::kBars + 8 * F::kNumBars);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
@@ -109,13 +107,13 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             ptx::mbar_init(v_full(s), 1);
             ptx::mbar_init(v_empty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            ptx::mbar_init(s_full(b), 1);
-            ptx::mbar_init(p_full(b), 4);
-            ptx::mbar_init(pv_done(b), 1);
-            ptx::mbar_init(w_full(b), 1);
-            ptx::mbar_init(w_empty(b), 10);
+        for (int i = 0; i < F::kBuffers; ++i) {
+            ptx::mbar_init(s_full(0, i), 1);
+            ptx::mbar_init(s_full(1, i), 1);
+            ptx::mbar_init(p_full(i), 4);
         }
+        for (int b = 0; b < 2; ++b) ptx::mbar_init(pv_done(b), 1);
+        works.init(10);
         ptx::fence_barrier_init();
     }
     if (warp == 9) {
@@ -128,31 +126,16 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     ptx::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    // The next piece of work for a reader of the answers: lane 0 of warps 8 and 9, or a
-    // whole softmax warp (whose lanes agree on it).
-    int asked = 0;
-    auto next_work = [&](bool &ok) {
-        const int s = asked & 1;
-        ok = ptx::mbar_wait(w_full(s), (asked >> 1) & 1, status);
-        if (warp < 8) ok = __all_sync(0xffffffffu, ok);
-        if (!ok) return -1;
-        const int x = read_next(w_slot(s));
-        ptx::fence_proxy_async_smem();
-        if (warp < 8) __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(w_empty(s));
-        ++asked;
-        return x;
-    };
-
+    Piece pc;
     if (warp >= 8) {
         setmaxnreg_dec<88>();
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, issued_k = 0;
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Span s = fwd_span(mask, args, work);
-                if (s.begin() >= s.end()) continue;
+            for (int w = 0; ok && works.take(pc, w, false, true, 0, status); ++w) {
+                const Span s = as_span(pc);
+                if (s.end() == 0) continue;
                 ok = ptx::mbar_wait(q_empty, (items & 1) ^ 1, status);
                 if (!ok) break;
                 ptx::mbar_arrive_expect_tx(q_full, 2 * F::kTile);
@@ -160,7 +143,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     for (int c = 0; c < kChunks; ++c)
                         tma_load_3d(base + F::kQ + b * F::kTile + c * kChunk, &mQ, q_full, 64 * c, s.h, s.i0 + 128 * b);
                 ++items;
-                for (int t = s.begin(); t < s.end(); ++t, ++n) {
+                for (int t = 0; t < s.end(); ++t, ++n) {
                     const int st = n % kStages;
                     const uint32_t ph = (n / kStages) & 1;
                     const int j = s.first + t * kRows;
@@ -184,73 +167,75 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         } else if (warp == 9 && lane == 0) {
             // ---------------- products
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_o = ptx::idesc_bf16(128, DP, false, true);
-            int n = 0, items = 0;       // key tiles and pieces of work so far
-            uint32_t np[2] = {0, 0};    // products P V so far, by row block
+            const uint32_t dq = desc_k(base + F::kQ), dk = desc_k(base + F::kK), dv = desc_mn(base + F::kV);
+            // Rings by index and parity, moved on without a division.
+            constexpr uint32_t kStep = F::kTile >> 4;
+            int items = 0;
+            uint32_t last = 0;                // the stage of the last key tile
+            uint32_t st_s = 0, ph_s = 0;      // stage of the next S
+            uint32_t st_v = 0, ph_v = 0;      // of the next P V
+            uint32_t buf_s = 0, buf_p = 0, ph_p = 0;  // score buffers of both
+            uint32_t of0 = 0, of1 = 0;        // the next s_full of A and of B
+            auto next = [](uint32_t i, uint32_t n) { return i + 1 == n ? 0u : i + 1; };
             bool ok = true;
-            for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-                const Span s = fwd_span(mask, args, work);
-                const int t0 = s.begin(), t1 = s.end();
-                if (t0 >= t1) continue;
+            for (int w = 0; ok && works.take(pc, w, false, false, 0, status); ++w) {
+                const Span s = as_span(pc);
+                const int t1 = s.end();
+                if (t1 == 0) continue;
                 ok = ptx::mbar_wait(q_full, items & 1, status);
                 ++items;
-                auto in = [&](int b, int t) { return b ? t >= s.b0 && t < s.b1 : t >= s.a0 && t < s.a1; };
-                const uint32_t dq = desc_k(base + F::kQ), dk = desc_k(base + F::kK), dv = desc_mn(base + F::kV);
-                auto score = [&](int b, int t) {  // S of row block b and tile t
-                    product_features<DP>(tmem + F::kS + 128 * b, dq + b * (F::kTile >> 4), dk + ((n + t - t0) % kStages) * (F::kTile >> 4), id_s);
-                    ptx::mma_commit(s_full(b));
-                };
-                auto wait_k = [&](int t) {
-                    const int i = n + t - t0;
-                    return ptx::mbar_wait(k_full(i % kStages), (i / kStages) & 1, status);
-                };
-                auto free_k = [&](int t) { ptx::mma_commit(k_empty((n + t - t0) % kStages)); };
-                ok = ok && wait_k(t0);
-                if (!ok) break;
-                ptx::tc_fence_after();
-                for (int b = 0; b < 2; ++b)
-                    if (in(b, t0)) score(b, t0);
-                free_k(t0);
-                if (t0 + 1 == t1) ptx::mma_commit(q_empty);
-                for (int t = t0; t < t1; ++t) {
-                    const int i = n + t - t0, st = i % kStages;
-                    if (t + 1 < t1) ok = wait_k(t + 1);
-                    ok = ok && ptx::mbar_wait(v_full(st), (i / kStages) & 1, status);
-                    if (!ok) break;
-                    for (int b = 0; b < 2 && ok; ++b) {
-                        if (in(b, t)) {
-                            ok = ptx::mbar_wait(p_full(b), np[b] & 1, status);
-                            if (!ok) break;
-                            ptx::tc_fence_after();
-                            const uint32_t p = tmem + F::kS + 128 * b;
-                            product_tokens(tmem + F::kO + DP * b, p, p + 32, dv + st * (F::kTile >> 4), id_o, t > (b ? s.b0 : s.a0));
-                            ptx::mma_commit(pv_done(b));
-                            ++np[b];
-                        }
+                int ts = 0;  // tile and row block of the next S
+                bool to_b = s.a1 == 0;
+                auto score = [&] {
+                    if (!to_b) {
+                        if (!ptx::mbar_wait(k_full(st_s), ph_s, status)) return false;
                         ptx::tc_fence_after();
-                        // over P, which the product above has read by then: products run in order
-                        if (t + 1 < t1 && in(b, t + 1)) score(b, t + 1);
+                        product_features<DP>(tmem + 128 * buf_s, dq, dk + st_s * kStep, id_s);
+                        ptx::mma_commit(s_full(0, of0));
+                        of0 = next(of0, F::kBuffers), buf_s = next(buf_s, F::kBuffers);
+                        if (ts >= s.b0 && ts < s.b1) {
+                            to_b = true;
+                            return true;
+                        }
+                    } else {
+                        if (ts >= s.a1 && !ptx::mbar_wait(k_full(st_s), ph_s, status)) return false;
+                        ptx::tc_fence_after();
+                        product_features<DP>(tmem + 128 * buf_s, dq + kStep, dk + st_s * kStep, id_s);
+                        ptx::mma_commit(s_full(1, of1));
+                        of1 = next(of1, F::kBuffers), buf_s = next(buf_s, F::kBuffers);
                     }
-                    if (!ok) break;
-                    ptx::mma_commit(v_empty(st));
-                    if (t + 1 < t1) free_k(t + 1);
-                    if (t + 2 == t1) ptx::mma_commit(q_empty);
+                    ptx::mma_commit(k_empty(st_s));
+                    st_s = next(st_s, kStages), ph_s ^= st_s == 0;
+                    ++ts;
+                    to_b = ts >= s.a1;
+                    if (ts == t1) ptx::mma_commit(q_empty);  // the last use of Q
+                    return true;
+                };
+                // P V of one row block; its buffer is then the next S's: products run in order
+                auto weigh = [&](uint32_t o, bool more, uint32_t done) {
+                    if (!ptx::mbar_wait(p_full(buf_p), ph_p, status)) return false;
+                    ptx::tc_fence_after();
+                    const uint32_t p = tmem + 128 * buf_p;
+                    product_tokens(o, p, p + 32, dv + st_v * kStep, id_o, more);
+                    ptx::mma_commit(done);
+                    buf_p = next(buf_p, F::kBuffers), ph_p ^= buf_p == 0;
+                    return ts == t1 || score();
+                };
+                for (int i = 0; ok && i < F::kBuffers && ts < t1; ++i) ok = score();
+                for (int t = 0; ok && t < t1; ++t) {
+                    ok = ptx::mbar_wait(v_full(st_v), ph_v, status);
+                    if (ok && t < s.a1) ok = weigh(tmem + F::kO, t > 0, pv_done(0));
+                    if (ok && t >= s.b0 && t < s.b1) ok = weigh(tmem + F::kO + DP, t > s.b0, pv_done(1));
+                    ptx::mma_commit(v_empty(st_v));
+                    last = 2 * st_v + ph_v + 1;
+                    st_v = next(st_v, kStages), ph_v ^= st_v == 0;
                 }
-                n += t1 - t0;
             }
             // every product has finished before TMEM is released below: commits complete in
             // order, and the last of a piece of work is that of its last V stage
-            if (n) ptx::mbar_wait(v_empty((n - 1) % kStages), ((n - 1) / kStages) & 1, nullptr);
+            if (last) ptx::mbar_wait(v_empty((last - 1) / 2), (last - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
-            // ---------------- work: one answer ahead; after the first "none left" no more is asked
-            for (int i = 0;; ++i) {
-                const int s = i & 1;
-                if (!ptx::mbar_wait(w_empty(s), ((i >> 1) & 1) ^ 1, status)) break;
-                ptx::mbar_arrive_expect_tx(w_full(s), 16);
-                ask_next(w_slot(s), w_full(s));
-                if (!ptx::mbar_wait(w_full(s), (i >> 1) & 1, status)) break;
-                if (read_next(w_slot(s)) < 0) break;
-                ptx::fence_proxy_async_smem();
-            }
+            works.hand_out([&](int work) { return fwd_piece(mask, args, work); }, status);
         }
         __syncwarp();
     } else {
@@ -258,19 +243,23 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         setmaxnreg_inc<208>();
         const int b = warp / 4;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
-        const uint32_t tS = tmem + lanes + F::kS + 128 * b, tO = tmem + lanes + F::kO + DP * b;
+        const uint32_t tO = tmem + lanes + F::kO + DP * b;
         const float sl = args.a.score.scale * kLog2e;
-        uint32_t ns = 0;  // score blocks so far
+        uint32_t ns = 0;  // score blocks so far: of this row block
+        int all = 0;      // and of both
         bool ok = true;
-        for (int work = blockIdx.x; ok && work >= 0; work = next_work(ok)) {
-            const Span s = fwd_span(mask, args, work);
-            const int i = s.i0 + threadIdx.x, t0 = b ? s.b0 : s.a0, t1 = b ? s.b1 : s.a1;
+        for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
+            const Span s = as_span(pc);
+            const int i = s.i0 + threadIdx.x, t0 = b ? s.b0 : 0, t1 = b ? s.b1 : s.a1;
             const Range rg = i < mask.T ? visible(mask, i) : Range{0, 0};
             const float slope = GENERAL && args.a.score.slope ? args.a.score.slope[s.h] * kLog2e : 0.f;
             float m = -INFINITY, l = 0.f;
             for (int t = t0; t < t1; ++t) {
                 const int j0 = s.first + t * kRows;
-                ok = ptx::mbar_wait(s_full(b), ns & 1, status);
+                const int nth = all + s.before(t, b);
+                const int buf = nth % F::kBuffers;
+                const uint32_t tS = tmem + lanes + 128 * buf;
+                ok = ptx::mbar_wait(s_full(b, ns % F::kBuffers), (ns / F::kBuffers) & 1, status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ptx::tc_fence_after();
@@ -343,13 +332,20 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
                     pk[c / 2 + 1] = ptx::pack_bf16x2(e[2], e[3]);
                 }
+                // one product P V of a row block at a time is outstanding, so that a phase of
+                // pv_done is never mistaken for the one before; by now it is done
+                if (ns > 0) {
+                    ok = ptx::mbar_wait(pv_done(b), (ns - 1) & 1, status);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                }
                 __syncwarp();
                 tmem_st32(tS, pk);
                 tmem_st32(tS + 32, pk + 32);
                 tmem_wait_st();
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(p_full(b));
+                if (lane == 0) ptx::mbar_arrive(p_full(buf));
                 ++ns;
                 float a0, a1, a2, a3;
                 unpack2(sum0, a0, a1);
@@ -357,6 +353,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 l += (a0 + a1) + (a2 + a3);
             }
             if (!ok) break;
+            all += s.a1 + s.b1 - s.b0;
             // ---------------- o and lse of this row
             const bool real = i < mask.T, none = rg.lo >= rg.hi;
             if (t1 > t0) {

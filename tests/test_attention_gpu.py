@@ -265,3 +265,19 @@ def test_gradients_against_differences(dtype, flags, softcap):
         diff = (value(*up) - value(*down)) / (2 * h)
         grad = got[2 + n].double()
         assert abs(float((grad * u).sum()) - diff) <= TOL[dtype] * float(grad.norm() * u.norm()) / math.sqrt(u.numel()) * 10
+
+
+@path
+@pytest.mark.parametrize("d", [64, 128])
+def test_several_pieces_per_block(d, dtype, flags):
+    """More work than a chip takes at once, of row blocks that see different key tiles: the
+    same documents side by side in many heads, each head as if it were alone."""
+    T, docs, n = 2000, [0, 260, 300, 301, 930, 1500, 1995], 40
+    q, k, v, d_o = _inputs(T, 2, 1, d, dtype)
+    wide = lambda x, m: x.repeat(1, m // x.shape[1], 1)  # noqa: E731
+    seen = ref.masks(T, docs, True, [100, 0, 0, 300, 7, 1], 150)
+    want = ref.attention(q, k, v, seen, 1 / math.sqrt(d), 0.0, None, d_o)
+    got = _run(wide(q, n), wide(k, n // 2), wide(v, n // 2), wide(d_o, n), docs, dtype,
+               prefix=[100, 0, 0, 300, 7, 1], window=150, flags=flags)
+    want = [wide(want[0], n), want[1].repeat(n // 2, 1), wide(want[2], n), wide(want[3], n // 2), wide(want[4], n // 2)]
+    _compare(got, want, dtype)
