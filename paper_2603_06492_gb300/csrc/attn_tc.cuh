@@ -30,7 +30,19 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
         : "memory");
 }
 
-// Products of one thread, whose every instruction delays the tensor pipe: descriptors
+// One lane of the warp, always the same.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(p));
+    return p != 0;
+}
+// A value that all lanes have, as one that the compiler knows they have.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+// Products are issued by one lane of a warp whose lanes otherwise stay together: operands
+// then are in uniform registers, which a product reads, and not moved there one by one
+// (65 clocks for each, as many as the tensor pipe takes for 128 columns).  Descriptors
 // are made of a low word per operand, to which a constant is added per step, and a
 // high word that all share (128-byte swizzle, 1024 bytes between groups of 8 rows).
 constexpr uint32_t kDescHigh = 64u | (1u << 14) | (2u << 29);
@@ -60,6 +72,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}\n" ::"r"(d_tmem),
         "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
         : "memory");
+}
+// A bounded wait of a whole warp: the same answer in all lanes.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint32_t *status)
+{
+    return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, status));
 }
 // D = A B^T over the features of two token tiles (DP of them)
 template <int DP>
@@ -238,7 +255,10 @@ struct Work {
         const uint32_t at = slot(k & 1);
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(p.v[0]), "=r"(p.v[1]), "=r"(p.v[2]), "=r"(p.v[3]) : "r"(at) : "memory");
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(p.v[4]), "=r"(p.v[5]), "=r"(p.v[6]), "=r"(p.v[7]) : "r"(at + 16) : "memory");
-        if (whole) __syncwarp();
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p.v[i] = (int)uniform((uint32_t)p.v[i]);
+        }
         if (lane == 0) ptx::mbar_arrive(empty(k & 1));
         if (loader && p.v[0] >= 0) ptx::mbar_arrive(taken());
         return p.v[0] >= 0;

@@ -124,7 +124,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
     float *part = reinterpret_cast<float *>(smem + B::kVec);  // [2][128]
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = (int)uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
     if (warp == 8 && lane == 0) {
@@ -159,7 +159,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = uniform(*tmem_slot);
 
     // piece of work: 128 queries from i0 of head h over keys from lo, `steps` tiles
     struct Rows {
@@ -207,36 +207,37 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             if (items) ptx::mbar_wait(q_full, (items - 1) & 1, nullptr);
             for (int i = max(nk - kStages, 0); i < nk; ++i) ptx::mbar_wait(k_full(i % kStages), (i / kStages) & 1, nullptr);
             for (int i = max(n - kStages, 0); i < n; ++i) ptx::mbar_wait(v_full(i % kStages), (i / kStages) & 1, nullptr);
-        } else if (warp == 9 && lane == 0) {
+        } else if (warp == 9) {
             // ---------------- products
+            const bool leader = elect_one();
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_q = ptx::idesc_bf16(128, DP, false, true);
             int n = 0, items = 0;
             bool ok = true;
-            for (int w = 0; ok && works.take(pc, w, false, false, 0, status); ++w) {
+            for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
                 const Rows p = as_rows(pc);
                 if (!p.steps) continue;
-                ok = ptx::mbar_wait(q_full, items & 1, status);
+                ok = wait_warp(q_full, items & 1, status);
                 if (!ok) break;
                 const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
                                dy = desc_k(base + B::kY), dm = desc_mn(base + B::kX);
                 constexpr uint32_t kStep = B::kTile >> 4;
                 auto score = [&](int i) {
-                    product_features<DP>(tmem + (i & 1 ? kS1 : kS0), dr0, dx + (i % kStages) * kStep, id_s);
-                    ptx::mma_commit(s_full(i));
+                    if (leader) product_features<DP>(tmem + (i & 1 ? kS1 : kS0), dr0, dx + (i % kStages) * kStep, id_s);
+                    if (leader) ptx::mma_commit(s_full(i));
                 };
                 auto dprob = [&](int i) {
-                    product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
-                    ptx::mma_commit(dp_full);
-                    ptx::mma_commit(v_empty(i % kStages));
-                    if (i == n + p.steps - 1) ptx::mma_commit(q_empty);  // the last use of Q and dO
+                    if (leader) product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
+                    if (leader) ptx::mma_commit(dp_full);
+                    if (leader) ptx::mma_commit(v_empty(i % kStages));
+                    if (i == n + p.steps - 1 && leader) ptx::mma_commit(q_empty);  // the last use of Q and dO
                 };
-                ok = ptx::mbar_wait(k_full(n % kStages), (n / kStages) & 1, status);
+                ok = wait_warp(k_full(n % kStages), (n / kStages) & 1, status);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 score(n);
                 // the last dP of the piece before is in registers
-                ok = ptx::mbar_wait(v_full(n % kStages), (n / kStages) & 1, status) &&
-                     (n == 0 || ptx::mbar_wait(dp_read, (n - 1) & 1, status));
+                ok = wait_warp(v_full(n % kStages), (n / kStages) & 1, status) &&
+                     (n == 0 || wait_warp(dp_read, (n - 1) & 1, status));
                 if (!ok) break;
                 ptx::tc_fence_after();
                 dprob(n);
@@ -245,29 +246,29 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                     if (t + 1 < p.steps) {
                         const int st = (i + 1) % kStages;
                         const uint32_t ph = ((i + 1) / kStages) & 1;
-                        ok = ptx::mbar_wait(k_full(st), ph, status);
+                        ok = wait_warp(k_full(st), ph, status);
                         if (!ok) break;
                         ptx::tc_fence_after();
                         score(i + 1);  // over the dS that the product before last has read
-                        ok = ptx::mbar_wait(v_full(st), ph, status) && ptx::mbar_wait(dp_read, i & 1, status);
+                        ok = wait_warp(v_full(st), ph, status) && wait_warp(dp_read, i & 1, status);
                         if (!ok) break;
                         ptx::tc_fence_after();
                         dprob(i + 1);
                     }
-                    ok = ptx::mbar_wait(ds_full, i & 1, status) &&
-                         (t > 0 || ptx::mbar_wait(acc_empty, (items & 1) ^ 1, status));
+                    ok = wait_warp(ds_full, i & 1, status) &&
+                         (t > 0 || wait_warp(acc_empty, (items & 1) ^ 1, status));
                     if (!ok) break;
                     ptx::tc_fence_after();
                     const uint32_t ds = tmem + (i & 1 ? kS1 : kS0);
-                    product_tokens(tmem + kAcc, ds, ds + 64, dm + (i % kStages) * kStep, id_q, t > 0);
-                    ptx::mma_commit(k_empty(i % kStages));
+                    if (leader) product_tokens(tmem + kAcc, ds, ds + 64, dm + (i % kStages) * kStep, id_q, t > 0);
+                    if (leader) ptx::mma_commit(k_empty(i % kStages));
                 }
-                ptx::mma_commit(acc_full);
+                if (leader) ptx::mma_commit(acc_full);
                 n += p.steps;
                 ++items;
             }
             // every product has finished before TMEM is released below
-            if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
+            if (items) wait_warp(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
             works.hand_out(describe, status);
         }
@@ -481,7 +482,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                    acc_full = one + 48, acc_empty = one + 56;
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = (int)uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
     if (warp == 8 && lane == 0) {
@@ -516,7 +517,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = uniform(*tmem_slot);
     const int group = args.a.n_q / args.a.n_kv;
 
     // piece of work: 128 keys from j0 of key head g, over query tiles from lo, `per` of a
@@ -567,55 +568,56 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             if (items) ptx::mbar_wait(kv_full, (items - 1) & 1, nullptr);
             for (int i = max(nq - kStages, 0); i < nq; ++i) ptx::mbar_wait(q_full(i % kStages), (i / kStages) & 1, nullptr);
             for (int i = max(n - kStages, 0); i < n; ++i) ptx::mbar_wait(o_full(i % kStages), (i / kStages) & 1, nullptr);
-        } else if (warp == 9 && lane == 0) {
+        } else if (warp == 9) {
             // ---------------- products
+            const bool leader = elect_one();
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_d = ptx::idesc_bf16(128, DP, false, true);
             int n = 0, items = 0;
             bool ok = true;
-            for (int w = 0; ok && works.take(pc, w, false, false, 0, status); ++w) {
+            for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
                 const Keys p = as_keys(pc);
                 if (!p.steps) continue;
                 const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
                                dy = desc_k(base + B::kY), mx = desc_mn(base + B::kX), my = desc_mn(base + B::kY);
                 constexpr uint32_t kStep = B::kTile >> 4;
                 auto score = [&](int i) {
-                    if (!ptx::mbar_wait(q_full(i % kStages), (i / kStages) & 1, status)) return false;
+                    if (!wait_warp(q_full(i % kStages), (i / kStages) & 1, status)) return false;
                     ptx::tc_fence_after();
-                    product_features<DP>(tmem + kS, dr0, dx + (i % kStages) * kStep, id_s);
-                    ptx::mma_commit(s_full);
+                    if (leader) product_features<DP>(tmem + kS, dr0, dx + (i % kStages) * kStep, id_s);
+                    if (leader) ptx::mma_commit(s_full);
                     return true;
                 };
                 auto dprob = [&](int i) {
-                    if (!ptx::mbar_wait(o_full(i % kStages), (i / kStages) & 1, status)) return false;
+                    if (!wait_warp(o_full(i % kStages), (i / kStages) & 1, status)) return false;
                     ptx::tc_fence_after();
-                    product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
-                    ptx::mma_commit(dp_full);
-                    if (i == n + p.steps - 1) ptx::mma_commit(kv_empty);  // the last use of K and V
+                    if (leader) product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
+                    if (leader) ptx::mma_commit(dp_full);
+                    if (i == n + p.steps - 1 && leader) ptx::mma_commit(kv_empty);  // the last use of K and V
                     return true;
                 };
-                ok = ptx::mbar_wait(kv_full, items & 1, status) && score(n) && dprob(n);
+                ok = wait_warp(kv_full, items & 1, status) && score(n) && dprob(n);
                 for (int t = 0; ok && t < p.steps; ++t) {
                     const int i = n + t;
-                    ok = ptx::mbar_wait(p_full, i & 1, status) && (t > 0 || ptx::mbar_wait(acc_empty, (items & 1) ^ 1, status));
+                    ok = wait_warp(p_full, i & 1, status) && (t > 0 || wait_warp(acc_empty, (items & 1) ^ 1, status));
                     if (!ok) break;
                     ptx::tc_fence_after();
-                    product_tokens(tmem + kDV, tmem + kS, tmem + kS + 64, my + (i % kStages) * kStep, id_d, t > 0);
-                    ptx::mma_commit(o_empty(i % kStages));
+                    if (leader) product_tokens(tmem + kDV, tmem + kS, tmem + kS + 64, my + (i % kStages) * kStep, id_d, t > 0);
+                    if (leader) ptx::mma_commit(o_empty(i % kStages));
                     if (t + 1 < p.steps) ok = score(i + 1);  // over P, read by then: products run in order
-                    ok = ok && ptx::mbar_wait(ds_full, i & 1, status);
+                    ok = ok && wait_warp(ds_full, i & 1, status);
                     if (!ok) break;
                     ptx::tc_fence_after();
-                    product_tokens(tmem + kDK, tmem + kDP, tmem + kDP + 64, mx + (i % kStages) * kStep, id_d, t > 0);
-                    ptx::mma_commit(q_empty(i % kStages));
+                    if (leader) product_tokens(tmem + kDK, tmem + kDP, tmem + kDP + 64, mx + (i % kStages) * kStep, id_d, t > 0);
+                    if (leader) ptx::mma_commit(q_empty(i % kStages));
                     if (t + 1 < p.steps) ok = dprob(i + 1);  // over dS
                 }
                 if (!ok) break;
-                ptx::mma_commit(acc_full);
+                if (leader) ptx::mma_commit(acc_full);
                 n += p.steps;
                 ++items;
             }
             // every product has finished before TMEM is released below
-            if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
+            if (items) wait_warp(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10) {
             // ---------------- lse, delta and ranges of the query tiles
             int n = 0;

@@ -92,7 +92,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     auto pv_done = [&](int b) { return bars + 8u * (2 + 4 * kStages + 3 * F::kBuffers + b); };
     const Work works{base + F::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + F::kBars + 8 * F::kNumBars);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int warp = (int)uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
     if (warp == 8 && lane == 0) {
@@ -124,7 +124,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = uniform(*tmem_slot);
 
     Piece pc;
     if (warp >= 8) {
@@ -164,8 +164,9 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             if (items) ptx::mbar_wait(q_full, (items - 1) & 1, nullptr);
             for (int i = max(issued_k - kStages, 0); i < issued_k; ++i) ptx::mbar_wait(k_full(i % kStages), (i / kStages) & 1, nullptr);
             for (int i = max(n - kStages, 0); i < n; ++i) ptx::mbar_wait(v_full(i % kStages), (i / kStages) & 1, nullptr);
-        } else if (warp == 9 && lane == 0) {
+        } else if (warp == 9) {
             // ---------------- products
+            const bool leader = elect_one();
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_o = ptx::idesc_bf16(128, DP, false, true);
             const uint32_t dq = desc_k(base + F::kQ), dk = desc_k(base + F::kK), dv = desc_mn(base + F::kV);
             // Rings by index and parity, moved on without a division.
@@ -178,62 +179,68 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             uint32_t of0 = 0, of1 = 0;        // the next s_full of A and of B
             auto next = [](uint32_t i, uint32_t n) { return i + 1 == n ? 0u : i + 1; };
             bool ok = true;
-            for (int w = 0; ok && works.take(pc, w, false, false, 0, status); ++w) {
+            for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
                 const Span s = as_span(pc);
                 const int t1 = s.end();
                 if (t1 == 0) continue;
-                ok = ptx::mbar_wait(q_full, items & 1, status);
+                ok = wait_warp(q_full, items & 1, status);
                 ++items;
                 int ts = 0;  // tile and row block of the next S
                 bool to_b = s.a1 == 0;
                 auto score = [&] {
                     if (!to_b) {
-                        if (!ptx::mbar_wait(k_full(st_s), ph_s, status)) return false;
+                        if (!wait_warp(k_full(st_s), ph_s, status)) return false;
                         ptx::tc_fence_after();
-                        product_features<DP>(tmem + 128 * buf_s, dq, dk + st_s * kStep, id_s);
-                        ptx::mma_commit(s_full(0, of0));
+                        if (leader) {
+                            product_features<DP>(tmem + 128 * buf_s, dq, dk + st_s * kStep, id_s);
+                            ptx::mma_commit(s_full(0, of0));
+                        }
                         of0 = next(of0, F::kBuffers), buf_s = next(buf_s, F::kBuffers);
                         if (ts >= s.b0 && ts < s.b1) {
                             to_b = true;
                             return true;
                         }
                     } else {
-                        if (ts >= s.a1 && !ptx::mbar_wait(k_full(st_s), ph_s, status)) return false;
+                        if (ts >= s.a1 && !wait_warp(k_full(st_s), ph_s, status)) return false;
                         ptx::tc_fence_after();
-                        product_features<DP>(tmem + 128 * buf_s, dq + kStep, dk + st_s * kStep, id_s);
-                        ptx::mma_commit(s_full(1, of1));
+                        if (leader) {
+                            product_features<DP>(tmem + 128 * buf_s, dq + kStep, dk + st_s * kStep, id_s);
+                            ptx::mma_commit(s_full(1, of1));
+                        }
                         of1 = next(of1, F::kBuffers), buf_s = next(buf_s, F::kBuffers);
                     }
-                    ptx::mma_commit(k_empty(st_s));
+                    if (leader) ptx::mma_commit(k_empty(st_s));
                     st_s = next(st_s, kStages), ph_s ^= st_s == 0;
                     ++ts;
                     to_b = ts >= s.a1;
-                    if (ts == t1) ptx::mma_commit(q_empty);  // the last use of Q
+                    if (ts == t1 && leader) ptx::mma_commit(q_empty);  // the last use of Q
                     return true;
                 };
                 // P V of one row block; its buffer is then the next S's: products run in order
                 auto weigh = [&](uint32_t o, bool more, uint32_t done) {
-                    if (!ptx::mbar_wait(p_full(buf_p), ph_p, status)) return false;
+                    if (!wait_warp(p_full(buf_p), ph_p, status)) return false;
                     ptx::tc_fence_after();
                     const uint32_t p = tmem + 128 * buf_p;
-                    product_tokens(o, p, p + 32, dv + st_v * kStep, id_o, more);
-                    ptx::mma_commit(done);
+                    if (leader) {
+                        product_tokens(o, p, p + 32, dv + st_v * kStep, id_o, more);
+                        ptx::mma_commit(done);
+                    }
                     buf_p = next(buf_p, F::kBuffers), ph_p ^= buf_p == 0;
                     return ts == t1 || score();
                 };
                 for (int i = 0; ok && i < F::kBuffers && ts < t1; ++i) ok = score();
                 for (int t = 0; ok && t < t1; ++t) {
-                    ok = ptx::mbar_wait(v_full(st_v), ph_v, status);
+                    ok = wait_warp(v_full(st_v), ph_v, status);
                     if (ok && t < s.a1) ok = weigh(tmem + F::kO, t > 0, pv_done(0));
                     if (ok && t >= s.b0 && t < s.b1) ok = weigh(tmem + F::kO + DP, t > s.b0, pv_done(1));
-                    ptx::mma_commit(v_empty(st_v));
+                    if (leader) ptx::mma_commit(v_empty(st_v));
                     last = 2 * st_v + ph_v + 1;
                     st_v = next(st_v, kStages), ph_v ^= st_v == 0;
                 }
             }
             // every product has finished before TMEM is released below: commits complete in
             // order, and the last of a piece of work is that of its last V stage
-            if (last) ptx::mbar_wait(v_empty((last - 1) / 2), (last - 1) & 1, nullptr);
+            if (last) wait_warp(v_empty((last - 1) / 2), (last - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
             works.hand_out([&](int work) { return fwd_piece(mask, args, work); }, status);
         }
