@@ -248,9 +248,12 @@ template <typename T>
 noble_status attn_prep(const attn::RowArgs<T> &a, float *delta, int2 *ranges, cudaStream_t st)
 {
     namespace s = attn::simt;
-    const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div((int64_t)a.mask.T * a.n_q, 8), 16 * kSms);
-    return run(st, {"attn_delta", kBoundHbm, 0.0, 2.0 * sizeof(T) * a.mask.T * a.n_q * a.d},
-               [&] { s::delta_kernel<T><<<blocks, 256, 0, st>>>(a, delta, ranges); });
+    const bool wide = a.d > 64;
+    const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div((int64_t)a.mask.T * a.n_q, 4 * (wide ? 16 : 32)), 8 * kSms);
+    return run(st, {"attn_delta", kBoundHbm, 0.0, 2.0 * sizeof(T) * a.mask.T * a.n_q * a.d}, [&] {
+        if (wide) s::delta_kernel<T, 16><<<blocks, 256, 0, st>>>(a, delta, ranges);
+        else s::delta_kernel<T, 8><<<blocks, 256, 0, st>>>(a, delta, ranges);
+    });
 }
 template <int DP, typename T>
 noble_status attn_bwd_simt(const attn::RowArgs<T> &a, float *delta, const int2 *ranges, cudaStream_t st)
@@ -342,18 +345,19 @@ template <int DP, bool GENERAL>
 noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4], float *delta, cudaStream_t st)
 {
     namespace t = attn::tc;
-    using B = t::Bwd<DP>;
+    using Q = t::BwdQ<DP>;
+    using KV = t::BwdKV<DP>;
     constexpr auto dq = &t::dq_kernel<DP, GENERAL>, dkv = &t::dkv_kernel<DP, GENERAL>;
     if (!registers_at_least<dq>(168) || !registers_at_least<dkv>(168)) return fail(NOBLE_ERR_CUDA, "attn_bwd: registers");
-    NOBLE_TRY((allow<dq>(B::kDynamic)));
-    NOBLE_TRY((allow<dkv>(B::kDynamic)));
+    NOBLE_TRY((allow<dq>(Q::kBytes)));
+    NOBLE_TRY((allow<dkv>(KV::kBytes)));
     t::BwdArgs f{a, delta, (int)ceil_div(a.mask.T, t::kRows), status_ptr()};
     if (!f.status) return fail(NOBLE_ERR_CUDA, "status word address");
     if ((int64_t)f.tiles * a.n_q > INT32_MAX) return fail(NOBLE_ERR_UNSUPPORTED, "%d tokens of %d heads", a.mask.T, a.n_q);
     NOBLE_TRY(run(st, {"attn_dq", kBoundTensor, 0.0, 0.0},
-                  [&] { dq<<<f.tiles * a.n_q, B::kThreads, B::kDynamic, st>>>(maps[0], maps[1], maps[2], maps[3], f); }));
+                  [&] { dq<<<f.tiles * a.n_q, Q::kThreads, Q::kBytes, st>>>(maps[0], maps[1], maps[2], maps[3], f); }));
     return run(st, {"attn_dkv", kBoundTensor, 0.0, 0.0},
-               [&] { dkv<<<f.tiles * a.n_kv, B::kThreads, B::kDynamic, st>>>(maps[0], maps[1], maps[2], maps[3], f); });
+               [&] { dkv<<<f.tiles * a.n_kv, KV::kThreads, KV::kBytes, st>>>(maps[0], maps[1], maps[2], maps[3], f); });
 }
 template <typename T>
 noble_status attn_fwd(const attn::RowArgs<T> &a, cudaStream_t st)
@@ -375,6 +379,7 @@ noble_status attn_bwd_tc(const noble_attn_desc *d, const attn::RowArgs<bf> &a, c
     NOBLE_TRY(make_heads_map(&maps[1], d_o, d->T, d->n_q, d->d));
     NOBLE_TRY(make_heads_map(&maps[2], k, d->T, d->n_kv, d->d));
     NOBLE_TRY(make_heads_map(&maps[3], v, d->T, d->n_kv, d->d));
+    NOBLE_TRY(attn_prep<bf>(a, delta, nullptr, st));
     if (general_scores(a.score))
         return d->d <= 64 ? attn_bwd_tc<64, true>(a, maps, delta, st) : attn_bwd_tc<128, true>(a, maps, delta, st);
     return d->d <= 64 ? attn_bwd_tc<64, false>(a, maps, delta, st) : attn_bwd_tc<128, false>(a, maps, delta, st);

@@ -200,25 +200,47 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ R
         if (redo[r]) row_fwd(a, i0 + r, h, tid % 32);
 }
 
-// delta[h][i] = sum_f o do, one warp per (token, head); with ranges, also the range
-// of every token.
-template <typename T>
+// delta[h][i] = sum_f o do; with ranges, also the range of every token.  Bound by reading o
+// and do: a lane takes 8 features of each, LP lanes a head, and four heads at a time
+// (grid strides apart) are in flight.
+template <typename T, int LP>
 __global__ void __launch_bounds__(256) delta_kernel(const __grid_constant__ RowArgs<T> a, float *delta, int2 *ranges)
 {
-    const int64_t n = (int64_t)a.mask.T * a.n_q, step = (int64_t)gridDim.x * 8;
-    const int lane = threadIdx.x % 32;
-    for (int64_t u = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; u < n; u += step) {
-        const int t = (int)(u / a.n_q), h = (int)(u % a.n_q);
-        float s = 0.f;
-        if (4 * lane < a.d) {
-            const float4 x = load4(a.o.at(t, h) + 4 * lane), y = load4(a.d_o.at(t, h) + 4 * lane);
-            s = x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
+    constexpr int kAtOnce = 4;
+    const int64_t n = (int64_t)a.mask.T * a.n_q, step = (int64_t)gridDim.x * (256 / LP);
+    const int f = threadIdx.x % LP * 8;
+    const int64_t first = (int64_t)blockIdx.x * (256 / LP) + threadIdx.x / LP;
+    for (int64_t u0 = first; u0 - threadIdx.x / LP < n; u0 += kAtOnce * step) {
+        float4 x[kAtOnce][2], y[kAtOnce][2];
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            const int64_t u = u0 + e * step, t = u / a.n_q;
+            const int h = (int)(u - t * a.n_q);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                x[e][c] = y[e][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (u < n && f < a.d) x[e][c] = load4(a.o.at(t, h) + f + 4 * c), y[e][c] = load4(a.d_o.at(t, h) + f + 4 * c);
+            }
         }
-        s = warp_sum(s);
-        if (lane == 0) delta[(int64_t)h * a.mask.T + t] = s;
-        if (h == 0 && lane == 0) {
-            const Range r = visible(a.mask, t);
-            ranges[t] = make_int2(r.lo, r.hi);
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            const int64_t u = u0 + e * step, t = u / a.n_q;
+            const int h = (int)(u - t * a.n_q);
+            float s = 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                s = fmaf(x[e][c].x, y[e][c].x, s), s = fmaf(x[e][c].y, y[e][c].y, s);
+                s = fmaf(x[e][c].z, y[e][c].z, s), s = fmaf(x[e][c].w, y[e][c].w, s);
+            }
+#pragma unroll
+            for (int o = 1; o < LP; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (u < n && f == 0) {
+                delta[(int64_t)h * a.mask.T + t] = s;
+                if (ranges && h == 0) {
+                    const Range r = visible(a.mask, (int)t);
+                    ranges[t] = make_int2(r.lo, r.hi);
+                }
+            }
         }
     }
 }

@@ -267,15 +267,16 @@ struct Work {
 
 // The document starts (and prefixes) in shared memory where they fit, since every
 // piece of work searches them; call with all threads, before a __syncthreads.
+template <int KEPT>
 __device__ __forceinline__ Mask mask_in_smem(const Mask &m, int32_t *sm)
 {
     Mask r = m;
-    if (m.n_docs >= kDocsInSmem) return r;
+    if (m.n_docs >= KEPT) return r;
     for (int i = threadIdx.x; i <= m.n_docs; i += blockDim.x) sm[i] = m.doc_start[i];
     r.doc_start = sm;
     if (m.prefix) {
-        for (int i = threadIdx.x; i < m.n_docs; i += blockDim.x) sm[kDocsInSmem + i] = m.prefix[i];
-        r.prefix = sm + kDocsInSmem;
+        for (int i = threadIdx.x; i < m.n_docs; i += blockDim.x) sm[KEPT + i] = m.prefix[i];
+        r.prefix = sm + KEPT;
     }
     return r;
 }

@@ -26,27 +26,32 @@ namespace tc {
 
 struct BwdArgs {
     RowArgs<__nv_bfloat16> a;
-    float *delta;  // [n_q][T]: sum of o do, by dq_kernel for dkv_kernel
+    float *delta;  // [n_q][T]: sum of o do
     int tiles;     // of 128 tokens
     uint32_t *status;
 };
 
-template <int DP>
+// Shared memory: two resident tiles, a ring of X stages of the tensor that is used twice
+// (K in dq_kernel, Q in dkv_kernel) and of Y of the other, document starts, vectors.
+template <int DP, int X, int Y, uint32_t VEC, int DOCS>
 struct Bwd {
-    static constexpr int kThreads = 384;
-    static constexpr int kStages = DP == 64 ? 4 : 2;
+    static constexpr int kThreads = 384, kXStages = X, kYStages = Y, kDocsKept = DOCS;
     static constexpr uint32_t kTile = kChunk * (DP / 64);
-    // two resident tiles, two streams of kStages, document starts, vectors by stage
-    static constexpr uint32_t kR0 = 0, kR1 = kTile, kX = 2 * kTile, kY = kX + kStages * kTile;
-    static constexpr uint32_t kDocs = kY + kStages * kTile;
-    static constexpr uint32_t kVec = kDocs + 2 * kDocsInSmem * 4;  // lse, delta [128], ranges [128], all visible
-    static constexpr uint32_t kVecBytes = 128 * 16 + 16;
-    static constexpr uint32_t kBars = kVec + kStages * kVecBytes;
-    static constexpr int kNumBars = 6 * kStages + 12;
-    static constexpr uint32_t kWork = kBars + 8 * kNumBars;
+    static constexpr uint32_t kR0 = 0, kR1 = kTile, kX = 2 * kTile, kY = kX + X * kTile;
+    static constexpr uint32_t kDocs = kY + Y * kTile;
+    static constexpr uint32_t kVec = kDocs + 2 * DOCS * 4;
+    static constexpr uint32_t kBars = kVec + VEC;
+    static constexpr int kNumBars = 2 * X + 4 * Y + 12;
+    static constexpr uint32_t kWork = kBars + 8 * ((kNumBars + 1) & ~1);
     static constexpr uint32_t kBytes = kWork + Work::kBytes + 16;
-    static constexpr uint32_t kDynamic = kBytes + 1024;
+    static_assert(kBytes <= 232448, "shared memory of a block");
 };
+// A K tile is in use from its S to its dQ, a step and a half: with 128 features a third
+// stage leaves its load the time it takes (3327 clocks a tile with two, of which 1080
+// waiting for it).
+template <int DP> using BwdQ = Bwd<DP, DP == 64 ? 4 : 3, DP == 64 ? 4 : 2, 1024, 128>;
+constexpr uint32_t kVecBytes = 128 * 16 + 16;  // lse, delta [128], ranges [128], whether all is visible
+template <int DP> using BwdKV = Bwd<DP, DP == 64 ? 4 : 2, DP == 64 ? 4 : 2, (DP == 64 ? 4 : 2) * kVecBytes, kDocsInSmem>;
 
 // Queries that see any key of [j0, j1): none if lo >= hi.
 __device__ __forceinline__ Range queries_of(const Mask &m, int j0, int j1)
@@ -94,30 +99,27 @@ __device__ __forceinline__ float score2(const Score &sc, float slope, float sl, 
     return fmaf(-slope, fabsf((float)far), y * kLog2e);
 }
 
-__device__ __forceinline__ float dot2(uint32_t a, uint32_t b)
-{
-    return fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), __uint_as_float(a & 0xffff0000u) * __uint_as_float(b & 0xffff0000u));
-}
-
 // ---------------------------------------------------------------- dq
 template <int DP, bool GENERAL>
-__global__ void __launch_bounds__(Bwd<DP>::kThreads, 1)
+__global__ void __launch_bounds__(384, 1)
 dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mDO, const __grid_constant__ CUtensorMap mK,
           const __grid_constant__ CUtensorMap mV, const __grid_constant__ BwdArgs args)
 {
-    using B = Bwd<DP>;
-    constexpr int kStages = B::kStages, kChunks = DP / 64;
+    using B = BwdQ<DP>;
+    constexpr int kXS = B::kXStages, kYS = B::kYStages, kChunks = DP / 64;
     constexpr uint32_t kS0 = 0, kDP = 128, kS1 = 256, kAcc = 384;  // TMEM columns
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = ptx::smem_u32(smem_raw);
-    const uint32_t base = (raw + 1023u) & ~1023u;
-    uint8_t *smem = smem_raw + (base - raw);
+    extern __shared__ __align__(1024) uint8_t smem[];  // nothing static: begins on the 1024 bytes of a swizzled tile
+    const uint32_t base = ptx::smem_u32(smem);
+    if (base & 1023u) {
+        if (threadIdx.x == 0) raise_status(args.status, kStatusBadShape);
+        return;
+    }
     const uint32_t bars = base + B::kBars;
     auto k_full = [&](int s) { return bars + 8u * s; };
-    auto k_empty = [&](int s) { return bars + 8u * (kStages + s); };
-    auto v_full = [&](int s) { return bars + 8u * (2 * kStages + s); };
-    auto v_empty = [&](int s) { return bars + 8u * (3 * kStages + s); };
-    const uint32_t one = bars + 8u * (4 * kStages);
+    auto k_empty = [&](int s) { return bars + 8u * (kXS + s); };
+    auto v_full = [&](int s) { return bars + 8u * (2 * kXS + s); };
+    auto v_empty = [&](int s) { return bars + 8u * (2 * kXS + kYS + s); };
+    const uint32_t one = bars + 8u * (2 * kXS + 2 * kYS);
     const uint32_t q_full = one, q_empty = one + 8, dp_full = one + 16, dp_read = one + 24, ds_full = one + 32, acc_full = one + 40,
                    acc_empty = one + 48, sums = one + 56;
     auto s_full = [&](int i) { return one + 64 + 8u * (i & 1); };  // by buffer: the next S does not wait for this one's readers
@@ -132,9 +134,11 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         ptx::tma_prefetch_desc(&mDO);
         ptx::tma_prefetch_desc(&mK);
         ptx::tma_prefetch_desc(&mV);
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < kXS; ++s) {
             ptx::mbar_init(k_full(s), 1);
             ptx::mbar_init(k_empty(s), 1);
+        }
+        for (int s = 0; s < kYS; ++s) {
             ptx::mbar_init(v_full(s), 1);
             ptx::mbar_init(v_empty(s), 1);
         }
@@ -155,7 +159,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
         ptx::tmem_relinquish();
     }
-    const Mask mask = mask_in_smem(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
+    const Mask mask = mask_in_smem<B::kDocsKept>(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
@@ -191,84 +195,77 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 }
                 ++items;
                 for (int t = 0; t < p.steps; ++t, ++n) {
-                    const int st = n % kStages, j = p.lo + t * kRows;
-                    const uint32_t ph = (n / kStages) & 1;
-                    ok = ptx::mbar_wait(k_empty(st), ph ^ 1, status);
+                    const int sx = n % kXS, sy = n % kYS, j = p.lo + t * kRows;
+                    ok = ptx::mbar_wait(k_empty(sx), ((n / kXS) & 1) ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(k_full(st), B::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + st * B::kTile + c * kChunk, &mK, k_full(st), 64 * c, p.g, j);
+                    ptx::mbar_arrive_expect_tx(k_full(sx), B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + sx * B::kTile + c * kChunk, &mK, k_full(sx), 64 * c, p.g, j);
                     ++nk;
-                    ok = ptx::mbar_wait(v_empty(st), ph ^ 1, status);
+                    ok = ptx::mbar_wait(v_empty(sy), ((n / kYS) & 1) ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(v_full(st), B::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + st * B::kTile + c * kChunk, &mV, v_full(st), 64 * c, p.g, j);
+                    ptx::mbar_arrive_expect_tx(v_full(sy), B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + sy * B::kTile + c * kChunk, &mV, v_full(sy), 64 * c, p.g, j);
                 }
             }
             if (items) ptx::mbar_wait(q_full, (items - 1) & 1, nullptr);
-            for (int i = max(nk - kStages, 0); i < nk; ++i) ptx::mbar_wait(k_full(i % kStages), (i / kStages) & 1, nullptr);
-            for (int i = max(n - kStages, 0); i < n; ++i) ptx::mbar_wait(v_full(i % kStages), (i / kStages) & 1, nullptr);
+            for (int i = max(nk - kXS, 0); i < nk; ++i) ptx::mbar_wait(k_full(i % kXS), (i / kXS) & 1, nullptr);
+            for (int i = max(n - kYS, 0); i < n; ++i) ptx::mbar_wait(v_full(i % kYS), (i / kYS) & 1, nullptr);
         } else if (warp == 9) {
             // ---------------- products
             const bool leader = elect_one();
             constexpr uint32_t id_s = ptx::idesc_bf16(128, 128, false, false), id_q = ptx::idesc_bf16(128, DP, false, true);
-            int n = 0, items = 0;
+            const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
+                           dy = desc_k(base + B::kY), dm = desc_mn(base + B::kX);
+            constexpr uint32_t kStep = B::kTile >> 4;
+            // rings by index and parity: K of the next S, of the next dQ; V; steps' parities
+            uint32_t st_s = 0, ph_s = 0, st_q = 0, st_v = 0, ph_v = 0, i_s = 0, i_p = 0, i_q = 0;
+            int items = 0;
+            auto next = [](uint32_t i, uint32_t n) { return i + 1 == n ? 0u : i + 1; };
+            auto score = [&] {
+                if (!wait_warp(k_full(st_s), ph_s, status)) return false;
+                ptx::tc_fence_after();
+                if (leader) {
+                    product_features<DP>(tmem + (i_s & 1 ? kS1 : kS0), dr0, dx + st_s * kStep, id_s);
+                    ptx::mma_commit(s_full(i_s));
+                }
+                st_s = next(st_s, kXS), ph_s ^= st_s == 0, ++i_s;
+                return true;
+            };
+            auto dprob = [&](bool last) {  // once the dP before is in registers
+                if (!wait_warp(v_full(st_v), ph_v, status) || (i_p > 0 && !wait_warp(dp_read, (i_p - 1) & 1, status))) return false;
+                ptx::tc_fence_after();
+                if (leader) {
+                    product_features<DP>(tmem + kDP, dr1, dy + st_v * kStep, id_s);
+                    ptx::mma_commit(dp_full);
+                    ptx::mma_commit(v_empty(st_v));
+                    if (last) ptx::mma_commit(q_empty);  // the last use of Q and dO
+                }
+                st_v = next(st_v, kYS), ph_v ^= st_v == 0, ++i_p;
+                return true;
+            };
             bool ok = true;
             for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
                 const Rows p = as_rows(pc);
                 if (!p.steps) continue;
-                ok = wait_warp(q_full, items & 1, status);
-                if (!ok) break;
-                const uint32_t dr0 = desc_k(base + B::kR0), dr1 = desc_k(base + B::kR1), dx = desc_k(base + B::kX),
-                               dy = desc_k(base + B::kY), dm = desc_mn(base + B::kX);
-                constexpr uint32_t kStep = B::kTile >> 4;
-                auto score = [&](int i) {
-                    if (leader) product_features<DP>(tmem + (i & 1 ? kS1 : kS0), dr0, dx + (i % kStages) * kStep, id_s);
-                    if (leader) ptx::mma_commit(s_full(i));
-                };
-                auto dprob = [&](int i) {
-                    if (leader) product_features<DP>(tmem + kDP, dr1, dy + (i % kStages) * kStep, id_s);
-                    if (leader) ptx::mma_commit(dp_full);
-                    if (leader) ptx::mma_commit(v_empty(i % kStages));
-                    if (i == n + p.steps - 1 && leader) ptx::mma_commit(q_empty);  // the last use of Q and dO
-                };
-                ok = wait_warp(k_full(n % kStages), (n / kStages) & 1, status);
-                if (!ok) break;
-                ptx::tc_fence_after();
-                score(n);
-                // the last dP of the piece before is in registers
-                ok = wait_warp(v_full(n % kStages), (n / kStages) & 1, status) &&
-                     (n == 0 || wait_warp(dp_read, (n - 1) & 1, status));
-                if (!ok) break;
-                ptx::tc_fence_after();
-                dprob(n);
-                for (int t = 0; t < p.steps; ++t) {
-                    const int i = n + t;
-                    if (t + 1 < p.steps) {
-                        const int st = (i + 1) % kStages;
-                        const uint32_t ph = ((i + 1) / kStages) & 1;
-                        ok = wait_warp(k_full(st), ph, status);
-                        if (!ok) break;
-                        ptx::tc_fence_after();
-                        score(i + 1);  // over the dS that the product before last has read
-                        ok = wait_warp(v_full(st), ph, status) && wait_warp(dp_read, i & 1, status);
-                        if (!ok) break;
-                        ptx::tc_fence_after();
-                        dprob(i + 1);
-                    }
-                    ok = wait_warp(ds_full, i & 1, status) &&
-                         (t > 0 || wait_warp(acc_empty, (items & 1) ^ 1, status));
+                ok = wait_warp(q_full, items & 1, status) && score() && dprob(p.steps == 1);
+                for (int t = 0; ok && t < p.steps; ++t) {
+                    // S over the dS that the product before last has read
+                    if (t + 1 < p.steps) ok = score() && dprob(t + 2 == p.steps);
+                    ok = ok && wait_warp(ds_full, i_q & 1, status) && (t > 0 || wait_warp(acc_empty, (items & 1) ^ 1, status));
                     if (!ok) break;
                     ptx::tc_fence_after();
-                    const uint32_t ds = tmem + (i & 1 ? kS1 : kS0);
-                    if (leader) product_tokens(tmem + kAcc, ds, ds + 64, dm + (i % kStages) * kStep, id_q, t > 0);
-                    if (leader) ptx::mma_commit(k_empty(i % kStages));
+                    const uint32_t ds = tmem + (i_q & 1 ? kS1 : kS0);
+                    if (leader) {
+                        product_tokens(tmem + kAcc, ds, ds + 64, dm + st_q * kStep, id_q, t > 0);
+                        ptx::mma_commit(k_empty(st_q));
+                    }
+                    st_q = next(st_q, kXS), ++i_q;
                 }
                 if (leader) ptx::mma_commit(acc_full);
-                n += p.steps;
                 ++items;
             }
             // every product has finished before TMEM is released below
-            if (items) wait_warp(acc_full, (items - 1) & 1, nullptr);
+            if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
             works.hand_out(describe, status);
         }
@@ -281,45 +278,31 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         const float sl = args.a.score.scale * kLog2e;
         uint32_t n = 0, items = 0, nsums = 0;
         bool ok = true;
-        for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
-            const Rows p = as_rows(pc);
-            const int i = p.i0 + row;
+        // a piece's row: its values are on their way while the piece before is written out
+        struct Row {
+            Rows p;
+            Range rg;
+            float lse, delta;
+        } r;
+        auto fetch = [&](Row &r) {
+            r.p = as_rows(pc);
+            const int i = r.p.i0 + row;
             const bool real = i < mask.T;
+            const int64_t at = (int64_t)r.p.h * mask.T + i;
+            r.lse = real ? args.a.lse[at] : 0.f;
+            r.delta = real ? args.delta[at] : 0.f;
+            r.rg = real ? visible(mask, i) : Range{0, 0};
+        };
+        bool more = works.take(pc, 0, true, false, lane, status);
+        if (more) fetch(r);
+        for (int w = 1; ok && more; ++w) {
+            const Rows p = r.p;
+            const Range rg = r.rg;
+            const int i = p.i0 + row;
+            const bool real = i < mask.T, none = rg.lo >= rg.hi;
             const int64_t at = (int64_t)p.h * mask.T + (real ? i : 0);
-            const Range rg = real ? visible(mask, i) : Range{0, 0};
-            const bool none = rg.lo >= rg.hi;
-            const float lse2 = none ? 0.f : args.a.lse[at] * kLog2e;
-            // delta: half of its features by each thread of a row, exchanged as below
-            float delta = 0.f;
-            if (real) {
-                const __nv_bfloat16 *o = args.a.o.at(i, p.h) + half * (DP / 2), *d_o = args.a.d_o.at(i, p.h) + half * (DP / 2);
-#pragma unroll
-                for (int f = 0; f < DP / 2; f += 8) {
-                    if (half * (DP / 2) + f >= args.a.d) break;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(o + f), y = *reinterpret_cast<const uint4 *>(d_o + f);
-                    delta += dot2(x.x, y.x) + dot2(x.y, y.y) + dot2(x.z, y.z) + dot2(x.w, y.w);
-                }
-            }
-            auto exchange = [&](float v) {  // the sum over both threads of a row
-                part[128 * half + row] = v;
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(sums);
-                ok = ptx::mbar_wait(sums, nsums & 1, status);
-                ok = __all_sync(0xffffffffu, ok);
-                ++nsums;
-                const float total = part[row] + part[128 + row];
-                // both have read it before either writes the next
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(sums);
-                ok = ok && ptx::mbar_wait(sums, nsums & 1, status);
-                ok = __all_sync(0xffffffffu, ok);
-                ++nsums;
-                return total;
-            };
-            delta = exchange(delta);
-            if (!ok) break;
-            if (none) delta = 0.f;
-            if (half == 0 && real) args.delta[at] = delta;
+            const float lse2 = none ? 0.f : r.lse * kLog2e;
+            float delta = none ? 0.f : r.delta;
             const float slope = GENERAL && args.a.score.slope ? args.a.score.slope[p.h] * kLog2e : 0.f;
             for (int t = 0; t < p.steps; ++t, ++n) {
                 const uint32_t tS = tmem + lanes + (n & 1 ? kS1 : kS0) + 64 * half, tP = tmem + lanes + kDP + 64 * half;
@@ -370,8 +353,14 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                         if (GENERAL) q = c >= lo && c < hi ? exp2_fast(score2<true>(args.a.score, slope, sl, s[c], i - j0 - c, g) - lse2) : 0.f;
                         sum = GENERAL && q == 0.f ? sum : fmaf(q, dp[c], sum);
                     }
-                    delta = exchange(sum);
+                    part[128 * half + row] = sum;
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(sums);
+                    ok = ptx::mbar_wait(sums, nsums & 1, status);
+                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
+                    ++nsums;
+                    delta = part[row] + part[128 + row];
                     if (half == 0 && !none) args.delta[at] = delta;
                 }
                 if (!GENERAL) {
@@ -404,6 +393,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 if (lane == 0) ptx::mbar_arrive(ds_full);
             }
             if (!ok) break;
+            more = works.take(pc, w, true, false, lane, status);
+            if (more) fetch(r);
             // ---------------- dq of this row, half of its features
             if (p.steps) {
                 ok = ptx::mbar_wait(acc_full, items & 1, status);
@@ -459,17 +450,19 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
 
 // ---------------------------------------------------------------- dk, dv
 template <int DP, bool GENERAL>
-__global__ void __launch_bounds__(Bwd<DP>::kThreads, 1)
+__global__ void __launch_bounds__(384, 1)
 dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtensorMap mDO, const __grid_constant__ CUtensorMap mK,
            const __grid_constant__ CUtensorMap mV, const __grid_constant__ BwdArgs args)
 {
-    using B = Bwd<DP>;
-    constexpr int kStages = B::kStages, kChunks = DP / 64;
+    using B = BwdKV<DP>;
+    constexpr int kStages = B::kXStages, kChunks = DP / 64;
     constexpr uint32_t kS = 0, kDP = 128, kDV = 256, kDK = 256 + DP;  // TMEM columns
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = ptx::smem_u32(smem_raw);
-    const uint32_t base = (raw + 1023u) & ~1023u;
-    uint8_t *smem = smem_raw + (base - raw);
+    extern __shared__ __align__(1024) uint8_t smem[];  // as in dq_kernel
+    const uint32_t base = ptx::smem_u32(smem);
+    if (base & 1023u) {
+        if (threadIdx.x == 0) raise_status(args.status, kStatusBadShape);
+        return;
+    }
     const uint32_t bars = base + B::kBars;
     auto q_full = [&](int s) { return bars + 8u * s; };
     auto q_empty = [&](int s) { return bars + 8u * (kStages + s); };
@@ -513,7 +506,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
         ptx::tmem_relinquish();
     }
-    const Mask mask = mask_in_smem(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
+    const Mask mask = mask_in_smem<B::kDocsKept>(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
@@ -645,7 +638,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     ok = ptx::mbar_wait(vec_empty(st), ((n / kStages) & 1) ^ 1, status);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
-                    float *vec = reinterpret_cast<float *>(smem + B::kVec + st * B::kVecBytes);
+                    float *vec = reinterpret_cast<float *>(smem + B::kVec + st * kVecBytes);
                     int2 *rg = reinterpret_cast<int2 *>(vec + 256);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
@@ -683,7 +676,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             const int j = p.j0 + row;
             for (int t = 0; t < p.steps; ++t, ++n) {
                 const int st = n % kStages;
-                const float *vec = reinterpret_cast<const float *>(smem + B::kVec + st * B::kVecBytes) + 64 * half;
+                const float *vec = reinterpret_cast<const float *>(smem + B::kVec + st * kVecBytes) + 64 * half;
                 const int2 *rg = reinterpret_cast<const int2 *>(vec - 64 * half + 256) + 64 * half;
                 ok = ptx::mbar_wait(vec_full(st), (n / kStages) & 1, status) && ptx::mbar_wait(s_full, n & 1, status);
                 ok = __all_sync(0xffffffffu, ok);

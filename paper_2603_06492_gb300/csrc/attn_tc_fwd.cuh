@@ -120,7 +120,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
         ptx::tmem_relinquish();
     }
-    const Mask mask = mask_in_smem(args.a.mask, reinterpret_cast<int32_t *>(smem + F::kDocs));
+    const Mask mask = mask_in_smem<kDocsInSmem>(args.a.mask, reinterpret_cast<int32_t *>(smem + F::kDocs));
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
