@@ -111,6 +111,20 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v)
     *reinterpret_cast<uint2 *>(p) = u;
 }
 
+// Eight.
+__device__ __forceinline__ void load8(float (&x)[8], const float *p)
+{
+    const float4 a = load4(p), b = load4(p + 4);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void load8(float (&x)[8], const __nv_bfloat16 *p)
+{
+    const uint4 u = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll

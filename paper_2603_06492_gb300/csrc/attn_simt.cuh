@@ -204,41 +204,40 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ R
 // and do: a lane takes 8 features of each, LP lanes a head, and four heads at a time
 // (grid strides apart) are in flight.
 template <typename T, int LP>
-__global__ void __launch_bounds__(256) delta_kernel(const __grid_constant__ RowArgs<T> a, float *delta, int2 *ranges)
+__global__ void __launch_bounds__(256) delta_kernel(const __grid_constant__ RowArgs<T> a, float *delta, int2 *ranges, int step_t,
+                                                    int step_h)
 {
-    constexpr int kAtOnce = 4;
-    const int64_t n = (int64_t)a.mask.T * a.n_q, step = (int64_t)gridDim.x * (256 / LP);
+    // head u = (t, h) of all; a step of the grid is step_t tokens and step_h heads
+    constexpr int kAtOnce = 4, kPer = 256 / LP;
     const int f = threadIdx.x % LP * 8;
-    const int64_t first = (int64_t)blockIdx.x * (256 / LP) + threadIdx.x / LP;
-    for (int64_t u0 = first; u0 - threadIdx.x / LP < n; u0 += kAtOnce * step) {
-        float4 x[kAtOnce][2], y[kAtOnce][2];
+    const int64_t u = (int64_t)blockIdx.x * kPer + threadIdx.x / LP;
+    int t = (int)(u / a.n_q), h = (int)(u % a.n_q);
+    const int steps = (int)(((int64_t)a.mask.T * a.n_q - (int64_t)blockIdx.x * kPer + (int64_t)gridDim.x * kPer - 1) / ((int64_t)gridDim.x * kPer));
+    for (int k = 0; k < steps; k += kAtOnce) {
+        float x[kAtOnce][8], y[kAtOnce][8];
+        int ts[kAtOnce], hs[kAtOnce];
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
-            const int64_t u = u0 + e * step, t = u / a.n_q;
-            const int h = (int)(u - t * a.n_q);
+            ts[e] = t, hs[e] = h;
+            t += step_t, h += step_h;
+            if (h >= a.n_q) h -= a.n_q, ++t;
+            const bool in = ts[e] < a.mask.T && f < a.d;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                x[e][c] = y[e][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (u < n && f < a.d) x[e][c] = load4(a.o.at(t, h) + f + 4 * c), y[e][c] = load4(a.d_o.at(t, h) + f + 4 * c);
-            }
+            for (int c = 0; c < 8; ++c) x[e][c] = y[e][c] = 0.f;
+            if (in) load8(x[e], a.o.at(ts[e], hs[e]) + f), load8(y[e], a.d_o.at(ts[e], hs[e]) + f);
         }
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
-            const int64_t u = u0 + e * step, t = u / a.n_q;
-            const int h = (int)(u - t * a.n_q);
             float s = 0.f;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                s = fmaf(x[e][c].x, y[e][c].x, s), s = fmaf(x[e][c].y, y[e][c].y, s);
-                s = fmaf(x[e][c].z, y[e][c].z, s), s = fmaf(x[e][c].w, y[e][c].w, s);
-            }
+            for (int c = 0; c < 8; ++c) s = fmaf(x[e][c], y[e][c], s);
 #pragma unroll
             for (int o = 1; o < LP; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (u < n && f == 0) {
-                delta[(int64_t)h * a.mask.T + t] = s;
-                if (ranges && h == 0) {
-                    const Range r = visible(a.mask, (int)t);
-                    ranges[t] = make_int2(r.lo, r.hi);
+            if (ts[e] < a.mask.T && f == 0) {
+                delta[(int64_t)hs[e] * a.mask.T + ts[e]] = s;
+                if (ranges && hs[e] == 0) {
+                    const Range r = visible(a.mask, ts[e]);
+                    ranges[ts[e]] = make_int2(r.lo, r.hi);
                 }
             }
         }

@@ -50,7 +50,7 @@ struct Bwd {
 // stage leaves its load the time it takes (3327 clocks a tile with two, of which 1080
 // waiting for it).
 template <int DP> using BwdQ = Bwd<DP, DP == 64 ? 4 : 3, DP == 64 ? 4 : 2, 1024, 128>;
-constexpr uint32_t kVecBytes = 128 * 16 + 16;  // lse, delta [128], ranges [128], whether all is visible
+constexpr uint32_t kVecBytes = 128 * 8;  // lse, delta [128]
 template <int DP> using BwdKV = Bwd<DP, DP == 64 ? 4 : 2, DP == 64 ? 4 : 2, (DP == 64 ? 4 : 2) * kVecBytes, kDocsInSmem>;
 
 // Queries that see any key of [j0, j1): none if lo >= hi.
@@ -612,18 +612,14 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             // every product has finished before TMEM is released below
             if (items) wait_warp(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10) {
-            // ---------------- lse, delta and ranges of the query tiles
+            // ---------------- lse and delta of the query tiles, a step ahead of the stage they go to
             int n = 0;
             bool ok = true;
             for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
                 const Keys p = as_keys(pc);
-                // a step's values are on their way while the stage before is waited for
                 float lse[4], delta[4];
-                bool all = false;
                 auto fetch = [&](int t) {
                     const int h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows;
-                    // by the order of the ranges: whether every query of the tile sees every key
-                    all = i0 + kRows <= mask.T && visible(mask, i0).hi >= p.j0 + kRows && visible(mask, i0 + kRows - 1).lo <= p.j0;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         const int i = i0 + lane + 32 * u;
@@ -634,25 +630,12 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 };
                 if (p.steps) fetch(0);
                 for (int t = 0; t < p.steps; ++t, ++n) {
-                    const int st = n % kStages, i0 = p.lo + t % p.per * kRows;
-                    ok = ptx::mbar_wait(vec_empty(st), ((n / kStages) & 1) ^ 1, status);
-                    ok = __all_sync(0xffffffffu, ok);
+                    const int st = n % kStages;
+                    ok = wait_warp(vec_empty(st), ((n / kStages) & 1) ^ 1, status);
                     if (!ok) break;
                     float *vec = reinterpret_cast<float *>(smem + B::kVec + st * kVecBytes);
-                    int2 *rg = reinterpret_cast<int2 *>(vec + 256);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int e = lane + 32 * u, i = i0 + e;
-                        bool sees = all;
-                        if (!all) {
-                            const Range r = i < mask.T ? visible(mask, i) : Range{0, 0};
-                            rg[e] = make_int2(r.lo, r.hi);
-                            sees = r.lo < r.hi;
-                        }
-                        vec[e] = sees ? lse[u] * kLog2e : 0.f;
-                        vec[128 + e] = sees ? delta[u] : 0.f;
-                    }
-                    if (lane == 0) *reinterpret_cast<int *>(vec + 512) = all;
+                    for (int u = 0; u < 4; ++u) vec[lane + 32 * u] = lse[u] * kLog2e, vec[128 + lane + 32 * u] = delta[u];
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(vec_full(st));
                     if (t + 1 < p.steps) fetch(t + 1);
@@ -671,18 +654,30 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         const float sl = args.a.score.scale * kLog2e;
         uint32_t n = 0, items = 0;
         bool ok = true;
-        for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
-            const Keys p = as_keys(pc);
+        // the queries that see a key are a range; a piece's is looked up before the one before
+        // it is written out
+        Keys p_next;
+        Range see_next;
+        auto fetch = [&] {
+            p_next = as_keys(pc);
+            const int j = p_next.j0 + row;
+            see_next = queries_of(mask, j, j + 1);
+        };
+        bool more = works.take(pc, 0, true, false, lane, status);
+        if (more) fetch();
+        for (int w = 1; ok && more; ++w) {
+            const Keys p = p_next;
+            const Range see = see_next;
             const int j = p.j0 + row;
             for (int t = 0; t < p.steps; ++t, ++n) {
                 const int st = n % kStages;
                 const float *vec = reinterpret_cast<const float *>(smem + B::kVec + st * kVecBytes) + 64 * half;
-                const int2 *rg = reinterpret_cast<const int2 *>(vec - 64 * half + 256) + 64 * half;
+                const int i0 = p.lo + t % p.per * kRows + 64 * half, lo = see.lo - i0, hi = see.hi - i0;
                 ok = ptx::mbar_wait(vec_full(st), (n / kStages) & 1, status) && ptx::mbar_wait(s_full, n & 1, status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                const bool all = *reinterpret_cast<const int *>(vec - 64 * half + 512) != 0;
+                const bool all = __all_sync(0xffffffffu, lo <= 0 && hi >= 64);
                 uint32_t xs[64], xp[64];
                 __syncwarp();
                 tmem_ld32(tS, xs);
@@ -691,15 +686,6 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 pin32(xs), pin32(xs + 32);
                 float s[64], dp[64];
                 as_floats(s, xs);
-                uint32_t in[2] = {0xffffffffu, 0xffffffffu};  // which of the queries see this key
-                if (!all) {
-                    in[0] = in[1] = 0;
-#pragma unroll
-                    for (int c = 0; c < 64; ++c) {
-                        const int2 r = rg[c];
-                        in[c / 32] |= (j >= r.x && j < r.y ? 1u : 0u) << (c % 32);
-                    }
-                }
                 // p over s; with a capped score, dp is to be multiplied by p and g
                 uint32_t gs[GENERAL ? 32 : 1];
                 if (!GENERAL) {
@@ -714,7 +700,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                         s[c + 2] = exp2_fast(a), s[c + 3] = exp2_fast(b);
                     }
                 } else {
-                    const int h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows + 64 * half;
+                    const int h = p.g * group + t / p.per;
                     const float slope = args.a.score.slope ? args.a.score.slope[h] * kLog2e : 0.f;
 #pragma unroll
                     for (int c = 0; c < 64; c += 2) {
@@ -729,7 +715,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 }
                 if (!all)
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) s[c] = in[c / 32] >> (c % 32) & 1 ? s[c] : 0.f;
+                    for (int c = 0; c < 64; ++c) s[c] = c >= lo && c < hi ? s[c] : 0.f;
                 uint32_t pk[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) pk[c / 2] = ptx::pack_bf16x2(s[c], s[c + 1]);
@@ -752,7 +738,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 as_floats(dp, xp);
                 if (!all)
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) dp[c] = in[c / 32] >> (c % 32) & 1 ? dp[c] : 0.f;
+                    for (int c = 0; c < 64; ++c) dp[c] = c >= lo && c < hi ? dp[c] : 0.f;
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
                     const float4 d = *reinterpret_cast<const float4 *>(vec + 128 + c);
@@ -778,6 +764,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 }
             }
             if (!ok) break;
+            more = works.take(pc, w, true, false, lane, status);
+            if (more) fetch();
             // ---------------- dv by the first warpgroup, dk by the second
             if (p.steps) {
                 ok = ptx::mbar_wait(acc_full, items & 1, status);

@@ -114,12 +114,7 @@ template <> struct Raw<float> {
         return r;
     }
 };
-__device__ __forceinline__ void load8(float (&x)[8], const float *p)
-{
-    Raw<float> r;
-    r.load(p);
-    r.get(x);
-}
+using attn::load8;
 
 // Factors of a lane's 8 features: y_f = c x_f + s x_(other of f), s = 0 where f does not
 // rotate; with gains (norm) c holds f's and s its partner's.
