@@ -250,7 +250,7 @@ noble_status attn_prep(const attn::RowArgs<T> &a, float *delta, int2 *ranges, cu
     namespace s = attn::simt;
     const bool wide = a.d > 64;
     const int64_t per = wide ? 16 : 32;  // heads of a block at a time
-    const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)a.mask.T * a.n_q, 4 * per), 8 * kSms);
+    const int64_t blocks = std::min<int64_t>(ceil_div((int64_t)a.mask.T * a.n_q, 4 * per), 4 * kSms);
     const int step_t = (int)(blocks * per / a.n_q), step_h = (int)(blocks * per % a.n_q);
     return run(st, {"attn_delta", kBoundHbm, 0.0, 2.0 * sizeof(T) * a.mask.T * a.n_q * a.d}, [&] {
         if (wide) s::delta_kernel<T, 16><<<(unsigned)blocks, 256, 0, st>>>(a, delta, ranges, step_t, step_h);

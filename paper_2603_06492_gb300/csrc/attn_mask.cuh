@@ -125,6 +125,73 @@ __device__ __forceinline__ void load8(float (&x)[8], const __nv_bfloat16 *p)
     for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
 }
 
+// 8 elements as they are in memory
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p)
+    {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p);
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ void zero() { w[0] = w[1] = w[2] = w[3] = 0; }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    __device__ __forceinline__ void set(const float (&x)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+    }
+    __device__ __forceinline__ Raw from(int lane) const
+    {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = __shfl_sync(0xffffffffu, w[i], lane);
+        return r;
+    }
+};
+template <> struct Raw<float> {
+    float x[8];
+    __device__ __forceinline__ void load(const float *p)
+    {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+    __device__ __forceinline__ void store(float *p) const
+    {
+        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    }
+    __device__ __forceinline__ void get(float (&y)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i];
+    }
+    __device__ __forceinline__ void set(const float (&y)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = y[i];
+    }
+    __device__ __forceinline__ Raw from(int lane) const
+    {
+        Raw r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.x[i] = __shfl_sync(0xffffffffu, x[i], lane);
+        return r;
+    }
+};
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll

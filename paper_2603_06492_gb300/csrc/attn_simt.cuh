@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ R
 // and do: a lane takes 8 features of each, LP lanes a head, and four heads at a time
 // (grid strides apart) are in flight.
 template <typename T, int LP>
-__global__ void __launch_bounds__(256) delta_kernel(const __grid_constant__ RowArgs<T> a, float *delta, int2 *ranges, int step_t,
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) delta_kernel(const __grid_constant__ RowArgs<T> a, float *delta, int2 *ranges, int step_t,
                                                     int step_h)
 {
     // head u = (t, h) of all; a step of the grid is step_t tokens and step_h heads
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(256) delta_kernel(const __grid_constant__ RowA
     int t = (int)(u / a.n_q), h = (int)(u % a.n_q);
     const int steps = (int)(((int64_t)a.mask.T * a.n_q - (int64_t)blockIdx.x * kPer + (int64_t)gridDim.x * kPer - 1) / ((int64_t)gridDim.x * kPer));
     for (int k = 0; k < steps; k += kAtOnce) {
-        float x[kAtOnce][8], y[kAtOnce][8];
+        Raw<T> x[kAtOnce], y[kAtOnce];
         int ts[kAtOnce], hs[kAtOnce];
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
@@ -222,15 +222,15 @@ __global__ void __launch_bounds__(256) delta_kernel(const __grid_constant__ RowA
             t += step_t, h += step_h;
             if (h >= a.n_q) h -= a.n_q, ++t;
             const bool in = ts[e] < a.mask.T && f < a.d;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) x[e][c] = y[e][c] = 0.f;
-            if (in) load8(x[e], a.o.at(ts[e], hs[e]) + f), load8(y[e], a.d_o.at(ts[e], hs[e]) + f);
+            x[e].zero(), y[e].zero();
+            if (in) x[e].load(a.o.at(ts[e], hs[e]) + f), y[e].load(a.d_o.at(ts[e], hs[e]) + f);
         }
 #pragma unroll
         for (int e = 0; e < kAtOnce; ++e) {
-            float s = 0.f;
+            float s = 0.f, v[8], w[8];
+            x[e].get(v), y[e].get(w);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) s = fmaf(x[e][c], y[e][c], s);
+            for (int c = 0; c < 8; ++c) s = fmaf(v[c], w[c], s);
 #pragma unroll
             for (int o = 1; o < LP; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
             if (ts[e] < a.mask.T && f == 0) {
