@@ -43,12 +43,12 @@ class _Slots:
         base = ctypes.addressof(self.mem)
         self.at = [ctypes.c_void_p(base + _HEADS * i) for i in range(n)]
 
-    def put(self, i, x, T, n, d, dtype):
+    def put(self, i, x, shape, dtype):
         """Tensor [T, n, d] as argument i; its features are next to each other."""
-        if x.shape != (T, n, d) or x.dtype is not dtype or not x.is_cuda:
-            raise ValueError(f"expected a {dtype} CUDA tensor [{T}, {n}, {d}], got {x.dtype} {list(x.shape)} on {x.device}")
+        if x.shape != shape or x.dtype is not dtype or not x.is_cuda:
+            raise ValueError(f"expected a {dtype} CUDA tensor {list(shape)}, got {x.dtype} {list(x.shape)} on {x.device}")
         row, head, one = x.stride()
-        if one != 1 and d > 1:
+        if one != 1:
             raise ValueError("the features of a head have to be next to each other")
         _PACK(self.mem, _HEADS * i, x.data_ptr(), row, head)
 
@@ -56,12 +56,14 @@ class _Slots:
         _PACK(self.mem, _HEADS * i, p, row, head)
 
 
-def _flat(x, name, dtype, *shape):
-    """A contiguous device tensor of the given shape, or None."""
-    if x is not None and (x.shape != shape or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous()):
+def _flat(x, name, dtype, shape):
+    """Address of a contiguous device tensor of the given shape; None stays None."""
+    if x is None:
+        return None
+    if x.shape != shape or x.dtype is not dtype or not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} CUDA tensor {list(shape)}, got {x.dtype} "
                          f"{list(x.shape)} on {x.device}")
-    return x
+    return x.data_ptr()
 
 
 # ---------------------------------------------------------------- rotary positions
@@ -93,6 +95,10 @@ class RopeBuffers:
         self.q, self.k = torch.empty((T, n_q, d), **new), torch.empty((T, n_kv, d), **new)
         self._h = _Slots(7)
         self._ref = ctypes.byref(self.desc)
+        self._q, self._k = (T, n_q, d), (T, n_kv, d)
+        self._qkv, self._pos, self._table, self._gain = (T, (n_q + 2 * n_kv) * d), (T,), (positions, self.rot), (d,)
+        step = d * (2 if self.desc.dtype == NOBLE_BF16 else 4)
+        self._to_k, self._to_v = n_q * step, (n_q + n_kv) * step
         if with_grads:
             self.workspace_bytes = binding.load().noble_rope_bwd_workspace_bytes(self._ref)
             self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
@@ -103,19 +109,19 @@ class RopeBuffers:
 
     def _put_qkv(self, qkv):
         """The queries, keys and values of a packed projection output as arguments 0 to 2."""
-        T, d, n_q, n_kv = self.T, self.d, self.n_q, self.n_kv
-        if qkv.shape != (T, (n_q + 2 * n_kv) * d) or qkv.dtype is not self.dtype or not qkv.is_cuda or qkv.stride(1) != 1:
-            raise ValueError(f"expected a {self.dtype} CUDA tensor [{T}, {(n_q + 2 * n_kv) * d}] of contiguous rows, got "
-                             f"{qkv.dtype} {list(qkv.shape)} on {qkv.device}")
-        p, row, step = qkv.data_ptr(), qkv.stride(0), d * qkv.element_size()
-        h = self._h
-        h.raw(0, p, row, d)
-        h.raw(1, p + n_q * step, row, d)
-        h.raw(2, p + (n_q + n_kv) * step, row, d)
+        if qkv.shape != self._qkv or qkv.dtype is not self.dtype or not qkv.is_cuda:
+            raise ValueError(f"expected a {self.dtype} CUDA tensor {list(self._qkv)}, got {qkv.dtype} {list(qkv.shape)} on "
+                             f"{qkv.device}")
+        p, (row, one), d, mem = qkv.data_ptr(), qkv.stride(), self.d, self._h.mem
+        if one != 1:
+            raise ValueError("the rows of a projection's output have to be contiguous")
+        _PACK(mem, 0, p, row, d)
+        _PACK(mem, _HEADS, p + self._to_k, row, d)
+        _PACK(mem, 2 * _HEADS, p + self._to_v, row, d)
 
     def _common(self, pos, table, gain_q, gain_k):
-        return (_p(_flat(pos, "pos", torch.int32, self.T)), _p(_flat(table, "table", torch.float32, self.positions, self.rot)),
-                _p(_flat(gain_q, "gain_q", torch.float32, self.d)), _p(_flat(gain_k, "gain_k", torch.float32, self.d)))
+        return (_flat(pos, "pos", torch.int32, self._pos), _flat(table, "table", torch.float32, self._table),
+                _flat(gain_q, "gain_q", torch.float32, self._gain), _flat(gain_k, "gain_k", torch.float32, self._gain))
 
 
 def rope_forward(buf: RopeBuffers, qkv, pos, table, gain_q=None, gain_k=None, stream=None):
@@ -123,8 +129,8 @@ def rope_forward(buf: RopeBuffers, qkv, pos, table, gain_q=None, gain_k=None, st
     buf._put_qkv(qkv)
     pos, table, gain_q, gain_k = buf._common(pos, table, gain_q, gain_k)
     h = buf._h
-    h.put(3, buf.q, buf.T, buf.n_q, buf.d, buf.dtype)
-    h.put(4, buf.k, buf.T, buf.n_kv, buf.d, buf.dtype)
+    h.put(3, buf.q, buf._q, buf.dtype)
+    h.put(4, buf.k, buf._k, buf.dtype)
     _check(binding.load().noble_rope_fwd(buf._ref, h.at[0], h.at[1], pos, table, gain_q, gain_k, h.at[3], h.at[4],
                                          _stream_handle(stream)))
     return buf.q, buf.k
@@ -136,10 +142,10 @@ def rope_backward(buf: RopeBuffers, dq, dk, qkv, pos, table, gain_q=None, gain_k
     buf._put_qkv(qkv)
     pos, table, gain_q, gain_k = buf._common(pos, table, gain_q, gain_k)
     h = buf._h
-    h.put(3, dq, buf.T, buf.n_q, buf.d, buf.dtype)
-    h.put(4, dk, buf.T, buf.n_kv, buf.d, buf.dtype)
-    h.put(5, buf.dxq, buf.T, buf.n_q, buf.d, buf.dtype)
-    h.put(6, buf.dxk, buf.T, buf.n_kv, buf.d, buf.dtype)
+    h.put(3, dq, buf._q, buf.dtype)
+    h.put(4, dk, buf._k, buf.dtype)
+    h.put(5, buf.dxq, buf._q, buf.dtype)
+    h.put(6, buf.dxk, buf._k, buf.dtype)
     _check(binding.load().noble_rope_bwd(buf._ref, h.at[3], h.at[4], h.at[0], h.at[1], pos, table, gain_q, gain_k,
                                          h.at[5], h.at[6], buf.dgain_q.data_ptr(), buf.dgain_k.data_ptr(),
                                          buf.workspace.data_ptr(), buf.workspace_bytes, _stream_handle(stream)))
@@ -174,9 +180,9 @@ def kv_append(buf: RopeBuffers, cache: PagedCache, qkv, pos, slots, table, gain_
     buf._put_qkv(qkv)
     pos, table, gain_q, gain_k = buf._common(pos, table, gain_q, gain_k)
     h = buf._h
-    h.put(3, buf.q, buf.T, buf.n_q, buf.d, buf.dtype)
+    h.put(3, buf.q, buf._q, buf.dtype)
     _check(binding.load().noble_kv_append(buf._ref, h.at[0], h.at[1], h.at[2], pos,
-                                          _p(_flat(slots, "slots", torch.int64, buf.T)), table, gain_q, gain_k, h.at[3],
+                                          _flat(slots, "slots", torch.int64, buf._pos), table, gain_q, gain_k, h.at[3],
                                           cache._ref, _stream_handle(stream)))
     return buf.q
 
@@ -198,6 +204,7 @@ class AttnBuffers:
         self.o = torch.empty((T, n_q, d), **new)
         self.lse = torch.empty((n_q, T), dtype=torch.float32, device=device)
         self._h = _Slots(8)
+        self._q, self._k, self._docs = (T, n_q, d), (T, n_kv, d), (n_docs + 1,)
         self._ref = ctypes.byref(self.desc)
         if with_grads:
             self.workspace_bytes = binding.load().noble_attn_bwd_workspace_bytes(self._ref)
@@ -206,13 +213,13 @@ class AttnBuffers:
             self.dv = torch.empty((T, n_kv, d), **new) if dv is None else dv
 
     def _inputs(self, q, k, v, doc_start, prefix, slope):
-        h, T, d, t = self._h, self.T, self.d, self.dtype
-        h.put(0, q, T, self.n_q, d, t)
-        h.put(1, k, T, self.n_kv, d, t)
-        h.put(2, v, T, self.n_kv, d, t)
-        h.put(3, self.o, T, self.n_q, d, t)
-        return (_p(_flat(doc_start, "doc_start", torch.int32, self.n_docs + 1)),
-                _p(_flat(prefix, "prefix", torch.int32, self.n_docs)), _p(_flat(slope, "slope", torch.float32, self.n_q)))
+        h, t = self._h, self.dtype
+        h.put(0, q, self._q, t)
+        h.put(1, k, self._k, t)
+        h.put(2, v, self._k, t)
+        h.put(3, self.o, self._q, t)
+        return (_flat(doc_start, "doc_start", torch.int32, self._docs), _flat(prefix, "prefix", torch.int32, (self.n_docs,)),
+                _flat(slope, "slope", torch.float32, (self.n_q,)))
 
 
 def attn_forward(buf: AttnBuffers, q, k, v, doc_start, prefix=None, slope=None, stream=None):
@@ -228,11 +235,11 @@ def attn_backward(buf: AttnBuffers, d_o, q, k, v, doc_start, prefix=None, slope=
     """Gradients of attn_forward, whose ``buf.o`` and ``buf.lse`` it reads, into ``buf.dq``,
     ``buf.dk`` and ``buf.dv``."""
     doc, pre, slo = buf._inputs(q, k, v, doc_start, prefix, slope)
-    h, T, d, t = buf._h, buf.T, buf.d, buf.dtype
-    h.put(4, d_o, T, buf.n_q, d, t)
-    h.put(5, buf.dq, T, buf.n_q, d, t)
-    h.put(6, buf.dk, T, buf.n_kv, d, t)
-    h.put(7, buf.dv, T, buf.n_kv, d, t)
+    h, t = buf._h, buf.dtype
+    h.put(4, d_o, buf._q, t)
+    h.put(5, buf.dq, buf._q, t)
+    h.put(6, buf.dk, buf._k, t)
+    h.put(7, buf.dv, buf._k, t)
     at = h.at
     _check(binding.load().noble_attn_bwd(buf._ref, at[4], at[0], at[1], at[2], doc, pre, slo, at[3], buf.lse.data_ptr(),
                                          at[5], at[6], at[7], buf.workspace.data_ptr(), buf.workspace_bytes,
@@ -254,6 +261,7 @@ class PagedBuffers:
         self.o = torch.empty((self.rows, n_q, d), dtype=self.dtype, device=device)
         self.lse = torch.empty((self.rows, n_q), dtype=torch.float32, device=device) if with_lse else None
         self._h = _Slots(2)
+        self._q, self._seqs = (self.rows, n_q, d), (n_seq,)
         self._ref = ctypes.byref(self.desc)
         self.workspace_bytes = binding.load().noble_attn_paged_workspace_bytes(self._ref)
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
@@ -266,11 +274,12 @@ def attn_paged(buf: PagedBuffers, q, cache: PagedCache, page_table, kv_len, slop
     if cache.n_kv != buf.n_kv or cache.d != buf.d or cache.dtype is not buf.dtype:
         raise ValueError("the cache has other heads or another type than the buffers")
     h = buf._h
-    h.put(0, q, buf.rows, buf.n_q, buf.d, buf.dtype)
-    h.put(1, buf.o, buf.rows, buf.n_q, buf.d, buf.dtype)
-    buf.desc.max_pages = page_table.shape[1]
+    h.put(0, q, buf._q, buf.dtype)
+    h.put(1, buf.o, buf._q, buf.dtype)
+    wide = page_table.shape[-1]
+    buf.desc.max_pages = wide
     _check(binding.load().noble_attn_paged(
-        buf._ref, h.at[0], cache._ref, _p(_flat(page_table, "page_table", torch.int32, buf.n_seq, page_table.shape[1])),
-        _p(_flat(kv_len, "kv_len", torch.int32, buf.n_seq)), _p(_flat(slope, "slope", torch.float32, buf.n_q)), h.at[1],
+        buf._ref, h.at[0], cache._ref, _flat(page_table, "page_table", torch.int32, (buf.n_seq, wide)),
+        _flat(kv_len, "kv_len", torch.int32, buf._seqs), _flat(slope, "slope", torch.float32, (buf.n_q,)), h.at[1],
         _p(buf.lse), buf.workspace.data_ptr(), buf.workspace_bytes, _stream_handle(stream)))
     return buf.o

@@ -240,7 +240,7 @@ noble_status attn_fwd_simt(const attn::RowArgs<T> &a, cudaStream_t st)
     namespace s = attn::simt;
     constexpr size_t smem = s::kFwdFloats<DP> * 4;
     NOBLE_TRY((allow<&s::fwd_kernel<DP, T>>(smem)));
-    const dim3 grid((unsigned)ceil_div(a.mask.T, s::kB), (unsigned)a.n_q);
+    const dim3 grid((unsigned)ceil_div(a.mask.T, s::kM), (unsigned)a.n_q);
     return run(st, {"attn_fwd_simt", kBoundAlu, 0.0, 0.0}, [&] { s::fwd_kernel<DP, T><<<grid, s::kThreads, smem, st>>>(a); });
 }
 
@@ -264,7 +264,7 @@ noble_status attn_bwd_simt(const attn::RowArgs<T> &a, float *delta, const int2 *
     constexpr size_t smem = s::kBwdFloats<DP> * 4;
     NOBLE_TRY((allow<&s::dkv_kernel<DP, T>>(smem)));
     NOBLE_TRY((allow<&s::dq_kernel<DP, T>>(smem)));
-    const unsigned blocks = (unsigned)ceil_div(a.mask.T, s::kB);
+    const unsigned blocks = (unsigned)ceil_div(a.mask.T, s::kM);
     NOBLE_TRY(run(st, {"attn_dq_simt", kBoundAlu, 0.0, 0.0},
                   [&] { s::dq_kernel<DP, T><<<dim3(blocks, (unsigned)a.n_q), s::kThreads, smem, st>>>(a, delta); }));
     return run(st, {"attn_dkv_simt", kBoundAlu, 0.0, 0.0},

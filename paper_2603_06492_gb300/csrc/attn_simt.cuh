@@ -2,7 +2,8 @@
 // with NOBLE_ATTN_SIMT_ONLY of bf16 ones.  One pass over the keys with the running
 // maximum and sum of a softmax (forward); probabilities again from lse (backward).
 //
-// Blocks of 64 x 64 scores, 256 threads of 4 x 4 each.  A step over four features
+// Blocks of 32 x 64 scores, 128 threads of 4 x 4 each: small ones, so that several share an
+// SM and hide each other's loads and barriers.  A step over four features
 // takes 4 + 4 16-byte loads from shared memory for 64 FMAs a thread: rows padded by
 // four floats make the strided loads of 16 consecutive rows free of conflicts.
 // Backward in two kernels, one per side of the scores, so that every sum has one
@@ -16,15 +17,16 @@ namespace noble {
 namespace attn {
 namespace simt {
 
-constexpr int kB = 64, kThreads = 256, kPP = kB + 4;
+constexpr int kM = 32, kB = 64, kThreads = 128, kPP = kB + 4;  // rows and columns of a block
 
 template <int DP> constexpr int kLd = DP + 4;  // floats of a padded row
 
-// Rows [r0, r0 + 64) of head h as fp32, zeros at rows >= limit and features >= d.
-template <int DP, typename T>
+// Rows [r0, r0 + ROWS) of head h as fp32, zeros at rows >= limit and features >= d.
+template <int DP, int ROWS, typename T>
 __device__ __forceinline__ void load_tile(float *sm, const Heads<const T> &x, int64_t h, int r0, int limit, int d)
 {
-    for (int c = threadIdx.x; c < kB * DP / 4; c += kThreads) {
+#pragma unroll 8
+    for (int c = threadIdx.x; c < ROWS * DP / 4; c += kThreads) {
         const int row = c / (DP / 4), f = c % (DP / 4) * 4;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (r0 + row < limit && f < d) v = load4(x.at(r0 + row, h) + f);
@@ -33,7 +35,7 @@ __device__ __forceinline__ void load_tile(float *sm, const Heads<const T> &x, in
 }
 
 // s[r][c] = rows (ty + RS r) of A . rows (tx + 16 c) of B
-template <int DP, int R = 4, int RS = 16>
+template <int DP, int R = 4, int RS = 8>
 __device__ __forceinline__ void dots(float (&s)[R][4], const float *A, const float *B, int ty, int tx)
 {
 #pragma unroll
@@ -60,7 +62,7 @@ __device__ __forceinline__ void dots(float (&s)[R][4], const float *A, const flo
 }
 
 // acc[r][u] += sum_k P[ty + RS r][k] * B[k][features of thread tx]; features 64 u + 4 tx + 0..3
-template <int DP, int R = 4, int RS = 16>
+template <int DP, int R = 4, int RS = 8>
 __device__ __forceinline__ void accumulate(float4 (&acc)[R][DP / 64], const float *P, const float *B, int ty, int tx)
 {
 #pragma unroll 2
@@ -104,8 +106,8 @@ __device__ __forceinline__ void store_row(T *p, const float4 (&x)[U], float f, i
 }
 
 // shared memory, floats
-template <int DP> constexpr int kFwdFloats = 2 * kB * kLd<DP> + kB * kPP;
-template <int DP> constexpr int kBwdFloats = 4 * kB * kLd<DP> + 2 * kB * kPP;
+template <int DP> constexpr int kFwdFloats = (kM + kB) * kLd<DP> + kM * kPP;
+template <int DP> constexpr int kBwdFloats = 2 * (kM + kB) * kLd<DP> + 2 * kM * kPP;
 
 // s in place of q.k, with its derivative by scale q.k (softcap only)
 __device__ __forceinline__ float score(const Score &sc, float slope, float qk, int far, float *deriv)
@@ -124,33 +126,33 @@ template <int DP, typename T>
 __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ RowArgs<T> a)
 {
     extern __shared__ float sm[];
-    float *Q = sm, *KV = Q + kB * kLd<DP>, *P = KV + kB * kLd<DP>;
-    __shared__ int redo[kB];
+    float *Q = sm, *KV = Q + kM * kLd<DP>, *P = KV + kB * kLd<DP>;
+    __shared__ int redo[kM];
     const int T_ = a.mask.T, tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    const int i0 = (int)(gridDim.x - 1 - blockIdx.x) * kB, h = blockIdx.y, g = h / (a.n_q / a.n_kv);
+    const int i0 = (int)(gridDim.x - 1 - blockIdx.x) * kM, h = blockIdx.y, g = h / (a.n_q / a.n_kv);
     const float slope = a.score.slope ? a.score.slope[h] : 0.f;
     Range rg[4];
     float m[4], l[4];
     float4 acc[4][DP / 64];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int i = i0 + ty + 16 * r;
+        const int i = i0 + ty + 8 * r;
         rg[r] = i < T_ ? visible(a.mask, i) : Range{0, 0};
         m[r] = -INFINITY, l[r] = 0.f;
 #pragma unroll
         for (int u = 0; u < DP / 64; ++u) acc[r][u] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    const int lo = visible(a.mask, i0).lo, hi = visible(a.mask, min(i0 + kB, T_) - 1).hi;
-    load_tile<DP>(Q, a.q, h, i0, T_, a.d);
+    const int lo = visible(a.mask, i0).lo, hi = visible(a.mask, min(i0 + kM, T_) - 1).hi;
+    load_tile<DP, kM>(Q, a.q, h, i0, T_, a.d);
     for (int j0 = lo; j0 < hi; j0 += kB) {
         __syncthreads();
-        load_tile<DP>(KV, a.k, g, j0, hi, a.d);
+        load_tile<DP, kB>(KV, a.k, g, j0, hi, a.d);
         __syncthreads();
         float s[4][4];
         dots<DP>(s, Q, KV, ty, tx);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = i0 + ty + 16 * r;
+            const int i = i0 + ty + 8 * r;
             float top = m[r];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ R
             for (int c = 0; c < 4; ++c) {
                 s[r][c] = exp2f((s[r][c] - base) * kLog2e);
                 sum += s[r][c];
-                P[(ty + 16 * r) * kPP + tx + 16 * c] = s[r][c];
+                P[(ty + 8 * r) * kPP + tx + 16 * c] = s[r][c];
             }
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -177,26 +179,26 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ R
                 acc[r][u].x *= f, acc[r][u].y *= f, acc[r][u].z *= f, acc[r][u].w *= f;
         }
         __syncthreads();
-        load_tile<DP>(KV, a.v, g, j0, hi, a.d);
+        load_tile<DP, kB>(KV, a.v, g, j0, hi, a.d);
         __syncthreads();
         accumulate<DP>(acc, P, KV, ty, tx);
     }
-    if (tid < kB) redo[tid] = 0;
+    if (tid < kM) redo[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int i = i0 + ty + 16 * r;
+        const int i = i0 + ty + 8 * r;
         if (i >= T_) continue;
         const bool none = rg[r].lo >= rg[r].hi;
         if (none)
 #pragma unroll
             for (int u = 0; u < DP / 64; ++u) acc[r][u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!finite(acc[r]) || !isfinite(none ? 0.f : l[r])) redo[ty + 16 * r] = 1;
+        if (!finite(acc[r]) || !isfinite(none ? 0.f : l[r])) redo[ty + 8 * r] = 1;
         store_row(a.out.at(i, h), acc[r], l[r] > 0.f ? 1.f / l[r] : 0.f, a.d, tx);
         if (tx == 0) a.lse[(int64_t)h * T_ + i] = l[r] > 0.f ? m[r] + logf(l[r]) : -INFINITY;
     }
     __syncthreads();
-    for (int r = tid / 32; r < kB; r += kThreads / 32)
+    for (int r = tid / 32; r < kM; r += kThreads / 32)
         if (redo[r]) row_fwd(a, i0 + r, h, tid % 32);
 }
 
@@ -271,27 +273,27 @@ template <int DP, typename T>
 __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ RowArgs<T> a, const int2 *ranges)
 {
     extern __shared__ float sm[];
-    float *K = sm, *V = K + kB * kLd<DP>, *Q = V + kB * kLd<DP>, *DO = Q + kB * kLd<DP>;
-    float *P = DO + kB * kLd<DP>, *DS = P + kB * kPP;
-    __shared__ int redo[kB];
+    float *K = sm, *V = K + kM * kLd<DP>, *Q = V + kM * kLd<DP>, *DO = Q + kB * kLd<DP>;
+    float *P = DO + kB * kLd<DP>, *DS = P + kM * kPP;
+    __shared__ int redo[kM];
     __shared__ int2 rg[kB];
     __shared__ float lse[kB], delta[kB];
     const int T_ = a.mask.T, tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    const int j0 = blockIdx.x * kB, g = blockIdx.y, group = a.n_q / a.n_kv;
-    const Range qs = queries_of(ranges, T_, j0, min(j0 + kB, docs_end(a.mask)));
+    const int j0 = blockIdx.x * kM, g = blockIdx.y, group = a.n_q / a.n_kv;
+    const Range qs = queries_of(ranges, T_, j0, min(j0 + kM, docs_end(a.mask)));
     float4 dk[4][DP / 64], dv[4][DP / 64];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int u = 0; u < DP / 64; ++u) dk[r][u] = dv[r][u] = make_float4(0.f, 0.f, 0.f, 0.f);
-    load_tile<DP>(K, a.k, g, j0, T_, a.d);
-    load_tile<DP>(V, a.v, g, j0, T_, a.d);
+    load_tile<DP, kM>(K, a.k, g, j0, T_, a.d);
+    load_tile<DP, kM>(V, a.v, g, j0, T_, a.d);
     for (int h = g * group; h < (g + 1) * group; ++h) {
         const float slope = a.score.slope ? a.score.slope[h] : 0.f;
         for (int i0 = qs.lo; i0 < qs.hi; i0 += kB) {
             __syncthreads();
-            load_tile<DP>(Q, a.q, h, i0, qs.hi, a.d);
-            load_tile<DP>(DO, a.d_o, h, i0, qs.hi, a.d);
+            load_tile<DP, kB>(Q, a.q, h, i0, qs.hi, a.d);
+            load_tile<DP, kB>(DO, a.d_o, h, i0, qs.hi, a.d);
             if (tid < kB) {
                 const int i = i0 + tid;
                 rg[tid] = i < qs.hi ? ranges[i] : make_int2(0, 0);
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ R
             for (int r = 0; r < 4; ++r)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const int j = j0 + ty + 16 * r, q = tx + 16 * c;
+                    const int j = j0 + ty + 8 * r, q = tx + 16 * c;
                     float p = 0.f, ds = 0.f;
                     if (j >= rg[q].x && j < rg[q].y) {
                         float g1 = 1.f;
@@ -314,26 +316,26 @@ __global__ void __launch_bounds__(kThreads) dkv_kernel(const __grid_constant__ R
                         p = exp2f((x - lse[q]) * kLog2e);
                         ds = p * (dp[r][c] - delta[q]) * g1;
                     }
-                    P[(ty + 16 * r) * kPP + q] = p;
-                    DS[(ty + 16 * r) * kPP + q] = ds;
+                    P[(ty + 8 * r) * kPP + q] = p;
+                    DS[(ty + 8 * r) * kPP + q] = ds;
                 }
             __syncthreads();
             accumulate<DP>(dv, P, DO, ty, tx);
             accumulate<DP>(dk, DS, Q, ty, tx);
         }
     }
-    if (tid < kB) redo[tid] = 0;
+    if (tid < kM) redo[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int j = j0 + ty + 16 * r;
+        const int j = j0 + ty + 8 * r;
         if (j >= T_) continue;
-        if (!finite(dk[r]) || !finite(dv[r])) redo[ty + 16 * r] = 1;
+        if (!finite(dk[r]) || !finite(dv[r])) redo[ty + 8 * r] = 1;
         store_row(a.dk.at(j, g), dk[r], a.score.scale, a.d, tx);
         store_row(a.dv.at(j, g), dv[r], 1.f, a.d, tx);
     }
     __syncthreads();
-    for (int r = tid / 32; r < kB; r += kThreads / 32)
+    for (int r = tid / 32; r < kM; r += kThreads / 32)
         if (redo[r]) row_dkv(a, j0 + r, g, tid % 32, true, true);
 }
 
@@ -344,31 +346,31 @@ template <int DP, typename T>
 __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ RowArgs<T> a, float *delta_out)
 {
     extern __shared__ float sm[];
-    float *Q = sm, *DO = Q + kB * kLd<DP>, *K = DO + kB * kLd<DP>, *V = K + kB * kLd<DP>, *DS = V + kB * kLd<DP>;
-    __shared__ int redo[kB];
+    float *Q = sm, *DO = Q + kM * kLd<DP>, *K = DO + kM * kLd<DP>, *V = K + kB * kLd<DP>, *DS = V + kB * kLd<DP>;
+    __shared__ int redo[kM];
     const int T_ = a.mask.T, tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    const int i0 = (int)(gridDim.x - 1 - blockIdx.x) * kB, h = blockIdx.y, g = h / (a.n_q / a.n_kv);
+    const int i0 = (int)(gridDim.x - 1 - blockIdx.x) * kM, h = blockIdx.y, g = h / (a.n_q / a.n_kv);
     const float slope = a.score.slope ? a.score.slope[h] : 0.f;
     Range rg[4];
     float lse[4], delta[4];
     float4 dq[4][DP / 64];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int i = i0 + ty + 16 * r;
+        const int i = i0 + ty + 8 * r;
         rg[r] = i < T_ ? visible(a.mask, i) : Range{0, 0};
         lse[r] = i < T_ ? a.lse[(int64_t)h * T_ + i] : 0.f;
         delta[r] = i < T_ ? a.delta[(int64_t)h * T_ + i] : 0.f;
 #pragma unroll
         for (int u = 0; u < DP / 64; ++u) dq[r][u] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    const int lo = visible(a.mask, i0).lo, hi = visible(a.mask, min(i0 + kB, T_) - 1).hi;
+    const int lo = visible(a.mask, i0).lo, hi = visible(a.mask, min(i0 + kM, T_) - 1).hi;
     const bool one = hi - lo <= kB;
-    load_tile<DP>(Q, a.q, h, i0, T_, a.d);
-    load_tile<DP>(DO, a.d_o, h, i0, T_, a.d);
+    load_tile<DP, kM>(Q, a.q, h, i0, T_, a.d);
+    load_tile<DP, kM>(DO, a.d_o, h, i0, T_, a.d);
     for (int j0 = lo; j0 < hi; j0 += kB) {
         __syncthreads();
-        load_tile<DP>(K, a.k, g, j0, hi, a.d);
-        load_tile<DP>(V, a.v, g, j0, hi, a.d);
+        load_tile<DP, kB>(K, a.k, g, j0, hi, a.d);
+        load_tile<DP, kB>(V, a.v, g, j0, hi, a.d);
         __syncthreads();
         float s[4][4], dp[4][4];
         dots<DP>(s, Q, K, ty, tx);
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Ro
                 const int j = j0 + tx + 16 * c;
                 g1[c] = 1.f;
                 const bool in = j >= rg[r].lo && j < rg[r].hi;
-                const float x = in ? score(a.score, slope, s[r][c], i0 + ty + 16 * r - j, &g1[c]) : 0.f;
+                const float x = in ? score(a.score, slope, s[r][c], i0 + ty + 8 * r - j, &g1[c]) : 0.f;
                 s[r][c] = in ? exp2f((x - lse[r]) * kLog2e) : 0.f;
                 if (!in) dp[r][c] = 0.f;
                 sum = fmaf(s[r][c], dp[r][c], sum);
@@ -390,32 +392,32 @@ __global__ void __launch_bounds__(kThreads) dq_kernel(const __grid_constant__ Ro
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 delta[r] = sum;
-                if (tx == 0 && rg[r].lo < rg[r].hi) delta_out[(int64_t)h * T_ + i0 + ty + 16 * r] = sum;
+                if (tx == 0 && rg[r].lo < rg[r].hi) delta_out[(int64_t)h * T_ + i0 + ty + 8 * r] = sum;
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int j = j0 + tx + 16 * c;
-                DS[(ty + 16 * r) * kPP + tx + 16 * c] =
+                DS[(ty + 8 * r) * kPP + tx + 16 * c] =
                     j >= rg[r].lo && j < rg[r].hi ? s[r][c] * (dp[r][c] - delta[r]) * g1[c] : 0.f;
             }
         }
         __syncthreads();
         accumulate<DP>(dq, DS, K, ty, tx);
     }
-    if (tid < kB) redo[tid] = 0;
+    if (tid < kM) redo[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int i = i0 + ty + 16 * r;
+        const int i = i0 + ty + 8 * r;
         if (i >= T_) continue;
         if (rg[r].lo >= rg[r].hi)
 #pragma unroll
             for (int u = 0; u < DP / 64; ++u) dq[r][u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!finite(dq[r])) redo[ty + 16 * r] = 1;
+        if (!finite(dq[r])) redo[ty + 8 * r] = 1;
         store_row(a.dq.at(i, h), dq[r], a.score.scale, a.d, tx);
     }
     __syncthreads();
-    for (int r = tid / 32; r < kB; r += kThreads / 32)
+    for (int r = tid / 32; r < kM; r += kThreads / 32)
         if (redo[r]) row_dq(a, i0 + r, h, tid % 32, delta_out[(int64_t)h * T_ + i0 + r], 0, a.d);
 }
 

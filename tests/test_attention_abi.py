@@ -158,6 +158,6 @@ def test_torch_side_refuses_other_tensors(lib):
     from paper_2603_06492_gb300 import attention as A
     x = torch.zeros(3, 2, 8)
     with pytest.raises(ValueError):
-        A._Slots(1).put(0, x, 3, 2, 8, torch.float32)  # not on a GPU
+        A._Slots(1).put(0, x, (3, 2, 8), torch.float32)  # not on a GPU
     with pytest.raises(ValueError):
-        A._flat(x, "x", torch.float32, 3, 2, 9)
+        A._flat(x, "x", torch.float32, (3, 2, 9))
