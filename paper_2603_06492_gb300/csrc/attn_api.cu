@@ -125,6 +125,20 @@ rope::Args<T> rope_args(const noble_rope_desc *d, const noble_heads *q, const no
     return a;
 }
 
+// f(mode, lanes per head) as constants; heads of 64 and 128 features have kernels of their own
+template <class F>
+void rope_kernel(int mode, int lp, F &&f)
+{
+    auto with = [&](auto m) {
+        if (lp == 8) f(m, std::integral_constant<int, 8>{});
+        else if (lp == 16) f(m, std::integral_constant<int, 16>{});
+        else f(m, std::integral_constant<int, 0>{});
+    };
+    if (mode == rope::kHalf) with(std::integral_constant<int, rope::kHalf>{});
+    else if (mode == rope::kInterleaved) with(std::integral_constant<int, rope::kInterleaved>{});
+    else f(std::integral_constant<int, rope::kAny>{}, std::integral_constant<int, 0>{});
+}
+
 template <bool APPEND, typename T>
 noble_status rope_fwd_launch(const noble_rope_desc *d, rope::Args<T> &a, cudaStream_t st)
 {
@@ -142,9 +156,7 @@ noble_status rope_fwd_launch(const noble_rope_desc *d, rope::Args<T> &a, cudaStr
     const int mode = rope_mode(d);
     return run(st, ki, [&] {
         const dim3 grid((unsigned)blocks), block(32 * rope::kWarps);
-        if (mode == rope::kHalf) rope::fwd_kernel<rope::kHalf, APPEND, T><<<grid, block, 0, st>>>(a);
-        else if (mode == rope::kInterleaved) rope::fwd_kernel<rope::kInterleaved, APPEND, T><<<grid, block, 0, st>>>(a);
-        else rope::fwd_kernel<rope::kAny, APPEND, T><<<grid, block, 0, st>>>(a);
+        rope_kernel(mode, a.lp, [&](auto m, auto lp) { rope::fwd_kernel<m.value, APPEND, lp.value, T><<<grid, block, 0, st>>>(a); });
     });
 }
 
@@ -167,9 +179,7 @@ noble_status rope_bwd_launch(const noble_rope_desc *d, rope::Args<T> &a, float *
     const KernelInfo ki{"rope_bwd", kBoundHbm, 0.0, (a.norm ? 3.0 : 2.0) * sizeof(T) * a.tokens * a.d * (a.n_q + a.n_kv)};
     const int mode = rope_mode(d);
     NOBLE_TRY(run(st, ki, [&] {
-        if (mode == rope::kHalf) rope::bwd_kernel<rope::kHalf, T><<<blocks, 32 * rope::kWarps, 0, st>>>(a);
-        else if (mode == rope::kInterleaved) rope::bwd_kernel<rope::kInterleaved, T><<<blocks, 32 * rope::kWarps, 0, st>>>(a);
-        else rope::bwd_kernel<rope::kAny, T><<<blocks, 32 * rope::kWarps, 0, st>>>(a);
+        rope_kernel(mode, a.lp, [&](auto m, auto lp) { rope::bwd_kernel<m.value, lp.value, T><<<blocks, 32 * rope::kWarps, 0, st>>>(a); });
     }));
     if (!a.part) return NOBLE_OK;
     const KernelInfo kg{"rope_gain", kBoundHbm, 0.0, 8.0 * blocks * a.d};

@@ -129,29 +129,32 @@ __device__ __forceinline__ void turn8(float (&x)[8], const float (&y)[8], const 
     }
 }
 
+// LP: lanes of a head, 0 for a number that only the arguments know
+template <int LP>
 __device__ __forceinline__ float head_sum(float v, int lp)
 {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
+    for (int o = 1; o < (LP ? LP : 32); o <<= 1) {
         const float w = __shfl_xor_sync(0xffffffffu, v, o);
-        v += o < lp ? w : 0.f;
+        v += LP || o < lp ? w : 0.f;
     }
     return v;
 }
 
 // A warp: `take` batches of a token, the next one's loads in flight while one is worked on.
-template <int MODE, bool APPEND, typename T>
+template <int MODE, bool APPEND, int LP, typename T>
 __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 3 : 2) fwd_kernel(const __grid_constant__ Args<T> a)
 {
     __shared__ float bufs[MODE == kAny ? kWarps : 1][256];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t u = (int64_t)blockIdx.x * kWarps + warp;
     if (u >= a.tokens * a.groups) return;
-    const int64_t t = u / a.groups;
-    const int hp = 32 / a.lp, f = lane % a.lp * 8, own = lane / a.lp;
+    // a 64-bit division costs as much as a head
+    const int64_t t = a.groups == 1 ? u : u >> 32 ? u / a.groups : (uint32_t)u / (uint32_t)a.groups;
+    const int lp = LP ? LP : a.lp, hp = 32 / lp, f = lane % lp * 8, own = lane / lp;
     const bool in = f < a.d;
     const int all = a.batches_q + (APPEND ? 2 : 1) * a.batches_kv;
-    const int b0 = (int)(u % a.groups) * a.take, b1 = min(b0 + a.take, all);
+    const int b0 = (int)(u - t * a.groups) * a.take, b1 = min(b0 + a.take, all);
     // batch b: heads first + own + p * hp of its kind (0 queries, 1 keys, 2 values)
     auto kind_of = [&](int b) { return b < a.batches_q ? 0 : b < a.batches_q + a.batches_kv ? 1 : 2; };
     auto first_of = [&](int b, int kind) { return (b - (kind ? a.batches_q + (kind - 1) * a.batches_kv : 0)) * kPasses * hp + own; };
@@ -220,7 +223,7 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 
                     float s = 0.f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-                    scale = rsqrtf(fmaf(head_sum(s, a.lp), a.inv_d, a.eps));
+                    scale = rsqrtf(fmaf(head_sum<LP>(s, a.lp), a.inv_d, a.eps));
                 }
                 turn8<MODE>(x, y, tn, f, a.rot);
 #pragma unroll
@@ -240,12 +243,12 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 
 
 // Persistent over the batches of the queries, then of the keys, so that a lane adds up its
 // features' gain gradients in registers, the block in shared memory: one partial per block.
-template <int MODE, typename T>
+template <int MODE, int LP, typename T>
 __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_constant__ Args<T> a)
 {
     __shared__ float bufs[kWarps][256];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int hp = 32 / a.lp, f = lane % a.lp * 8, own = lane / a.lp;
+    const int lp = LP ? LP : a.lp, hp = 32 / lp, f = lane % lp * 8, own = lane / lp;
     const bool in = f < a.d;
     for (int kind = 0; kind < 2; ++kind) {
         const Heads<const T> &xs = kind ? a.k : a.q, &ds = kind ? a.dk : a.dq;
@@ -256,12 +259,14 @@ __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_consta
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = 1.f, sum[i] = 0.f;
         if (gain && in) load8(g, gain + f);
-        const int64_t units = a.tokens * per, stride = (int64_t)gridDim.x * kWarps;
+        // unit = (token, batch); a stride of the grid's warps is step_t tokens and step_b batches
         const int64_t u0 = (int64_t)blockIdx.x * kWarps + warp;
-        int pos = u0 < units ? a.pos[u0 / per] : 0;
-        for (int64_t u = u0; u < units; u += stride) {
-            const int64_t t = u / per;
-            const int h0 = (int)(u % per) * kPasses * hp + own;
+        const int stride = gridDim.x * kWarps, step_t = stride / per, step_b = stride - step_t * per;
+        int64_t t = u0 / per;
+        int b = (int)(u0 - t * per);
+        int pos = t < a.tokens ? a.pos[t] : 0;
+        while (t < a.tokens) {
+            const int h0 = b * kPasses * hp + own;
             Raw<T> rx[kPasses], rd[kPasses];
 #pragma unroll
             for (int p = 0; p < kPasses; ++p) {
@@ -275,7 +280,10 @@ __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_consta
             if (!known && lane == 0) raise_status(a.status, kStatusBadIndex);
             Turn tn;
             load_turn<MODE, -1>(tn, a.table + (int64_t)(known ? pos : 0) * a.rot, known && in ? f : a.rot, a.rot, a.interleaved);
-            if (u + stride < units) pos = a.pos[(u + stride) / per];
+            int64_t t_next = t + step_t;
+            b += step_b;
+            if (b >= per) b -= per, ++t_next;
+            if (t_next < a.tokens) pos = a.pos[t_next];
 #pragma unroll
             for (int p = 0; p < kPasses; ++p) {
                 const bool real = in && h0 + p * hp < n;
@@ -291,7 +299,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_consta
                     rx[p].get(x);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-                    const float scale = rsqrtf(fmaf(head_sum(s, a.lp), a.inv_d, a.eps));
+                    const float scale = rsqrtf(fmaf(head_sum<LP>(s, a.lp), a.inv_d, a.eps));
                     s = 0.f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -300,7 +308,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_consta
                         w[i] *= g[i];
                         s = fmaf(w[i], x[i], s);
                     }
-                    s = head_sum(s, a.lp) * a.inv_d;
+                    s = head_sum<LP>(s, a.lp) * a.inv_d;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) w[i] = scale * fmaf(-x[i], s, w[i]);
                 }
@@ -308,6 +316,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_consta
                 o.set(w);
                 if (real) o.store(out.at(t, h0 + p * hp) + f);
             }
+            t = t_next;
         }
         if (!a.part) continue;
         // over the heads side by side in the warp, then over the warps, in order
@@ -318,7 +327,7 @@ __global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_consta
         for (int e = threadIdx.x; e < a.d; e += 32 * kWarps) {
             float s = 0.f;
             for (int w = 0; w < kWarps; ++w)
-                for (int j = 0; j < hp; ++j) s += bufs[w][j * a.lp * 8 + e];
+                for (int j = 0; j < hp; ++j) s += bufs[w][j * lp * 8 + e];
             a.part[((int64_t)blockIdx.x * 2 + kind) * a.d + e] = s;
         }
         __syncthreads();
