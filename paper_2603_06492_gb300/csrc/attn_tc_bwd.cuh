@@ -16,8 +16,6 @@
 // dV and the next S run while dS is formed, dK and the next dP while the next P is.
 #pragma once
 
-#include <cuda_fp16.h>
-
 #include "attn_tc.cuh"
 
 namespace noble {
@@ -82,21 +80,6 @@ __device__ __forceinline__ Range queries_of(const Mask &m, int j0, int j1)
     const int s = clampi(m.doc_start[z], 0, m.T), e = clampi(m.doc_start[z + 1], s, m.T);
     r.hi = m.window ? min(e, j1 - 1 + m.window) : e;
     return r;
-}
-
-// 64 score columns: x holds q.k, out s in units of log 2, g ds / d(scale q.k)
-template <bool GENERAL>
-__device__ __forceinline__ float score2(const Score &sc, float slope, float sl, float x, int far, float &g)
-{
-    if (!GENERAL) return x * sl;
-    float y = x * sc.scale;
-    g = 1.f;
-    if (sc.softcap > 0.f) {
-        const float t = tanh_exp(y * (1.f / sc.softcap));
-        g = fmaf(-t, t, 1.f);
-        y = sc.softcap * t;
-    }
-    return fmaf(-slope, fabsf((float)far), y * kLog2e);
 }
 
 // ---------------------------------------------------------------- dq
@@ -328,7 +311,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 uint32_t pk[32];
                 const int lo = rg.lo - j0, hi = rg.hi - j0;
                 const bool all = __all_sync(0xffffffffu, lo <= 0 && hi >= 64);
-                // p over s; over dp what multiplies p - with the score's derivative, if it has one
+                // p over s, and 0 for it and dp where nothing is seen
+                uint32_t gs[GENERAL ? 32 : 1];
                 if (!GENERAL) {
                     const uint64_t sl2 = pack2(sl, sl), l2 = pack2(-lse2, -lse2);
 #pragma unroll
@@ -337,22 +321,22 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                         unpack2(fma2(pack2(s[c], s[c + 1]), sl2, l2), a, b);
                         s[c] = exp2_fast(a), s[c + 1] = exp2_fast(b);
                     }
-                    if (!all)
+                } else {
+                    general_scores<64, GENERAL>(s, gs, args.a.score, slope, (float)(i - j0));
 #pragma unroll
-                        for (int c = 0; c < 64; ++c) {
-                            const bool in = c >= lo && c < hi;
-                            s[c] = in ? s[c] : 0.f, dp[c] = in ? dp[c] : 0.f;
-                        }
+                    for (int c = 0; c < 64; ++c) s[c] = exp2_fast(s[c] - lse2);
                 }
+                if (!all)
+#pragma unroll
+                    for (int c = 0; c < 64; ++c) {
+                        const bool in = c >= lo && c < hi;
+                        s[c] = in ? s[c] : 0.f, dp[c] = in ? dp[c] : 0.f;
+                    }
                 if (p.steps == 1) {
                     // all that the row sees is here: delta from p and dp themselves (see simt::dq_kernel)
                     float sum = 0.f;
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) {
-                        float g, q = s[c];
-                        if (GENERAL) q = c >= lo && c < hi ? exp2_fast(score2<true>(args.a.score, slope, sl, s[c], i - j0 - c, g) - lse2) : 0.f;
-                        sum = GENERAL && q == 0.f ? sum : fmaf(q, dp[c], sum);
-                    }
+                    for (int c = 0; c < 64; ++c) sum = fmaf(s[c], dp[c], sum);
                     part[128 * half + row] = sum;
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive(sums);
@@ -363,27 +347,16 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                     delta = part[row] + part[128 + row];
                     if (half == 0 && !none) args.delta[at] = delta;
                 }
-                if (!GENERAL) {
-                    const uint64_t d2 = pack2(-delta, -delta);
+                const uint64_t d2 = pack2(-delta, -delta);
 #pragma unroll
-                    for (int c = 0; c < 64; c += 2) {
-                        float a, b;
-                        unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), d2)), a, b);
-                        pk[c / 2] = ptx::pack_bf16x2(a, b);
+                for (int c = 0; c < 64; c += 2) {
+                    float a, b;
+                    unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), d2)), a, b);
+                    if (GENERAL) {
+                        const float2 g = __half22float2(*reinterpret_cast<const __half2 *>(&gs[c / 2]));
+                        a *= g.x, b *= g.y;
                     }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 64; c += 2) {
-                        float e[2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            float g;
-                            const float x = score2<true>(args.a.score, slope, sl, s[c + u], i - j0 - c - u, g);
-                            const float d = exp2_fast(x - lse2) * (dp[c + u] - delta) * g;
-                            e[u] = c + u >= lo && c + u < hi ? d : 0.f;
-                        }
-                        pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
-                    }
+                    pk[c / 2] = ptx::pack_bf16x2(a, b);
                 }
                 __syncwarp();
                 tmem_st32(tS, pk);
@@ -702,15 +675,12 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 } else {
                     const int h = p.g * group + t / p.per;
                     const float slope = args.a.score.slope ? args.a.score.slope[h] * kLog2e : 0.f;
+                    general_scores<64, GENERAL>(s, gs, args.a.score, slope, (float)(j - i0));
 #pragma unroll
-                    for (int c = 0; c < 64; c += 2) {
-                        float g[2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            s[c + u] = exp2_fast(score2<true>(args.a.score, slope, sl, s[c + u], i0 + c + u - j, g[u]) - vec[c + u]);
-                        // the derivative to 16 bits of the product that dS is rounded to 8 of
-                        const __half2 hg = __floats2half2_rn(g[0], g[1]);
-                        gs[c / 2] = *reinterpret_cast<const uint32_t *>(&hg);
+                    for (int c = 0; c < 64; c += 4) {
+                        const float4 l = *reinterpret_cast<const float4 *>(vec + c);
+                        s[c] = exp2_fast(s[c] - l.x), s[c + 1] = exp2_fast(s[c + 1] - l.y);
+                        s[c + 2] = exp2_fast(s[c + 2] - l.z), s[c + 3] = exp2_fast(s[c + 3] - l.w);
                     }
                 }
                 if (!all)

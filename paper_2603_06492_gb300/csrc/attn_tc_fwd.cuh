@@ -280,13 +280,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 float v[128];
                 as_floats(v, x);
                 if (GENERAL) {
-                    // in units of log 2
-#pragma unroll
-                    for (int c = 0; c < 128; ++c) {
-                        float y = v[c] * args.a.score.scale;
-                        if (args.a.score.softcap > 0.f) y = args.a.score.softcap * tanh_exp(y * (1.f / args.a.score.softcap));
-                        v[c] = fmaf(-slope, fabsf((float)(i - j0 - c)), y * kLog2e);
-                    }
+                    uint32_t none[1];
+                    general_scores<128, false>(v, none, args.a.score, slope, (float)(i - j0));
                 }
                 const int lo = rg.lo - j0, hi = rg.hi - j0;
                 if (!__all_sync(0xffffffffu, lo <= 0 && hi >= kRows)) {
