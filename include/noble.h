@@ -608,6 +608,14 @@ noble_status noble_debug_raise_device_status(uint32_t bits);
 noble_status noble_debug_wait_expiry(uint64_t limit_ns, uint32_t *result, noble_stream stream);
 
 /*
+ * Testing hook (no paper counterpart): synchronises `stream`, then reads and
+ * clears the number of rows (of o, dq, dk, dv, or of o over a cache) that the
+ * attention kernels of the current device have computed again because they came
+ * out not finite.  Zero for inputs that are finite throughout.
+ */
+noble_status noble_debug_rows_again(uint64_t *count, noble_stream stream);
+
+/*
  * Testing hook (no paper counterpart): the library's tensor-core GEMM alone,
  *     C[z][m][n] = sum_k A0(m,k) B0(n,k) + sum_k A1(m,k) B1(n,k) (+ bias[n])
  * with bf16 operands and fp32 accumulation.  A_s is row-major [M][K_s]

@@ -207,6 +207,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
         lib.noble_attn_bwd.argtypes = [AD] + [P] * 13 + [S, P]
         lib.noble_attn_paged_workspace_bytes.argtypes = [PD]
         lib.noble_attn_paged.argtypes = [PD] + [P] * 8 + [S, P]
+        lib.noble_debug_rows_again.argtypes = [ctypes.POINTER(ctypes.c_uint64), P]
+        lib.noble_debug_rows_again.restype = ctypes.c_int
         for n in ("rope_table", "rope_fwd", "rope_bwd", "kv_append", "attn_fwd", "attn_bwd", "attn_paged"):
             getattr(lib, "noble_" + n).restype = ctypes.c_int
         for n in ("rope_bwd", "attn_bwd", "attn_paged"):
@@ -373,6 +375,13 @@ def noble_debug_raise_device_status(bits: int):
 
 def noble_debug_wait_expiry(limit_ns: int, result, stream=None):
     _check(load().noble_debug_wait_expiry(limit_ns, _p(result), _stream_handle(stream)))
+
+
+def noble_debug_rows_again(stream=None) -> int:
+    """Rows that attention kernels computed again since the last call (see noble.h)."""
+    n = ctypes.c_uint64()
+    _check(load().noble_debug_rows_again(ctypes.byref(n), stream))
+    return n.value
 
 
 def profile_read() -> dict:

@@ -752,4 +752,19 @@ noble_status noble_attn_paged(const noble_paged_desc *desc, const noble_heads *q
     return paged<float>(desc, q, cache, page_table, kv_len, slope, o, lse, static_cast<char *>(workspace), st);
 }
 
+noble_status noble_debug_rows_again(uint64_t *count, noble_stream stream)
+{
+    g_last_error[0] = 0;
+    if (!count) return fail(NOBLE_ERR_INVALID_ARG, "count is NULL");
+    NOBLE_TRY(check_device());
+    const unsigned long long zero = 0;
+    unsigned long long v = 0;
+    cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, attn::g_rows_again, sizeof(v));
+    if (e == cudaSuccess && v) e = cudaMemcpyToSymbol(attn::g_rows_again, &zero, sizeof(zero));
+    if (e != cudaSuccess) return fail(NOBLE_ERR_CUDA, "count: %s", cudaGetErrorString(e));
+    *count = v;
+    return NOBLE_OK;
+}
+
 }  // extern "C"

@@ -204,6 +204,13 @@ __device__ __forceinline__ float warp_sum(float v)
 // The tiled kernels multiply masked places by zero, which an infinity or a NaN in
 // such a place turns into NaN; a row that comes out not finite is computed again
 // here, where masked places are not read at all.  Lanes hold features lane + 32 u.
+// They count, so that a test can tell that nothing else sends rows here.
+__device__ unsigned long long g_rows_again = 0;
+__device__ __forceinline__ void count_row(int lane)
+{
+    if (lane == 0) atomicAdd(&g_rows_again, 1ull);
+}
+
 template <typename T>
 struct RowArgs {
     Mask mask;
@@ -250,6 +257,7 @@ __device__ __forceinline__ float row_score(const Score &s, float qk, int h, int 
 template <typename T>
 __device__ __noinline__ void row_fwd(const RowArgs<T> &a, int i, int h, int lane)
 {
+    count_row(lane);
     const Range r = visible(a.mask, i);
     const int g = h / (a.n_q / a.n_kv);
     float q[4], acc[4] = {}, m = -INFINITY, l = 0.f;
@@ -287,6 +295,7 @@ __device__ __forceinline__ void row_pair(const RowArgs<T> &a, const float (&q)[4
 template <typename T>
 __device__ __noinline__ void row_dq(const RowArgs<T> &a, int i, int h, int lane, float delta, int f0, int f1)
 {
+    count_row(lane);
     const Range r = visible(a.mask, i);
     const int g = h / (a.n_q / a.n_kv);
     const float lse = a.lse[(int64_t)h * a.mask.T + i];
@@ -329,6 +338,7 @@ __device__ __forceinline__ Range seen_by(const Mask &m, int j)
 template <typename T>
 __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane, bool to_dv, bool to_dk)
 {
+    count_row(lane);
     const Range r = seen_by(a.mask, j);
     const int group = a.n_q / a.n_kv;
     float k[4], v[4], dk[4] = {}, dv[4] = {};

@@ -60,6 +60,7 @@ __device__ __forceinline__ int64_t place(const Args<T> &a, int n, int j)
 template <typename T>
 __device__ __noinline__ void row_paged(const Args<T> &a, int64_t t, int h, int lane)
 {
+    count_row(lane);
     const int n = (int)(t / a.q_len), g = h / (a.n_q / a.n_kv);
     const Span sp = span(a, n);
     const int pos = sp.raw - a.q_len + (int)(t % a.q_len);

@@ -103,9 +103,12 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     auto v_full = [&](int s) { return bars + 8u * (2 * kXS + s); };
     auto v_empty = [&](int s) { return bars + 8u * (2 * kXS + kYS + s); };
     const uint32_t one = bars + 8u * (2 * kXS + 2 * kYS);
-    const uint32_t q_full = one, q_empty = one + 8, dp_full = one + 16, dp_read = one + 24, ds_full = one + 32, acc_full = one + 40,
-                   acc_empty = one + 48, sums = one + 56;
-    auto s_full = [&](int i) { return one + 64 + 8u * (i & 1); };  // by buffer: the next S does not wait for this one's readers
+    const uint32_t q_full = one, q_empty = one + 8, dp_full = one + 16, dp_read = one + 24, acc_full = one + 32,
+                   acc_empty = one + 40, sums = one + 48;
+    // By S buffer, since both run a step ahead: the next S does not wait for this one's
+    // readers, and a warp can be through with the next dS while another is at this one.
+    auto s_full = [&](int i) { return one + 56 + 8u * (i & 1); };
+    auto ds_full = [&](int i) { return one + 72 + 8u * (i & 1); };
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
     float *part = reinterpret_cast<float *>(smem + B::kVec);  // [2][128]
@@ -131,7 +134,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         ptx::mbar_init(s_full(1), 1);
         ptx::mbar_init(dp_full, 1);
         ptx::mbar_init(dp_read, 8);
-        ptx::mbar_init(ds_full, 8);
+        ptx::mbar_init(ds_full(0), 8);
+        ptx::mbar_init(ds_full(1), 8);
         ptx::mbar_init(acc_full, 1);
         ptx::mbar_init(acc_empty, 8);
         ptx::mbar_init(sums, 8);
@@ -234,7 +238,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 for (int t = 0; ok && t < p.steps; ++t) {
                     // S over the dS that the product before last has read
                     if (t + 1 < p.steps) ok = score() && dprob(t + 2 == p.steps);
-                    ok = ok && wait_warp(ds_full, i_q & 1, status) && (t > 0 || wait_warp(acc_empty, (items & 1) ^ 1, status));
+                    ok = ok && wait_warp(ds_full(i_q), (i_q >> 1) & 1, status) && (t > 0 || wait_warp(acc_empty, (items & 1) ^ 1, status));
                     if (!ok) break;
                     ptx::tc_fence_after();
                     const uint32_t ds = tmem + (i_q & 1 ? kS1 : kS0);
@@ -363,7 +367,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 tmem_wait_st();
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ds_full);
+                if (lane == 0) ptx::mbar_arrive(ds_full(n));
             }
             if (!ok) break;
             more = works.take(pc, w, true, false, lane, status);
