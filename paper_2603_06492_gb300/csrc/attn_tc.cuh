@@ -10,6 +10,7 @@
 #pragma once
 
 #include <cuda_fp16.h>
+#include <type_traits>
 
 #include "attn_mask.cuh"
 #include "sm100_ptx.cuh"
@@ -179,57 +180,72 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 // tanh takes an exponential and a reciprocal, which with the softmax's own exponential
 // make the special function unit the limit.  Where all of a warp's arguments are within
 // 0.6 its Taylor series to x^15 does, whose first term left out is 6e-4 x^17: at most
-// 2e-7 of the result.  One document of 4096 tokens, 16 + 4 heads of 128, cap 30, us without
-// the series / with it: forward TANH_FWD, backward TANH_BWD.
+// 2e-7 of the result.  Ragged documents of 7001 tokens, 16 + 4 heads of 128, cap 30: forward
+// 136 us without the series, 123 with it.
+enum : int { kNoCap = 0, kCapSeries = 1, kCapExact = 2 };
+struct Capping {
+    float in, out;  // kNoCap: s = out q.k
+    int mode;
+};
+template <int N>
+__device__ __forceinline__ Capping capping(const float (&x)[N], const Score &sc)
+{
+    if (!(sc.softcap > 0.f)) return {0.f, sc.scale * kLog2e, kNoCap};
+    const float in = sc.scale / sc.softcap;
+    float top[4] = {};
+#pragma unroll
+    for (int c = 0; c < N; c += 4)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], fabsf(x[c + u]));
+    const bool small = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(in) < 0.6f;
+    return {in, sc.softcap * kLog2e, __all_sync(0xffffffffu, small) ? kCapSeries : kCapExact};
+}
+// Two scores, in place, and their derivatives.
+template <int MODE, bool GRAD>
+__device__ __forceinline__ void cap_pair(float &x, float &y, float &gx, float &gy, const Capping &cap)
+{
+    if (MODE == kNoCap) {
+        x *= cap.out, y *= cap.out;
+        if (GRAD) gx = gy = 1.f;
+    } else if (MODE == kCapSeries) {
+        const float k[7] = {-1.f / 3.f, 2.f / 15.f, -17.f / 315.f, 62.f / 2835.f, -1382.f / 155925.f, 21844.f / 6081075.f,
+                            -929569.f / 638512875.f};
+        const uint64_t one2 = pack2(1.f, 1.f), a = mul2(pack2(x, y), pack2(cap.in, cap.in)), u = mul2(a, a);
+        uint64_t p = pack2(k[6], k[6]);
+#pragma unroll
+        for (int e = 5; e >= 0; --e) p = fma2(p, u, pack2(k[e], k[e]));
+        const uint64_t t = mul2(a, fma2(p, u, one2));
+        unpack2(mul2(t, pack2(cap.out, cap.out)), x, y);
+        if (GRAD) unpack2(fma2(mul2(t, t), pack2(-1.f, -1.f), one2), gx, gy);
+    } else {
+        const float t = tanh_exp(x * cap.in), u = tanh_exp(y * cap.in);
+        if (GRAD) gx = fmaf(-t, t, 1.f), gy = fmaf(-u, u, 1.f);
+        x = t * cap.out, y = u * cap.out;
+    }
+}
+// f(MODE) for the mode of a Capping
+template <class F>
+__device__ __forceinline__ void with_cap(int mode, F &&f)
+{
+    if (mode == kNoCap) f(std::integral_constant<int, kNoCap>{});
+    else if (mode == kCapSeries) f(std::integral_constant<int, kCapSeries>{});
+    else f(std::integral_constant<int, kCapExact>{});
+}
 template <int N, bool GRAD>
 __device__ __forceinline__ void general_scores(float (&x)[N], uint32_t (&gs)[GRAD ? N / 2 : 1], const Score &sc, float slope, float far)
 {
-    auto keep = [&](int c, float a, float b) {
-        const __half2 h = __floats2half2_rn(a, b);
-        gs[GRAD ? c / 2 : 0] = *reinterpret_cast<const uint32_t *>(&h);
-    };
-    if (sc.softcap > 0.f) {
-        const float in = sc.scale / sc.softcap, out = sc.softcap * kLog2e;
-        float top[4] = {};
-#pragma unroll
-        for (int c = 0; c < N; c += 4)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], fabsf(x[c + u]));
-        const bool small = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(in) < 0.6f;
-        const uint64_t in2 = pack2(in, in), out2 = pack2(out, out), one2 = pack2(1.f, 1.f), minus2 = pack2(-1.f, -1.f);
-        if (__all_sync(0xffffffffu, small)) {
-            const float k[7] = {-1.f / 3.f, 2.f / 15.f, -17.f / 315.f, 62.f / 2835.f, -1382.f / 155925.f, 21844.f / 6081075.f,
-                                -929569.f / 638512875.f};
-#pragma unroll
-            for (int c = 0; c < N; c += 2) {
-                const uint64_t a = mul2(pack2(x[c], x[c + 1]), in2), u = mul2(a, a);
-                uint64_t p = pack2(k[6], k[6]);
-#pragma unroll
-                for (int e = 5; e >= 0; --e) p = fma2(p, u, pack2(k[e], k[e]));
-                const uint64_t t = mul2(a, fma2(p, u, one2));
-                unpack2(mul2(t, out2), x[c], x[c + 1]);
-                if (GRAD) {
-                    float g, h;
-                    unpack2(fma2(mul2(t, t), minus2, one2), g, h);
-                    keep(c, g, h);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < N; c += 2) {
-                const float t = tanh_exp(x[c] * in), u = tanh_exp(x[c + 1] * in);
-                if (GRAD) keep(c, fmaf(-t, t, 1.f), fmaf(-u, u, 1.f));
-                x[c] = t * out, x[c + 1] = u * out;
-            }
-        }
-    } else {
-        const float f = sc.scale * kLog2e;
+    const Capping cap = capping(x, sc);
+    with_cap(cap.mode, [&](auto mode) {
 #pragma unroll
         for (int c = 0; c < N; c += 2) {
-            x[c] *= f, x[c + 1] *= f;
-            if (GRAD) keep(c, 1.f, 1.f);
+            float a, b;
+            cap_pair<mode.value, GRAD>(x[c], x[c + 1], a, b, cap);
+            if (GRAD) {
+                const __half2 h = __floats2half2_rn(a, b);
+                gs[GRAD ? c / 2 : 0] = *reinterpret_cast<const uint32_t *>(&h);
+            }
         }
-    }
+    });
     if (sc.slope) {
 #pragma unroll
         for (int c = 0; c < N; ++c) x[c] = fmaf(-slope, fabsf(far - (float)c), x[c]);

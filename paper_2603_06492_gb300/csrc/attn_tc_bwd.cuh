@@ -315,9 +315,19 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 uint32_t pk[32];
                 const int lo = rg.lo - j0, hi = rg.hi - j0;
                 const bool all = __all_sync(0xffffffffu, lo <= 0 && hi >= 64);
-                // p over s, and 0 for it and dp where nothing is seen
-                uint32_t gs[GENERAL ? 32 : 1];
+                auto total = [&](float sum) {  // over both threads of a row; in a bounded wait's time
+                    part[128 * half + row] = sum;
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(sums);
+                    ok = ptx::mbar_wait(sums, nsums & 1, status);
+                    ok = __all_sync(0xffffffffu, ok);
+                    ++nsums;
+                    return part[row] + part[128 + row];
+                };
+                // With one step, all that the row sees is here: delta is then summed from p and dp
+                // themselves (see simt::dq_kernel).
                 if (!GENERAL) {
+                    // p over s, and 0 for it and dp where nothing is seen
                     const uint64_t sl2 = pack2(sl, sl), l2 = pack2(-lse2, -lse2);
 #pragma unroll
                     for (int c = 0; c < 64; c += 2) {
@@ -325,43 +335,59 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                         unpack2(fma2(pack2(s[c], s[c + 1]), sl2, l2), a, b);
                         s[c] = exp2_fast(a), s[c + 1] = exp2_fast(b);
                     }
+                    if (!all)
+#pragma unroll
+                        for (int c = 0; c < 64; ++c) {
+                            const bool in = c >= lo && c < hi;
+                            s[c] = in ? s[c] : 0.f, dp[c] = in ? dp[c] : 0.f;
+                        }
+                    if (p.steps == 1) {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int c = 0; c < 64; ++c) sum = fmaf(s[c], dp[c], sum);
+                        delta = total(sum);
+                    }
+                    const uint64_t d2 = pack2(-delta, -delta);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2) {
+                        float a, b;
+                        unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), d2)), a, b);
+                        pk[c / 2] = ptx::pack_bf16x2(a, b);
+                    }
                 } else {
-                    general_scores<64, GENERAL>(s, gs, args.a.score, slope, (float)(i - j0));
+                    // a pair of columns at a time from score to dS, since the derivatives have no room beside both
+                    const Capping cap = capping(s, args.a.score);
+                    const float far = (float)(i - j0);
+                    with_cap(cap.mode, [&](auto mode) {
+                        auto probs = [&](int c, float &x, float &y, float &gx, float &gy) {
+                            x = s[c], y = s[c + 1];
+                            cap_pair<mode.value, true>(x, y, gx, gy, cap);
+                            x = exp2_fast(fmaf(-slope, fabsf(far - (float)c), x) - lse2);
+                            y = exp2_fast(fmaf(-slope, fabsf(far - (float)(c + 1)), y) - lse2);
+                        };
+                        if (p.steps == 1) {
+                            float sum = 0.f;
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) s[c] = exp2_fast(s[c] - lse2);
+                            for (int c = 0; c < 64; c += 2) {
+                                float x, y, gx, gy;
+                                probs(c, x, y, gx, gy);
+                                sum += c >= lo && c < hi ? x * dp[c] : 0.f;
+                                sum += c + 1 >= lo && c + 1 < hi ? y * dp[c + 1] : 0.f;
+                            }
+                            delta = total(sum);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) {
+                            float x, y, gx, gy;
+                            probs(c, x, y, gx, gy);
+                            x *= (dp[c] - delta) * gx, y *= (dp[c + 1] - delta) * gy;
+                            if (!all) x = c >= lo && c < hi ? x : 0.f, y = c + 1 >= lo && c + 1 < hi ? y : 0.f;
+                            pk[c / 2] = ptx::pack_bf16x2(x, y);
+                        }
+                    });
                 }
-                if (!all)
-#pragma unroll
-                    for (int c = 0; c < 64; ++c) {
-                        const bool in = c >= lo && c < hi;
-                        s[c] = in ? s[c] : 0.f, dp[c] = in ? dp[c] : 0.f;
-                    }
-                if (p.steps == 1) {
-                    // all that the row sees is here: delta from p and dp themselves (see simt::dq_kernel)
-                    float sum = 0.f;
-#pragma unroll
-                    for (int c = 0; c < 64; ++c) sum = fmaf(s[c], dp[c], sum);
-                    part[128 * half + row] = sum;
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(sums);
-                    ok = ptx::mbar_wait(sums, nsums & 1, status);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    ++nsums;
-                    delta = part[row] + part[128 + row];
-                    if (half == 0 && !none) args.delta[at] = delta;
-                }
-                const uint64_t d2 = pack2(-delta, -delta);
-#pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    float a, b;
-                    unpack2(mul2(pack2(s[c], s[c + 1]), add2(pack2(dp[c], dp[c + 1]), d2)), a, b);
-                    if (GENERAL) {
-                        const float2 g = __half22float2(*reinterpret_cast<const __half2 *>(&gs[c / 2]));
-                        a *= g.x, b *= g.y;
-                    }
-                    pk[c / 2] = ptx::pack_bf16x2(a, b);
-                }
+                if (!ok) break;
+                if (p.steps == 1 && half == 0 && !none) args.delta[at] = delta;
                 __syncwarp();
                 tmem_st32(tS, pk);
                 tmem_wait_st();
