@@ -105,7 +105,7 @@ int64_t rope_batches(int64_t heads, int64_t d) { return ceil_div(heads, rope::kP
 int64_t rope_bwd_blocks(const noble_rope_desc *d)
 {
     const int64_t per = std::max(rope_batches(d->n_q, d->d), rope_batches(d->n_kv, d->d));
-    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->T * per, rope::kWarps), 2 * kSms));
+    return std::max<int64_t>(1, std::min<int64_t>(ceil_div(d->T * per, rope::kWarps), (d->dtype == NOBLE_BF16 ? rope::kBwdBlocks<bf> : rope::kBwdBlocks<float>)*kSms));
 }
 
 template <typename T>
@@ -154,9 +154,14 @@ noble_status rope_fwd_launch(const noble_rope_desc *d, rope::Args<T> &a, cudaStr
     const KernelInfo ki{APPEND ? "kv_append" : "rope_fwd", kBoundHbm, 0.0,
                         2.0 * sizeof(T) * a.tokens * a.d * (a.n_q + (APPEND ? 2 : 1) * a.n_kv)};
     const int mode = rope_mode(d);
+    noble_status allowed = NOBLE_OK;
+    rope_kernel(mode, a.lp, [&](auto m, auto lp) { allowed = allow<&rope::fwd_kernel<m.value, APPEND, lp.value, T>>(rope::kFwdBytes<T>); });
+    NOBLE_TRY(allowed);
     return run(st, ki, [&] {
         const dim3 grid((unsigned)blocks), block(32 * rope::kWarps);
-        rope_kernel(mode, a.lp, [&](auto m, auto lp) { rope::fwd_kernel<m.value, APPEND, lp.value, T><<<grid, block, 0, st>>>(a); });
+        rope_kernel(mode, a.lp, [&](auto m, auto lp) {
+            rope::fwd_kernel<m.value, APPEND, lp.value, T><<<grid, block, rope::kFwdBytes<T>, st>>>(a);
+        });
     });
 }
 
@@ -178,8 +183,13 @@ noble_status rope_bwd_launch(const noble_rope_desc *d, rope::Args<T> &a, float *
     const int blocks = (int)rope_bwd_blocks(d);
     const KernelInfo ki{"rope_bwd", kBoundHbm, 0.0, (a.norm ? 3.0 : 2.0) * sizeof(T) * a.tokens * a.d * (a.n_q + a.n_kv)};
     const int mode = rope_mode(d);
+    noble_status allowed = NOBLE_OK;
+    rope_kernel(mode, a.lp, [&](auto m, auto lp) { allowed = allow<&rope::bwd_kernel<m.value, lp.value, T>>(rope::kRingBytes<T>); });
+    NOBLE_TRY(allowed);
     NOBLE_TRY(run(st, ki, [&] {
-        rope_kernel(mode, a.lp, [&](auto m, auto lp) { rope::bwd_kernel<m.value, lp.value, T><<<blocks, 32 * rope::kWarps, 0, st>>>(a); });
+        rope_kernel(mode, a.lp, [&](auto m, auto lp) {
+            rope::bwd_kernel<m.value, lp.value, T><<<blocks, 32 * rope::kWarps, rope::kRingBytes<T>, st>>>(a);
+        });
     }));
     if (!a.part) return NOBLE_OK;
     const KernelInfo kg{"rope_gain", kBoundHbm, 0.0, 8.0 * blocks * a.d};

@@ -125,6 +125,39 @@ __device__ __forceinline__ void load8(float (&x)[8], const __nv_bfloat16 *p)
     for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ float sum2(uint64_t v)
+{
+    float a, b;
+    unpack2(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // 8 elements as they are in memory
 template <typename T> struct Raw;
 template <> struct Raw<__nv_bfloat16> {
@@ -140,6 +173,11 @@ template <> struct Raw<__nv_bfloat16> {
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    __device__ __forceinline__ void get(uint64_t (&x)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
     __device__ __forceinline__ void set(const float (&x)[8])
     {
@@ -178,6 +216,11 @@ template <> struct Raw<float> {
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[i];
+    }
+    __device__ __forceinline__ void get(uint64_t (&y)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = pack2(x[2 * i], x[2 * i + 1]);
     }
     __device__ __forceinline__ void set(const float (&y)[8])
     {

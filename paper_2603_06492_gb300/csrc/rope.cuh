@@ -3,10 +3,11 @@
 //
 // All of it moves every element once each way and is bound by that.  A lane holds 8
 // consecutive features of a head (16 bytes of bf16), LP lanes a head, so a warp
-// reads whole heads in 16-byte pieces; the sum of a norm is a butterfly over LP
+// reads whole heads in 16-byte pieces; the sums of norms go over LP
 // lanes.  A batch is kPasses * 32 / LP heads of one token and one kind (queries, keys or
-// values), whose loads are all issued before the first is used; they stay packed, and it
-// is the packed words that go to the other lane of a pair.  Gains are multiplied
+// values), copied to shared memory by the lanes that will use it; the values stay packed until
+// then, and it is the packed words that go to the other lane of a pair.  Arithmetic is two
+// features per instruction.  Gains are multiplied
 // into the cosines and sines once per kind, which leaves two products and a scale
 // per element.
 #pragma once
@@ -48,7 +49,12 @@ struct Args {
 };
 
 using attn::Raw;
+using attn::fma2;
 using attn::load8;
+using attn::mul2;
+using attn::pack2;
+using attn::sum2;
+using attn::unpack2;
 
 // Factors of a lane's 8 features: y_f = c x_f + s x_(other of f), s = 0 where f does not
 // rotate; with gains (norm) c holds f's and s its partner's.
@@ -98,54 +104,114 @@ __device__ __forceinline__ void load_turn(Turn &t, const float *row, int f, int 
     }
 }
 
-// The other features of the pairs of a lane's 8.  `buf`: 256 floats of the warp (kAny).
+// The other features of the pairs of a lane's 8, zeros for those that do not rotate (which
+// so do not meet their neighbours' values).  `buf`: 256 floats of the warp (kAny).
 template <int MODE, typename T>
-__device__ __forceinline__ void others(float (&y)[8], const Raw<T> &r, const float (&x)[8], int f, int rot, int interleaved,
-                                       float *buf, int lane)
+__device__ __forceinline__ void others(uint64_t (&y)[4], const Raw<T> &r, int f, int rot, int interleaved, float *buf, int lane)
 {
     if (MODE == kHalf) {
-        const int other = f >= rot ? lane : f < rot / 2 ? lane + rot / 16 : lane - rot / 16;
-        r.from(other & 31).get(y);
+        Raw<T> o = r.from((f >= rot ? lane : f < rot / 2 ? lane + rot / 16 : lane - rot / 16) & 31);
+        if (f >= rot) o.zero();
+        o.get(y);
     } else if (MODE == kInterleaved) {
+        Raw<T> o = r;
+        if (f >= rot) o.zero();
+        float x[8];
+        o.get(x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+        for (int i = 0; i < 4; ++i) y[i] = pack2(x[2 * i + 1], x[2 * i]);
     } else {
+        float x[8];
+        r.get(x);
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) buf[lane * 8 + i] = x[i];
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = f + i < rot ? buf[lane * 8 - f + partner<kAny>(f + i, rot, interleaved)] : 0.f;
+        for (int i = 0; i < 8; ++i) x[i] = f + i < rot ? buf[lane * 8 - f + partner<kAny>(f + i, rot, interleaved)] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = pack2(x[2 * i], x[2 * i + 1]);
     }
 }
-// x turned, in place; features that do not rotate do not meet their neighbours' values
-template <int MODE>
-__device__ __forceinline__ void turn8(float (&x)[8], const float (&y)[8], const Turn &t, int f, int rot)
+__device__ __forceinline__ void pack8(uint64_t (&p)[4], const float (&x)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float a = x[i] * t.c[i];
-        x[i] = (MODE == kAny ? f + i < rot : f < rot) ? fmaf(y[i], t.s[i], a) : a;
+    for (int i = 0; i < 4; ++i) p[i] = pack2(x[2 * i], x[2 * i + 1]);
+}
+
+// v[i] = the sum of every v[i] over the head's LP lanes (LP 0: lp of them, which only the
+// arguments know).  At each step of the butterfly a lane keeps half of the values, while there are
+// several, and hands the other half on; the sums go back to all at the end: 16 exchanges
+// for 8 values and 16 lanes, where a butterfly each would take 32, at one per clock and SM.
+template <int LP, int N>
+__device__ __forceinline__ void head_sums(float (&v)[N], int lp, int lane)
+{
+    if constexpr (LP == 0) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float w = __shfl_xor_sync(0xffffffffu, v[i], o);
+                v[i] += o < lp ? w : 0.f;
+            }
+    } else {
+        static_assert(LP >= N, "lanes for all values");
+        float u[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = v[i];
+#pragma unroll
+        for (int o = 1; o < LP; o <<= 1) {
+            const int n = N / (2 * o);  // values that are kept: those with this lane's bits so far
+            if (n) {
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    const float give = lane & o ? u[i] : u[i + n];
+                    u[i] = (lane & o ? u[i + n] : u[i]) + __shfl_xor_sync(0xffffffffu, give, o);
+                }
+            } else {
+                u[0] += __shfl_xor_sync(0xffffffffu, u[0], o);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            int from = 0;  // bit by bit, the upper half of what was left came from lanes with the bit set
+            for (int o = 1, n = N / 2, at = i; n; o <<= 1, n >>= 1)
+                if (at >= n) from |= o, at -= n;
+            v[i] = __shfl_sync(0xffffffffu, u[0], (lane & ~(LP - 1)) | from);
+        }
     }
 }
 
-// LP: lanes of a head, 0 for a number that only the arguments know
-template <int LP>
-__device__ __forceinline__ float head_sum(float v, int lp)
+// 16 bytes to shared memory, zeros if they are not `real`; a lane waits for its own.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool real)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+// What a lane copied: pieces of 16 bytes, 512 apart.
+template <typename T>
+__device__ __forceinline__ void taken(Raw<T> &r, const char *at)
 {
 #pragma unroll
-    for (int o = 1; o < (LP ? LP : 32); o <<= 1) {
-        const float w = __shfl_xor_sync(0xffffffffu, v, o);
-        v += LP || o < lp ? w : 0.f;
-    }
-    return v;
+    for (int c = 0; c < (int)sizeof(T) / 2; ++c) reinterpret_cast<uint4 *>(&r)[c] = *reinterpret_cast<const uint4 *>(at + c * 512);
 }
 
-// A warp: `take` batches of a token, the next one's loads in flight while one is worked on.
+// A warp: `take` batches of a token, which wait in shared memory: what is on its way costs no
+// registers there.  Bound by reading and
+// writing with the latency of what comes first (position, then its cosines): 16384 tokens of
+// 16 + 16 heads of 128 features 55 us, 4.9 TB/s; a batch ahead in registers 63.
+template <typename T> constexpr int kFwdRing = sizeof(T) == 2 ? 4 : 3;    // batches
+template <typename T> constexpr int kFwdBlocks = sizeof(T) == 2 ? 3 : 2;  // of an SM
+template <typename T> constexpr uint32_t kFwdBytes = kWarps * kFwdRing<T> * kPasses * 256 * sizeof(T);
 template <int MODE, bool APPEND, int LP, typename T>
-__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 3 : 2) fwd_kernel(const __grid_constant__ Args<T> a)
+__global__ void __launch_bounds__(32 * kWarps, MODE == kAny ? 2 : kFwdBlocks<T>) fwd_kernel(const __grid_constant__ Args<T> a)
 {
+    extern __shared__ __align__(16) char ring[];  // [warp][stage][pass][16 bytes][lane]
     __shared__ float bufs[MODE == kAny ? kWarps : 1][256];
+    constexpr int kPieces = sizeof(T) / 2, kStages = kFwdRing<T>;
+    constexpr uint32_t kStage = kPasses * 256 * sizeof(T);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t u = (int64_t)blockIdx.x * kWarps + warp;
     if (u >= a.tokens * a.groups) return;
@@ -158,17 +224,24 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 
     // batch b: heads first + own + p * hp of its kind (0 queries, 1 keys, 2 values)
     auto kind_of = [&](int b) { return b < a.batches_q ? 0 : b < a.batches_q + a.batches_kv ? 1 : 2; };
     auto first_of = [&](int b, int kind) { return (b - (kind ? a.batches_q + (kind - 1) * a.batches_kv : 0)) * kPasses * hp + own; };
-    auto load = [&](Raw<T> (&r)[kPasses], int b) {
-        const int kind = kind_of(b), h0 = first_of(b, kind), n = kind ? a.n_kv : a.n_q;
-        const Heads<const T> &x = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+    char *const mine = ring + warp * (kStages * kStage) + lane * 16;
+    const uint32_t mine_s = (uint32_t)__cvta_generic_to_shared(mine);
+    auto fetch = [&](int b) {
+        if (b < b1) {
+            const int kind = kind_of(b), h0 = first_of(b, kind), n = in ? kind ? a.n_kv : a.n_q : 0;
+            const Heads<const T> &x = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+            const T *at = x.at(t, h0) + f;
+            const uint32_t to = mine_s + (b - b0) % kStages * kStage;
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-            if (in && b < b1 && h0 + p * hp < n) r[p].load(x.at(t, h0 + p * hp) + f);
-            else r[p].zero();
+            for (int p = 0; p < kPasses; ++p, at += hp * x.head)
+#pragma unroll
+                for (int c = 0; c < kPieces; ++c)
+                    copy16(to + (p * kPieces + c) * 512, h0 + p * hp < n ? at + 4 * c : x.p, h0 + p * hp < n);
         }
+        copies_group();
     };
-    Raw<T> r[kPasses];
-    load(r, b0);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) fetch(b0 + i);
     const int pos = a.pos[t];
     const bool known = pos >= 0 && pos < a.positions;
     if (!known && lane == 0) raise_status(a.status, kStatusBadIndex);
@@ -183,18 +256,22 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 
             kc = a.k_cache + at, vc = a.v_cache + at;
         }
     }
-    Turn tn;
-    int have = -1;  // the kind that tn is for
+    uint64_t tc[4], ts[4];  // factors
+    int have = -1;          // of this kind
     for (int b = b0; b < b1; ++b) {
         const int kind = kind_of(b), h0 = first_of(b, kind), n = kind ? a.n_kv : a.n_q;
-        Raw<T> next[kPasses];
-        load(next, b + 1);
+        fetch(b + kStages - 1);
+        copies_wait<kStages - 1>();
+        Raw<T> r[kPasses];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) taken(r[p], mine + (b - b0) % kStages * kStage + p * kPieces * 512);
         if (APPEND && kind == 2) {
 #pragma unroll
             for (int p = 0; p < kPasses; ++p)
                 if (in && vc && h0 + p * hp < n) r[p].store(vc + (h0 + p * hp) * a.head + f);
         } else {
             const float *gain = kind ? a.gain_k : a.gain_q;
+            Turn tn;
             if (kind != have) load_turn<MODE, 1>(tn, row, known && in ? f : a.rot, a.rot, a.interleaved);
             if (kind != have && gain && in) {
                 float g[8];
@@ -211,118 +288,187 @@ __global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 && MODE != kAny ? 
                     for (int i = 0; i < 8; ++i) tn.s[i] *= g[i];
                 }
             }
+            if (kind != have) pack8(tc, tn.c), pack8(ts, tn.s);
             have = kind;
+            float scale[kPasses];
 #pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                const int h = h0 + p * hp;
-                float x[8], y[8];
-                r[p].get(x);
-                others<MODE>(y, r[p], x, f, a.rot, a.interleaved, bufs[MODE == kAny ? warp : 0], lane);
-                float scale = 1.f;
-                if (a.norm) {
-                    float s = 0.f;
+            for (int p = 0; p < kPasses; ++p) scale[p] = 1.f;
+            if (a.norm) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-                    scale = rsqrtf(fmaf(head_sum<LP>(s, a.lp), a.inv_d, a.eps));
+                for (int p = 0; p < kPasses; ++p) {
+                    uint64_t x[4], s = 0;
+                    r[p].get(x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s = fma2(x[i], x[i], s);
+                    scale[p] = sum2(s);
                 }
-                turn8<MODE>(x, y, tn, f, a.rot);
+                head_sums<LP>(scale, a.lp, lane);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = known ? x[i] * scale : 0.f;
+                for (int p = 0; p < kPasses; ++p) scale[p] = rsqrtf(fmaf(scale[p], a.inv_d, a.eps));
+            }
+            if (!known)
+#pragma unroll
+                for (int p = 0; p < kPasses; ++p) r[p].zero(), scale[p] = 0.f;
+            T *out = kind == 0 ? a.q_out.at(t, h0) + f : APPEND ? kc + h0 * a.head + f : a.k_out.at(t, h0) + f;
+            const int64_t step = hp * (kind == 0 ? a.q_out.head : APPEND ? a.head : a.k_out.head);
+            const int real = in && (!APPEND || kind == 0 || kc) ? n : 0;
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p, out += step) {
+                uint64_t x[4], y[4];
+                float z[8];
+                r[p].get(x);
+                others<MODE>(y, r[p], f, a.rot, a.interleaved, bufs[MODE == kAny ? warp : 0], lane);
+                const uint64_t s2 = pack2(scale[p], scale[p]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) unpack2(mul2(fma2(y[i], ts[i], mul2(x[i], tc[i])), s2), z[2 * i], z[2 * i + 1]);
                 Raw<T> o;
-                o.set(x);
-                if (!in || h >= n) continue;
-                if (kind == 0) o.store(a.q_out.at(t, h) + f);
-                else if (!APPEND) o.store(a.k_out.at(t, h) + f);
-                else if (kc) o.store(kc + h * a.head + f);
+                o.set(z);
+                if (h0 + p * hp < real) o.store(out);
             }
         }
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) r[p] = next[p];
     }
 }
 
 // Persistent over the batches of the queries, then of the keys, so that a lane adds up its
 // features' gain gradients in registers, the block in shared memory: one partial per block.
+// Two batches per warp are on their way to shared memory while one is worked on, 128 KB per
+// SM: in registers there is no room for more than the one.  16384 tokens of 16 + 16 heads of
+// 128 features 78 us, 5.1 TB/s, with loads to registers 85 (and 100 with a butterfly per sum):
+// reading and the issue of about 600 instructions a batch, four warps per scheduler.
+constexpr int kRing = 3;
+template <typename T> constexpr int kBwdBlocks = sizeof(T) == 2 ? 2 : 1;  // of an SM
+template <typename T> constexpr uint32_t kRingBytes = kWarps * kRing * 2 * kPasses * 256 * sizeof(T);
 template <int MODE, int LP, typename T>
-__global__ void __launch_bounds__(32 * kWarps, 2) bwd_kernel(const __grid_constant__ Args<T> a)
+__global__ void __launch_bounds__(32 * kWarps, kBwdBlocks<T>) bwd_kernel(const __grid_constant__ Args<T> a)
 {
+    extern __shared__ __align__(16) char ring[];  // [warp][stage][dy, x][pass][16 bytes][lane]
     __shared__ float bufs[kWarps][256];
+    constexpr int kPieces = sizeof(T) / 2;  // of 16 bytes of a lane's features
+    constexpr uint32_t kStage = 2 * kPasses * 256 * sizeof(T);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int lp = LP ? LP : a.lp, hp = 32 / lp, f = lane % lp * 8, own = lane / lp;
     const bool in = f < a.d;
+    char *const mine = ring + warp * (kRing * kStage) + lane * 16;
+    const uint32_t mine_s = (uint32_t)__cvta_generic_to_shared(mine);
     for (int kind = 0; kind < 2; ++kind) {
         const Heads<const T> &xs = kind ? a.k : a.q, &ds = kind ? a.dk : a.dq;
         const Heads<T> &out = kind ? a.k_out : a.q_out;
         const float *gain = kind ? a.gain_k : a.gain_q;
         const int n = kind ? a.n_kv : a.n_q, per = kind ? a.batches_kv : a.batches_q;
-        float g[8], sum[8];
+        float ones[8];
+        uint64_t g[4], sum[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = 1.f, sum[i] = 0.f;
-        if (gain && in) load8(g, gain + f);
+        for (int i = 0; i < 8; ++i) ones[i] = 1.f;
+        if (gain && in) load8(ones, gain + f);
+        pack8(g, ones);
         // unit = (token, batch); a stride of the grid's warps is step_t tokens and step_b batches
         const int64_t u0 = (int64_t)blockIdx.x * kWarps + warp;
         const int stride = gridDim.x * kWarps, step_t = stride / per, step_b = stride - step_t * per;
-        int64_t t = u0 / per;
-        int b = (int)(u0 - t * per);
-        int pos = t < a.tokens ? a.pos[t] : 0;
-        while (t < a.tokens) {
-            const int h0 = b * kPasses * hp + own;
-            Raw<T> rx[kPasses], rd[kPasses];
+        struct At {
+            int64_t t;
+            int b;
+        };
+        auto next = [&](At &x) {
+            x.t += step_t, x.b += step_b;
+            if (x.b >= per) x.b -= per, ++x.t;
+        };
+        const int real = in ? n : 0;
+        auto fetch = [&](const At &x, int stage) {
+            if (x.t < a.tokens) {
+                const int h0 = x.b * kPasses * hp + own;
+                const T *d_at = ds.at(x.t, h0) + f, *x_at = xs.at(x.t, h0) + f;
+                const uint32_t to = mine_s + stage * kStage;
 #pragma unroll
-            for (int p = 0; p < kPasses; ++p) {
-                rx[p].zero(), rd[p].zero();
-                if (in && h0 + p * hp < n) {
-                    rd[p].load(ds.at(t, h0 + p * hp) + f);
-                    if (a.norm) rx[p].load(xs.at(t, h0 + p * hp) + f);
+                for (int p = 0; p < kPasses; ++p, d_at += hp * ds.head, x_at += hp * xs.head) {
+                    const bool r = h0 + p * hp < real;
+#pragma unroll
+                    for (int c = 0; c < kPieces; ++c) {
+                        copy16(to + (p * kPieces + c) * 512, r ? d_at + 4 * c : ds.p, r);
+                        if (a.norm) copy16(to + ((kPasses + p) * kPieces + c) * 512, r ? x_at + 4 * c : xs.p, r);
+                    }
                 }
             }
+            copies_group();
+        };
+        At at{u0 / per, 0};
+        at.b = (int)(u0 - at.t * per);
+        At ahead = at;
+        int stage = 0;
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) fetch(ahead, i), next(ahead);
+        int pos = at.t < a.tokens ? a.pos[at.t] : 0;
+        while (at.t < a.tokens) {
+            fetch(ahead, stage ? stage - 1 : kRing - 1);
+            next(ahead);
+            const int64_t t = at.t;
+            const int h0 = at.b * kPasses * hp + own;
             const bool known = pos >= 0 && pos < a.positions;
             if (!known && lane == 0) raise_status(a.status, kStatusBadIndex);
             Turn tn;
             load_turn<MODE, -1>(tn, a.table + (int64_t)(known ? pos : 0) * a.rot, known && in ? f : a.rot, a.rot, a.interleaved);
-            int64_t t_next = t + step_t;
-            b += step_b;
-            if (b >= per) b -= per, ++t_next;
-            if (t_next < a.tokens) pos = a.pos[t_next];
+            next(at);
+            if (at.t < a.tokens) pos = a.pos[at.t];
+            copies_wait<kRing - 1>();
+            Raw<T> rx[kPasses], rd[kPasses];
 #pragma unroll
             for (int p = 0; p < kPasses; ++p) {
-                const bool real = in && h0 + p * hp < n;
-                float w[8], y[8];
-                rd[p].get(w);
-                others<MODE>(y, rd[p], w, f, a.rot, a.interleaved, bufs[warp], lane);
-                turn8<MODE>(w, y, tn, f, a.rot);
-                if (!known)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = 0.f;
-                if (a.norm) {
-                    float x[8], s = 0.f;
-                    rx[p].get(x);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
-                    const float scale = rsqrtf(fmaf(head_sum<LP>(s, a.lp), a.inv_d, a.eps));
-                    s = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        x[i] *= scale;
-                        sum[i] = fmaf(w[i], x[i], sum[i]);  // 0 in lanes without a head
-                        w[i] *= g[i];
-                        s = fmaf(w[i], x[i], s);
-                    }
-                    s = head_sum<LP>(s, a.lp) * a.inv_d;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = scale * fmaf(-x[i], s, w[i]);
-                }
-                Raw<T> o;
-                o.set(w);
-                if (real) o.store(out.at(t, h0 + p * hp) + f);
+                taken(rd[p], mine + stage * kStage + p * kPieces * 512);
+                if (a.norm) taken(rx[p], mine + stage * kStage + (kPasses + p) * kPieces * 512);
             }
-            t = t_next;
+            stage = stage == kRing - 1 ? 0 : stage + 1;
+            uint64_t tc[4], ts[4];
+            pack8(tc, tn.c), pack8(ts, tn.s);
+            if (!known)
+#pragma unroll
+                for (int p = 0; p < kPasses; ++p) rd[p].zero();
+            auto turned = [&](uint64_t (&w)[4], int p) {
+                uint64_t y[4];
+                rd[p].get(w);
+                others<MODE>(y, rd[p], f, a.rot, a.interleaved, bufs[warp], lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = fma2(y[i], ts[i], mul2(w[i], tc[i]));
+            };
+            uint64_t w[kPasses][4];
+            float v[2 * kPasses];  // sums of x², then of g w x
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p) {
+                turned(w[p], p);
+                if (!a.norm) continue;
+                uint64_t x[4], xx = 0, wx = 0;
+                rx[p].get(x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) xx = fma2(x[i], x[i], xx), wx = fma2(mul2(w[p][i], g[i]), x[i], wx);
+                v[p] = sum2(xx), v[kPasses + p] = sum2(wx);
+            }
+            if (a.norm) head_sums<LP>(v, a.lp, lane);
+            T *o_at = out.at(t, h0) + f;
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p, o_at += hp * out.head) {
+                if (a.norm) {
+                    uint64_t x[4];
+                    rx[p].get(x);
+                    const float scale = rsqrtf(fmaf(v[p], a.inv_d, a.eps)), c = -(v[kPasses + p] * scale * a.inv_d * scale) * scale;
+                    const uint64_t s2 = pack2(scale, scale), c2 = pack2(c, c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        sum[i] = fma2(mul2(w[p][i], x[i]), s2, sum[i]);  // 0 in lanes without a head
+                        w[p][i] = fma2(x[i], c2, mul2(mul2(w[p][i], g[i]), s2));
+                    }
+                }
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) unpack2(w[p][i], z[2 * i], z[2 * i + 1]);
+                Raw<T> o;
+                o.set(z);
+                if (h0 + p * hp < real) o.store(o_at);
+            }
         }
+        copies_wait<0>();
         if (!a.part) continue;
         // over the heads side by side in the warp, then over the warps, in order
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bufs[warp][lane * 8 + i] = sum[i];
+        for (int i = 0; i < 4; ++i) unpack2(sum[i], bufs[warp][lane * 8 + 2 * i], bufs[warp][lane * 8 + 2 * i + 1]);
         __syncthreads();
         for (int e = threadIdx.x; e < a.d; e += 32 * kWarps) {
             float s = 0.f;
