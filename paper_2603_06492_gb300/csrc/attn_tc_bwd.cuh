@@ -82,6 +82,24 @@ __device__ __forceinline__ Range queries_of(const Mask &m, int j0, int j1)
     return r;
 }
 
+// Those that see key j.
+__device__ __forceinline__ Range queries_of(const Mask &m, int j)
+{
+    if (j >= docs_end(m)) return {0, 0};
+    int a = -1, b = m.n_docs + 1;
+    while (b - a > 1) {
+        const int c = (a + b) >> 1;
+        if (m.doc_start[c] <= j) a = c;
+        else b = c;
+    }
+    if (a < 0) return {0, 0};
+    const int s = clampi(m.doc_start[a], 0, m.T), e = clampi(m.doc_start[a + 1], s, m.T);
+    Range r = {s, m.window ? min(e, j + m.window) : e};
+    if (!m.causal) r.lo = m.window ? max(s, j - m.window + 1) : s;
+    else if (!m.prefix || j >= s + clampi(m.prefix[a], 0, e - s)) r.lo = j;
+    return r;
+}
+
 // ---------------------------------------------------------------- dq
 template <int DP, bool GENERAL>
 __global__ void __launch_bounds__(384, 1)
@@ -327,7 +345,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 // With one step, all that the row sees is here: delta is then summed from p and dp
                 // themselves (see simt::dq_kernel).
                 if (!GENERAL) {
-                    // p over s, and 0 for it and dp where nothing is seen
+                    // p over s, and 0 where nothing is seen
                     const uint64_t sl2 = pack2(sl, sl), l2 = pack2(-lse2, -lse2);
 #pragma unroll
                     for (int c = 0; c < 64; c += 2) {
@@ -339,12 +357,12 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
 #pragma unroll
                         for (int c = 0; c < 64; ++c) {
                             const bool in = c >= lo && c < hi;
-                            s[c] = in ? s[c] : 0.f, dp[c] = in ? dp[c] : 0.f;
+                            s[c] = in ? s[c] : 0.f;  // dp is finite, or the row is done again
                         }
                     if (p.steps == 1) {
                         float sum = 0.f;
 #pragma unroll
-                        for (int c = 0; c < 64; ++c) sum = fmaf(s[c], dp[c], sum);
+                        for (int c = 0; c < 64; ++c) sum = fmaf(s[c], c >= lo && c < hi ? dp[c] : 0.f, sum);
                         delta = total(sum);
                     }
                     const uint64_t d2 = pack2(-delta, -delta);
@@ -406,33 +424,22 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 ++items;
                 ptx::tc_fence_after();
             }
-            uint32_t o[DP / 2];
-            if (p.steps) {
-                __syncwarp();
-#pragma unroll
-                for (int c = 0; c < DP / 2; c += 32) tmem_ld32(tmem + lanes + kAcc + half * (DP / 2) + c, o + c);
-                tmem_wait_ld();
-#pragma unroll
-                for (int c = 0; c < DP / 2; c += 32) pin32(o + c);
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(acc_empty);
-            }
             bool fine = true;
-            __nv_bfloat16 *out = args.a.dq.at(real ? i : 0, p.h);
-#pragma unroll
-            for (int e = 0; e < DP / 2; e += 8) {
-                float f[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    f[u] = none ? 0.f : __uint_as_float(o[e + u]) * args.a.score.scale;
-                    fine = fine && isfinite(f[u]);
+            __nv_bfloat16 *out = args.a.dq.at(i - lane, p.h) + half * (DP / 2);
+#pragma unroll 1
+            for (int c = 0; c < DP / 2; c += 32) {
+                uint32_t o[32];
+                if (p.steps) {
+                    __syncwarp();
+                    tmem_ld32(tmem + lanes + kAcc + half * (DP / 2) + c, o);
+                    tmem_wait_ld();
+                    pin32(o);
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && c + 32 == DP / 2) ptx::mbar_arrive(acc_empty);
                 }
-                const int col = half * (DP / 2) + e;
-                if (real && col < args.a.d)
-                    *reinterpret_cast<uint4 *>(out + col) =
-                        make_uint4(ptx::pack_bf16x2(f[0], f[1]), ptx::pack_bf16x2(f[2], f[3]), ptx::pack_bf16x2(f[4], f[5]),
-                                   ptx::pack_bf16x2(f[6], f[7]));
+                fine &= write_rows(o, args.a.score.scale, none || !p.steps, out + c, args.a.dq.row, mask.T - (i - lane),
+                                   args.a.d - half * (DP / 2) - c, lane);
             }
             uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
             __syncwarp();
@@ -664,7 +671,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         auto fetch = [&] {
             p_next = as_keys(pc);
             const int j = p_next.j0 + row;
-            see_next = queries_of(mask, j, j + 1);
+            see_next = queries_of(mask, j);
         };
         bool more = works.take(pc, 0, true, false, lane, status);
         if (more) fetch();
@@ -736,9 +743,6 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 tmem_wait_ld();
                 pin32(xp), pin32(xp + 32);
                 as_floats(dp, xp);
-                if (!all)
-#pragma unroll
-                    for (int c = 0; c < 64; ++c) dp[c] = c >= lo && c < hi ? dp[c] : 0.f;
 #pragma unroll
                 for (int c = 0; c < 64; c += 4) {
                     const float4 d = *reinterpret_cast<const float4 *>(vec + 128 + c);
@@ -776,34 +780,22 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             }
             const bool real = j < mask.T;
             const float f = half ? args.a.score.scale : 1.f;
-            __nv_bfloat16 *out = (half ? args.a.dk : args.a.dv).at(real ? j : 0, p.g);
+            const Heads<__nv_bfloat16> &to = half ? args.a.dk : args.a.dv;
+            __nv_bfloat16 *out = to.at(j - lane, p.g);
             bool fine = true;
-            uint32_t o[DP];
-            if (p.steps) {
-                __syncwarp();
-#pragma unroll
-                for (int c = 0; c < DP; c += 32) tmem_ld32(tmem + lanes + (half ? kDK : kDV) + c, o + c);
-                tmem_wait_ld();
-#pragma unroll
-                for (int c = 0; c < DP; c += 32) pin32(o + c);
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(acc_empty);
-            } else {
-#pragma unroll
-                for (int c = 0; c < DP; ++c) o[c] = 0;
-            }
-#pragma unroll
-            for (int e = 0; e < DP; e += 8) {
-                float v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    v[u] = __uint_as_float(o[e + u]) * f;
-                    fine = fine && isfinite(v[u]);
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                if (p.steps) {
+                    __syncwarp();
+                    tmem_ld32(tmem + lanes + (half ? kDK : kDV) + c, o);
+                    tmem_wait_ld();
+                    pin32(o);
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && c + 32 == DP) ptx::mbar_arrive(acc_empty);
                 }
-                if (real && e < args.a.d)
-                    *reinterpret_cast<uint4 *>(out + e) = make_uint4(ptx::pack_bf16x2(v[0], v[1]), ptx::pack_bf16x2(v[2], v[3]),
-                                                                     ptx::pack_bf16x2(v[4], v[5]), ptx::pack_bf16x2(v[6], v[7]));
+                fine &= write_rows(o, f, !p.steps, out + c, to.row, mask.T - (j - lane), args.a.d - c, lane);
             }
             uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
             __syncwarp();

@@ -366,7 +366,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             }
             const float inv = none || !(l > 0.f) ? 0.f : 1.f / l;
             bool fine = none || isfinite(l);
-            __nv_bfloat16 *out = args.a.out.at(real ? i : 0, s.h);
+            __nv_bfloat16 *out = args.a.out.at(i - lane, s.h);
 #pragma unroll 1
             for (int c = 0; c < DP; c += 32) {
                 uint32_t o[32];
@@ -376,22 +376,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     tmem_wait_ld();
                     pin32(o);
                 }
-                if (t1 <= t0 || none)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0;
-#pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    float f[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        f[u] = __uint_as_float(o[e + u]) * inv;
-                        fine = fine && isfinite(f[u]);
-                    }
-                    if (real && c + e < args.a.d)
-                        *reinterpret_cast<uint4 *>(out + c + e) =
-                            make_uint4(ptx::pack_bf16x2(f[0], f[1]), ptx::pack_bf16x2(f[2], f[3]), ptx::pack_bf16x2(f[4], f[5]),
-                                       ptx::pack_bf16x2(f[6], f[7]));
-                }
+                fine &= write_rows(o, inv, t1 <= t0 || none, out + c, args.a.out.row, mask.T - (i - lane), args.a.d - c, lane);
             }
             if (real) args.a.lse[(int64_t)s.h * mask.T + i] = inv > 0.f || !fine ? (m + log2f(l)) * kLn2 : -INFINITY;
             // rows that masked infinities or NaN have reached
