@@ -230,14 +230,31 @@ noble_status check_aligned4(const void *p, const char *name, bool nullable)
     return NOBLE_OK;
 }
 
+// Parts that the query heads of a key head are split into for dk and dv: a block of 128 keys
+// and all of them is one piece of work, and the longest of a causal mask is as long as an
+// SM's share of all once there are two pieces per SM.  Up to four per SM, which bounds what the
+// parts take (4096 tokens, 16 heads on 4 of 128 features, causal: the backward 270 us in one
+// part, 203 in four; 7001 tokens, 11 documents with prefixes, capped scores: 429 and, in two,
+// 377).
+int attn_splits(const noble_attn_desc *d)
+{
+    const int64_t group = d->n_q / d->n_kv, pieces = ceil_div(d->T, attn::tc::kRows) * d->n_kv;
+    if (d->dtype != NOBLE_BF16 || (d->flags & NOBLE_ATTN_SIMT_ONLY)) return 1;
+    int64_t s = 1;
+    for (int64_t t = 2; t <= group && pieces * s < 2 * kSms && pieces * t <= 4 * kSms; ++t)
+        if (group % t == 0) s = t;
+    return (int)s;
+}
 struct AttnWork {
-    size_t delta, ranges, total;
+    size_t delta, rest, total;  // rest: ranges of the CUDA cores, parts of the tensor cores
 };
 AttnWork attn_work(const noble_attn_desc *d)
 {
     AttnWork w{};
-    w.ranges = align_up((size_t)d->T * (size_t)d->n_q * 4, 256);
-    w.total = std::max<size_t>(256, w.ranges + align_up((size_t)d->T * 8, 256));
+    w.rest = align_up((size_t)d->T * (size_t)d->n_q * 4, 256);
+    const size_t splits = (size_t)attn_splits(d), unit = 2 * attn::tc::kRows * (d->d <= 64 ? 64 : 128) * 4;
+    const size_t parts = splits > 1 ? splits * (size_t)d->n_kv * (size_t)ceil_div(d->T, attn::tc::kRows) * unit : 0;
+    w.total = std::max<size_t>(256, w.rest + std::max(align_up((size_t)d->T * 8, 256), parts));
     return w;
 }
 
@@ -364,7 +381,8 @@ bool attn_use_tc(const noble_attn_desc *d, std::initializer_list<std::pair<const
 }
 
 template <int DP, bool GENERAL>
-noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4], float *delta, cudaStream_t st)
+noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4], float *delta, int splits, float *part,
+                         cudaStream_t st)
 {
     namespace t = attn::tc;
     using Q = t::BwdQ<DP>;
@@ -373,13 +391,16 @@ noble_status attn_bwd_tc(const attn::RowArgs<bf> &a, const CUtensorMap (&maps)[4
     if (!registers_at_least<dq>(168) || !registers_at_least<dkv>(168)) return fail(NOBLE_ERR_CUDA, "attn_bwd: registers");
     NOBLE_TRY((allow<dq>(Q::kBytes)));
     NOBLE_TRY((allow<dkv>(KV::kBytes)));
-    t::BwdArgs f{a, delta, (int)ceil_div(a.mask.T, t::kRows), status_ptr()};
+    t::BwdArgs f{a, delta, (int)ceil_div(a.mask.T, t::kRows), splits, a.n_q / (a.n_kv * splits), a.n_kv * splits, part, status_ptr()};
     if (!f.status) return fail(NOBLE_ERR_CUDA, "status word address");
     if ((int64_t)f.tiles * a.n_q > INT32_MAX) return fail(NOBLE_ERR_UNSUPPORTED, "%d tokens of %d heads", a.mask.T, a.n_q);
     NOBLE_TRY(run(st, {"attn_dq", kBoundTensor, 0.0, 0.0},
                   [&] { dq<<<f.tiles * a.n_q, Q::kThreads, Q::kBytes, st>>>(maps[0], maps[1], maps[2], maps[3], f); }));
-    return run(st, {"attn_dkv", kBoundTensor, 0.0, 0.0},
-               [&] { dkv<<<f.tiles * a.n_kv, KV::kThreads, KV::kBytes, st>>>(maps[0], maps[1], maps[2], maps[3], f); });
+    NOBLE_TRY(run(st, {"attn_dkv", kBoundTensor, 0.0, 0.0},
+                  [&] { dkv<<<f.tiles * f.parts, KV::kThreads, KV::kBytes, st>>>(maps[0], maps[1], maps[2], maps[3], f); }));
+    if (splits == 1) return NOBLE_OK;
+    const KernelInfo ki{"attn_dkv_join", kBoundHbm, 0.0, 2.0 * 4 * splits * a.mask.T * a.n_kv * a.d};
+    return run(st, ki, [&] { t::join_kernel<DP><<<2 * f.tiles * a.n_kv, t::kRows * DP / 32, 0, st>>>(f); });
 }
 template <typename T>
 noble_status attn_fwd(const attn::RowArgs<T> &a, cudaStream_t st)
@@ -394,8 +415,9 @@ noble_status attn_bwd(const attn::RowArgs<T> &a, float *delta, int2 *ranges, cud
 }
 
 noble_status attn_bwd_tc(const noble_attn_desc *d, const attn::RowArgs<bf> &a, const noble_heads *q, const noble_heads *d_o,
-                         const noble_heads *k, const noble_heads *v, float *delta, cudaStream_t st)
+                         const noble_heads *k, const noble_heads *v, float *delta, float *part, cudaStream_t st)
 {
+    const int splits = attn_splits(d);
     CUtensorMap maps[4];
     NOBLE_TRY(make_heads_map(&maps[0], q, d->T, d->n_q, d->d));
     NOBLE_TRY(make_heads_map(&maps[1], d_o, d->T, d->n_q, d->d));
@@ -403,8 +425,8 @@ noble_status attn_bwd_tc(const noble_attn_desc *d, const attn::RowArgs<bf> &a, c
     NOBLE_TRY(make_heads_map(&maps[3], v, d->T, d->n_kv, d->d));
     NOBLE_TRY(attn_prep<bf>(a, delta, nullptr, st));
     if (general_scores(a.score))
-        return d->d <= 64 ? attn_bwd_tc<64, true>(a, maps, delta, st) : attn_bwd_tc<128, true>(a, maps, delta, st);
-    return d->d <= 64 ? attn_bwd_tc<64, false>(a, maps, delta, st) : attn_bwd_tc<128, false>(a, maps, delta, st);
+        return d->d <= 64 ? attn_bwd_tc<64, true>(a, maps, delta, splits, part, st) : attn_bwd_tc<128, true>(a, maps, delta, splits, part, st);
+    return d->d <= 64 ? attn_bwd_tc<64, false>(a, maps, delta, splits, part, st) : attn_bwd_tc<128, false>(a, maps, delta, splits, part, st);
 }
 
 // ---------------------------------------------------------------- attention over the cache
@@ -721,11 +743,11 @@ noble_status noble_attn_bwd(const noble_attn_desc *desc, const noble_heads *d_o,
         float *delta = static_cast<float *>(workspace);
         a.o = heads<const E>(o), a.d_o = heads<const E>(d_o), a.lse = const_cast<float *>(lse), a.delta = delta;
         a.dq = heads<E>(dq), a.dk = heads<E>(dk), a.dv = heads<E>(dv);
-        int2 *ranges = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + attn_work(desc).ranges);
+        char *rest = static_cast<char *>(workspace) + attn_work(desc).rest;
         if constexpr (std::is_same_v<E, bf>)
             if (attn_use_tc(desc, {{q, desc->n_q}, {d_o, desc->n_q}, {k, desc->n_kv}, {v, desc->n_kv}}))
-                return attn_bwd_tc(desc, a, q, d_o, k, v, delta, (cudaStream_t)stream);
-        return attn_bwd<E>(a, delta, ranges, (cudaStream_t)stream);
+                return attn_bwd_tc(desc, a, q, d_o, k, v, delta, reinterpret_cast<float *>(rest), (cudaStream_t)stream);
+        return attn_bwd<E>(a, delta, reinterpret_cast<int2 *>(rest), (cudaStream_t)stream);
     };
     return desc->dtype == NOBLE_BF16 ? go(bf{}) : go(float{});
 }

@@ -6,7 +6,8 @@
 // dq_kernel, 128 queries of a head over the key tiles that they see:
 //     S = Q K^T, dP = dO V^T;  dS = P (dP - delta);  dQ += dS K
 // dkv_kernel, 128 keys of a key head over the query tiles that see them, of every query
-// head that shares it (rows of the score block are keys):
+// head that shares it, or of one of `splits` parts of them, which join_kernel then adds up
+// (rows of the score block are keys):
 //     S = K Q^T, dP = V dO^T;  dV += P dO,  dK += dS Q
 // P and dS are written as bf16 over S and dP in TMEM and read from there as operands.
 // Two warpgroups of 128 rows take half of the columns each.
@@ -26,6 +27,11 @@ struct BwdArgs {
     RowArgs<__nv_bfloat16> a;
     float *delta;  // [n_q][T]: sum of o do
     int tiles;     // of 128 tokens
+    // dkv_kernel: parts that a key head's query heads are split into, of how many of them each,
+    // in all; with several their fp32 results go to part, [tile][key head][split][dv, dk]
+    // [features / 4][128 tokens][4]
+    int splits, heads, parts;
+    float *part;
     uint32_t *status;
 };
 
@@ -521,19 +527,18 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = uniform(*tmem_slot);
-    const int group = args.a.n_q / args.a.n_kv;
 
     // piece of work: 128 keys from j0 of key head g, over query tiles from lo, `per` of a
-    // head and `steps` in all
+    // head and `steps` in all, of the query heads from h0
     struct Keys {
-        int j0, g, lo, per, steps;
+        int j0, g, lo, per, steps, h0, part;
     };
-    auto as_keys = [](const Piece &p) { return Keys{p.v[0], p.v[1], p.v[2], p.v[3], p.v[4]}; };
+    auto as_keys = [](const Piece &p) { return Keys{p.v[0], p.v[1], p.v[2], p.v[3], p.v[4], p.v[5], p.v[6]}; };
     auto describe = [&](int work) {
-        const int g = work % args.a.n_kv, j0 = work / args.a.n_kv * kRows;
+        const int tile = work / args.parts, part = work - tile * args.parts, j0 = tile * kRows;
         const Range r = queries_of(mask, j0, j0 + kRows);
         const int per = (max(r.hi - r.lo, 0) + kRows - 1) / kRows;
-        return Piece{{j0, g, r.lo, per, per * group, 0, 0, 0}};
+        return Piece{{j0, args.splits == 1 ? part : part / args.splits, r.lo, per, per * args.heads, part * args.heads, part, 0}};
     };
     Piece pc;
 
@@ -555,7 +560,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 }
                 ++items;
                 for (int t = 0; t < p.steps; ++t, ++n) {
-                    const int st = n % kStages, h = p.g * group + t / p.per, i = p.lo + t % p.per * kRows;
+                    const int st = n % kStages, h = p.h0 + t / p.per, i = p.lo + t % p.per * kRows;
                     const uint32_t ph = (n / kStages) & 1;
                     ok = ptx::mbar_wait(q_empty(st), ph ^ 1, status);
                     if (!ok) break;
@@ -629,7 +634,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 const Keys p = as_keys(pc);
                 float lse[4], delta[4];
                 auto fetch = [&](int t) {
-                    const int h = p.g * group + t / p.per, i0 = p.lo + t % p.per * kRows;
+                    const int h = p.h0 + t / p.per, i0 = p.lo + t % p.per * kRows;
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         const int i = i0 + lane + 32 * u;
@@ -710,7 +715,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                         s[c + 2] = exp2_fast(a), s[c + 3] = exp2_fast(b);
                     }
                 } else {
-                    const int h = p.g * group + t / p.per;
+                    const int h = p.h0 + t / p.per;
                     const float slope = args.a.score.slope ? args.a.score.slope[h] * kLog2e : 0.f;
                     general_scores<64, GENERAL>(s, gs, args.a.score, slope, (float)(j - i0));
 #pragma unroll
@@ -795,7 +800,15 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     __syncwarp();
                     if (lane == 0 && c + 32 == DP) ptx::mbar_arrive(acc_empty);
                 }
-                fine &= write_rows(o, f, !p.steps, out + c, to.row, mask.T - (j - lane), args.a.d - c, lane);
+                if (args.splits == 1) {
+                    fine &= write_rows(o, f, !p.steps, out + c, to.row, mask.T - (j - lane), args.a.d - c, lane);
+                } else {
+                    const int64_t unit = (int64_t)(p.j0 / kRows) * args.parts + p.part;
+                    uint4 *part = reinterpret_cast<uint4 *>(args.part) + ((unit * 2 + half) * (DP / 4) + c / 4) * kRows + row;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        part[e / 4 * kRows] = p.steps ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0, 0, 0, 0);
+                }
             }
             uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
             __syncwarp();
@@ -809,6 +822,44 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, 512);
     }
+}
+
+// dk and dv of 128 keys from the parts of their query heads, in order: a thread per key and 32
+// features.  Bound by reading the parts, most of them still in L2 (4096 tokens, 16 heads of
+// 128 in four parts: 12 us).
+template <int DP>
+__global__ void __launch_bounds__(kRows *DP / 32) join_kernel(const __grid_constant__ BwdArgs args)
+{
+    __shared__ uint32_t bad[4];  // keys that are not finite, 32 a word
+    const int row = threadIdx.x % kRows, chunk = threadIdx.x / kRows, warp = row / 32, lane = row % 32;
+    const int half = blockIdx.x & 1, unit = blockIdx.x >> 1, g = unit % args.a.n_kv, j = unit / args.a.n_kv * kRows + row;
+    if (threadIdx.x < 4) bad[threadIdx.x] = 0;
+    __syncthreads();
+    const Heads<__nv_bfloat16> &to = half ? args.a.dk : args.a.dv;
+    const float4 *part = reinterpret_cast<const float4 *>(args.part) + (((int64_t)unit * args.splits * 2 + half) * (DP / 4) + 8 * chunk) * kRows + row;
+    float4 sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = part[e * kRows];
+    for (int s = 1; s < args.splits; ++s) {
+        part += 2 * (DP / 4) * kRows;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float4 x = part[e * kRows];
+            sum[e].x += x.x, sum[e].y += x.y, sum[e].z += x.z, sum[e].w += x.w;
+        }
+    }
+    uint32_t o[32];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        o[4 * e] = __float_as_uint(sum[e].x), o[4 * e + 1] = __float_as_uint(sum[e].y), o[4 * e + 2] = __float_as_uint(sum[e].z),
+              o[4 * e + 3] = __float_as_uint(sum[e].w);
+    const bool fine = write_rows(o, half ? args.a.score.scale : 1.f, false, to.at(j - lane, g) + 32 * chunk, to.row,
+                                 args.a.mask.T - (j - lane), args.a.d - 32 * chunk, lane);
+    const uint32_t word = __ballot_sync(0xffffffffu, j < args.a.mask.T && !fine);
+    if (lane == 0 && word) atomicOr(&bad[warp], word);
+    __syncthreads();
+    if (chunk) return;
+    for (uint32_t b = bad[warp]; b; b &= b - 1) row_dkv(args.a, j - lane + __ffs(b) - 1, g, lane, half == 0, half == 1);
 }
 
 }  // namespace tc

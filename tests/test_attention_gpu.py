@@ -311,3 +311,22 @@ def test_no_row_again_at_length(nq, nkv, d, kw):
         first = first or now
         for n, a, b in zip(NAMES, first, now):
             assert torch.equal(a, b), n
+
+
+@path
+@pytest.mark.parametrize("nq,nkv,d", [(12, 2, 128), (5, 1, 64), (16, 4, 40), (14, 2, 96)])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(softcap=4.0, alibi=True), dict(window=70)])
+def test_few_key_heads(nq, nkv, d, kw, dtype, flags):
+    # query heads of a key head in several parts, whose gradients are added up
+    _check(413, nq, nkv, d, [0, 90, 91, 380], dtype, flags=flags, seed=4, **kw)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_values_that_nothing_sees_of_few_key_heads(bad):
+    q, k, v, d_o = _inputs(300, 8, 1, 64, "bf16", 5)
+    docs = [0, 130, 280]
+    clean = [x.clone() for x in (q, k, v, d_o)]
+    for x, c in zip((q, k, v, d_o), clean):
+        x[280:], c[280:] = bad, 0.0
+    want = ref.attention(*clean[:3], ref.masks(300, docs), 1 / math.sqrt(64), 0.0, None, clean[3])
+    _compare(_run(q, k, v, d_o, docs, "bf16"), want, "bf16")
