@@ -217,25 +217,28 @@ __device__ __forceinline__ Capping capping(const float (&x)[N], const Score &sc)
 }
 // Two scores, in place, and their derivatives.
 template <int MODE, bool GRAD>
-__device__ __forceinline__ void cap_pair(float &x, float &y, float &gx, float &gy, const Capping &cap)
+__device__ __forceinline__ void cap_pair(uint64_t &x, uint64_t &g, const Capping &cap)
 {
+    const uint64_t one2 = pack2(1.f, 1.f), minus2 = pack2(-1.f, -1.f), out2 = pack2(cap.out, cap.out);
     if (MODE == kNoCap) {
-        x *= cap.out, y *= cap.out;
-        if (GRAD) gx = gy = 1.f;
+        x = mul2(x, out2);
+        if (GRAD) g = one2;
     } else if (MODE == kCapSeries) {
         const float k[7] = {-1.f / 3.f, 2.f / 15.f, -17.f / 315.f, 62.f / 2835.f, -1382.f / 155925.f, 21844.f / 6081075.f,
                             -929569.f / 638512875.f};
-        const uint64_t one2 = pack2(1.f, 1.f), a = mul2(pack2(x, y), pack2(cap.in, cap.in)), u = mul2(a, a);
+        const uint64_t a = mul2(x, pack2(cap.in, cap.in)), u = mul2(a, a);
         uint64_t p = pack2(k[6], k[6]);
 #pragma unroll
         for (int e = 5; e >= 0; --e) p = fma2(p, u, pack2(k[e], k[e]));
         const uint64_t t = mul2(a, fma2(p, u, one2));
-        unpack2(mul2(t, pack2(cap.out, cap.out)), x, y);
-        if (GRAD) unpack2(fma2(mul2(t, t), pack2(-1.f, -1.f), one2), gx, gy);
+        x = mul2(t, out2);
+        if (GRAD) g = fma2(mul2(t, minus2), t, one2);
     } else {
-        const float t = tanh_exp(x * cap.in), u = tanh_exp(y * cap.in);
-        if (GRAD) gx = fmaf(-t, t, 1.f), gy = fmaf(-u, u, 1.f);
-        x = t * cap.out, y = u * cap.out;
+        float a, b;
+        unpack2(mul2(x, pack2(cap.in, cap.in)), a, b);
+        const uint64_t t = pack2(tanh_exp(a), tanh_exp(b));
+        x = mul2(t, out2);
+        if (GRAD) g = fma2(mul2(t, minus2), t, one2);
     }
 }
 // f(MODE) for the mode of a Capping
@@ -253,9 +256,12 @@ __device__ __forceinline__ void general_scores(float (&x)[N], uint32_t (&gs)[GRA
     with_cap(cap.mode, [&](auto mode) {
 #pragma unroll
         for (int c = 0; c < N; c += 2) {
-            float a, b;
-            cap_pair<mode.value, GRAD>(x[c], x[c + 1], a, b, cap);
+            uint64_t v = pack2(x[c], x[c + 1]), g = 0;
+            cap_pair<mode.value, GRAD>(v, g, cap);
+            unpack2(v, x[c], x[c + 1]);
             if (GRAD) {
+                float a, b;
+                unpack2(g, a, b);
                 const __half2 h = __floats2half2_rn(a, b);
                 gs[GRAD ? c / 2 : 0] = *reinterpret_cast<const uint32_t *>(&h);
             }

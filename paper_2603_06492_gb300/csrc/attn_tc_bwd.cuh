@@ -382,32 +382,46 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                     // a pair of columns at a time from score to dS, since the derivatives have no room beside both
                     const Capping cap = capping(s, args.a.score);
                     const float far = (float)(i - j0);
-                    with_cap(cap.mode, [&](auto mode) {
-                        auto probs = [&](int c, float &x, float &y, float &gx, float &gy) {
-                            x = s[c], y = s[c + 1];
-                            cap_pair<mode.value, true>(x, y, gx, gy, cap);
-                            x = exp2_fast(fmaf(-slope, fabsf(far - (float)c), x) - lse2);
-                            y = exp2_fast(fmaf(-slope, fabsf(far - (float)(c + 1)), y) - lse2);
+                    const uint64_t far2 = pack2(far, far), l2 = pack2(-lse2, -lse2), slope2 = pack2(-slope, -slope);
+                    auto as_ds = [&](auto mode, auto biased) {
+                        auto probs = [&](int c, uint64_t &x, uint64_t &g) {
+                            x = pack2(s[c], s[c + 1]);
+                            cap_pair<mode.value, true>(x, g, cap);
+                            if constexpr (decltype(biased)::value) {
+                                const uint64_t by = add2(far2, pack2(-(float)c, -(float)(c + 1))) & 0x7fffffff7fffffffull;
+                                x = fma2(slope2, by, x);
+                            }
+                            float a, b;
+                            unpack2(add2(x, l2), a, b);
+                            x = pack2(exp2_fast(a), exp2_fast(b));
                         };
                         if (p.steps == 1) {
                             float sum = 0.f;
 #pragma unroll
                             for (int c = 0; c < 64; c += 2) {
-                                float x, y, gx, gy;
-                                probs(c, x, y, gx, gy);
+                                uint64_t v, g;
+                                float x, y;
+                                probs(c, v, g);
+                                unpack2(v, x, y);
                                 sum += c >= lo && c < hi ? x * dp[c] : 0.f;
                                 sum += c + 1 >= lo && c + 1 < hi ? y * dp[c + 1] : 0.f;
                             }
                             delta = total(sum);
                         }
+                        const uint64_t d2 = pack2(-delta, -delta);
 #pragma unroll
                         for (int c = 0; c < 64; c += 2) {
-                            float x, y, gx, gy;
-                            probs(c, x, y, gx, gy);
-                            x *= (dp[c] - delta) * gx, y *= (dp[c + 1] - delta) * gy;
+                            uint64_t v, g;
+                            float x, y;
+                            probs(c, v, g);
+                            unpack2(mul2(mul2(v, g), add2(pack2(dp[c], dp[c + 1]), d2)), x, y);
                             if (!all) x = c >= lo && c < hi ? x : 0.f, y = c + 1 >= lo && c + 1 < hi ? y : 0.f;
                             pk[c / 2] = ptx::pack_bf16x2(x, y);
                         }
+                    };
+                    with_cap(cap.mode, [&](auto mode) {
+                        if (args.a.score.slope) as_ds(mode, std::true_type{});
+                        else as_ds(mode, std::false_type{});
                     });
                 }
                 if (!ok) break;
@@ -721,8 +735,11 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
 #pragma unroll
                     for (int c = 0; c < 64; c += 4) {
                         const float4 l = *reinterpret_cast<const float4 *>(vec + c);
-                        s[c] = exp2_fast(s[c] - l.x), s[c + 1] = exp2_fast(s[c + 1] - l.y);
-                        s[c + 2] = exp2_fast(s[c + 2] - l.z), s[c + 3] = exp2_fast(s[c + 3] - l.w);
+                        float a, b;
+                        unpack2(add2(pack2(s[c], s[c + 1]), pack2(-l.x, -l.y)), a, b);
+                        s[c] = exp2_fast(a), s[c + 1] = exp2_fast(b);
+                        unpack2(add2(pack2(s[c + 2], s[c + 3]), pack2(-l.z, -l.w)), a, b);
+                        s[c + 2] = exp2_fast(a), s[c + 3] = exp2_fast(b);
                     }
                 }
                 if (!all)
@@ -757,7 +774,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     if (GENERAL) {
                         const float2 g0 = __half22float2(*reinterpret_cast<const __half2 *>(&gs[c / 2]));
                         const float2 g1 = __half22float2(*reinterpret_cast<const __half2 *>(&gs[c / 2 + 1]));
-                        e[0] *= g0.x, e[1] *= g0.y, e[2] *= g1.x, e[3] *= g1.y;
+                        unpack2(mul2(pack2(e[0], e[1]), pack2(g0.x, g0.y)), e[0], e[1]);
+                        unpack2(mul2(pack2(e[2], e[3]), pack2(g1.x, g1.y)), e[2], e[3]);
                     }
                     pk[c / 2] = ptx::pack_bf16x2(e[0], e[1]);
                     pk[c / 2 + 1] = ptx::pack_bf16x2(e[2], e[3]);
