@@ -194,10 +194,11 @@ __device__ __forceinline__ bool write_rows(const uint32_t (&o)[32], float f, boo
 //
 // tanh takes an exponential and a reciprocal, which with the softmax's own exponential
 // make the special function unit the limit.  Where all of a warp's arguments are within
-// 0.6 its Taylor series to x^15 does, whose first term left out is 6e-4 x^17: at most
-// 2e-7 of the result.  Ragged documents of 7001 tokens, 16 + 4 heads of 128, cap 30: forward
-// 136 us without the series, 123 with it.
-enum : int { kNoCap = 0, kCapSeries = 1, kCapExact = 2 };
+// 0.6 its Taylor series to x^15 does, within 0.33 that to x^9: the first term left out,
+// 6e-4 x^17 and 9e-3 x^11, is at most 2e-7 of the result.  Ragged documents of 7001 tokens,
+// 16 + 4 heads of 128, cap 30: forward 136 us without series, 125 with the longer one, 113
+// with both.
+enum : int { kNoCap = 0, kCapShort = 1, kCapSeries = 2, kCapExact = 3 };
 struct Capping {
     float in, out;  // kNoCap: s = out q.k
     int mode;
@@ -212,8 +213,9 @@ __device__ __forceinline__ Capping capping(const float (&x)[N], const Score &sc)
     for (int c = 0; c < N; c += 4)
 #pragma unroll
         for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], fabsf(x[c + u]));
-    const bool small = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(in) < 0.6f;
-    return {in, sc.softcap * kLog2e, __all_sync(0xffffffffu, small) ? kCapSeries : kCapExact};
+    const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(in);
+    const int mode = __all_sync(0xffffffffu, most < 0.33f) ? kCapShort : __all_sync(0xffffffffu, most < 0.6f) ? kCapSeries : kCapExact;
+    return {in, sc.softcap * kLog2e, mode};
 }
 // Two scores, in place, and their derivatives.
 template <int MODE, bool GRAD>
@@ -223,13 +225,14 @@ __device__ __forceinline__ void cap_pair(uint64_t &x, uint64_t &g, const Capping
     if (MODE == kNoCap) {
         x = mul2(x, out2);
         if (GRAD) g = one2;
-    } else if (MODE == kCapSeries) {
+    } else if (MODE != kCapExact) {
+        constexpr int kTerms = MODE == kCapShort ? 4 : 7;
         const float k[7] = {-1.f / 3.f, 2.f / 15.f, -17.f / 315.f, 62.f / 2835.f, -1382.f / 155925.f, 21844.f / 6081075.f,
                             -929569.f / 638512875.f};
         const uint64_t a = mul2(x, pack2(cap.in, cap.in)), u = mul2(a, a);
-        uint64_t p = pack2(k[6], k[6]);
+        uint64_t p = pack2(k[kTerms - 1], k[kTerms - 1]);
 #pragma unroll
-        for (int e = 5; e >= 0; --e) p = fma2(p, u, pack2(k[e], k[e]));
+        for (int e = kTerms - 2; e >= 0; --e) p = fma2(p, u, pack2(k[e], k[e]));
         const uint64_t t = mul2(a, fma2(p, u, one2));
         x = mul2(t, out2);
         if (GRAD) g = fma2(mul2(t, minus2), t, one2);
@@ -246,6 +249,7 @@ template <class F>
 __device__ __forceinline__ void with_cap(int mode, F &&f)
 {
     if (mode == kNoCap) f(std::integral_constant<int, kNoCap>{});
+    else if (mode == kCapShort) f(std::integral_constant<int, kCapShort>{});
     else if (mode == kCapSeries) f(std::integral_constant<int, kCapSeries>{});
     else f(std::integral_constant<int, kCapExact>{});
 }
