@@ -4,7 +4,8 @@
 // new tokens of a sequence, are the rows of one block (16 of them), so that a key is
 // read for all of them at once.  The keys of a sequence are split into chunks, a
 // block each, since a batch alone has too few sequences to load 152 SMs; a second
-// kernel joins the chunks' results by their maxima and sums, in order.
+// kernel joins the chunks' results by their maxima and sums, in order.  fp32 is bound by its
+// FMAs instead: 24 sequences up to 1024 tokens, 16 heads of 64: 107 us.
 #pragma once
 
 #include "attn_simt.cuh"

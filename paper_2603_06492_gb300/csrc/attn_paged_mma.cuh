@@ -14,6 +14,11 @@
 // The warps of a block take turns at its chunk's groups of 16 keys, each with a softmax of
 // its own; the four are joined in shared memory at the end.  The next keys load while the
 // values' product runs, the next values during the keys'.
+//
+// 64 sequences up to 32768 tokens, 32 heads on 4 of 128 features: 371 us, 5.6 TB/s.  4 tokens of
+// one sequence over 131072: 58 us, 4.7 TB/s.  24 sequences up to 1024 tokens, 16 heads of 64:
+// 23 us, of which reading takes 7: two dependent launches, and lengths, pages and keys each wait
+// for what is before them.
 #pragma once
 
 #include "attn_paged.cuh"

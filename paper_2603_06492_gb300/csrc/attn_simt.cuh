@@ -9,6 +9,10 @@
 // Backward in two kernels, one per side of the scores, so that every sum has one
 // block and a fixed order: dk and dv by key block over the queries (and the query
 // heads that share the key head), dq by query block over the keys.
+//
+// Bound by the reads from shared memory beside the FMAs, and by blocks of uneven length: 1024
+// tokens, 16 heads of 64, causal, fp32: forward 125 us (17 TFLOP/s), backward 355 (15); both
+// together 659 with blocks of 64 x 64.
 #pragma once
 
 #include "attn_mask.cuh"
@@ -204,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) fwd_kernel(const __grid_constant__ R
 
 // delta[h][i] = sum_f o do; with ranges, also the range of every token.  Bound by reading o
 // and do: a lane takes 8 features of each, LP lanes a head, and four heads at a time
-// (grid strides apart) are in flight.
+// (grid strides apart) are in flight.  16384 tokens, 16 heads of 128: 24 us, 5.6 TB/s.
 template <typename T, int LP>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) delta_kernel(const __grid_constant__ RowArgs<T> a, float *delta, int2 *ranges, int step_t,
                                                     int step_h)

@@ -13,6 +13,12 @@
 // maximum has grown by more than 2^8 since the last time, which after the first tiles
 // happens rarely.  Sums and maxima are fp32; P is rounded to bf16 for the product (each
 // to 2^-9 of itself), its sum is that of the unrounded values.
+//
+// What bounds it: with heads of 128 features the tensor pipe (16384 tokens, 16 heads: 1390 us
+// with all seen, 705 causal, 1580 and 1556 TFLOP/s), with 64 the exponentials (1055 us, 1040
+// TFLOP/s).  Short documents pay for each piece's start, masked tiles and rows written (8 of 1024
+// tokens, 16 heads of 64: 43 us, 64 of 197, 12 heads: 48), capped scores for their tanh on the
+// FMA pipe (7001 tokens, 16 heads on 4 of 128: 113 us, 71 without a cap).
 #pragma once
 
 #include "attn_tc.cuh"
