@@ -507,7 +507,8 @@ noble_status noble_kv_append(const noble_rope_desc *desc, const noble_heads *q, 
  * bf16 runs on the tensor cores, with fp32 scores, softmax and sums; the
  * probabilities and the scores' gradients are rounded to bf16 for their
  * products.  fp32 operands run in fp32 FMA, as does bf16 with
- * NOBLE_ATTN_SIMT_ONLY.  Results do not depend on the order in which a GPU
+ * NOBLE_ATTN_SIMT_ONLY or with a stride of 0, below 0 or from 2^38 on (in
+ * elements).  Outputs must not overlap inputs.  Results do not depend on the order in which a GPU
  * runs the blocks: repeated calls agree bit by bit.
  */
 #define NOBLE_ATTN_CAUSAL 1u
@@ -548,7 +549,7 @@ noble_status noble_attn_bwd(const noble_attn_desc *desc, const noble_heads *d_o,
  * softcap and slope as in noble_attn_fwd.  Position j of sequence n lies in
  * page page_table[n][j / page_size] of the cache, at place j % page_size.  A
  * token at a negative position sees nothing: o = 0, lse = -inf.
- * Only what is seen is read from the cache.  A page number outside the cache,
+ * Only what some new token of the sequence sees is read from the cache.  A page number outside the cache,
  * or a kv_len beyond max_pages * page_size or max_len, is a caller's error: the
  * keys concerned are left out, and noble_get_device_status() reports it.
  */
