@@ -508,8 +508,8 @@ noble_status noble_kv_append(const noble_rope_desc *desc, const noble_heads *q, 
  * probabilities and the scores' gradients are rounded to bf16 for their
  * products.  fp32 operands run in fp32 FMA, as does bf16 with
  * NOBLE_ATTN_SIMT_ONLY or with a stride of 0, below 0 or from 2^38 on (in
- * elements).  Outputs must not overlap inputs.  Results do not depend on the order in which a GPU
- * runs the blocks: repeated calls agree bit by bit.
+ * elements).  Outputs must not overlap inputs.  Results do not depend on the
+ * order in which a GPU runs the blocks: repeated calls agree bit by bit.
  */
 #define NOBLE_ATTN_CAUSAL 1u
 #define NOBLE_ATTN_SIMT_ONLY 2u
