@@ -49,6 +49,18 @@ __device__ __forceinline__ Span span(const Args<T> &a, int n)
     return {raw, len, a.window && first - a.window + 1 > 0 ? min(first - a.window + 1, len) : 0};
 }
 
+// The chunks with keys that sequence n sees, one at least, which also writes what a sequence
+// without such keys gets: a window behind a length that was cut leaves none.
+struct Chunks {
+    int first, last;
+};
+template <typename T>
+__device__ __forceinline__ Chunks chunks(const Args<T> &a, const Span &sp)
+{
+    const int last = max(sp.len - 1, 0) / a.chunk;
+    return {min(sp.from / a.chunk, last), last};
+}
+
 // Place of the key at position j, or -1 if its page is not one of the cache's.
 template <typename T>
 __device__ __forceinline__ int64_t place(const Args<T> &a, int n, int j)
@@ -101,8 +113,8 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(const __grid_constant__ 
     const int group = a.n_q / a.n_kv, rows = group * a.q_len;
     const Span sp = span(a, n);
     const int raw = sp.raw, c0 = chunk * a.chunk, j0 = max(c0, sp.from), j1 = min(c0 + a.chunk, sp.len);
-    const int first_chunk = sp.from / a.chunk, last_chunk = max(sp.len - 1, 0) / a.chunk;
-    if (chunk < first_chunk || chunk > last_chunk) return;
+    const Chunks cs = chunks(a, sp);
+    if (chunk < cs.first || chunk > cs.last) return;
     // row r: token r / group, head g * group + r % group
     float m[R], l[R], slope[R];
     int hi[R], lo[R];
@@ -185,7 +197,7 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(const __grid_constant__ 
         if (row >= rows) continue;
         const int64_t t = (int64_t)n * a.q_len + row / group;
         const int h = g * group + row % group;
-        if (first_chunk == last_chunk) {
+        if (cs.first == cs.last) {
             if (!simt::finite(acc[r]) || !isfinite(l[r])) redo[ty + RS * r] = 1;
             simt::store_row(a.o.at(t, h), acc[r], l[r] > 0.f ? 1.f / l[r] : 0.f, a.d, tx);
             if (a.lse && tx == 0) a.lse[t * a.n_q + h] = l[r] > 0.f ? m[r] + logf(l[r]) : -INFINITY;
@@ -216,8 +228,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Args<
     const int h = (int)(u % a.n_q);
     int c0 = 0, c1 = -1;
     if (u < rows) {
-        const Span sp = span(a, (int)(t / a.q_len));
-        c0 = sp.from / a.chunk, c1 = max(sp.len - 1, 0) / a.chunk;
+        const Chunks cs = chunks(a, span(a, (int)(t / a.q_len)));
+        c0 = cs.first, c1 = cs.last;
     }
     const bool work = c1 > c0;  // a single chunk has written the result itself
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);

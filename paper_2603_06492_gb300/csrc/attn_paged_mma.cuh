@@ -65,8 +65,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<DP>) mma_kernel(const _
     const int guess = chunk * a.chunk + 16 * warp, guess_j = guess + (PAGE16 ? 0 : lane & 15);
     const int guessed = guess_j / a.page_size < a.max_pages ? a.page_table[(int64_t)n * a.max_pages + guess_j / a.page_size] : -1;
     const Span sp = span(a, n);
-    const int first_chunk = sp.from / a.chunk, last_chunk = max(sp.len - 1, 0) / a.chunk;
-    if (chunk < first_chunk || chunk > last_chunk) return;
+    const Chunks cs = chunks(a, sp);
+    if (chunk < cs.first || chunk > cs.last) return;
     const int j0 = max(chunk * a.chunk, sp.from), j1 = min(chunk * a.chunk + a.chunk, sp.len);
 
     // rows g and g + 8 of the block: Q, positions, ranges
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<DP>) mma_kernel(const _
         for (int i = 0; i < 4; ++i) w[i] = exp2_fast(join_m[i][r] - base), sum += w[i] * join_l[i][r];
         const int64_t tok = (int64_t)n * a.q_len + row / group;
         const int h = kvh * group + row % group;
-        const bool single = first_chunk == last_chunk;
+        const bool single = cs.first == cs.last;
         const int64_t pt = (tok * a.n_q + h) * a.chunks + chunk;
         const float inv = !single ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
         bool fine = isfinite(sum);
