@@ -452,7 +452,8 @@ noble_status noble_rope_fwd(const noble_rope_desc *desc, const noble_heads *q, c
  * Backward: with w the rotation of dy by the negative angle and xn = x / rms,
  *     dgain = sum over tokens and heads of w * xn
  *     dx    = (gain * w - xn * mean(gain * w * xn)) / rms
- * (dx = w without NOBLE_ROPE_NORM).  q and k are the forward's inputs (NULL
+ * (dx = w without NOBLE_ROPE_NORM).  A token whose position is outside the table
+ * has dx = 0 and no part in dgain, whatever its inputs are, and is reported as above.  q and k are the forward's inputs (NULL
  * descriptors allowed without NOBLE_ROPE_NORM); dq_in, dk_in may be dq, dk with
  * the same strides.  dgain_q, dgain_k [d] fp32, NULL to skip; they are added up
  * in a fixed order, and not written without NOBLE_ROPE_NORM.

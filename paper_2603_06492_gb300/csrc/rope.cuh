@@ -418,9 +418,9 @@ __global__ void __launch_bounds__(32 * kWarps, kBwdBlocks<T>) bwd_kernel(const _
             stage = stage == kRing - 1 ? 0 : stage + 1;
             uint64_t tc[4], ts[4];
             pack8(tc, tn.c), pack8(ts, tn.s);
-            if (!known)
+            if (!known)  // the forward's outputs are 0 whatever x holds
 #pragma unroll
-                for (int p = 0; p < kPasses; ++p) rd[p].zero();
+                for (int p = 0; p < kPasses; ++p) rd[p].zero(), rx[p].zero();
             auto turned = [&](uint64_t (&w)[4], int p) {
                 uint64_t y[4];
                 rd[p].get(w);
@@ -447,8 +447,8 @@ __global__ void __launch_bounds__(32 * kWarps, kBwdBlocks<T>) bwd_kernel(const _
                 if (a.norm) {
                     uint64_t x[4];
                     rx[p].get(x);
-                    // without a head there is no norm: with eps 0 the zeros in its place would have an infinite one
-                    const float scale = h0 + p * hp < real ? rsqrtf(fmaf(v[p], a.inv_d, a.eps)) : 0.f;
+                    // no head, no norm: with eps 0 the zeros in its place would have an infinite one
+                    const float scale = known && h0 + p * hp < real ? rsqrtf(fmaf(v[p], a.inv_d, a.eps)) : 0.f;
                     const float c = -(v[kPasses + p] * scale * a.inv_d * scale) * scale;
                     const uint64_t s2 = pack2(scale, scale), c2 = pack2(c, c);
 #pragma unroll
