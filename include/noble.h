@@ -559,7 +559,8 @@ typedef struct {
     int64_t q_len;     /* new tokens of each, 1 to 64                          */
     int64_t n_q, n_kv, d; /* as in noble_attn_desc                             */
     int64_t max_pages; /* entries of a row of page_table                       */
-    int64_t max_len;   /* no kv_len is longer; it sets how the work is split   */
+    int64_t max_len;   /* no kv_len is longer; it sets how the work is split.  More
+                          than 2^31 - 65536, up to 2^31 - 1, counts as that     */
     int64_t window;
     float scale, softcap;
     int32_t dtype;

@@ -481,21 +481,23 @@ noble_status check_cache(const noble_kv_cache *c, int64_t n_kv, int64_t d, int32
 struct Split {
     int chunk, chunks;
 };
+int64_t paged_max_len(const noble_paged_desc *d) { return std::min<int64_t>(d->max_len, attn::paged::kMaxLen); }
 Split paged_split(const noble_paged_desc *d)
 {
+    const int64_t max_len = paged_max_len(d);
     const int64_t rows = d->n_q / d->n_kv * d->q_len;
     const int64_t units = d->n_seq * d->n_kv * ceil_div(rows, attn::paged::kRows);
     const int64_t slots = kSms * (d->d <= 64 ? attn::paged::kBlocksPerSm<64> : attn::paged::kBlocksPerSm<128>);
-    const int64_t one = ceil_div(d->max_len * std::max<int64_t>(units, 1), slots);
+    const int64_t one = ceil_div(max_len * std::max<int64_t>(units, 1), slots);
     // fp32 is bound by its products, not by reading: pieces enough to balance (24 sequences up
     // to 1024 tokens, 16 heads of 64: chunks of 384 107 us, of 512 139)
-    int64_t chunk = d->dtype == NOBLE_FP32 ? ceil_div(d->max_len * std::max<int64_t>(units, 1), 8 * kSms)
+    int64_t chunk = d->dtype == NOBLE_FP32 ? ceil_div(max_len * std::max<int64_t>(units, 1), 8 * kSms)
                     : d->n_seq <= 1        ? one
                                            : std::max(one / 8, std::min<int64_t>(one, 1024));
     chunk = std::max<int64_t>(chunk, 256);
-    const int64_t chunks = std::max<int64_t>(1, ceil_div(d->max_len, chunk));
-    chunk = std::max<int64_t>(1, ceil_div(ceil_div(d->max_len, chunks), attn::paged::kKeys)) * attn::paged::kKeys;
-    return {(int)chunk, (int)std::max<int64_t>(1, ceil_div(d->max_len, chunk))};
+    const int64_t chunks = std::max<int64_t>(1, ceil_div(max_len, chunk));
+    chunk = std::max<int64_t>(1, ceil_div(ceil_div(max_len, chunks), attn::paged::kKeys)) * attn::paged::kKeys;
+    return {(int)chunk, (int)std::max<int64_t>(1, ceil_div(max_len, chunk))};
 }
 struct PagedWork {
     size_t ml, total;
@@ -546,7 +548,7 @@ noble_status paged(const noble_paged_desc *d, const noble_heads *q, const noble_
     a.page_table = page_table, a.kv_len = kv_len, a.lse = lse;
     a.part_o = reinterpret_cast<float *>(ws), a.part_ml = reinterpret_cast<float *>(ws + paged_work(d).ml);
     a.page = c->page, a.row = c->row, a.head = c->head;
-    a.max_pages = d->max_pages, a.max_len = d->max_len;
+    a.max_pages = d->max_pages, a.max_len = paged_max_len(d);
     a.pages = (int)c->pages, a.page_size = (int)c->page_size;
     a.n_seq = (int)d->n_seq, a.q_len = (int)d->q_len, a.n_q = (int)d->n_q, a.n_kv = (int)d->n_kv, a.d = (int)d->d;
     a.window = (int)std::min<int64_t>(d->window, 1 << 30);

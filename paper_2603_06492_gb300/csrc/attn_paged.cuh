@@ -16,6 +16,9 @@ namespace attn {
 namespace paged {
 
 constexpr int kRows = 16, kKeys = 64, kThreads = 128;
+// Tokens of a sequence: the positions that a block works out beyond its last key, a step or two of
+// 64, stay within 32 bits.
+constexpr int kMaxLen = INT32_MAX - 65535;
 
 template <typename T>
 struct Args {
@@ -112,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) simt_kernel(const __grid_constant__ 
     const int chunk = blockIdx.x % a.chunks, rb = blockIdx.x / a.chunks, g = blockIdx.y, n = blockIdx.z;
     const int group = a.n_q / a.n_kv, rows = group * a.q_len;
     const Span sp = span(a, n);
-    const int raw = sp.raw, c0 = chunk * a.chunk, j0 = max(c0, sp.from), j1 = min(c0 + a.chunk, sp.len);
+    const int raw = sp.raw, c0 = chunk * a.chunk, j0 = max(c0, sp.from), j1 = c0 + min(a.chunk, sp.len - c0);
     const Chunks cs = chunks(a, sp);
     if (chunk < cs.first || chunk > cs.last) return;
     // row r: token r / group, head g * group + r % group

@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm<DP>) mma_kernel(const _
     const Span sp = span(a, n);
     const Chunks cs = chunks(a, sp);
     if (chunk < cs.first || chunk > cs.last) return;
-    const int j0 = max(chunk * a.chunk, sp.from), j1 = min(chunk * a.chunk + a.chunk, sp.len);
+    const int c0 = chunk * a.chunk, j0 = max(c0, sp.from), j1 = c0 + min(a.chunk, sp.len - c0);
 
     // rows g and g + 8 of the block: Q, positions, ranges
     uint32_t q[2][C][4];
