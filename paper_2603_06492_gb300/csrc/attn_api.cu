@@ -551,7 +551,7 @@ noble_status paged(const noble_paged_desc *d, const noble_heads *q, const noble_
     a.max_pages = d->max_pages, a.max_len = paged_max_len(d);
     a.pages = (int)c->pages, a.page_size = (int)c->page_size;
     a.n_seq = (int)d->n_seq, a.q_len = (int)d->q_len, a.n_q = (int)d->n_q, a.n_kv = (int)d->n_kv, a.d = (int)d->d;
-    a.window = (int)std::min<int64_t>(d->window, 1 << 30);
+    a.window = (int)std::min<int64_t>(d->window, attn::paged::kMaxLen);  // as far as any key is from its query
     const Split s = paged_split(d);
     a.chunk = s.chunk, a.chunks = s.chunks;
     a.score = {d->scale, d->softcap, slope};

@@ -89,3 +89,14 @@ def test_lengths_beyond_the_longest_are_reported():
     k, v, table = _one_page(2 ** 31 - 1, "bf16")
     with pytest.raises(binding.NobleError):
         _run_long(n + 1, "bf16", k, v, table, 2 ** 31 - 1)
+
+
+def test_window_beyond_30_bits():
+    """A window of 2^30 + 500 of 2^30 + 1000 tokens: 500 to 600 are seen and outweigh all others
+    (100 e^30 to 2^30 e^0), those before 500 would outweigh them."""
+    n, window = 2 ** 30 + 1000, 2 ** 30 + 500
+    k, v, table = _one_page(n, "bf16")
+    k[0, 500:600, 0, 0], v[0, 500:600] = 30.0, 1.0
+    k[0, :500, 0, 0], v[0, :500] = 60.0, -1.0
+    o, lse = _run_long(n, "bf16", k, v, table, n, window)
+    assert float((o - 1).abs().max()) <= TOL["bf16"] and abs(lse - 30.0 - math.log(100)) <= 1e-5 * 35
