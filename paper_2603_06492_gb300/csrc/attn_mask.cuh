@@ -247,6 +247,7 @@ __device__ __forceinline__ float warp_sum(float v)
 // The tiled kernels multiply masked places by zero, which an infinity or a NaN in
 // such a place turns into NaN; a row that comes out not finite is computed again
 // here, where masked places are not read at all.  Lanes hold features lane + 32 u.
+// A sum that is NaN stays so: a row stops there, as all do soon when everything is NaN.
 // They count, so that a test can tell that nothing else sends rows here.
 __device__ unsigned long long g_rows_again = 0;
 __device__ __forceinline__ void count_row(int lane)
@@ -283,7 +284,15 @@ __device__ __forceinline__ float row_dot(const float (&a)[4], const float (&b)[4
 {
     return warp_sum(a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]);
 }
-// the score, and in `slope_x` its derivative by scale q.k
+// Whether all features of a row are NaN.
+__device__ __forceinline__ bool all_nan(const float (&x)[4], int d, int lane)
+{
+    bool all = true;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) all = all && (lane + 32 * u >= d || isnan(x[u]));
+    return __all_sync(0xffffffffu, all);
+}
+// the score, and in `deriv` its derivative by scale q.k
 __device__ __forceinline__ float row_score(const Score &s, float qk, int h, int i, int j, float *deriv)
 {
     float x = qk * s.scale, g = 1.f;
@@ -315,6 +324,7 @@ __device__ __noinline__ void row_fwd(const RowArgs<T> &a, int i, int h, int lane
         m = mn, l = l * c + p;
 #pragma unroll
         for (int u = 0; u < 4; ++u) acc[u] = acc[u] * c + p * x[u];
+        if (isnan(l)) break;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -352,6 +362,7 @@ __device__ __noinline__ void row_dq(const RowArgs<T> &a, int i, int h, int lane,
         row_pair(a, q, k, v, d_o, lse, delta, h, i, j, p, ds);
 #pragma unroll
         for (int u = 0; u < 4; ++u) acc[u] += ds * k[u];
+        if (isnan(ds)) break;
     }
     row_store(a.dq.at(i, h), acc, min(f1, a.d), lane, f0);
 }
@@ -387,8 +398,9 @@ __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane
     float k[4], v[4], dk[4] = {}, dv[4] = {};
     row_load(k, a.k.at(j, g), a.d, lane);
     row_load(v, a.v.at(j, g), a.d, lane);
+    bool no_dk = !to_dk, no_dv = !to_dv;  // nothing to add to
     for (int h = g * group; h < (g + 1) * group; ++h)
-        for (int i = r.lo; i < r.hi; ++i) {
+        for (int i = r.lo; i < r.hi && !(no_dk && no_dv); ++i) {
             const Range s = visible(a.mask, i);
             if (j < s.lo || j >= s.hi) continue;
             float q[4], d_o[4], p, ds;
@@ -397,6 +409,7 @@ __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane
             row_pair(a, q, k, v, d_o, a.lse[(int64_t)h * a.mask.T + i], a.delta[(int64_t)h * a.mask.T + i], h, i, j, p, ds);
 #pragma unroll
             for (int u = 0; u < 4; ++u) dk[u] += ds * q[u], dv[u] += p * d_o[u];
+            no_dk |= isnan(ds), no_dv |= all_nan(dv, a.d, lane);
         }
     if (to_dk) row_store(a.dk.at(j, g), dk, a.d, lane);
     if (to_dv) row_store(a.dv.at(j, g), dv, a.d, lane);

@@ -94,6 +94,7 @@ __device__ __noinline__ void row_paged(const Args<T> &a, int64_t t, int h, int l
         m = mn, l = l * c + p;
 #pragma unroll
         for (int u = 0; u < 4; ++u) acc[u] = acc[u] * c + p * x[u];
+        if (isnan(l)) break;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll

@@ -282,6 +282,50 @@ __device__ __forceinline__ void setmaxnreg_inc() { asm volatile("setmaxnreg.inc.
 template <int N>
 __device__ __forceinline__ void setmaxnreg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// ---------------------------------------------------------------- rows computed again
+// Rows that come out not finite (row_fwd and its like say why) are noted while a block's pieces of
+// work run and computed again when the block is through with them: one such row of a
+// long document takes milliseconds, many take longer than the other warps' waits last.  A block
+// that has noted rows asks for no further piece, and the launch starts another one for what is
+// left.  So a warp notes rows of at most 7 pieces: those of piece w when it has taken w + 1 at most;
+// w + 5 would be asked for only after it has taken w + 2; and no warp is behind w - 2.
+struct Again {
+    static constexpr int kPieces = 8, kWarps = 8;
+    static constexpr uint32_t kBytes = 4 * (1 + kWarps + 2 * kWarps * kPieces) + 4;
+    uint32_t *mem;  // whether any rows are noted; pieces noted per warp; (first row of 32 and head, rows) of each
+    __device__ __forceinline__ volatile uint32_t *any() const { return mem; }
+    __device__ __forceinline__ void init() const  // all threads, before a __syncthreads
+    {
+        if (threadIdx.x <= kWarps) mem[threadIdx.x] = 0;
+    }
+    // The warp's `rows` of row0 (a multiple of 32) and on, of a head; all lanes together.
+    __device__ __forceinline__ void note(int warp, int lane, int row0, int head, uint32_t rows) const
+    {
+        if (rows && lane == 0) {
+            uint32_t *at = mem + 1 + kWarps + 2 * (warp * kPieces + mem[1 + warp]++);
+            at[0] = (uint32_t)row0 >> 5 | (uint32_t)head << 19, at[1] = rows;
+            *any() = 1;
+        }
+        __syncwarp();
+    }
+    // f(warp that noted it, row, head) for every row noted, by the warps in turn, all of which call
+    // this when they have no more to note.
+    template <class F>
+    __device__ __forceinline__ void each(int warp, F &&f) const
+    {
+        __syncwarp();
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");
+        if (!*any()) return;
+        int k = 0;
+        for (int w = 0; w < kWarps; ++w)
+            for (uint32_t e = 0; e < mem[1 + w]; ++e) {
+                const uint32_t *at = mem + 1 + kWarps + 2 * (w * kPieces + e);
+                for (uint32_t rows = at[1]; rows; rows &= rows - 1)
+                    if (k++ % kWarps == warp) f(w, (int)((at[0] & 0x7ffffu) << 5) + __ffs(rows) - 1, (int)(at[0] >> 19));
+            }
+    }
+};
+
 // ---------------------------------------------------------------- work handed out by the launch
 // A block that has finished its piece of work takes over that of a block of the grid
 // that has not started (cluster launch control), so that blocks set up once and
@@ -331,9 +375,10 @@ struct Work {
             ptx::mbar_init(empty(s), readers);
         }
     }
-    // The thread that hands out; describe(index) is the piece of a block.
+    // The thread that hands out; describe(index) is the piece of a block.  It asks for no more once
+    // `enough` is set.
     template <class F>
-    __device__ __forceinline__ void hand_out(F &&describe, uint32_t *status) const
+    __device__ __forceinline__ void hand_out(F &&describe, volatile uint32_t *enough, uint32_t *status) const
     {
         int work = blockIdx.x;
         for (int k = 0;; ++k) {
@@ -347,6 +392,10 @@ struct Work {
             ptx::mbar_arrive(full(k & 1));
             if (work < 0) break;  // no more is asked after the first "none left"
             if (!ptx::mbar_wait(taken(), k & 1, status)) break;
+            if (*enough) {
+                work = -1;
+                continue;
+            }
             ptx::mbar_arrive_expect_tx(answered(), 16);
             ask_next(answer(), answered());
             if (!ptx::mbar_wait(answered(), k & 1, status)) break;

@@ -52,7 +52,8 @@ struct Bwd {
     static constexpr uint32_t kBars = kVec + VEC;
     static constexpr int kNumBars = 2 * X + 4 * Y + 12;
     static constexpr uint32_t kWork = kBars + 8 * ((kNumBars + 1) & ~1);
-    static constexpr uint32_t kBytes = kWork + Work::kBytes + 16;
+    static constexpr uint32_t kAgain = kWork + Work::kBytes + 16;
+    static constexpr uint32_t kBytes = kAgain + Again::kBytes;
     static_assert(kBytes <= 232448, "shared memory of a block");
 };
 // A K tile is in use from its S to its dQ, a step and a half: with 128 features a third
@@ -140,6 +141,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     auto ds_full = [&](int i) { return one + 72 + 8u * (i & 1); };
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
+    const Again again{reinterpret_cast<uint32_t *>(smem + B::kAgain)};
     float *part = reinterpret_cast<float *>(smem + B::kVec);  // [2][128]
     const int warp = (int)uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
     uint32_t *status = args.status;
@@ -175,6 +177,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
         ptx::tmem_relinquish();
     }
+    again.init();
     const Mask mask = mask_in_smem<B::kDocsKept>(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
     ptx::tc_fence_before();
     __syncthreads();
@@ -283,7 +286,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             // every product has finished before TMEM is released below
             if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
-            works.hand_out(describe, status);
+            works.hand_out(describe, again.any(), status);
         }
         __syncwarp();
     } else {
@@ -466,13 +469,13 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                 fine &= write_rows(o, args.a.score.scale, none || !p.steps, out + c, args.a.dq.row, mask.T - (i - lane),
                                    args.a.d - half * (DP / 2) - c, lane);
             }
-            uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
-            __syncwarp();
-            for (; bad; bad &= bad - 1) {
-                const int r = __ffs(bad) - 1;
-                row_dq(args.a, i - lane + r, p.h, lane, __shfl_sync(0xffffffffu, delta, r), half * (DP / 2), half * (DP / 2) + DP / 2);
-            }
+            again.note(warp, lane, i - lane, p.h, __ballot_sync(0xffffffffu, real && !fine));
         }
+        // half of a row's features, as the warp that noted it; delta in memory is this kernel's by now
+        again.each(warp, [&](int w, int i, int h) {
+            const int f = w / 4 * (DP / 2);
+            row_dq(args.a, i, h, lane, args.delta[(int64_t)h * mask.T + i], f, f + DP / 2);
+        });
     }
 
     ptx::tc_fence_before();
@@ -510,6 +513,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                    acc_full = one + 48, acc_empty = one + 56;
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
+    const Again again{reinterpret_cast<uint32_t *>(smem + B::kAgain)};
     const int warp = (int)uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
@@ -541,6 +545,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
         ptx::tmem_relinquish();
     }
+    again.init();
     const Mask mask = mask_in_smem<B::kDocsKept>(args.a.mask, reinterpret_cast<int32_t *>(smem + B::kDocs));
     ptx::tc_fence_before();
     __syncthreads();
@@ -676,7 +681,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 }
             }
         } else if (warp == 11 && lane == 0) {
-            works.hand_out(describe, status);
+            works.hand_out(describe, again.any(), status);
         }
         __syncwarp();
     } else {
@@ -833,10 +838,9 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                         part[e / 4 * kRows] = p.steps ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0, 0, 0, 0);
                 }
             }
-            uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
-            __syncwarp();
-            for (; bad; bad &= bad - 1) row_dkv(args.a, j - lane + __ffs(bad) - 1, p.g, lane, half == 0, half == 1);
+            again.note(warp, lane, j - lane, p.g, __ballot_sync(0xffffffffu, real && !fine));
         }
+        again.each(warp, [&](int w, int j, int g) { row_dkv(args.a, j, g, lane, w / 4 == 0, w / 4 == 1); });
     }
 
     ptx::tc_fence_before();

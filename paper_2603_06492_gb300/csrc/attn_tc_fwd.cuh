@@ -39,7 +39,8 @@ struct Fwd {
     // score blocks (a phase of another's would be taken for one of its own); p full by
     // buffer; pv done by row block
     static constexpr int kNumBars = 2 + 4 * kStages + 3 * kBuffers + 2;
-    static constexpr uint32_t kBytes = kBars + 8 * kNumBars + 16;
+    static constexpr uint32_t kAgain = kBars + 8 * kNumBars + 16;
+    static constexpr uint32_t kBytes = kAgain + Again::kBytes;
     static constexpr uint32_t kDynamic = kBytes + 1024;
     static constexpr uint32_t kO = 128 * kBuffers;  // TMEM column of O
 };
@@ -98,6 +99,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     auto pv_done = [&](int b) { return bars + 8u * (2 + 4 * kStages + 3 * F::kBuffers + b); };
     const Work works{base + F::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + F::kBars + 8 * F::kNumBars);
+    const Again again{reinterpret_cast<uint32_t *>(smem + F::kAgain)};
     const int warp = (int)uniform(threadIdx.x / 32), lane = threadIdx.x % 32;
     uint32_t *status = args.status;
 
@@ -126,6 +128,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
         ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
         ptx::tmem_relinquish();
     }
+    again.init();
     const Mask mask = mask_in_smem<kDocsInSmem>(args.a.mask, reinterpret_cast<int32_t *>(smem + F::kDocs));
     ptx::tc_fence_before();
     __syncthreads();
@@ -248,7 +251,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             // order, and the last of a piece of work is that of its last V stage
             if (last) wait_warp(v_empty((last - 1) / 2), (last - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
-            works.hand_out([&](int work) { return fwd_piece(mask, args, work); }, status);
+            works.hand_out([&](int work) { return fwd_piece(mask, args, work); }, again.any(), status);
         }
         __syncwarp();
     } else {
@@ -386,10 +389,9 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             }
             if (real) args.a.lse[(int64_t)s.h * mask.T + i] = inv > 0.f || !fine ? (m + log2f(l)) * kLn2 : -INFINITY;
             // rows that masked infinities or NaN have reached
-            uint32_t bad = __ballot_sync(0xffffffffu, real && !fine);
-            __syncwarp();
-            for (; bad; bad &= bad - 1) row_fwd(args.a, i - lane + __ffs(bad) - 1, s.h, lane);
+            again.note(warp, lane, i - lane, s.h, __ballot_sync(0xffffffffu, real && !fine));
         }
+        again.each(warp, [&](int, int i, int h) { row_fwd(args.a, i, h, lane); });
     }
 
     ptx::tc_fence_before();
