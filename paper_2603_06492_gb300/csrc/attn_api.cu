@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
+#include <limits>
 
 #include "host.cuh"
 #include "attn_mask.cuh"
@@ -124,7 +125,9 @@ rope::Args<T> rope_args(const noble_rope_desc *d, const noble_heads *q, const no
     a.interleaved = (d->flags & NOBLE_ROPE_INTERLEAVED) != 0;
     a.gain_q = a.norm ? gain_q : nullptr, a.gain_k = a.norm ? gain_k : nullptr;
     a.tokens = d->T, a.n_q = (int)d->n_q, a.n_kv = (int)d->n_kv, a.d = (int)d->d, a.rot = (int)d->rot;
-    a.positions = (int)d->positions, a.eps = d->eps;
+    // eps 0: places without a head hold zeros, which times a finite factor stay 0; no head whose
+    // norm fp32 can hold notices
+    a.positions = (int)d->positions, a.eps = std::max(d->eps, std::numeric_limits<float>::denorm_min());
     a.lp = lanes_per_head(d->d), a.inv_d = 1.f / (float)d->d;
     a.batches_q = (int)rope_batches(d->n_q, d->d), a.batches_kv = (int)rope_batches(d->n_kv, d->d);
     return a;

@@ -447,9 +447,7 @@ __global__ void __launch_bounds__(32 * kWarps, kBwdBlocks<T>) bwd_kernel(const _
                 if (a.norm) {
                     uint64_t x[4];
                     rx[p].get(x);
-                    // no head, no norm: with eps 0 the zeros in its place would have an infinite one
-                    const float scale = known && h0 + p * hp < real ? rsqrtf(fmaf(v[p], a.inv_d, a.eps)) : 0.f;
-                    const float c = -(v[kPasses + p] * scale * a.inv_d * scale) * scale;
+                    const float scale = rsqrtf(fmaf(v[p], a.inv_d, a.eps)), c = -(v[kPasses + p] * scale * a.inv_d * scale) * scale;
                     const uint64_t s2 = pack2(scale, scale), c2 = pack2(c, c);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
