@@ -398,9 +398,9 @@ __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane
     float k[4], v[4], dk[4] = {}, dv[4] = {};
     row_load(k, a.k.at(j, g), a.d, lane);
     row_load(v, a.v.at(j, g), a.d, lane);
-    bool no_dk = !to_dk, no_dv = !to_dv;  // nothing to add to
+    bool lost = false;
     for (int h = g * group; h < (g + 1) * group; ++h)
-        for (int i = r.lo; i < r.hi && !(no_dk && no_dv); ++i) {
+        for (int i = r.lo; i < r.hi && !lost; ++i) {
             const Range s = visible(a.mask, i);
             if (j < s.lo || j >= s.hi) continue;
             float q[4], d_o[4], p, ds;
@@ -409,7 +409,7 @@ __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane
             row_pair(a, q, k, v, d_o, a.lse[(int64_t)h * a.mask.T + i], a.delta[(int64_t)h * a.mask.T + i], h, i, j, p, ds);
 #pragma unroll
             for (int u = 0; u < 4; ++u) dk[u] += ds * q[u], dv[u] += p * d_o[u];
-            no_dk |= isnan(ds), no_dv |= all_nan(dv, a.d, lane);
+            lost = (!to_dk || isnan(ds)) && (!to_dv || all_nan(dv, a.d, lane));
         }
     if (to_dk) row_store(a.dk.at(j, g), dk, a.d, lane);
     if (to_dv) row_store(a.dv.at(j, g), dv, a.d, lane);
