@@ -187,6 +187,33 @@ __device__ __forceinline__ bool write_rows(const uint32_t (&o)[32], float f, boo
     return zero || sum2(left) == 0.f;
 }
 
+// The last tile of the last document may reach into padding, the tokens behind all documents, which
+// hold anything, infinities and NaN too.  Such a tile is loaded to a barrier of its own; a warp
+// that has little else to do clears its padding rows when it has landed and then arrives
+// on the barrier that the products wait for: these know nothing of it (checks among their waits
+// cost 16384 tokens of 64 features 5 % forward, 3 % backward).  Other tokens that a tile holds and a row does
+// not see belong to a document, and are finite unless something went wrong: see row_fwd.
+__device__ __forceinline__ int padding_from(const Mask &m) { const int end = docs_end(m); return end < m.T ? end : INT32_MAX; }
+// Barriers `landed` + 8 st by stage, in use for tiles with padding only: parities by stage.
+struct Padding {
+    uint32_t landed, parities;
+    __device__ __forceinline__ uint32_t at(int st) const { return landed + 8u * st; }
+    // A whole warp: rows `from` and on of the tile of stage st.
+    template <int DP>
+    __device__ __forceinline__ bool clear(uint8_t *tile, int st, int from, uint32_t full, int lane, uint32_t *status)
+    {
+        if (!wait_warp(at(st), parities >> st & 1, status)) return false;
+        parities ^= 1u << st;
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+            for (int x = 8 * max(from, 0) + lane; x < 8 * kRows; x += 32) *reinterpret_cast<uint4 *>(tile + c * kChunk + 16 * x) = make_uint4(0, 0, 0, 0);
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(full);
+        return true;
+    }
+};
+
 // Scores of N columns of a row in units of log 2, from q.k: capped, and biased by the
 // distance `far` - column of query and key; gs their derivatives by scale q.k as pairs
 // of 16-bit floats, for a product that is rounded to 8 bits.  Nothing here converts an
@@ -203,8 +230,9 @@ struct Capping {
     float in, out;  // kNoCap: s = out q.k
     int mode;
 };
+// seen: whether the row sees anything; if not, its scores have no part in the choice.
 template <int N>
-__device__ __forceinline__ Capping capping(const float (&x)[N], const Score &sc)
+__device__ __forceinline__ Capping capping(const float (&x)[N], const Score &sc, bool seen)
 {
     if (!(sc.softcap > 0.f)) return {0.f, sc.scale * kLog2e, kNoCap};
     const float in = sc.scale / sc.softcap;
@@ -213,7 +241,7 @@ __device__ __forceinline__ Capping capping(const float (&x)[N], const Score &sc)
     for (int c = 0; c < N; c += 4)
 #pragma unroll
         for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], fabsf(x[c + u]));
-    const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(in);
+    const float most = seen ? fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * fabsf(in) : 0.f;
     const int mode = __all_sync(0xffffffffu, most < 0.33f) ? kCapShort : __all_sync(0xffffffffu, most < 0.6f) ? kCapSeries : kCapExact;
     return {in, sc.softcap * kLog2e, mode};
 }
@@ -254,9 +282,9 @@ __device__ __forceinline__ void with_cap(int mode, F &&f)
     else f(std::integral_constant<int, kCapExact>{});
 }
 template <int N, bool GRAD>
-__device__ __forceinline__ void general_scores(float (&x)[N], uint32_t (&gs)[GRAD ? N / 2 : 1], const Score &sc, float slope, float far)
+__device__ __forceinline__ void general_scores(float (&x)[N], uint32_t (&gs)[GRAD ? N / 2 : 1], const Score &sc, float slope, float far, bool seen)
 {
-    const Capping cap = capping(x, sc);
+    const Capping cap = capping(x, sc, seen);
     with_cap(cap.mode, [&](auto mode) {
 #pragma unroll
         for (int c = 0; c < N; c += 2) {

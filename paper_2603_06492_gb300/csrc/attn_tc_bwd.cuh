@@ -50,7 +50,7 @@ struct Bwd {
     static constexpr uint32_t kDocs = kY + Y * kTile;
     static constexpr uint32_t kVec = kDocs + 2 * DOCS * 4;
     static constexpr uint32_t kBars = kVec + VEC;
-    static constexpr int kNumBars = 2 * X + 4 * Y + 12;
+    static constexpr int kNumBars = 3 * X + 5 * Y + 12;
     static constexpr uint32_t kWork = kBars + 8 * ((kNumBars + 1) & ~1);
     static constexpr uint32_t kAgain = kWork + Work::kBytes + 16;
     static constexpr uint32_t kBytes = kAgain + Again::kBytes;
@@ -139,6 +139,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
     // readers, and a warp can be through with the next dS while another is at this one.
     auto s_full = [&](int i) { return one + 56 + 8u * (i & 1); };
     auto ds_full = [&](int i) { return one + 72 + 8u * (i & 1); };
+    Padding pad_k{one + 88, 0}, pad_v{pad_k.at(kXS), 0};
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
     const Again again{reinterpret_cast<uint32_t *>(smem + B::kAgain)};
@@ -154,10 +155,12 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         for (int s = 0; s < kXS; ++s) {
             ptx::mbar_init(k_full(s), 1);
             ptx::mbar_init(k_empty(s), 1);
+            ptx::mbar_init(pad_k.at(s), 1);
         }
         for (int s = 0; s < kYS; ++s) {
             ptx::mbar_init(v_full(s), 1);
             ptx::mbar_init(v_empty(s), 1);
+            ptx::mbar_init(pad_v.at(s), 1);
         }
         ptx::mbar_init(q_full, 1);
         ptx::mbar_init(q_empty, 1);
@@ -170,7 +173,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
         ptx::mbar_init(acc_full, 1);
         ptx::mbar_init(acc_empty, 8);
         ptx::mbar_init(sums, 8);
-        works.init(10);
+        works.init(11);
         ptx::fence_barrier_init();
     }
     if (warp == 9) {
@@ -198,6 +201,8 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
 
     if (warp >= 8) {
         setmaxnreg_dec<88>();
+        const int padding = padding_from(mask);
+        auto padded = [&](const Rows &p) { return p.lo + p.steps * kRows > padding; };  // its last tile
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, nk = 0;
@@ -217,13 +222,15 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                     const int sx = n % kXS, sy = n % kYS, j = p.lo + t * kRows;
                     ok = ptx::mbar_wait(k_empty(sx), ((n / kXS) & 1) ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(k_full(sx), B::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + sx * B::kTile + c * kChunk, &mK, k_full(sx), 64 * c, p.g, j);
+                    const bool pad = t + 1 == p.steps && padded(p);
+                    const uint32_t to_k = pad ? pad_k.at(sx) : k_full(sx), to_v = pad ? pad_v.at(sy) : v_full(sy);
+                    ptx::mbar_arrive_expect_tx(to_k, B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + sx * B::kTile + c * kChunk, &mK, to_k, 64 * c, p.g, j);
                     ++nk;
                     ok = ptx::mbar_wait(v_empty(sy), ((n / kYS) & 1) ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(v_full(sy), B::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + sy * B::kTile + c * kChunk, &mV, v_full(sy), 64 * c, p.g, j);
+                    ptx::mbar_arrive_expect_tx(to_v, B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + sy * B::kTile + c * kChunk, &mV, to_v, 64 * c, p.g, j);
                 }
             }
             if (items) ptx::mbar_wait(q_full, (items - 1) & 1, nullptr);
@@ -287,6 +294,17 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
             if (items) ptx::mbar_wait(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
             works.hand_out(describe, again.any(), status);
+        } else if (warp == 11) {
+            // ---------------- padding
+            int n = 0;
+            for (int w = 0; works.take(pc, w, true, false, lane, status); ++w) {
+                const Rows p = as_rows(pc);
+                n += p.steps;
+                if (p.steps == 0 || !padded(p)) continue;
+                const int sx = (n - 1) % kXS, sy = (n - 1) % kYS, from = padding - (p.lo + (p.steps - 1) * kRows);
+                if (!pad_k.clear<DP>(smem + B::kX + sx * B::kTile, sx, from, k_full(sx), lane, status)) break;
+                if (!pad_v.clear<DP>(smem + B::kY + sy * B::kTile, sy, from, v_full(sy), lane, status)) break;
+            }
         }
         __syncwarp();
     } else {
@@ -388,7 +406,7 @@ dq_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUtens
                     }
                 } else {
                     // a pair of columns at a time from score to dS, since the derivatives have no room beside both
-                    const Capping cap = capping(s, args.a.score);
+                    const Capping cap = capping(s, args.a.score, !none);
                     const float far = (float)(i - j0);
                     const uint64_t far2 = pack2(far, far), l2 = pack2(-lse2, -lse2), slope2 = pack2(-slope, -slope);
                     auto as_ds = [&](auto mode, auto biased) {
@@ -511,6 +529,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     const uint32_t one = bars + 8u * (6 * kStages);
     const uint32_t kv_full = one, kv_empty = one + 8, s_full = one + 16, dp_full = one + 24, p_full = one + 32, ds_full = one + 40,
                    acc_full = one + 48, acc_empty = one + 56;
+    Padding pad_q{one + 64, 0}, pad_o{pad_q.at(kStages), 0};
     const Work works{base + B::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + B::kWork + Work::kBytes);
     const Again again{reinterpret_cast<uint32_t *>(smem + B::kAgain)};
@@ -529,6 +548,8 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             ptx::mbar_init(o_empty(s), 1);
             ptx::mbar_init(vec_full(s), 1);
             ptx::mbar_init(vec_empty(s), 8);
+            ptx::mbar_init(pad_q.at(s), 1);
+            ptx::mbar_init(pad_o.at(s), 1);
         }
         ptx::mbar_init(kv_full, 1);
         ptx::mbar_init(kv_empty, 1);
@@ -568,6 +589,9 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
 
     if (warp >= 8) {
         setmaxnreg_dec<88>();
+        const int padding = padding_from(mask);
+        // the last tile of every head
+        auto padded = [&](const Keys &p, int t) { return p.lo + p.per * kRows > padding && (t + 1) % p.per == 0; };
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, nq = 0;
@@ -588,13 +612,15 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     const uint32_t ph = (n / kStages) & 1;
                     ok = ptx::mbar_wait(q_empty(st), ph ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(q_full(st), B::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + st * B::kTile + c * kChunk, &mQ, q_full(st), 64 * c, h, i);
+                    const bool pad = padded(p, t);
+                    const uint32_t to_q = pad ? pad_q.at(st) : q_full(st), to_o = pad ? pad_o.at(st) : o_full(st);
+                    ptx::mbar_arrive_expect_tx(to_q, B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kX + st * B::kTile + c * kChunk, &mQ, to_q, 64 * c, h, i);
                     ++nq;
                     ok = ptx::mbar_wait(o_empty(st), ph ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(o_full(st), B::kTile);
-                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + st * B::kTile + c * kChunk, &mDO, o_full(st), 64 * c, h, i);
+                    ptx::mbar_arrive_expect_tx(to_o, B::kTile);
+                    for (int c = 0; c < kChunks; ++c) tma_load_3d(base + B::kY + st * B::kTile + c * kChunk, &mDO, to_o, 64 * c, h, i);
                 }
             }
             if (items) ptx::mbar_wait(kv_full, (items - 1) & 1, nullptr);
@@ -651,9 +677,11 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             // every product has finished before TMEM is released below
             if (items) wait_warp(acc_full, (items - 1) & 1, nullptr);
         } else if (warp == 10) {
-            // ---------------- lse and delta of the query tiles, a step ahead of the stage they go to
+            // ---------------- lse and delta of the query tiles, a step ahead of the stage they go to;
+            // their padding
             int n = 0;
             bool ok = true;
+            const int end = docs_end(mask);
             for (int w = 0; ok && works.take(pc, w, true, false, lane, status); ++w) {
                 const Keys p = as_keys(pc);
                 float lse[4], delta[4];
@@ -663,14 +691,19 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     for (int u = 0; u < 4; ++u) {
                         const int i = i0 + lane + 32 * u;
                         const int64_t at = (int64_t)h * mask.T + i;
-                        lse[u] = i < mask.T ? args.a.lse[at] : 0.f;
-                        delta[u] = i < mask.T ? args.delta[at] : 0.f;
+                        lse[u] = i < end ? args.a.lse[at] : 0.f;
+                        delta[u] = i < end ? args.delta[at] : 0.f;
                     }
                 };
                 if (p.steps) fetch(0);
                 for (int t = 0; t < p.steps; ++t, ++n) {
                     const int st = n % kStages;
                     ok = wait_warp(vec_empty(st), ((n / kStages) & 1) ^ 1, status);
+                    if (ok && padded(p, t)) {
+                        const int from = padding - (p.lo + (p.per - 1) * kRows);
+                        ok = pad_q.clear<DP>(smem + B::kX + st * B::kTile, st, from, q_full(st), lane, status) &&
+                             pad_o.clear<DP>(smem + B::kY + st * B::kTile, st, from, o_full(st), lane, status);
+                    }
                     if (!ok) break;
                     float *vec = reinterpret_cast<float *>(smem + B::kVec + st * kVecBytes);
 #pragma unroll
@@ -741,7 +774,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 } else {
                     const int h = p.h0 + t / p.per;
                     const float slope = args.a.score.slope ? args.a.score.slope[h] * kLog2e : 0.f;
-                    general_scores<64, GENERAL>(s, gs, args.a.score, slope, (float)(j - i0));
+                    general_scores<64, GENERAL>(s, gs, args.a.score, slope, (float)(j - i0), see.lo < see.hi);
 #pragma unroll
                     for (int c = 0; c < 64; c += 4) {
                         const float4 l = *reinterpret_cast<const float4 *>(vec + c);
@@ -811,7 +844,7 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 ++items;
                 ptx::tc_fence_after();
             }
-            const bool real = j < mask.T;
+            const bool real = j < mask.T, none = see.lo >= see.hi;
             const float f = half ? args.a.score.scale : 1.f;
             const Heads<__nv_bfloat16> &to = half ? args.a.dk : args.a.dv;
             __nv_bfloat16 *out = to.at(j - lane, p.g);
@@ -829,13 +862,13 @@ dkv_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     if (lane == 0 && c + 32 == DP) ptx::mbar_arrive(acc_empty);
                 }
                 if (args.splits == 1) {
-                    fine &= write_rows(o, f, !p.steps, out + c, to.row, mask.T - (j - lane), args.a.d - c, lane);
+                    fine &= write_rows(o, f, none || !p.steps, out + c, to.row, mask.T - (j - lane), args.a.d - c, lane);
                 } else {
                     const int64_t unit = (int64_t)(p.j0 / kRows) * args.parts + p.part;
                     uint4 *part = reinterpret_cast<uint4 *>(args.part) + ((unit * 2 + half) * (DP / 4) + c / 4) * kRows + row;
 #pragma unroll
                     for (int e = 0; e < 32; e += 4)
-                        part[e / 4 * kRows] = p.steps ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0, 0, 0, 0);
+                        part[e / 4 * kRows] = p.steps && !none ? make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_uint4(0, 0, 0, 0);
                 }
             }
             again.note(warp, lane, j - lane, p.g, __ballot_sync(0xffffffffu, real && !fine));

@@ -29,7 +29,7 @@ namespace tc {
 
 template <int DP>
 struct Fwd {
-    static constexpr int kThreads = 384;  // two softmax warpgroups; loading, product and work threads, a spare warp
+    static constexpr int kThreads = 384;  // two softmax warpgroups; loading, product, work and padding warps
     static constexpr int kStages = DP == 64 ? 4 : 2;
     static constexpr int kBuffers = DP == 64 ? 3 : 2;  // of 128 TMEM columns for S
     static constexpr uint32_t kTile = kChunk * (DP / 64);
@@ -37,8 +37,8 @@ struct Fwd {
     static constexpr uint32_t kWork = kDocs + 2 * kDocsInSmem * 4, kBars = kWork + Work::kBytes;
     // q full/empty; k and v full/empty by stage; s full by row block and its own count of
     // score blocks (a phase of another's would be taken for one of its own); p full by
-    // buffer; pv done by row block
-    static constexpr int kNumBars = 2 + 4 * kStages + 3 * kBuffers + 2;
+    // buffer; pv done by row block; k and v with padding landed by stage
+    static constexpr int kNumBars = 2 + 4 * kStages + 3 * kBuffers + 2 + 2 * kStages;
     static constexpr uint32_t kAgain = kBars + 8 * kNumBars + 16;
     static constexpr uint32_t kBytes = kAgain + Again::kBytes;
     static constexpr uint32_t kDynamic = kBytes + 1024;
@@ -97,6 +97,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     auto s_full = [&](int b, int i) { return bars + 8u * (2 + 4 * kStages + b * F::kBuffers + i); };
     auto p_full = [&](int i) { return bars + 8u * (2 + 4 * kStages + 2 * F::kBuffers + i); };
     auto pv_done = [&](int b) { return bars + 8u * (2 + 4 * kStages + 3 * F::kBuffers + b); };
+    Padding pad_k{bars + 8u * (4 + 4 * kStages + 3 * F::kBuffers), 0}, pad_v{pad_k.at(kStages), 0};
     const Work works{base + F::kWork};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + F::kBars + 8 * F::kNumBars);
     const Again again{reinterpret_cast<uint32_t *>(smem + F::kAgain)};
@@ -114,6 +115,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             ptx::mbar_init(k_empty(s), 1);
             ptx::mbar_init(v_full(s), 1);
             ptx::mbar_init(v_empty(s), 1);
+            ptx::mbar_init(pad_k.at(s), 1);
+            ptx::mbar_init(pad_v.at(s), 1);
         }
         for (int i = 0; i < F::kBuffers; ++i) {
             ptx::mbar_init(s_full(0, i), 1);
@@ -121,7 +124,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             ptx::mbar_init(p_full(i), 4);
         }
         for (int b = 0; b < 2; ++b) ptx::mbar_init(pv_done(b), 1);
-        works.init(10);
+        works.init(11);
         ptx::fence_barrier_init();
     }
     if (warp == 9) {
@@ -138,6 +141,8 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
     Piece pc;
     if (warp >= 8) {
         setmaxnreg_dec<88>();
+        const int padding = padding_from(mask);
+        auto padded = [&](const Span &s) { return s.first + s.end() * kRows > padding; };  // its last tile
         if (warp == 8 && lane == 0) {
             // ---------------- loads
             int n = 0, items = 0, issued_k = 0;
@@ -158,15 +163,17 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                     const int j = s.first + t * kRows;
                     ok = ptx::mbar_wait(k_empty(st), ph ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(k_full(st), F::kTile);
+                    const bool pad = t + 1 == s.end() && padded(s);
+                    const uint32_t to_k = pad ? pad_k.at(st) : k_full(st), to_v = pad ? pad_v.at(st) : v_full(st);
+                    ptx::mbar_arrive_expect_tx(to_k, F::kTile);
                     for (int c = 0; c < kChunks; ++c)
-                        tma_load_3d(base + F::kK + st * F::kTile + c * kChunk, &mK, k_full(st), 64 * c, s.g, j);
+                        tma_load_3d(base + F::kK + st * F::kTile + c * kChunk, &mK, to_k, 64 * c, s.g, j);
                     ++issued_k;
                     ok = ptx::mbar_wait(v_empty(st), ph ^ 1, status);
                     if (!ok) break;
-                    ptx::mbar_arrive_expect_tx(v_full(st), F::kTile);
+                    ptx::mbar_arrive_expect_tx(to_v, F::kTile);
                     for (int c = 0; c < kChunks; ++c)
-                        tma_load_3d(base + F::kV + st * F::kTile + c * kChunk, &mV, v_full(st), 64 * c, s.g, j);
+                        tma_load_3d(base + F::kV + st * F::kTile + c * kChunk, &mV, to_v, 64 * c, s.g, j);
                 }
             }
             // no copy may still be landing in shared memory when the block exits
@@ -252,6 +259,17 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
             if (last) wait_warp(v_empty((last - 1) / 2), (last - 1) & 1, nullptr);
         } else if (warp == 10 && lane == 0) {
             works.hand_out([&](int work) { return fwd_piece(mask, args, work); }, again.any(), status);
+        } else if (warp == 11) {
+            // ---------------- padding
+            int n = 0;
+            for (int w = 0; works.take(pc, w, true, false, lane, status); ++w) {
+                const Span s = as_span(pc);
+                n += s.end();
+                if (s.end() == 0 || !padded(s)) continue;
+                const int st = (n - 1) % kStages, from = padding - (s.first + (s.end() - 1) * kRows);
+                if (!pad_k.clear<DP>(smem + F::kK + st * F::kTile, st, from, k_full(st), lane, status)) break;
+                if (!pad_v.clear<DP>(smem + F::kV + st * F::kTile, st, from, v_full(st), lane, status)) break;
+            }
         }
         __syncwarp();
     } else {
@@ -290,7 +308,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap mQ, const __grid_constant__ CUten
                 as_floats(v, x);
                 if (GENERAL) {
                     uint32_t none[1];
-                    general_scores<128, false>(v, none, args.a.score, slope, (float)(i - j0));
+                    general_scores<128, false>(v, none, args.a.score, slope, (float)(i - j0), rg.lo < rg.hi);
                 }
                 const int lo = rg.lo - j0, hi = rg.hi - j0;
                 if (!__all_sync(0xffffffffu, lo <= 0 && hi >= kRows)) {

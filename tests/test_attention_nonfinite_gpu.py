@@ -82,3 +82,31 @@ def test_nothing_finite():
     q, k, v, d_o = (x.fill_(float("nan")) for x in _inputs(T, 8, 8, d, "bf16"))
     for n, x in zip(NAMES, _run(q, k, v, d_o, [0, T], "bf16")):
         assert torch.isnan(x).all(), n
+
+
+@pytest.mark.parametrize("docs,nq,nkv,d,kw", [
+    ([0, 333, 1290], 4, 4, 64, dict()), ([0, 333, 1290], 16, 2, 128, dict(causal=False)), ([0, 333, 1290], 3, 1, 40, dict(softcap=5.0)),
+    ([0, 333, 1290], 16, 2, 128, dict(softcap=5.0)), ([0, 333, 1290], 16, 2, 128, dict(window=150)),
+    ([70, 129, 1281], 4, 4, 64, dict(causal=False)), ([70, 129, 1281], 16, 2, 128, dict()), ([70, 129, 1281], 3, 1, 40, dict(window=150)),
+    ([70, 129, 1281], 4, 4, 128, dict(prefix=[30, 500])), ([70, 129, 1281], 16, 2, 64, dict(softcap=5.0, causal=False))])
+def test_padding_counts_for_nothing(docs, nq, nkv, d, kw):
+    """What is behind the last document leaves every bit as it is and no row to compute again."""
+    from paper_2603_06492_gb300 import binding
+    T = 1400
+    q, k, v, d_o = _inputs(T, nq, nkv, d, "bf16")
+    first = None
+    for bad in (0.0, float("nan"), float("inf"), 3e38):
+        for x in (q, k, v, d_o):
+            x[docs[-1]:] = bad
+        binding.noble_debug_rows_again()
+        now = _run(q, k, v, d_o, docs, "bf16", **kw)
+        assert binding.noble_debug_rows_again() == 0
+        first = first or now
+        for n, a, b in zip(NAMES, first, now):
+            assert torch.equal(a, b), (n, bad)
+    seen = ref.masks(T, docs, kw.get("causal", True), kw.get("prefix"), kw.get("window", 0))
+    want = ref.attention(q, k, v, seen, 1 / math.sqrt(d), kw.get("softcap", 0.0), None, d_o)
+    for n, a, b in zip(NAMES, first, want):
+        assert torch.equal(torch.isinf(a), torch.isinf(b)), n
+        assert rel_err(torch.where(torch.isinf(a), 0.0, a), torch.where(torch.isinf(b), 0.0, b)) <= (
+            1e-5 if n == "lse" else TOL["bf16"]), n
