@@ -20,6 +20,7 @@ from __future__ import annotations
 import argparse
 import json
 import os
+import re
 import statistics
 import subprocess
 import sys
@@ -49,26 +50,38 @@ WORKLOADS = {
 # DRAM bytes (dram__bytes_read.sum + dram__bytes_write.sum) per launch of the
 # dominant kernel class, mean over the three layers of the 1.5B-scale workload,
 # from one ncu capture.  "sources" is the hash (kernel_sources_hash) of the
-# CUDA sources the capture ran on: when the sources differ, the figure no
+# CUDA sources of the layer the capture ran on: when they differ, the figure no
 # longer describes the kernels and the bench line reports traffic as null.
-TRAFFIC_PER_LAUNCH = {3: {"sources": "b3cee78b47af68fb",
+TRAFFIC_PER_LAUNCH = {3: {"sources": "2661e7328398582f",
                           "capture": "ncu --metrics dram__bytes_read.sum,dram__bytes_write.sum on the backward's grouped "
                                      "GEMM launches of the three layers (python bench.py --profile-run --steps 1 "
                                      "--warmup 0), mean per launch",
-                          "bytes": {"tc_bwd_gemms": 1445.2e6}}}
+                          "bytes": {"tc_bwd_gemms": 1449.0e6}}}
 METRIC = "NOBLE linear fwd+bwd TFLOP/s"
 # dense BF16 tensor-core rate of one sm_100-family SM: 8192 FLOP per clock
 BF16_FLOP_PER_CLK_SM = 8192
 
 
+def kernel_sources() -> list:
+    """The CUDA sources of the layer's kernels: noble_api.cu and what it includes of csrc (the
+    attention operators are a translation unit of their own)."""
+    csrc = os.path.join(ROOT, "paper_2603_06492_gb300", "csrc")
+    found, left = set(), ["noble_api.cu"]
+    while left:
+        name = left.pop()
+        if name in found or not os.path.exists(os.path.join(csrc, name)):
+            continue
+        found.add(name)
+        with open(os.path.join(csrc, name)) as f:
+            left += re.findall(r'^#include "([^"/]+)"', f.read(), re.M)
+    return [os.path.join(csrc, name) for name in sorted(found)]
+
+
 def kernel_sources_hash() -> str:
-    """sha256 (first 16 hex digits) over the CUDA sources and the C header."""
+    """sha256 (first 16 hex digits) over kernel_sources()."""
     import hashlib
     h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2603_06492_gb300", "csrc")
-    files = sorted(os.path.join(csrc, f) for f in os.listdir(csrc) if f.endswith((".cu", ".cuh")))
-    files.append(os.path.join(ROOT, "include", "noble.h"))
-    for f in files:
+    for f in kernel_sources():
         h.update(os.path.basename(f).encode())
         with open(f, "rb") as fh:
             h.update(fh.read())
