@@ -68,7 +68,7 @@ __device__ __forceinline__ Piece fwd_piece(const Mask &m, const FwdArgs &f, int 
     const int first = visible(m, i0).lo;
     int a1 = (max(visible(m, min(i0 + 127, m.T - 1)).hi - first, 0) + kRows - 1) / kRows, b0 = a1, b1 = a1;
     if (i0 + 128 < m.T) {
-        b0 = (visible(m, i0 + 128).lo - first) / kRows;
+        b0 = max(visible(m, i0 + 128).lo - first, 0) / kRows;  // below 0 only if the documents' starts do not ascend
         b1 = (max(visible(m, min(i0 + 255, m.T - 1)).hi - first, 0) + kRows - 1) / kRows;
         if (b1 <= b0) b0 = b1 = a1;
         else a1 = max(a1, b0);

@@ -205,3 +205,27 @@ def test_captured_generation_step(dtype):
         p.o.fill_(float("nan"))
         graph.replay()
         assert torch.equal(p.o, want) and torch.isfinite(want).all()
+
+
+# ---------------------------------------------------------------- a caller's error
+@pytest.mark.parametrize("flags", [0, 2])
+@pytest.mark.parametrize("docs", [[400, 0, 700], [0, 600, 100, 650], [690, 300, 200, 100, 0], [-50, 10 ** 9, 5, 300], [5, 5, 3, 3]])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=40), dict(prefix=[200, -5, 10 ** 6, 7])])
+def test_starts_that_do_not_ascend(docs, kw, flags):
+    """Results are undefined, but calls end without an error of the device and leave the memory around
+    their outputs as it is."""
+    from paper_2603_06492_gb300 import attention as A, binding
+    T, nq, nkv, d = 700, 4, 2, 64
+    kw = dict(kw)
+    prefix = kw.pop("prefix", None)
+    x = [t.cuda() for t in _inputs(T, nq, nkv, d, "bf16")]
+    buf = A.AttnBuffers(T, nq, nkv, d, "bf16", n_docs=len(docs) - 1, flags=flags, **kw)
+    mem = torch.full((4, T + 256, nq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    buf.o, buf.dq, buf.dk, buf.dv = (mem[i, 128:-128, :n] for i, n in enumerate((nq, nq, nkv, nkv)))
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    rest = (ints(docs), None if prefix is None else ints((prefix * 2)[:len(docs) - 1]))
+    A.attn_forward(buf, *x[:3], *rest)
+    A.attn_backward(buf, x[3], *x[:3], *rest)
+    binding.noble_get_device_status(None)
+    binding.noble_debug_rows_again()
+    assert (mem[:, :128] == 7).all() and (mem[:, -128:] == 7).all() and (mem[2:, :, nkv:] == 7).all()
