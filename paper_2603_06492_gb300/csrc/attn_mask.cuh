@@ -368,7 +368,7 @@ __device__ __noinline__ void row_dq(const RowArgs<T> &a, int i, int h, int lane,
 }
 
 // First query whose range ends after key j, and first whose range starts after it:
-// the queries that see j lie between them.
+// the queries that see j are those from one to the other.
 __device__ __forceinline__ Range seen_by(const Mask &m, int j)
 {
     Range out;
@@ -401,8 +401,6 @@ __device__ __noinline__ void row_dkv(const RowArgs<T> &a, int j, int g, int lane
     bool lost = false;
     for (int h = g * group; h < (g + 1) * group; ++h)
         for (int i = r.lo; i < r.hi && !lost; ++i) {
-            const Range s = visible(a.mask, i);
-            if (j < s.lo || j >= s.hi) continue;
             float q[4], d_o[4], p, ds;
             row_load(q, a.q.at(i, h), a.d, lane);
             row_load(d_o, a.d_o.at(i, h), a.d, lane);
