@@ -503,7 +503,12 @@ noble_status noble_kv_append(const noble_rope_desc *desc, const noble_heads *q, 
  * doc_start [n_docs + 1] must ascend within [0, T]; if it does not, results are
  * undefined, but no access leaves the tensors.
  * What a query does not see does not change its results, whatever values are
- * there (infinities and NaN too).
+ * there, infinities and NaN too.  Of padding, the tokens behind the last document,
+ * that holds to the bit.  Other infinities and NaN make the rows that share
+ * a block of 128 tokens with them, and do not see them, be computed again one by
+ * one: in fp32 throughout, so that their last digits may differ, and slowly, about
+ * 1 us per query and key on one warp (64 such keys under 8 query heads of a
+ * 32768-token document take the backward 3.8 s).
  *
  * bf16 runs on the tensor cores, with fp32 scores, softmax and sums; the
  * probabilities and the scores' gradients are rounded to bf16 for their
@@ -550,9 +555,12 @@ noble_status noble_attn_bwd(const noble_attn_desc *desc, const noble_heads *d_o,
  * softcap and slope as in noble_attn_fwd.  Position j of sequence n lies in
  * page page_table[n][j / page_size] of the cache, at place j % page_size.  A
  * token at a negative position sees nothing: o = 0, lse = -inf.
- * Only what some new token of the sequence sees is read from the cache.  A page number outside the cache,
- * or a kv_len beyond max_pages * page_size or max_len, is a caller's error: the
- * keys concerned are left out, and noble_get_device_status() reports it.
+ * Only what some new token of the sequence sees is read from the cache.  A page
+ * number outside the cache, or a kv_len beyond max_pages * page_size or max_len,
+ * is a caller's error: the keys concerned are left out, and
+ * noble_get_device_status() reports it.
+ * Scores, softmax and sums are fp32; of bf16 operands the probabilities are
+ * rounded to bf16 for their product with the values.  fp32 runs in fp32 FMA.
  */
 typedef struct {
     int64_t n_seq;     /* sequences, up to 65535                               */

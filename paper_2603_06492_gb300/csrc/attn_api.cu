@@ -153,8 +153,10 @@ noble_status rope_fwd_launch(const noble_rope_desc *d, rope::Args<T> &a, cudaStr
     a.status = status_ptr();
     if (!a.status) return fail(NOBLE_ERR_CUDA, "status word address");
     // one batch a warp while that leaves SMs idle, else all batches of a token, which then
-    // share its cosines and sines (forward, heads of 128: 24 tokens of 16 + 4 heads 3.0 us one a
-    // warp, 5.0 all; 600 of 16 + 16 4.0 and 6.2; 1024 7.1 and 6.5; 2048 11.5 and 10.1)
+    // share its cosines and sines.  Forward, 16 + 16 heads, us one a warp and all, at 15 (heads of
+    // 64: 13), 26 and 52 batches per SM: heads of 128 bf16 4.0 and 6.3, 7.0 and 6.3, 9.8 and 8.4; fp32
+    // 6.1 and 10.4, 10.4 and 10.5, 18.7 and 16.2; of 64 bf16 3.6 and 4.1, 6.7 and 5.6, 9.1 and 9.6;
+    // fp32 5.9 and 6.4, 10.2 and 9.3, 18.3 and 17.2
     const int all = a.batches_q + (APPEND ? 2 : 1) * a.batches_kv;
     a.take = a.tokens * all <= 24 * kSms ? 1 : all;
     a.groups = (int)ceil_div(all, a.take);
@@ -492,8 +494,9 @@ Split paged_split(const noble_paged_desc *d)
     const int64_t units = d->n_seq * d->n_kv * ceil_div(rows, attn::paged::kRows);
     const int64_t slots = kSms * (d->d <= 64 ? attn::paged::kBlocksPerSm<64> : attn::paged::kBlocksPerSm<128>);
     const int64_t one = ceil_div(max_len * std::max<int64_t>(units, 1), slots);
-    // fp32 is bound by its products, not by reading: pieces enough to balance (24 sequences up
-    // to 1024 tokens, 16 heads of 64: chunks of 384 107 us, of 512 139)
+    // fp32 is not bound by reading: eight blocks per SM, which balances (24 sequences up to 1000
+    // tokens, 16 heads of 64, with 4, 6, 8, 12 and 16 per SM: 106, 83, 73, 72 and 73 us; 16 up to
+    // 8000: 644, 524, 429, 492 and 422; 32 heads on 4 of 128: 314, 220, 224, 261 and 220)
     int64_t chunk = d->dtype == NOBLE_FP32 ? ceil_div(max_len * std::max<int64_t>(units, 1), 8 * kSms)
                     : d->n_seq <= 1        ? one
                                            : std::max(one / 8, std::min<int64_t>(one, 1024));

@@ -1,11 +1,13 @@
 // Attention of a few new tokens per sequence over a paged cache.
 //
-// Bound by reading the cache once.  The query heads that share a key head, and the
-// new tokens of a sequence, are the rows of one block (16 of them), so that a key is
-// read for all of them at once.  The keys of a sequence are split into chunks, a
+// Bound by reading the cache.  The query heads that share a key head, and the new tokens
+// of a sequence, are the rows of one block (16 of them), so that a key is read for all of
+// them at once; each further 16 rows are a block that reads the keys again (16 sequences up to
+// 16380 tokens, 32 heads on 4 of 128, bf16: 1 new token 71 us, 2 76, 4 120, 8 200).  The keys of a sequence are split into chunks, a
 // block each, since a batch alone has too few sequences to load 152 SMs; a second
-// kernel joins the chunks' results by their maxima and sums, in order.  fp32 is bound by its
-// FMAs instead: 24 sequences up to 1024 tokens, 16 heads of 64: 107 us.
+// kernel joins the chunks' results by their maxima and sums, in order.  fp32
+// works out all 16 rows whatever is real and loads nothing during a product: 24 sequences up to
+// 1000 tokens, 16 heads of 64, one row each: 73 us, 1.4 TB/s.
 #pragma once
 
 #include "attn_simt.cuh"

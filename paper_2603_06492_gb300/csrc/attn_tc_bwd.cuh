@@ -1,6 +1,6 @@
 // Backward attention over documents on the tensor cores: two kernels, so that each sum
-// has one block and a fixed order, without atomics or partial sums in memory.  Both form the
-// scores again (seven products of the size of one score block's, where sharing them
+// has one block and a fixed order, without atomics; only dk and dv of few key heads go through
+// fp32 parts in memory, which are added up in order.  Both form the scores again (seven products of the size of one score block's, where sharing them
 // would take five).
 //
 // dq_kernel, 128 queries of a head over the key tiles that they see:
@@ -18,8 +18,8 @@
 //
 // What bounds it: the warps' instructions between the products, then the tensor pipe
 // (16384 tokens, 16 heads of 128, causal: dq 1.10 ms, dk and dv 1.35, 1170 TFLOP/s of five
-// products; heads of 64: 0.73 and 1.01).  Short documents pay per piece as in the forward: 8 of
-// 1024 tokens, 16 heads of 64: 50 and 63 us; 64 of 197, 12 heads: 53 and 67.
+// products; heads of 64: 0.73 and 1.02).  Short documents pay per piece as in the forward: 8 of
+// 1024 tokens, 16 heads of 64: 50 and 63 us; 64 of 197, 12 heads: 53 and 68.
 #pragma once
 
 #include "attn_tc.cuh"

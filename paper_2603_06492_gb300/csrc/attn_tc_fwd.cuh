@@ -14,11 +14,11 @@
 // happens rarely.  Sums and maxima are fp32; P is rounded to bf16 for the product (each
 // to 2^-9 of itself), its sum is that of the unrounded values.
 //
-// What bounds it: with heads of 128 features the tensor pipe (16384 tokens, 16 heads: 1390 us
-// with all seen, 705 causal, 1580 and 1556 TFLOP/s), with 64 the exponentials (1055 us, 1040
+// What bounds it: with heads of 128 features the tensor pipe (16384 tokens, 16 heads: 1383 us
+// with all seen, 700 causal, 1590 and 1571 TFLOP/s), with 64 the exponentials (1007 us, 1092
 // TFLOP/s).  Short documents pay for each piece's start, masked tiles and rows written (8 of 1024
-// tokens, 16 heads of 64: 43 us, 64 of 197, 12 heads: 48), capped scores for their tanh on the
-// FMA pipe (7001 tokens, 16 heads on 4 of 128: 113 us, 71 without a cap).
+// tokens, 16 heads of 64: 41 us, 64 of 197, 12 heads: 46), capped scores for their tanh on the
+// FMA pipe (7001 tokens, 16 heads on 4 of 128: 110 us, 69 without a cap).
 #pragma once
 
 #include "attn_tc.cuh"

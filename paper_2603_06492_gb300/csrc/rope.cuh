@@ -201,7 +201,7 @@ __device__ __forceinline__ void taken(Raw<T> &r, const char *at)
 // A warp: `take` batches of a token, which wait in shared memory: what is on its way costs no
 // registers there.  Bound by reading and
 // writing with the latency of what comes first (position, then its cosines): 16384 tokens of
-// 16 + 16 heads of 128 features 55 us, 4.9 TB/s; a batch ahead in registers 63.
+// 16 + 16 heads of 128 features 57 us, 4.7 TB/s (a batch ahead in registers 63); fp32 118, 4.6.
 template <typename T> constexpr int kFwdRing = sizeof(T) == 2 ? 4 : 3;    // batches
 template <typename T> constexpr int kFwdBlocks = sizeof(T) == 2 ? 3 : 2;  // of an SM
 template <typename T> constexpr uint32_t kFwdBytes = kWarps * kFwdRing<T> * kPasses * 256 * sizeof(T);
