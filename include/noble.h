@@ -581,6 +581,122 @@ noble_status noble_attn_paged(const noble_paged_desc *desc, const noble_heads *q
                               void *workspace, size_t workspace_bytes, noble_stream stream);
 
 /*
+ * Around the projections of a training step
+ * -----------------------------------------
+ * What a model of NOBLE layers and attention takes besides them: the table that turns
+ * tokens into rows, the norm in front of each projection, and, beside noble_adamw_step, the
+ * optimizer step for matrices by orthogonalised momentum.  The conventions above hold.
+ * Results repeat bit for bit.  A workspace belongs to one call at a time: calls that share
+ * one, captured graphs included, must be ordered by the caller.
+ */
+
+/*
+ * Layer norm of rows, with the residual stream in front of it.
+ *     s = x + res, rounded to the operand type    (res optional: s = x)
+ *     y = (s - mean(s)) rstd gain + bias,  rstd = 1 / sqrt(var(s) + eps)
+ * with mean and variance (the mean square of s - mean(s)) over the d elements of a row, in
+ * fp32.  gain, bias [d] fp32 (NULL: ones, zeros).  `sum` receives s where res is given and
+ * is not written otherwise.  stats [T][2] fp32 receives mean and rstd, which the backward
+ * pass reads (NULL to skip: inference).  sum may be x or res, and y may be x or res, but
+ * sum and y differ; otherwise outputs do not overlap inputs.
+ */
+typedef struct {
+    int64_t T;      /* rows, up to 2^31 - 1                                    */
+    int64_t d;      /* elements of a row: a multiple of 8, 8 to 16384          */
+    float eps;      /* >= 0                                                    */
+    int32_t dtype;  /* noble_dtype of x, res, s, y and their gradients         */
+    uint32_t flags; /* 0                                                       */
+} noble_norm_desc;
+noble_status noble_norm_fwd(const noble_norm_desc *desc, const void *x, const void *res, const float *gain,
+                            const float *bias, void *sum, void *y, float *stats, noble_stream stream);
+
+/*
+ * Backward: with n = (s - mean) rstd and w = dy gain,
+ *     dx = rstd (w - mean(w) - n mean(w n)) + dstream
+ *     dgain = sum over rows of dy n,  dbias = sum over rows of dy
+ * s is what the forward normed (its `sum`, or x), stats what it wrote.  dstream [T][d]
+ * (NULL: zero) is the gradient that reaches s by the residual stream; dx is then the gradient
+ * of x and of res alike.  dx may be dy or dstream.  dgain, dbias [d] fp32, NULL to skip; they
+ * are added up in a fixed order.
+ */
+size_t noble_norm_bwd_workspace_bytes(const noble_norm_desc *desc);
+noble_status noble_norm_bwd(const noble_norm_desc *desc, const void *dy, const void *s, const float *stats,
+                            const float *gain, const void *dstream, void *dx, float *dgain, float *dbias,
+                            void *workspace, size_t workspace_bytes, noble_stream stream);
+
+/*
+ * Embedding: y[t] = scale table[ids[t]], rounded once.  A negative token is padding: its row
+ * of y is 0, and it has no part in the gradient.  A token from vocab on is a caller's
+ * error: treated as padding, and noble_get_device_status() reports it (NOBLE_ERR_CUDA).
+ */
+typedef struct {
+    int64_t T;      /* tokens, up to 2^24                                      */
+    int64_t vocab;  /* rows of the table, 1 to 2^28                            */
+    int64_t d;      /* elements of a row: a multiple of 8, 8 to 65536          */
+    float scale;    /* finite                                                  */
+    int32_t dtype;  /* noble_dtype of table, y and dy                          */
+    uint32_t flags; /* 0                                                       */
+} noble_embed_desc;
+noble_status noble_embed_fwd(const noble_embed_desc *desc, const int32_t *ids /* [T] */,
+                             const void *table /* [vocab][d] */, void *y /* [T][d] */, noble_stream stream);
+
+/*
+ * The table's gradient, dtable[v] = scale * (sum of dy[t] over the tokens t with ids[t] = v), fp32
+ * throughout and in an order that only the tokens set.  Every row of dtable [vocab][d] is
+ * written, rows without tokens as 0.
+ */
+size_t noble_embed_bwd_workspace_bytes(const noble_embed_desc *desc);
+noble_status noble_embed_bwd(const noble_embed_desc *desc, const int32_t *ids, const void *dy, float *dtable,
+                             void *workspace, size_t workspace_bytes, noble_stream stream);
+
+/*
+ * Optimizer step by orthogonalised momentum (Muon), for matrices, beside noble_adamw_step
+ * for everything else.  For each tensor [rows][cols], with a = lr * lr_mult:
+ *     m <- momentum m + g
+ *     u = g + momentum m  (NOBLE_MUON_NESTEROV), else u = m
+ *     X = u / (|u|_F + eps)
+ *     `steps` times:  A = X X^T,  X <- 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ *     p <- p - a weight_decay p                             (only if `decay`)
+ *     p <- p - a sqrt(max(1, rows / cols)) X
+ * (with more rows than columns, the same on the transpose).  Five steps bring the singular values
+ * of u, but for those that are next to nothing beside |u|_F, near 1.
+ *
+ * Products take fp16 operands, scaled, with fp32 sums: X is off by about 1e-3 of its norm
+ * when u's singular values are of one order, more when they decay fast (1e-2 over six orders).
+ * With NOBLE_MUON_PRECISE operands have 22 bits, in pairs of fp16: three times the
+ * products, and 1e-6 of the norm in place of 1e-3.  Matrices of up to 256 rows or columns
+ * always have them.  Everything else is fp32, the norm fp64.
+ *
+ * `param_bf16` (optional) receives the new parameters and `update` (optional) X, in bf16.  With
+ * `update` alone (param NULL) a data-parallel job whose ranks share out the matrices exchanges
+ * X and applies it itself.  A tensor whose u is 0 gets X = 0; one whose u is not finite gets
+ * NaN, and no other does.  No memory that is written may belong to two tensors, or to a grad.
+ * Which tensors share a call may change the last bits of the results.
+ */
+#define NOBLE_MUON_NESTEROV 1u
+#define NOBLE_MUON_PRECISE 2u
+typedef struct {
+    float *param;      /* fp32, updated in place; NULL: only `update` is wanted */
+    void *param_bf16;  /* optional                                              */
+    const float *grad; /* fp32                                                  */
+    float *momentum;   /* fp32, updated in place                                */
+    void *update;      /* optional, bf16                                        */
+    int64_t rows, cols; /* 0 to 65536; empty tensors are skipped                */
+    float lr_mult;
+    int32_t decay;     /* 1: apply weight decay to this tensor                  */
+} noble_muon_tensor;
+
+typedef struct {
+    float lr, momentum, weight_decay, eps; /* momentum in [0, 1), the others >= 0 */
+    int32_t steps;                         /* 0 to 16, usually 5                  */
+    uint32_t flags;                        /* NOBLE_MUON_* bits                   */
+} noble_muon_hparams;
+
+size_t noble_muon_workspace_bytes(const noble_muon_tensor *tensors, int n_tensors, uint32_t flags);
+noble_status noble_muon_step(const noble_muon_tensor *tensors, int n_tensors, const noble_muon_hparams *hp,
+                             void *workspace, size_t workspace_bytes, noble_stream stream);
+
+/*
  * Synchronises `stream`, then reads and clears the device status word of the
  * current device.  NOBLE_ERR_TIMEOUT if any kernel gave up a bounded wait
  * since the last call, NOBLE_ERR_CUDA if the stream reported an error or a

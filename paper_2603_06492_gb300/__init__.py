@@ -5,4 +5,4 @@ The compute path is the C-ABI library ``libnoble.so`` built from ``csrc/``
 Importing this package does not load the library; ``binding.load()`` does and
 raises if it is missing.
 """
-__all__ = ["attention", "binding", "inputs", "build"]
+__all__ = ["attention", "binding", "inputs", "layers", "build"]

@@ -118,6 +118,29 @@ class PagedDesc(ctypes.Structure):
         ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "d")] + [
+        ("eps", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class EmbedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("T", "vocab", "d")] + [
+        ("scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class MuonTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "param_bf16", "grad", "momentum", "update")] + [
+        ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("lr_mult", ctypes.c_float), ("decay", ctypes.c_int32)]
+
+
+class MuonHparams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("lr", "momentum", "weight_decay", "eps")] + [
+        ("steps", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+NOBLE_MUON_NESTEROV, NOBLE_MUON_PRECISE = 1, 2
+
+
 def make_desc(T, d_in, d_out, r, dtype, flags=0) -> Desc:
     if isinstance(dtype, str):
         dtype = {"bf16": NOBLE_BF16, "fp32": NOBLE_FP32}[dtype]
@@ -213,6 +236,20 @@ def load(path: str | None = None) -> ctypes.CDLL:
             getattr(lib, "noble_" + n).restype = ctypes.c_int
         for n in ("rope_bwd", "attn_bwd", "attn_paged"):
             getattr(lib, "noble_" + n + "_workspace_bytes").restype = S
+        # around the projections of a training step (layers.py, noble_muon_step)
+        ND, ED, MT = (ctypes.POINTER(t) for t in (NormDesc, EmbedDesc, MuonTensor))
+        lib.noble_norm_fwd.argtypes = [ND] + [P] * 8
+        lib.noble_norm_bwd_workspace_bytes.argtypes = [ND]
+        lib.noble_norm_bwd.argtypes = [ND] + [P] * 9 + [S, P]
+        lib.noble_embed_fwd.argtypes = [ED] + [P] * 4
+        lib.noble_embed_bwd_workspace_bytes.argtypes = [ED]
+        lib.noble_embed_bwd.argtypes = [ED] + [P] * 4 + [S, P]
+        lib.noble_muon_workspace_bytes.argtypes = [MT, ci, ctypes.c_uint32]
+        lib.noble_muon_step.argtypes = [MT, ci, ctypes.POINTER(MuonHparams), P, S, P]
+        for n in ("norm_fwd", "norm_bwd", "embed_fwd", "embed_bwd", "muon_step"):
+            getattr(lib, "noble_" + n).restype = ctypes.c_int
+        for n in ("norm_bwd_workspace_bytes", "embed_bwd_workspace_bytes", "muon_workspace_bytes"):
+            getattr(lib, "noble_" + n).restype = S
         _lib = lib
         return lib
 
@@ -326,6 +363,51 @@ def noble_adamw_step(tensors, lr, beta1=0.9, beta2=0.98, eps=1e-8, weight_decay=
                                  _p(t["exp_avg_sq"]), n, float(t.get("lr_mult", 1.0)), int(t.get("decay", True)))
     hp = AdamwHparams(lr, beta1, beta2, eps, weight_decay, step)
     _check(load().noble_adamw_step(arr, len(tensors), ctypes.byref(hp), stream))
+
+
+def _muon_array(tensors):
+    arr = (MuonTensor * max(1, len(tensors)))()
+    for i, t in enumerate(tensors):
+        g = t["grad"]
+        if g.dim() != 2:
+            raise ValueError(f"tensor {i}: a matrix is needed, got {list(g.shape)}")
+        for name, dtype in _MUON_TYPES:
+            x = t.get(name)
+            if x is not None and (x.shape != g.shape or str(x.dtype) != dtype or x.device != g.device or not x.is_cuda or
+                                  not x.is_contiguous()):
+                raise ValueError(f"tensor {i}, {name}: expected a contiguous {dtype} CUDA tensor {list(g.shape)} on {g.device}, "
+                                 f"got {x.dtype} {list(x.shape)} on {x.device}")
+        arr[i] = MuonTensor(_p(t.get("param")), _p(t.get("param_bf16")), _p(g), _p(t["momentum"]), _p(t.get("update")),
+                            g.shape[0], g.shape[1], float(t.get("lr_mult", 1.0)), int(t.get("decay", True)))
+    return arr
+
+
+_MUON_TYPES = (("param", "torch.float32"), ("param_bf16", "torch.bfloat16"), ("grad", "torch.float32"),
+               ("momentum", "torch.float32"), ("update", "torch.bfloat16"))
+
+
+def muon_workspace(tensors, precise=False):
+    """Workspace (torch) of noble_muon_step on tensors of these shapes; ``precise`` as there."""
+    import torch
+    n = load().noble_muon_workspace_bytes(_muon_array(tensors), len(tensors), NOBLE_MUON_PRECISE if precise else 0)
+    if n == 0:
+        raise NobleError(3, "matrices of more than 65536 rows or columns")
+    return torch.empty(n, dtype=torch.uint8, device=tensors[0]["grad"].device if tensors else "cuda")
+
+
+def noble_muon_step(tensors, lr, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, eps=1e-7, precise=False,
+                    workspace=None, stream=None):
+    """One optimizer step by orthogonalised momentum.  ``tensors``: dicts with grad and
+    momentum, and param (with optional param_bf16) or update or both -- contiguous device
+    matrices of one shape, fp32 but for param_bf16 and update in bf16 --, optional lr_mult
+    (default 1) and decay (default True).  ``workspace``: of muon_workspace; a new one if None."""
+    arr = _muon_array(tensors)
+    if workspace is None:
+        workspace = muon_workspace(tensors, precise)
+    hp = MuonHparams(lr, momentum, weight_decay, eps, steps,
+                     (NOBLE_MUON_NESTEROV if nesterov else 0) | (NOBLE_MUON_PRECISE if precise else 0))
+    _check(load().noble_muon_step(arr, len(tensors), ctypes.byref(hp), _p(workspace), workspace.numel(),
+                                  _stream_handle(stream)))
 
 
 def noble_linear_lr_multipliers(desc, gamma=0.3, gamma_M=0.45, omega_mult=3.0, phi_mult=5.0):

@@ -1,0 +1,285 @@
+// Layer norm of rows, with the residual stream in front of it, and its gradients.
+//
+//   s = x + res (rounded to the stream's type), mean and r = 1 / sqrt(var + eps) of s,
+//   y = (s - mean) r gain + bias
+//   dx = r (w - mean(w) - n mean(w n)) + dstream,   n = (s - mean) r,  w = dy gain
+//   dgain = sum over rows of dy n,   dbias = sum over rows of dy
+//
+// A row stays in the registers of the threads that read it: the variance is the mean square
+// of what is left after the mean, and no row is read twice.
+#pragma once
+
+#include "cluster.cuh"
+#include "sums.cuh"
+
+namespace noble {
+namespace norm {
+
+constexpr int kThreads = 256;  // of a block, unless a row takes more
+constexpr int kMaxVecs = 4;    // 16-byte pieces of a row that a thread of the forward holds
+
+// 16 bytes of operands as floats and back
+template <typename T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int n = 8;
+    static __device__ __forceinline__ void unpack(const uint4 &q, float (&f)[8])
+    {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(w[i] << 16), f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&f)[8])
+    {
+        return make_uint4(ptx::pack_bf16x2(f[0], f[1]), ptx::pack_bf16x2(f[2], f[3]), ptx::pack_bf16x2(f[4], f[5]),
+                          ptx::pack_bf16x2(f[6], f[7]));
+    }
+};
+template <> struct Vec<float> {
+    static constexpr int n = 4;
+    static __device__ __forceinline__ void unpack(const uint4 &q, float (&f)[4])
+    {
+        f[0] = __uint_as_float(q.x), f[1] = __uint_as_float(q.y), f[2] = __uint_as_float(q.z), f[3] = __uint_as_float(q.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&f)[4])
+    {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+
+template <int N>
+__device__ __forceinline__ void load_floats(const float *p, int64_t at, float (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        const float4 q = reinterpret_cast<const float4 *>(p + at)[i];
+        f[4 * i] = q.x, f[4 * i + 1] = q.y, f[4 * i + 2] = q.z, f[4 * i + 3] = q.w;
+    }
+}
+
+// Sums of N values each over the threads of a row, `warps` of them from a multiple of it on:
+// every thread gets them.  sm: N floats for each warp of the block.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int warps, float *sm)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    if (warps == 1) return;
+    const int warp = threadIdx.x / 32, first = warp / warps * warps;
+    if (threadIdx.x % 32 == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sm[warp * N + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += sm[(first + w) * N + i];
+}
+
+template <typename T>
+struct FwdArgs {
+    const T *x, *res;
+    const float *gain, *bias;
+    T *sum, *y;
+    float2 *stats;
+    int64_t rows;
+    int d, warps;  // warps: of a row
+    float inv_d, eps;
+};
+
+template <typename T, int NV, bool RES>
+__global__ void __launch_bounds__(1024) fwd_kernel(const FwdArgs<T> a)
+{
+    constexpr int V = Vec<T>::n;
+    __shared__ float sm[2][32];
+    const int per_row = a.warps * 32, lane = threadIdx.x % per_row;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / per_row) + threadIdx.x / per_row;
+    const int vecs = row < a.rows ? a.d / V : 0;
+    const int64_t base = row * a.d;
+    uint4 q[NV];
+    float f[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = i * per_row + lane;
+        q[i] = make_uint4(0, 0, 0, 0);
+        if (at < vecs) q[i] = reinterpret_cast<const uint4 *>(a.x + base)[at];
+    }
+    if constexpr (RES) {
+        uint4 p[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * per_row + lane;
+            p[i] = make_uint4(0, 0, 0, 0);
+            if (at < vecs) p[i] = reinterpret_cast<const uint4 *>(a.res + base)[at];
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float g[V];
+            Vec<T>::unpack(q[i], f[i]);
+            Vec<T>::unpack(p[i], g);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[i][j] += g[j];
+            q[i] = Vec<T>::pack(f[i]);
+        }
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        Vec<T>::unpack(q[i], f[i]);  // the stream as it is stored
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[0] += f[i][j];
+    }
+    row_sums(s, a.warps, sm[0]);
+    const float mean = s[0] * a.inv_d;
+    s[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i * per_row + lane < vecs)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                f[i][j] -= mean;
+                s[0] = fmaf(f[i][j], f[i][j], s[0]);
+            }
+    row_sums(s, a.warps, sm[1]);
+    const float r = 1.f / sqrtf(fmaf(s[0], a.inv_d, a.eps));
+    if (a.stats && vecs && lane == 0) a.stats[row] = make_float2(mean, r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = i * per_row + lane;
+        if (at < vecs) {
+            float g[V], b[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) g[j] = 1.f, b[j] = 0.f;
+            if (a.gain) load_floats(a.gain, at * V, g);
+            if (a.bias) load_floats(a.bias, at * V, b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[i][j] = fmaf(f[i][j] * r, g[j], b[j]);
+            if (RES) reinterpret_cast<uint4 *>(a.sum + base)[at] = q[i];
+            reinterpret_cast<uint4 *>(a.y + base)[at] = Vec<T>::pack(f[i]);
+        }
+    }
+}
+
+template <typename T>
+struct BwdArgs {
+    const T *dy, *s, *dstream;
+    const float2 *stats;
+    const float *gain;
+    T *dx;
+    float *part;  // [parts][2][d], or NULL: no gradients of gain and bias
+    int64_t rows;
+    int d, warps, rows_per_part;
+    float inv_d;
+};
+
+// Block p takes the rows of part p, `groups` of them at a time; a thread has the same columns
+// of every row, whose sums for dgain and dbias it keeps in registers and the block then adds
+// up in order of the groups.
+template <typename T, int NV, bool STREAM>
+__global__ void __launch_bounds__(1024) bwd_kernel(const BwdArgs<T> a)
+{
+    constexpr int V = Vec<T>::n;
+    extern __shared__ float cols[];  // [groups][2][d] for the sums over rows
+    __shared__ float sm[2][64];
+    const int per_row = a.warps * 32, lane = threadIdx.x % per_row, group = threadIdx.x / per_row,
+              groups = blockDim.x / per_row;
+    const int vecs = a.d / V;
+    float dg[NV][V], db[NV][V], g[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f, g[i][j] = 1.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (a.gain && i * per_row + lane < vecs) load_floats(a.gain, (i * per_row + lane) * V, g[i]);
+    const int64_t first = (int64_t)blockIdx.x * a.rows_per_part;
+    const int rows = (int)min((int64_t)a.rows_per_part, a.rows - first);
+    int turn = 0;
+    for (int k = 0; k < rows; k += groups, turn ^= 1) {
+        const bool in = k + group < rows;
+        const int64_t row = first + k + group, base = row * a.d;
+        float2 st = make_float2(0.f, 0.f);
+        if (in) st = a.stats[row];
+        uint4 qy[NV], qs[NV], qd[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * per_row + lane;
+            qy[i] = qs[i] = qd[i] = make_uint4(0, 0, 0, 0);
+            if (in && at < vecs) {
+                qy[i] = reinterpret_cast<const uint4 *>(a.dy + base)[at];
+                qs[i] = reinterpret_cast<const uint4 *>(a.s + base)[at];
+                if (STREAM) qd[i] = reinterpret_cast<const uint4 *>(a.dstream + base)[at];
+            }
+        }
+        float t[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (!in || i * per_row + lane >= vecs) continue;
+            float y[V], n[V];
+            Vec<T>::unpack(qy[i], y);
+            Vec<T>::unpack(qs[i], n);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                n[j] = (n[j] - st.x) * st.y;
+                dg[i][j] = fmaf(y[j], n[j], dg[i][j]);
+                db[i][j] += y[j];
+                const float w = y[j] * g[i][j];
+                t[0] += w;
+                t[1] = fmaf(w, n[j], t[1]);
+            }
+        }
+        row_sums(t, a.warps, sm[turn]);
+        const float mw = t[0] * a.inv_d, mwn = t[1] * a.inv_d;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * per_row + lane;
+            if (!in || at >= vecs) continue;
+            float y[V], n[V], e[V];
+            Vec<T>::unpack(qy[i], y);
+            Vec<T>::unpack(qs[i], n);
+            Vec<T>::unpack(qd[i], e);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                n[j] = (n[j] - st.x) * st.y;
+                y[j] = st.y * (fmaf(y[j], g[i][j], -mw) - n[j] * mwn);
+                if (STREAM) y[j] += e[j];
+            }
+            reinterpret_cast<uint4 *>(a.dx + base)[at] = Vec<T>::pack(y);
+        }
+    }
+    if (!a.part) return;
+    float *out = a.part + (int64_t)blockIdx.x * 2 * a.d;
+    if (groups == 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * per_row + lane < vecs)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    out[(i * per_row + lane) * V + j] = dg[i][j];
+                    out[a.d + (i * per_row + lane) * V + j] = db[i][j];
+                }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i * per_row + lane < vecs)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                cols[group * 2 * a.d + (i * per_row + lane) * V + j] = dg[i][j];
+                cols[group * 2 * a.d + a.d + (i * per_row + lane) * V + j] = db[i][j];
+            }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
+        float v = 0.f;
+        for (int k = 0; k < groups; ++k) v += cols[k * 2 * a.d + c];
+        out[c] = v;
+    }
+}
+
+// dgain and dbias from the parts, in order
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SplitJobs J) { sum_block(J, blockIdx.x); }
+
+}  // namespace norm
+}  // namespace noble
