@@ -50,6 +50,8 @@ struct Batch {
     int n;
     float momentum, eps;
     int nesterov;
+    uint32_t *counts;   // of the products (muon_gemm.cuh), set to zero
+    int ncounts;
 };
 
 constexpr int kMomentBlocks = 304;  // of a matrix, at most: two per SM
@@ -132,6 +134,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batc
     __shared__ float inv[2];  // 1 / norm as a power of two and the rest: fp32 need not hold it
     const Matrix &M = b.t[tile_matrix(b, blockIdx.x)];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < b.ncounts; i += gridDim.x * 256) b.counts[i] = 0;
     // the norm, the same in every block
     double s = 0.0;
     for (int i = threadIdx.x; i < M.nsums; i += 256) s += M.sums[i];
@@ -203,62 +206,6 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Batc
             if (M.param_bf16) M.param_bf16[e] = __float2bfloat16_rn(p);
         }
     }
-}
-
-// ---------------------------------------------------------------- products
-// C = alpha A B^T (+ beta D on the same places, + diag on the diagonal); B [K][N] if b_mn.
-// Low parts (NULL: none) count as A + A_lo.
-struct Product {
-    const __half *a, *a_lo, *b, *b_lo, *d, *d_lo;
-    __half *c, *c_lo;
-    int m, n, k, lda, ldb, ldc, ldd;
-    float alpha, beta, diag;
-    int b_mn;
-    int tile_begin, tiles_n;
-};
-struct Products {
-    Product p[kMost];
-    int n;
-};
-
-__global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ Products g)
-{
-    constexpr int kT = 64, kK = 16;
-    __shared__ float sa[kK][kT + 4], sb[kK][kT + 4];
-    int j = 0;
-    while (j + 1 < g.n && (int)blockIdx.x >= g.p[j + 1].tile_begin) ++j;
-    const Product &P = g.p[j];
-    const int at = blockIdx.x - P.tile_begin, m0 = at / P.tiles_n * kT, n0 = at % P.tiles_n * kT;
-    auto value = [](const __half *p, const __half *lo, int64_t e) { return __half2float(p[e]) + (lo ? __half2float(lo[e]) : 0.f); };
-    const int tr = threadIdx.x / 16 * 4, tc = threadIdx.x % 16 * 4;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < P.k; k0 += kK) {
-        for (int i = threadIdx.x; i < kT * kK; i += 256) {
-            const int r = i / kK, k = i % kK;
-            const bool in = k0 + k < P.k;
-            sa[k][r] = in && m0 + r < P.m ? value(P.a, P.a_lo, (int64_t)(m0 + r) * P.lda + k0 + k) : 0.f;
-            sb[k][r] = in && n0 + r < P.n ? value(P.b, P.b_lo, P.b_mn ? (int64_t)(k0 + k) * P.ldb + n0 + r : (int64_t)(n0 + r) * P.ldb + k0 + k) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kK; ++k)
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) acc[x][y] = fmaf(sa[k][tr + x], sb[k][tc + y], acc[x][y]);
-        __syncthreads();
-    }
-    for (int x = 0; x < 4; ++x)
-        for (int y = 0; y < 4; ++y) {
-            const int r = m0 + tr + x, c = n0 + tc + y;
-            if (r >= P.m || c >= P.n) continue;
-            float v = P.alpha * acc[x][y];
-            if (P.d) v = fmaf(P.beta, value(P.d, P.d_lo, (int64_t)r * P.ldd + c), v);
-            if (r == c) v += P.diag;
-            const __half h = __float2half_rn(v);
-            P.c[(int64_t)r * P.ldc + c] = h;
-            if (P.c_lo) P.c_lo[(int64_t)r * P.ldc + c] = __float2half_rn(v - __half2float(h));
-        }
 }
 
 }  // namespace muon

@@ -7,7 +7,7 @@
 
 #include "host.cuh"
 #include "embed.cuh"
-#include "muon.cuh"
+#include "muon_gemm.cuh"
 #include "norm.cuh"
 
 namespace noble {
@@ -255,57 +255,200 @@ noble_status check_apart(const noble_muon_tensor *t, int n)
     return NOBLE_OK;
 }
 
-// Workspace of one launch's matrices: X twice, A and B (each with its low parts if precise),
-// partial sums.
-struct MuonLayout {
-    size_t x[2], a, b, sums, total;
-};
-int64_t muon_ld(int64_t cols) { return (int64_t)align_up((size_t)cols, 8); }
 // Small matrices cost launches, not products, and the error of a small X is not averaged.
 bool muon_precise(const noble_muon_tensor &t, uint32_t flags)
 {
     return (flags & NOBLE_MUON_PRECISE) != 0 || std::min(t.rows, t.cols) <= 256;
 }
-MuonLayout muon_layout(const noble_muon_tensor &t, bool precise, size_t at)
+int64_t muon_ld(int64_t cols) { return (int64_t)align_up((size_t)cols, 8); }
+
+// The three products of a step, in this order: A = X X^T, B = a I + b A + c A A, X <- B X.
+enum { kGram, kPoly, kNext, kPhases };
+
+// A group of up to kMost matrices: their places in the workspace, and how each product is cut
+// into units.  The shapes decide, so that results are the same on every device.
+struct MuonPlan {
+    int n;
+    int pick[muon::kMost];
+    struct {
+        size_t x[2], a, b, sums;
+    } at[muon::kMost];
+    size_t counts, part, total;
+    int ncounts;
+    muon::mma::Problem p[kPhases][muon::kMost];  // sizes only
+    int order[kPhases][muon::kMost];             // place in the launch -> matrix
+    int units[kPhases];
+};
+
+// Tiles of a problem with tiles of bn columns.
+int muon_tiles(const muon::mma::Problem &p, int bn)
 {
-    MuonLayout w{};
+    const int tm = (int)ceil_div(p.m, muon::mma::kRows), tn = (int)ceil_div(p.n, bn);
+    return p.sym ? muon::mma::sym_tiles_before(tm, tn, muon::mma::kRows / bn) : tm * tn;
+}
+// Time of a unit in k-blocks of a tile of 256 columns: a tile of 128 takes 0.6 of one per
+// k-block, and 8 pass between a unit's last k-block and what waits for it.
+double muon_cost(int kb, int bn, int nsplit) { return kb * (bn == 256 ? 1.0 : 0.6) + (bn == 256 ? 8 : 5) + (nsplit > 1 ? 4 + nsplit : 0); }
+
+// Columns of tiles and splits of K for the problems of a launch, by the time of the busiest pair.
+void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
+{
+    using namespace muon::mma;
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) tiles += muon_tiles(p[i], 256);
+    double best = 1e300;
+    Problem kept[muon::kMost];
+    int kept_order[muon::kMost], kept_units = 0;
+    for (int bn : {256, 128}) {
+        for (int most = 1 << 20; most >= 4; most = most > 1024 ? 1024 : most * 3 / 4) {  // k-blocks of a unit
+            int total = 0;
+            for (int i = 0; i < n; ++i) {
+                Problem &q = p[i];
+                const int kb = q.kb * q.segs;
+                q.bn = q.n <= 128 ? 128 : bn;
+                q.tiles_m = (int)ceil_div(q.m, kRows), q.tiles_n = (int)ceil_div(q.n, q.bn);
+                const int splits = (int)std::min<int64_t>(kMostSplits, ceil_div(kb, most));
+                q.kb_per_split = (int)ceil_div(kb, splits);
+                q.nsplit = (int)ceil_div(kb, q.kb_per_split);
+                order[i] = i;
+            }
+            std::stable_sort(order, order + n, [&](int a, int b) {
+                return muon_cost(p[a].kb_per_split, p[a].bn, p[a].nsplit) > muon_cost(p[b].kb_per_split, p[b].bn, p[b].nsplit);
+            });
+            double load[kPairs] = {}, longest = 0.0;
+            bool split = false;
+            for (int k = 0; k < n; ++k) {
+                Problem &q = p[order[k]];
+                q.unit_begin = total;
+                split |= q.nsplit > 1;
+                const int count = muon_tiles(q, q.bn) * q.nsplit;
+                const double cost = muon_cost(q.kb_per_split, q.bn, q.nsplit);
+                for (int c = 0; c < kPairs; ++c) {  // units total + c, total + c + kPairs, ...
+                    double &l = load[(total + c) % kPairs];
+                    if (c < count) l += cost * ((count - c - 1) / kPairs + 1);
+                    longest = std::max(longest, l);
+                }
+                total += count;
+            }
+            if (longest < best) {
+                best = longest;
+                std::copy(p, p + n, kept), std::copy(order, order + n, kept_order);
+                kept_units = total;
+            }
+            if (tiles >= 8 * kPairs) break;  // splits gain nothing
+        }
+    }
+    std::copy(kept, kept + n, p), std::copy(kept_order, kept_order + n, order);
+    *units = kept_units;
+}
+
+// Takes the next matrices that are not empty, from *next on.
+MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
+{
+    MuonPlan w{};
+    for (; *next < n && w.n < muon::kMost; ++*next)
+        if (t[*next].rows * t[*next].cols > 0) w.pick[w.n++] = *next;
     auto take = [&](size_t bytes) {
-        const size_t p = at;
-        at = align_up(at + bytes, 256);
+        const size_t p = w.total;
+        w.total = align_up(w.total + bytes, 256);
         return p;
     };
-    const size_t m = (size_t)std::min(t.rows, t.cols), k = (size_t)std::max(t.rows, t.cols), e = precise ? 4 : 2;
-    for (size_t &x : w.x) x = take(m * (size_t)muon_ld((int64_t)k) * e);
-    w.a = take(m * (size_t)muon_ld((int64_t)m) * e);
-    w.b = take(m * (size_t)muon_ld((int64_t)m) * e);
-    w.sums = take(muon::kMomentBlocks * sizeof(double));
-    w.total = at;
+    for (int i = 0; i < w.n; ++i) {
+        const noble_muon_tensor &s = t[w.pick[i]];
+        const bool precise = muon_precise(s, flags);
+        const int m = (int)std::min(s.rows, s.cols), k = (int)std::max(s.rows, s.cols);
+        const size_t e = precise ? 4 : 2;
+        for (size_t &x : w.at[i].x) x = take((size_t)m * (size_t)muon_ld(k) * e);
+        w.at[i].a = take((size_t)m * (size_t)muon_ld(m) * e);
+        w.at[i].b = take((size_t)m * (size_t)muon_ld(m) * e);
+        w.at[i].sums = take(muon::kMomentBlocks * sizeof(double));
+        for (int j = 0; j < kPhases; ++j) {
+            muon::mma::Problem &p = w.p[j][i];
+            p.m = m, p.n = j == kNext ? k : m;
+            p.kb = (int)ceil_div(j == kGram ? k : m, muon::mma::kBK);
+            p.segs = precise ? 3 : 1, p.pairs = precise;
+            p.sym = j != kNext, p.b_mn = j == kNext;
+        }
+    }
+    size_t part = 0;
+    for (int j = 0; j < kPhases; ++j) {
+        muon_cut(w.p[j], w.order[j], w.n, &w.units[j]);
+        size_t bytes = 0;
+        int counts = 0;
+        for (int i = 0; i < w.n; ++i) {
+            muon::mma::Problem &p = w.p[j][i];
+            if (p.nsplit == 1) continue;
+            const size_t tiles = (size_t)muon_tiles(p, p.bn);
+            bytes += tiles * p.nsplit * muon::mma::kRows * p.bn * 4;
+            counts += (int)tiles * 16;
+        }
+        part = std::max(part, bytes), w.ncounts = std::max(w.ncounts, counts);
+    }
+    w.counts = take((size_t)w.ncounts * 4);
+    w.part = take(part);
     return w;
 }
 
-// The matrices of the next launch: up to kMost that are not empty, from *next on.
-int muon_group(const noble_muon_tensor *t, int n, int *next, int (&pick)[muon::kMost])
+// TMA map of an fp16 matrix: boxes of `cols` by `rows`, with the swizzle of that width.
+noble_status make_half_map(CUtensorMap *m, const __half *p, int rows, int cols, int64_t ld, uint32_t box_cols, uint32_t box_rows)
 {
-    int got = 0;
-    for (; *next < n && got < muon::kMost; ++*next)
-        if (t[*next].rows * t[*next].cols > 0) pick[got++] = *next;
-    return got;
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[2] = {box_cols, box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half *>(p), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS)
+        return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d): rows=%d cols=%d ld=%lld", (int)r, rows, cols, (long long)ld);
+    return NOBLE_OK;
 }
 
-noble_status muon_run(const noble_muon_tensor *t, const int *pick, int n, const noble_muon_hparams *hp, char *ws, cudaStream_t st)
+// A matrix of the iteration: its high parts, and low parts behind them or NULL.
+struct HalfMatrix {
+    __half *hi, *lo;
+    int rows, cols;
+    int64_t ld;
+    noble_status maps(CUtensorMap *m, uint32_t box_cols, uint32_t box_rows) const
+    {
+        NOBLE_TRY(make_half_map(m, hi, rows, cols, ld, box_cols, box_rows));
+        return make_half_map(m + 1, lo ? lo : hi, rows, cols, ld, box_cols, box_rows);
+    }
+};
+
+noble_status muon_product(const muon::mma::Args &g, double flops, cudaStream_t st)
 {
+    using muon::mma::Smem;
+    static std::atomic<CUcontext> allowed{nullptr};
+    const CUcontext ctx = current_context();
+    if (!ctx || allowed.load(std::memory_order_relaxed) != ctx) {
+        if (cudaFuncSetAttribute(muon::mma::product_pairs, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem::kDynamic) != cudaSuccess)
+            return fail(NOBLE_ERR_CUDA, "shared memory: %s", cudaGetErrorString(cudaGetLastError()));
+        allowed.store(current_context(), std::memory_order_relaxed);
+    }
+    // each pair takes units of its own: no pair waits for another, so that they need not all be resident
+    const int pairs = std::min({g.units, muon::mma::kPairs, std::max(1, num_sms() / 2)});
+    const bool pdl = pdl_ok();
+    return run(st, {"muon_product", kBoundTensor, flops, 0.0}, [&] {
+        launch_maybe_pdl(muon::mma::product_pairs, dim3(2 * (unsigned)pairs), dim3(tc::pair::kPairThreads), Smem::kDynamic, st, pdl, g);
+    });
+}
+
+noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble_muon_hparams *hp, char *ws, cudaStream_t st)
+{
+    using muon::mma::Args;
     muon::Batch b{};
-    b.n = n, b.momentum = hp->momentum, b.eps = hp->eps, b.nesterov = (hp->flags & NOBLE_MUON_NESTEROV) != 0;
-    muon::Products pa{}, pb{}, px[2];
-    size_t at = 0;
+    b.n = w.n, b.momentum = hp->momentum, b.eps = hp->eps, b.nesterov = (hp->flags & NOBLE_MUON_NESTEROV) != 0;
+    b.counts = reinterpret_cast<uint32_t *>(ws + w.counts), b.ncounts = w.ncounts;
+    HalfMatrix X[2][muon::kMost], A[muon::kMost], B[muon::kMost];
     int tiles = 0, blocks = 0;
     double bytes = 0.0;
-    for (int i = 0; i < n; ++i) {
-        const noble_muon_tensor &s = t[pick[i]];
+    for (int i = 0; i < w.n; ++i) {
+        const noble_muon_tensor &s = t[w.pick[i]];
         muon::Matrix &M = b.t[i];
-        const bool precise = muon_precise(s, hp->flags);
-        const MuonLayout w = muon_layout(s, precise, at);
-        at = w.total;
+        const bool precise = w.p[kGram][i].pairs != 0;
         M.param = s.param, M.param_bf16 = static_cast<bf *>(s.param_bf16), M.update = static_cast<bf *>(s.update);
         M.grad = s.grad, M.mom = s.momentum;
         M.n = s.rows * s.cols, M.rows = (int)s.rows, M.cols = (int)s.cols;
@@ -314,53 +457,76 @@ noble_status muon_run(const noble_muon_tensor *t, const int *pick, int n, const 
         const float lr = hp->lr * s.lr_mult;
         M.lr = lr * std::sqrt(std::max(1.f, (float)M.rows / (float)M.cols));
         M.decay = s.decay ? lr * hp->weight_decay : 0.f;
-        M.sums = reinterpret_cast<double *>(ws + w.sums);
+        M.sums = reinterpret_cast<double *>(ws + w.at[i].sums);
         M.nsums = (int)std::min<int64_t>(muon::kMomentBlocks, ceil_div(M.n, 4096));
         M.tile_begin = tiles, M.tiles_c = (int)ceil_div(M.cols, 64);
         tiles += (int)ceil_div(M.rows, 64) * M.tiles_c;
         blocks = std::max(blocks, M.nsums);
         bytes += (double)M.n * (12 + (s.update ? 2 : 0) + (s.param ? 8 : 0) + (s.param_bf16 ? 2 : 0));
-
-        const int lda = (int)muon_ld(M.m);
-        auto half = [&](size_t off) { return reinterpret_cast<__half *>(ws + off); };
-        auto low = [&](size_t off, int64_t ld) { return precise ? half(off) + (int64_t)M.m * ld : nullptr; };
-        M.x = half(w.x[0]), M.x_lo = low(w.x[0], M.ld);
-        M.o = half(w.x[hp->steps % 2]), M.o_lo = low(w.x[hp->steps % 2], M.ld);
-        __half *A = half(w.a), *Al = low(w.a, lda), *B = half(w.b), *Bl = low(w.b, lda);
-        for (int h = 0; h < 2; ++h) {
-            __half *X = half(w.x[h]), *Xl = low(w.x[h], M.ld), *Y = half(w.x[!h]), *Yl = low(w.x[!h], M.ld);
-            // X <- B X from this half of the pair into the other
-            px[h].p[i] = {B, Bl, X, Xl, nullptr, nullptr, Y, Yl, M.m, M.k, M.m, lda, M.ld, M.ld, 0, 1.f / muon::kScaleB, 0.f, 0.f, 1, 0, 0};
-        }
-        pa.p[i] = {M.x, M.x_lo, M.x, M.x_lo, nullptr, nullptr, A, Al, M.m, M.m, M.k, M.ld, M.ld, lda, 0,
-                   muon::kScaleA / (muon::kScaleX * muon::kScaleX), 0.f, 0.f, 0, 0, 0};
-        pb.p[i] = {A, Al, A, Al, A, Al, B, Bl, M.m, M.m, M.m, lda, lda, lda, lda,
-                   muon::kC * muon::kScaleB / (muon::kScaleA * muon::kScaleA), muon::kB * muon::kScaleB / muon::kScaleA,
-                   muon::kA * muon::kScaleB, 0, 0, 0};
+        auto matrix = [&](size_t off, int cols) {
+            const int64_t ld = muon_ld(cols);
+            __half *p = reinterpret_cast<__half *>(ws + off);
+            return HalfMatrix{p, precise ? p + M.m * ld : nullptr, M.m, cols, ld};
+        };
+        for (int h = 0; h < 2; ++h) X[h][i] = matrix(w.at[i].x[h], M.k);
+        A[i] = matrix(w.at[i].a, M.m), B[i] = matrix(w.at[i].b, M.m);
+        M.x = X[0][i].hi, M.x_lo = X[0][i].lo;
+        M.o = X[hp->steps % 2][i].hi, M.o_lo = X[hp->steps % 2][i].lo;
     }
-    auto count = [&](muon::Products &g) {
-        int total = 0;
-        g.n = n;
-        for (int i = 0; i < n; ++i) {
-            g.p[i].tile_begin = total, g.p[i].tiles_n = (int)ceil_div(g.p[i].n, 64);
-            total += (int)ceil_div(g.p[i].m, 64) * g.p[i].tiles_n;
+    // a product's arguments: what it multiplies, what it writes
+    double flops[kPhases] = {};
+    auto arguments = [&](Args &g, int phase, int half) -> noble_status {
+        g.n = w.n, g.units = w.units[phase];
+        NOBLE_TRY(get_status(&g.status));
+        size_t part = w.part;
+        uint32_t *count = b.counts;
+        flops[phase] = 0.0;
+        for (int k = 0; k < w.n; ++k) {
+            const int i = w.order[phase][k];
+            muon::mma::Problem &p = g.p[k];
+            CUtensorMap *m = g.map[k];
+            p = w.p[phase][i];
+            const uint32_t wide = 64, rows = (uint32_t)p.bn / 2;
+            if (phase == kGram) {
+                NOBLE_TRY(X[half][i].maps(m, wide, 128));
+                NOBLE_TRY(X[half][i].maps(m + 2, wide, rows));
+                NOBLE_TRY(A[i].maps(m + 4, 32, 32));
+                p.alpha = muon::kScaleA / (muon::kScaleX * muon::kScaleX);
+            } else if (phase == kPoly) {
+                NOBLE_TRY(A[i].maps(m, wide, 128));
+                NOBLE_TRY(A[i].maps(m + 2, wide, rows));
+                NOBLE_TRY(B[i].maps(m + 4, 32, 32));
+                p.alpha = muon::kC * muon::kScaleB / (muon::kScaleA * muon::kScaleA);
+                p.beta = muon::kB * muon::kScaleB / muon::kScaleA, p.diag = muon::kA * muon::kScaleB;
+                p.d = A[i].hi, p.d_lo = A[i].lo, p.ldd = (int)A[i].ld;
+            } else {
+                NOBLE_TRY(B[i].maps(m, wide, 128));
+                NOBLE_TRY(X[half][i].maps(m + 2, wide, 64));
+                NOBLE_TRY(X[!half][i].maps(m + 4, 32, 32));
+                p.alpha = 1.f / muon::kScaleB;
+            }
+            flops[phase] += 2.0 * p.m * p.n * (phase == kGram ? b.t[i].k : p.m) * (p.sym ? 0.5 : 1.0);
+            if (p.nsplit > 1) {
+                const int n = muon_tiles(p, p.bn);
+                p.part = reinterpret_cast<float *>(ws + part), p.count = count;
+                part += (size_t)n * p.nsplit * muon::mma::kRows * p.bn * 4;
+                count += n * 16;
+            }
         }
-        return total;
+        return NOBLE_OK;
     };
-    const int ta = count(pa), tb = count(pb), tx = count(px[0]);
-    count(px[1]);
-    const KernelInfo hbm{"muon_elementwise", kBoundHbm, 0.0, bytes / 3}, mma{"muon_product", kBoundTensor, 0.0, 0.0};
-    NOBLE_TRY(run(st, hbm, [&] { muon::momentum_kernel<<<dim3((unsigned)blocks, (unsigned)n), 256, 0, st>>>(b); }));
+    const KernelInfo hbm{"muon_elementwise", kBoundHbm, 0.0, bytes / 3};
+    NOBLE_TRY(run(st, hbm, [&] { muon::momentum_kernel<<<dim3((unsigned)blocks, (unsigned)w.n), 256, 0, st>>>(b); }));
     NOBLE_TRY(run(st, hbm, [&] { muon::scale_kernel<<<(unsigned)tiles, 256, 0, st>>>(b); }));
+    Args gram[2] = {}, poly = {}, next[2] = {};
     for (int k = 0; k < hp->steps; ++k) {
         const int h = k % 2;
-        for (int i = 0; i < n; ++i) {
-            pa.p[i].a = pa.p[i].b = px[h].p[i].b;
-            pa.p[i].a_lo = pa.p[i].b_lo = px[h].p[i].b_lo;
-        }
-        NOBLE_TRY(run(st, mma, [&] { muon::product_kernel<<<(unsigned)ta, 256, 0, st>>>(pa); }));
-        NOBLE_TRY(run(st, mma, [&] { muon::product_kernel<<<(unsigned)tb, 256, 0, st>>>(pb); }));
-        NOBLE_TRY(run(st, mma, [&] { muon::product_kernel<<<(unsigned)tx, 256, 0, st>>>(px[h]); }));
+        if (k < 2) NOBLE_TRY(arguments(gram[h], kGram, h));
+        NOBLE_TRY(muon_product(gram[h], flops[kGram], st));
+        if (k == 0) NOBLE_TRY(arguments(poly, kPoly, 0));
+        NOBLE_TRY(muon_product(poly, flops[kPoly], st));
+        if (k < 2) NOBLE_TRY(arguments(next[h], kNext, h));
+        NOBLE_TRY(muon_product(next[h], flops[kNext], st));
     }
     return run(st, hbm, [&] { muon::apply_kernel<<<(unsigned)tiles, 256, 0, st>>>(b); });
 }
@@ -476,13 +642,7 @@ size_t noble_muon_workspace_bytes(const noble_muon_tensor *tensors, int n_tensor
 {
     if (validate_muon(tensors, n_tensors, flags) != NOBLE_OK) return 0;
     size_t most = 256;
-    int pick[muon::kMost];
-    for (int next = 0; next < n_tensors;) {
-        size_t at = 0;
-        const int n = muon_group(tensors, n_tensors, &next, pick);
-        for (int i = 0; i < n; ++i) at = muon_layout(tensors[pick[i]], muon_precise(tensors[pick[i]], flags), at).total;
-        most = std::max(most, at);
-    }
+    for (int next = 0; next < n_tensors;) most = std::max(most, muon_plan(tensors, n_tensors, &next, flags).total);
     return most;
 }
 
@@ -512,12 +672,20 @@ noble_status noble_muon_step(const noble_muon_tensor *tensors, int n_tensors, co
     }
     NOBLE_TRY(check_apart(tensors, n_tensors));
     if (!work) return NOBLE_OK;
-    NOBLE_TRY(check_workspace(workspace, workspace_bytes, noble_muon_workspace_bytes(tensors, n_tensors, hp->flags)));
+    // all groups' plans fit before anything is enqueued; a single group's is kept
+    MuonPlan plan{};
+    int next = 0;
+    size_t need = 256;
+    while (next < n_tensors) {
+        plan = muon_plan(tensors, n_tensors, &next, hp->flags);
+        need = std::max(need, plan.total);
+    }
+    NOBLE_TRY(check_workspace(workspace, workspace_bytes, need));
     NOBLE_TRY(check_device());
-    int pick[muon::kMost];
-    for (int next = 0; next < n_tensors;) {
-        const int n = muon_group(tensors, n_tensors, &next, pick);
-        if (n) NOBLE_TRY(muon_run(tensors, pick, n, hp, static_cast<char *>(workspace), (cudaStream_t)stream));
+    if (n_tensors <= muon::kMost) return muon_run(tensors, plan, hp, static_cast<char *>(workspace), (cudaStream_t)stream);
+    for (next = 0; next < n_tensors;) {
+        const MuonPlan w = muon_plan(tensors, n_tensors, &next, hp->flags);
+        if (w.n) NOBLE_TRY(muon_run(tensors, w, hp, static_cast<char *>(workspace), (cudaStream_t)stream));
     }
     return NOBLE_OK;
 }
