@@ -36,10 +36,11 @@ struct Matrix {
     float *mom;
     int64_t n;          // elements
     int rows, cols;
-    int m, k, ld;       // of X: rows (the smaller side), columns, elements between rows
+    int m, k, ld, m8;   // of X: rows (the smaller side), columns, elements between rows, rows with padding
     int tall;           // X is the transpose
     float lr, decay;    // lr sqrt(max(1, rows / cols)), lr weight_decay
     __half *x, *x_lo;   // X as the iteration begins; x_lo: low parts (precise)
+    __half *x_other, *x_other_lo;  // its other place
     const __half *o, *o_lo;  // ... and ends
     double *sums;       // partial sums of squares of u
     int nsums;
@@ -126,7 +127,66 @@ __device__ __forceinline__ int tile_matrix(const Batch &b, int tile)
     return j;
 }
 
-// X = u / (|u| + eps) in fp16, a 64 x 64 tile of u per block.
+// Eight elements of a row, of which the first `n` are there; `wide`: 16-byte accesses are aligned.
+__device__ __forceinline__ void load8(const float *p, int n, bool wide, float (&f)[8])
+{
+    if (wide && n >= 8) {
+        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+        f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? p[i] : 0.f;
+    }
+}
+__device__ __forceinline__ void store8(float *p, int n, bool wide, const float (&f)[8])
+{
+    if (wide && n >= 8) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = f[i];
+    }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, int n, bool wide, const float (&f)[8])
+{
+    if (wide && n >= 8) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(ptx::pack_bf16x2(f[0], f[1]), ptx::pack_bf16x2(f[2], f[3]),
+                                                   ptx::pack_bf16x2(f[4], f[5]), ptx::pack_bf16x2(f[6], f[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = __float2bfloat16_rn(f[i]);
+    }
+}
+// Rows of X and of the like are padded to whole groups of eight.
+__device__ __forceinline__ void store_halves(__half *p, float (&f)[8])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+        const float2 r = __half22float2(h);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        f[2 * i] -= r.x, f[2 * i + 1] -= r.y;  // what is left
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void add_halves(const __half *p, float (&f)[8])
+{
+    const uint4 q = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 r = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+        f[2 * i] += r.x, f[2 * i + 1] += r.y;
+    }
+}
+
+// X = u / (|u| + eps) in fp16, a 64 x 64 tile of u per block: 512 groups of eight, two per thread.
+// Rows that pad X to a multiple of eight are zero in both of its places, as the products
+// read them (times zeros).
 __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batch b)
 {
     __shared__ float tile[64][65];
@@ -134,7 +194,25 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batc
     __shared__ float inv[2];  // 1 / norm as a power of two and the rest: fp32 need not hold it
     const Matrix &M = b.t[tile_matrix(b, blockIdx.x)];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int at = blockIdx.x - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
+    const bool wide = M.cols % 4 == 0;
+    float g[2][8], u[2][8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int r = r0 + 32 * k + threadIdx.x / 8, c = c0 + threadIdx.x % 8 * 8, n = r < M.rows ? M.cols - c : 0;
+        const int64_t e = (int64_t)r * M.cols + c;
+        load8(M.mom + e, n, wide, u[k]);
+        if (b.nesterov) load8(M.grad + e, n, wide, g[k]);
+    }
     for (int i = blockIdx.x * 256 + threadIdx.x; i < b.ncounts; i += gridDim.x * 256) b.counts[i] = 0;
+    if (at == 0) {
+        const int pad = (M.m8 - M.m) * M.ld;
+        for (int i = threadIdx.x; i < pad; i += 256) {
+            const int64_t e = (int64_t)M.m * M.ld + i;
+            M.x[e] = M.x_other[e] = __ushort_as_half(0);
+            if (M.x_lo) M.x_lo[e] = M.x_other_lo[e] = __ushort_as_half(0);
+        }
+    }
     // the norm, the same in every block
     double s = 0.0;
     for (int i = threadIdx.x; i < M.nsums; i += 256) s += M.sums[i];
@@ -151,26 +229,30 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batc
         inv[0] = ldexpf(1.f, e);
         inv[1] = (float)ldexp(f, -e);
     }
-    const int at = blockIdx.x - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
-    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-        const int r = r0 + i / 64, c = c0 + i % 64;
-        float u = 0.f;
-        if (r < M.rows && c < M.cols) {
-            const int64_t e = (int64_t)r * M.cols + c;
-            u = blend(b, b.nesterov ? M.grad[e] : 0.f, M.mom[e]);
-        }
-        tile[i / 64][i % 64] = u;
-    }
     __syncthreads();
-    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-        const int r = i / 64, c = i % 64;  // of X
-        const float u = (M.tall ? tile[c][r] : tile[r][c]) * inv[0] * inv[1];
-        const int xr = (M.tall ? c0 : r0) + r, xc = (M.tall ? r0 : c0) + c;
-        if (xr < M.m && xc < M.k) {
-            const __half h = __float2half_rn(u);
-            M.x[(int64_t)xr * M.ld + xc] = h;
-            if (M.x_lo) M.x_lo[(int64_t)xr * M.ld + xc] = __float2half_rn(u - __half2float(h));
+    const float i0 = inv[0], i1 = inv[1];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            u[k][i] = (b.nesterov ? blend(b, g[k][i], u[k][i]) : u[k][i]) * i0 * i1;
+            if (M.tall) tile[r][c + i] = u[k][i];
         }
+    }
+    if (M.tall) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        // of X: row, column within the tile
+        const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+        if (M.tall)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[k][i] = tile[c + i][r];
+        const int xr = (M.tall ? c0 : r0) + r, xc = (M.tall ? r0 : c0) + c;
+        if (xr >= M.m || xc >= M.k) continue;
+        const int64_t e = (int64_t)xr * M.ld + xc;
+        store_halves(M.x + e, u[k]);
+        if (M.x_lo) store_halves(M.x_lo + e, u[k]);
     }
 }
 
@@ -180,31 +262,42 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Batc
     __shared__ float tile[64][65];
     const Matrix &M = b.t[tile_matrix(b, blockIdx.x)];
     const int at = blockIdx.x - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
-    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-        const int r = i / 64, c = i % 64;  // of X
+    const bool wide = M.cols % 4 == 0, wide_bf16 = M.cols % 8 == 0;
+    float o[2][8], p[2][8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+        if (M.param) {
+            const int n = r0 + r < M.rows ? M.cols - c0 - c : 0;
+            load8(M.param + (int64_t)(r0 + r) * M.cols + c0 + c, n, wide, p[k]);
+        }
         const int xr = (M.tall ? c0 : r0) + r, xc = (M.tall ? r0 : c0) + c;
-        float o = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[k][i] = 0.f;
         if (xr < M.m && xc < M.k) {
             const int64_t e = (int64_t)xr * M.ld + xc;
-            o = __half2float(M.o[e]);
-            if (M.o_lo) o += __half2float(M.o_lo[e]);
+            add_halves(M.o + e, o[k]);
+            if (M.o_lo) add_halves(M.o_lo + e, o[k]);
         }
-        if (M.tall) tile[c][r] = o;
-        else tile[r][c] = o;
+        if (M.tall)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tile[c + i][r] = o[k][i];
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-        const int r = r0 + i / 64, c = c0 + i % 64;
-        if (r >= M.rows || c >= M.cols) continue;
-        const int64_t e = (int64_t)r * M.cols + c;
-        const float o = tile[i / 64][i % 64] * (1.f / kScaleX);
-        if (M.update) M.update[e] = __float2bfloat16_rn(o);
-        if (M.param) {
-            float p = M.param[e];
-            p = fmaf(-M.lr, o, fmaf(-M.decay, p, p));
-            M.param[e] = p;
-            if (M.param_bf16) M.param_bf16[e] = __float2bfloat16_rn(p);
-        }
+    if (M.tall) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+        const int n = r0 + r < M.rows ? M.cols - c0 - c : 0;
+        if (n <= 0) continue;
+        const int64_t e = (int64_t)(r0 + r) * M.cols + c0 + c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[k][i] = (M.tall ? tile[r][c + i] : o[k][i]) * (1.f / kScaleX);
+        if (M.update) store8(M.update + e, n, wide_bf16, o[k]);
+        if (!M.param) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[k][i] = fmaf(-M.lr, o[k][i], fmaf(-M.decay, p[k][i], p[k][i]));
+        store8(M.param + e, n, wide, p[k]);
+        if (M.param_bf16) store8(M.param_bf16 + e, n, wide_bf16, p[k]);
     }
 }
 

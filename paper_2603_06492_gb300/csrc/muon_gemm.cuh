@@ -12,8 +12,9 @@
 //  - A and A A are symmetric: tiles that lie below the diagonal are not computed, the others
 //    are also stored transposed.  (2048 x 8192: 72 units in place of 128 for X X^T.)
 //  - A product of few tiles and long K is split along K.  Each warp stores its part of the
-//    accumulator; the last of a tile's splits to arrive, known by a counter, adds all of them
-//    up in order, so that no sum depends on who is last, and nobody waits.
+//    accumulator, 32 columns at a time; the last of a tile's splits to arrive there, known by a
+//    counter, adds all of them up in order, so that no sum depends on who is last, and
+//    nobody waits.
 #pragma once
 
 #include "muon.cuh"
@@ -25,7 +26,9 @@ namespace mma {
 
 constexpr int kRows = 256;  // of a tile: 128 in each CTA of the pair
 constexpr int kBK = 64;
-constexpr int kStages = 6;
+// Bytes of operands in flight hide the latency of L2: six stages of tiles of 256 columns, or eight
+// of 128 (2048 x 2048 by itself, 72 units of 32 k-blocks: 8.5 us a unit with six).
+constexpr int kStagesWide = 6, kStagesNarrow = 8;
 constexpr int kPairs = 76;  // of a GB300; a constant, as the splits set the order of sums
 constexpr int kMostSplits = 16;
 
@@ -39,20 +42,24 @@ struct Problem {
     int unit_begin;    // first of the launch: unit = tile * nsplit + split
     float alpha, beta, diag;
     const __half *d, *d_lo;
-    int ldd;
+    int ldd;           // elements between rows of D, a multiple of 8
     int pairs;         // C has low parts
     float *part;       // [unit][256][bn] as the warps hold them
-    uint32_t *count;   // [tile][2 CTAs][8 warps], zero before and after
+    uint32_t *count;   // [tile][2 CTAs][8 warps][4 chunks], zero before and after
 };
+// N: matrices at most; a launch's arguments are copied to the GPU, so that few take less.
+template <int N>
 struct Args {
-    CUtensorMap map[kMost][6];  // P, P low, Q, Q low, C, C low
-    Problem p[kMost];
+    CUtensorMap map[N][6];  // P, P low, Q, Q low, C, C low
+    Problem p[N];
     int n, units;
     uint32_t *status;
 };
 
+template <bool WIDE>
 struct Smem {
-    static constexpr uint32_t kA = 128 * kBK * 2, kStage = 2 * kA;
+    static constexpr int kStages = WIDE ? kStagesWide : kStagesNarrow;
+    static constexpr uint32_t kA = 128 * kBK * 2, kStage = kA + (WIDE ? 128 : 64) * kBK * 2;
     static constexpr uint32_t kStgOff = kStages * kStage;  // 4 KB per epilogue warp
     static constexpr uint32_t kBarOff = kStgOff + 8 * 4096;
     static constexpr uint32_t kNumBars = 2 * kStages + 5;  // full, empty, tfull[2], tempty[2], done
@@ -70,7 +77,8 @@ struct Unit {
 // First tile of row block mp of a symmetric C: those before it keep at or above the diagonal.
 __host__ __device__ inline int sym_tiles_before(int mp, int tiles_n, int per) { return mp * tiles_n - per * (mp * (mp - 1) / 2); }
 
-__device__ __forceinline__ Unit locate(const Args &g, int u)
+template <int N>
+__device__ __forceinline__ Unit locate(const Args<N> &g, int u)
 {
     int j = 0;
 #pragma unroll 1
@@ -116,9 +124,14 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThreads, 1) product_pairs(const __grid_constant__ Args g)
+// WIDE: some tiles have 256 columns.
+template <int N, bool WIDE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThreads, 1)
+product_pairs(const __grid_constant__ Args<N> g)
 {
     using namespace tc;
+    using Smem = mma::Smem<WIDE>;
+    constexpr int kStages = Smem::kStages;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = ptx::smem_u32(smem_raw);
     const uint32_t sbase = (raw + 1023u) & ~1023u;
@@ -138,6 +151,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThrea
 
     if (warp == 0 && lane == 0) {
         ptx::griddep_launch();
+        for (int i = 0; i < 6; ++i) ptx::tma_prefetch_desc(&g.map[locate(g, first).prob][i]);
         for (int s = 0; s < kStages; ++s) {
             ptx::mbar_init(full_bar(s), 1);
             ptx::mbar_init(empty_bar(s), 1);
@@ -186,7 +200,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThrea
                     const int k = kb * kBK;
                     pair::tma_load_2d_pair(sA, mP, fb, k, m0);
                     if (b_mn)
-                        for (int c = 0; c < bh / 64; ++c) pair::tma_load_2d_pair(sB + c * tc::kChunkBytes, mQ, fb, n0 + 64 * c, k);
+                        pair::tma_load_4d_pair(sB, mQ, fb, n0 / 64, k / 8);
                     else
                         pair::tma_load_2d_pair(sB, mQ, fb, k, n0);
                     if (++kb == kb_of_seg) kb = 0, ++seg;
@@ -213,9 +227,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThrea
                 const bool b_mn = P.b_mn != 0;
                 const uint32_t idesc = idesc_f16(kRows, P.bn, b_mn);
                 const uint64_t a0 = ptx::smem_desc_sw128(sbase, 16, 1024);
-                const uint64_t b0 = b_mn ? ptx::smem_desc_sw128(sbase + Smem::kA, tc::kChunkBytes, 1024)
+                const uint32_t nch = (uint32_t)P.bn / 128;  // chunks of 64 columns in a CTA
+                const uint64_t b0 = b_mn ? ptx::smem_desc_sw128(sbase + Smem::kA, 1024, 1024 * nch)
                                          : ptx::smem_desc_sw128(sbase + Smem::kA, 16, 1024);
-                const uint32_t stepB = b_mn ? 128u : 2u;
+                const uint32_t stepB = b_mn ? 128u * nch : 2u;
                 const int nkb = t.kb_end - t.kb_begin, b = acc & 1;
                 if (!ptx::mbar_wait(tempty_bar(b), ((uint32_t)(acc >> 1) & 1u) ^ 1u, status)) break;
                 ptx::tc_fence_after();
@@ -265,105 +280,133 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThrea
             const Unit t = locate(g, u);
             const Problem &P = g.p[t.prob];
             const int b = acc & 1;
+            const int row0 = t.m0 + 128 * (int)rank + 32 * quarter, chunks = P.bn / 64, row = row0 + lane;
+            const bool rows_in = row0 < P.m, lows = P.pairs != 0;
+            // chunk c in the order of this split: each ends with another one, so that not one of them
+            // is the last for all
+            auto chunk = [&](int i) { return (i + t.split) & (chunks - 1); };
+            auto column = [&](int c) { return t.n0 + 32 * half + 64 * c; };
+            // D of a chunk, on its way a chunk ahead
+            uint4 d[4], dl[4];
+            auto fetch = [&](int i) {
+                const int col0 = column(chunk(i));
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    d[q] = dl[q] = make_uint4(0, 0, 0, 0);
+                    if (P.d && i < chunks && row < P.m && col0 + 8 * q < P.n) {
+                        const int64_t e = (int64_t)row * P.ldd + col0 + 8 * q;
+                        d[q] = __ldcg(reinterpret_cast<const uint4 *>(P.d + e));
+                        if (lows) dl[q] = __ldcg(reinterpret_cast<const uint4 *>(P.d_lo + e));
+                    }
+                }
+            };
+            fetch(0);
             bool ok = ptx::mbar_wait(tfull_bar(b), (uint32_t)(acc >> 1) & 1u, g.status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             ptx::tc_fence_after();
-            const uint32_t lane_addr = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16);
-            const int row0 = t.m0 + 128 * (int)rank + 32 * quarter, chunks = P.bn / 64;
-            auto hand_back = [&] {
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) cluster::mbar_arrive(b ? leader_tempty1 : leader_tempty0);
-            };
-            const bool rows_in = row0 < P.m;
-            const float *part = nullptr;
+            const uint32_t lane_addr = tmem + b * 256 + ((uint32_t)(quarter * 32) << 16) + 32 * half;
+            // parts[tile][split][CTA][warp][chunk][column][lane]
             const int64_t split_stride = (int64_t)kRows * P.bn;
-            if (P.nsplit > 1) {
-                // parts[tile][split][CTA][warp][chunk][column][lane]
-                float *mine = P.part + (int64_t)t.tile * P.nsplit * split_stride + ((int)rank * 8 + w8) * chunks * 1024 + lane;
-                part = mine;
-                mine += t.split * split_stride;
-                if (rows_in)
-                    for (int c = 0; c < chunks; ++c) {
-                        if (t.n0 + 32 * half + 64 * c >= P.n) break;
-                        float v[32];
-                        ptx::tmem_ld_32x32b_x32(lane_addr + 32 * half + 64 * c, v);
+            float *parts = P.part + (int64_t)t.tile * P.nsplit * split_stride + ((int)rank * 8 + w8) * chunks * 1024 + lane;
+            uint32_t *count = P.count + ((t.tile * 2 + (int)rank) * 8 + w8) * 4;
+            const bool split = P.nsplit > 1;
+            if (split && rows_in) {
+                for (int c = 0; c < chunks && column(c) < P.n; ++c) {
+                    float v[32];
+                    ptx::tmem_ld_32x32b_x32(lane_addr + 64 * c, v);
+                    float *mine = parts + t.split * split_stride + c * 1024;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) __stcg(mine + c * 1024 + 32 * i, v[i]);
-                    }
-                hand_back();
-                uint32_t got = 0;
-                uint32_t *count = P.count + (t.tile * 2 + (int)rank) * 8 + w8;
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) got = atomicAdd(count, 1u);
-                got = __shfl_sync(0xffffffffu, got, 0);
-                if (got != (uint32_t)P.nsplit - 1) continue;
-                if (lane == 0) *count = 0;
+                    for (int j = 0; j < 32; ++j) __stcg(mine + 32 * j, v[j]);
+                }
                 __threadfence();
             }
-            const int row = row0 + lane;
-            for (int c = 0; rows_in && c < chunks; ++c) {
-                const int col0 = t.n0 + 32 * half + 64 * c;
-                if (col0 >= P.n) break;
+            for (int i = 0; rows_in && i < chunks; ++i) {
+                const int c = chunk(i), col0 = column(c);
+                if (col0 >= P.n) {
+                    fetch(i + 1);
+                    continue;
+                }
+                if (split) {
+                    uint32_t got = 0;
+                    __syncwarp();
+                    if (lane == 0) got = atomicAdd(count + c, 1u);
+                    got = __shfl_sync(0xffffffffu, got, 0);
+                    if (got != (uint32_t)P.nsplit - 1) {
+                        fetch(i + 1);
+                        continue;
+                    }
+                    if (lane == 0) count[c] = 0;
+                    __threadfence();
+                }
+                __syncwarp();  // TMEM loads take the whole warp
                 float v[32];
-                if (part) {
-                    const float *p = part + c * 1024;
+                if (split) {
+                    // all parts in order, three on their way at first, then two
+                    const float *p = parts + c * 1024;
+                    auto part = [&](int z, float (&w)[32]) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __ldcg(p + 32 * i);
-                    for (int z = 1; z < P.nsplit; ++z) {
-                        p += split_stride;
-                        float w[32];
+                        for (int j = 0; j < 32; ++j) w[j] = z < P.nsplit ? __ldcg(p + z * split_stride + 32 * j) : 0.f;
+                    };
+                    part(0, v);
+#pragma unroll 1
+                    for (int z = 1; z < P.nsplit; z += 2) {
+                        float w[2][32];
+                        part(z, w[0]);
+                        part(z + 1, w[1]);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) w[i] = __ldcg(p + 32 * i);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] += w[i];
+                        for (int j = 0; j < 32; ++j) v[j] = v[j] + w[0][j] + w[1][j];
                     }
                 } else {
-                    ptx::tmem_ld_32x32b_x32(lane_addr + 32 * half + 64 * c, v);
+                    ptx::tmem_ld_32x32b_x32(lane_addr + 64 * c, v);
                 }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] *= P.alpha;
-                if (P.d && row < P.m) {
+                for (int j = 0; j < 32; ++j) v[j] *= P.alpha;
+                if (P.d) {
+                    auto add = [&](const uint4 &x, int q) {
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (col0 + 8 * q >= P.n) break;
-                        const int64_t e = (int64_t)row * P.ldd + col0 + 8 * q;
-                        auto add = [&](const uint4 &x) {
-                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[j]));
+                            v[8 * q + 2 * j] = fmaf(P.beta, f.x, v[8 * q + 2 * j]);
+                            v[8 * q + 2 * j + 1] = fmaf(P.beta, f.y, v[8 * q + 2 * j + 1]);
+                        }
+                    };
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-                                v[8 * q + 2 * i] = fmaf(P.beta, f.x, v[8 * q + 2 * i]);
-                                v[8 * q + 2 * i + 1] = fmaf(P.beta, f.y, v[8 * q + 2 * i + 1]);
-                            }
-                        };
-                        add(*reinterpret_cast<const uint4 *>(P.d + e));
-                        if (P.d_lo) add(*reinterpret_cast<const uint4 *>(P.d_lo + e));
-                    }
+                    for (int q = 0; q < 4; ++q) add(d[q], q);
+                    if (lows)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) add(dl[q], q);
                 }
+                fetch(i + 1);
                 if (P.diag != 0.f && row >= col0 && row < col0 + 32) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (row == col0 + i) v[i] += P.diag;
+                    for (int j = 0; j < 32; ++j)
+                        if (row == col0 + j) v[j] += P.diag;
                 }
-                // 32 x 32 boxes of C, its rows 64 bytes in the 64-byte swizzle; the transposed one behind
-                auto store = [&](const CUtensorMap *map) {
-                    if (lane == 0) ptx::bulk_wait_read_all();
-                    __syncwarp();
+                // 32 x 32 boxes of C, and of it transposed, by TMA: a warp's own stores of them would
+                // delay the arrival that hands the accumulator back until they are through
+                auto store = [&](const CUtensorMap *map, bool more) {
                     uint32_t h[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) h[i] = pack_half(v[2 * i], v[2 * i + 1]);
+                    for (int j = 0; j < 16; ++j) h[j] = pack_half(v[2 * j], v[2 * j + 1]);
+                    if (lane == 0) ptx::bulk_wait_read_all();
+                    __syncwarp();
+                    // rows of 64 bytes in the 64-byte swizzle
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
                         *reinterpret_cast<uint4 *>(stg_ptr + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
                             make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
                     if (t.mirror) {
+                        // two rows' elements of a column side by side: an even lane the even column's, an odd
+                        // lane the odd column's
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            *reinterpret_cast<uint16_t *>(stg_ptr + 2048 + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) +
-                                                          (lane & 7) * 2) = (uint16_t)(h[i / 2] >> (16 * (i & 1)));
+                        for (int j = 0; j < 16; ++j) {
+                            const uint32_t other = __shfl_xor_sync(0xffffffffu, h[j], 1);
+                            *reinterpret_cast<uint32_t *>(stg_ptr + 2048 + (2 * j + (lane & 1)) * 64 +
+                                                          (((lane >> 3) ^ (j & 3)) << 4) + ((lane >> 1) & 3) * 4) =
+                                lane & 1 ? __byte_perm(other, h[j], 0x7632) : __byte_perm(h[j], other, 0x5410);
+                        }
                     }
                     ptx::fence_proxy_async_smem();
                     __syncwarp();
@@ -372,16 +415,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(tc::pair::kPairThrea
                         if (t.mirror) ptx::tma_store_2d(map, stg + 2048, row0, col0);
                         ptx::bulk_commit_group();
                     }
+                    if (!more) return;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
-                        v[2 * i] -= f.x, v[2 * i + 1] -= f.y;
+                    for (int j = 0; j < 16; ++j) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
+                        v[2 * j] -= f.x, v[2 * j + 1] -= f.y;
                     }
                 };
-                store(&g.map[t.prob][4]);
-                if (P.pairs) store(&g.map[t.prob][5]);
+                store(&g.map[t.prob][4], lows);
+                if (lows) store(&g.map[t.prob][5], false);
             }
-            if (P.nsplit == 1) hand_back();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) cluster::mbar_arrive(b ? leader_tempty1 : leader_tempty0);
         }
         if (lane == 0) ptx::bulk_wait_all();  // stores done before the staging buffer goes away
     }

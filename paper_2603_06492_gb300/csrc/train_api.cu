@@ -260,7 +260,8 @@ bool muon_precise(const noble_muon_tensor &t, uint32_t flags)
 {
     return (flags & NOBLE_MUON_PRECISE) != 0 || std::min(t.rows, t.cols) <= 256;
 }
-int64_t muon_ld(int64_t cols) { return (int64_t)align_up((size_t)cols, 8); }
+// Elements between rows of X, A and B; X also has whole groups of eight rows (make_half_map4).
+int64_t muon_ld(int64_t cols) { return (int64_t)align_up((size_t)cols, 64); }
 
 // The three products of a step, in this order: A = X X^T, B = a I + b A + c A A, X <- B X.
 enum { kGram, kPoly, kNext, kPhases };
@@ -358,7 +359,7 @@ MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
         const bool precise = muon_precise(s, flags);
         const int m = (int)std::min(s.rows, s.cols), k = (int)std::max(s.rows, s.cols);
         const size_t e = precise ? 4 : 2;
-        for (size_t &x : w.at[i].x) x = take((size_t)m * (size_t)muon_ld(k) * e);
+        for (size_t &x : w.at[i].x) x = take(align_up((size_t)m, 8) * (size_t)muon_ld(k) * e);
         w.at[i].a = take((size_t)m * (size_t)muon_ld(m) * e);
         w.at[i].b = take((size_t)m * (size_t)muon_ld(m) * e);
         w.at[i].sums = take(muon::kMomentBlocks * sizeof(double));
@@ -380,7 +381,7 @@ MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
             if (p.nsplit == 1) continue;
             const size_t tiles = (size_t)muon_tiles(p, p.bn);
             bytes += tiles * p.nsplit * muon::mma::kRows * p.bn * 4;
-            counts += (int)tiles * 16;
+            counts += (int)tiles * 64;
         }
         part = std::max(part, bytes), w.ncounts = std::max(w.ncounts, counts);
     }
@@ -389,8 +390,8 @@ MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
     return w;
 }
 
-// TMA map of an fp16 matrix: boxes of `cols` by `rows`, with the swizzle of that width.
-noble_status make_half_map(CUtensorMap *m, const __half *p, int rows, int cols, int64_t ld, uint32_t box_cols, uint32_t box_rows)
+// TMA map of an fp16 matrix: boxes of 64 or 32 columns, with the swizzle of that width.
+noble_status make_half_map(CUtensorMap *m, const __half *p, int rows, int cols, int64_t ld, uint32_t box_rows, uint32_t box_cols = 64)
 {
     EncodeTiledFn enc = encode_fn();
     if (!enc) return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
@@ -406,39 +407,71 @@ noble_status make_half_map(CUtensorMap *m, const __half *p, int rows, int cols, 
     return NOBLE_OK;
 }
 
+// The 4-D map of X as the operand that is not along K (make_map_mn4 of noble_api.cu has the
+// layout): whole groups of eight rows, the last filled up with zeros, and of 64 columns.  A 2-D map of
+// boxes of 64 rows makes the products 1.4 times slower (0.37 us a k-block of 256 x 256, not 0.26).
+noble_status make_half_map4(CUtensorMap *m, const __half *p, int rows, int64_t ld, uint32_t chunks)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
+    const cuuint64_t pitch = (cuuint64_t)ld * 2;
+    cuuint64_t dims[4] = {64, 8, (cuuint64_t)ld / 64, (cuuint64_t)ceil_div(rows, 8)};
+    cuuint64_t strides[3] = {pitch, 128, 8 * pitch};
+    cuuint32_t box[4] = {64, 8, chunks, 8};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<__half *>(p), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(NOBLE_ERR_CUDA, "cuTensorMapEncodeTiled (4-D) failed (%d): rows=%d ld=%lld", (int)r, rows, (long long)ld);
+    return NOBLE_OK;
+}
+
 // A matrix of the iteration: its high parts, and low parts behind them or NULL.
 struct HalfMatrix {
     __half *hi, *lo;
     int rows, cols;
     int64_t ld;
-    noble_status maps(CUtensorMap *m, uint32_t box_cols, uint32_t box_rows) const
+    noble_status maps4(CUtensorMap *m, uint32_t chunks) const
     {
-        NOBLE_TRY(make_half_map(m, hi, rows, cols, ld, box_cols, box_rows));
-        return make_half_map(m + 1, lo ? lo : hi, rows, cols, ld, box_cols, box_rows);
+        NOBLE_TRY(make_half_map4(m, hi, rows, ld, chunks));
+        return lo ? make_half_map4(m + 1, lo, rows, ld, chunks) : NOBLE_OK;
+    }
+    noble_status store_maps(CUtensorMap *m) const
+    {
+        NOBLE_TRY(make_half_map(m, hi, rows, cols, ld, 32, 32));
+        return lo ? make_half_map(m + 1, lo, rows, cols, ld, 32, 32) : NOBLE_OK;
+    }
+    noble_status maps(CUtensorMap *m, uint32_t box_rows) const
+    {
+        NOBLE_TRY(make_half_map(m, hi, rows, cols, ld, box_rows));
+        return lo ? make_half_map(m + 1, lo, rows, cols, ld, box_rows) : NOBLE_OK;
     }
 };
 
-noble_status muon_product(const muon::mma::Args &g, double flops, cudaStream_t st)
+template <int N, bool WIDE>
+noble_status muon_product(const muon::mma::Args<N> &g, const KernelInfo &ki, cudaStream_t st)
 {
-    using muon::mma::Smem;
+    constexpr size_t smem = muon::mma::Smem<WIDE>::kDynamic;
     static std::atomic<CUcontext> allowed{nullptr};
     const CUcontext ctx = current_context();
     if (!ctx || allowed.load(std::memory_order_relaxed) != ctx) {
-        if (cudaFuncSetAttribute(muon::mma::product_pairs, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem::kDynamic) != cudaSuccess)
+        if (cudaFuncSetAttribute(muon::mma::product_pairs<N, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
             return fail(NOBLE_ERR_CUDA, "shared memory: %s", cudaGetErrorString(cudaGetLastError()));
         allowed.store(current_context(), std::memory_order_relaxed);
     }
     // each pair takes units of its own: no pair waits for another, so that they need not all be resident
     const int pairs = std::min({g.units, muon::mma::kPairs, std::max(1, num_sms() / 2)});
     const bool pdl = pdl_ok();
-    return run(st, {"muon_product", kBoundTensor, flops, 0.0}, [&] {
-        launch_maybe_pdl(muon::mma::product_pairs, dim3(2 * (unsigned)pairs), dim3(tc::pair::kPairThreads), Smem::kDynamic, st, pdl, g);
+    return run(st, ki, [&] {
+        launch_maybe_pdl(muon::mma::product_pairs<N, WIDE>, dim3(2 * (unsigned)pairs), dim3(tc::pair::kPairThreads), smem, st, pdl, g);
     });
 }
 
+template <int N>
 noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble_muon_hparams *hp, char *ws, cudaStream_t st)
 {
-    using muon::mma::Args;
+    using Args = muon::mma::Args<N>;
+    bool wide[kPhases] = {};
     muon::Batch b{};
     b.n = w.n, b.momentum = hp->momentum, b.eps = hp->eps, b.nesterov = (hp->flags & NOBLE_MUON_NESTEROV) != 0;
     b.counts = reinterpret_cast<uint32_t *>(ws + w.counts), b.ncounts = w.ncounts;
@@ -454,6 +487,7 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
         M.n = s.rows * s.cols, M.rows = (int)s.rows, M.cols = (int)s.cols;
         M.tall = s.rows > s.cols;
         M.m = std::min(M.rows, M.cols), M.k = std::max(M.rows, M.cols), M.ld = (int)muon_ld(M.k);
+        M.m8 = (int)align_up((size_t)M.m, 8);
         const float lr = hp->lr * s.lr_mult;
         M.lr = lr * std::sqrt(std::max(1.f, (float)M.rows / (float)M.cols));
         M.decay = s.decay ? lr * hp->weight_decay : 0.f;
@@ -463,14 +497,14 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
         tiles += (int)ceil_div(M.rows, 64) * M.tiles_c;
         blocks = std::max(blocks, M.nsums);
         bytes += (double)M.n * (12 + (s.update ? 2 : 0) + (s.param ? 8 : 0) + (s.param_bf16 ? 2 : 0));
-        auto matrix = [&](size_t off, int cols) {
+        auto matrix = [&](size_t off, int rows, int cols) {
             const int64_t ld = muon_ld(cols);
             __half *p = reinterpret_cast<__half *>(ws + off);
-            return HalfMatrix{p, precise ? p + M.m * ld : nullptr, M.m, cols, ld};
+            return HalfMatrix{p, precise ? p + rows * ld : nullptr, M.m, cols, ld};
         };
-        for (int h = 0; h < 2; ++h) X[h][i] = matrix(w.at[i].x[h], M.k);
-        A[i] = matrix(w.at[i].a, M.m), B[i] = matrix(w.at[i].b, M.m);
-        M.x = X[0][i].hi, M.x_lo = X[0][i].lo;
+        for (int h = 0; h < 2; ++h) X[h][i] = matrix(w.at[i].x[h], M.m8, M.k);
+        A[i] = matrix(w.at[i].a, M.m, M.m), B[i] = matrix(w.at[i].b, M.m, M.m);
+        M.x = X[0][i].hi, M.x_lo = X[0][i].lo, M.x_other = X[1][i].hi, M.x_other_lo = X[1][i].lo;
         M.o = X[hp->steps % 2][i].hi, M.o_lo = X[hp->steps % 2][i].lo;
     }
     // a product's arguments: what it multiplies, what it writes
@@ -486,23 +520,24 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
             muon::mma::Problem &p = g.p[k];
             CUtensorMap *m = g.map[k];
             p = w.p[phase][i];
-            const uint32_t wide = 64, rows = (uint32_t)p.bn / 2;
+            const uint32_t rows = (uint32_t)p.bn / 2;
+            wide[phase] |= p.bn == 256;
             if (phase == kGram) {
-                NOBLE_TRY(X[half][i].maps(m, wide, 128));
-                NOBLE_TRY(X[half][i].maps(m + 2, wide, rows));
-                NOBLE_TRY(A[i].maps(m + 4, 32, 32));
+                NOBLE_TRY(X[half][i].maps(m, 128));
+                NOBLE_TRY(X[half][i].maps(m + 2, rows));
+                NOBLE_TRY(A[i].store_maps(m + 4));
                 p.alpha = muon::kScaleA / (muon::kScaleX * muon::kScaleX);
             } else if (phase == kPoly) {
-                NOBLE_TRY(A[i].maps(m, wide, 128));
-                NOBLE_TRY(A[i].maps(m + 2, wide, rows));
-                NOBLE_TRY(B[i].maps(m + 4, 32, 32));
+                NOBLE_TRY(A[i].maps(m, 128));
+                NOBLE_TRY(A[i].maps(m + 2, rows));
+                NOBLE_TRY(B[i].store_maps(m + 4));
                 p.alpha = muon::kC * muon::kScaleB / (muon::kScaleA * muon::kScaleA);
                 p.beta = muon::kB * muon::kScaleB / muon::kScaleA, p.diag = muon::kA * muon::kScaleB;
                 p.d = A[i].hi, p.d_lo = A[i].lo, p.ldd = (int)A[i].ld;
             } else {
-                NOBLE_TRY(B[i].maps(m, wide, 128));
-                NOBLE_TRY(X[half][i].maps(m + 2, wide, 64));
-                NOBLE_TRY(X[!half][i].maps(m + 4, 32, 32));
+                NOBLE_TRY(B[i].maps(m, 128));
+                NOBLE_TRY(X[half][i].maps4(m + 2, rows / 64));
+                NOBLE_TRY(X[!half][i].store_maps(m + 4));
                 p.alpha = 1.f / muon::kScaleB;
             }
             flops[phase] += 2.0 * p.m * p.n * (phase == kGram ? b.t[i].k : p.m) * (p.sym ? 0.5 : 1.0);
@@ -510,7 +545,7 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
                 const int n = muon_tiles(p, p.bn);
                 p.part = reinterpret_cast<float *>(ws + part), p.count = count;
                 part += (size_t)n * p.nsplit * muon::mma::kRows * p.bn * 4;
-                count += n * 16;
+                count += n * 64;
             }
         }
         return NOBLE_OK;
@@ -519,14 +554,19 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
     NOBLE_TRY(run(st, hbm, [&] { muon::momentum_kernel<<<dim3((unsigned)blocks, (unsigned)w.n), 256, 0, st>>>(b); }));
     NOBLE_TRY(run(st, hbm, [&] { muon::scale_kernel<<<(unsigned)tiles, 256, 0, st>>>(b); }));
     Args gram[2] = {}, poly = {}, next[2] = {};
+    auto product = [&](const Args &g, int phase) {
+        static const char *const names[kPhases] = {"muon_gram", "muon_poly", "muon_next"};
+        const KernelInfo ki{names[phase], kBoundTensor, flops[phase], 0.0};
+        return wide[phase] ? muon_product<N, true>(g, ki, st) : muon_product<N, false>(g, ki, st);
+    };
     for (int k = 0; k < hp->steps; ++k) {
         const int h = k % 2;
         if (k < 2) NOBLE_TRY(arguments(gram[h], kGram, h));
-        NOBLE_TRY(muon_product(gram[h], flops[kGram], st));
+        NOBLE_TRY(product(gram[h], kGram));
         if (k == 0) NOBLE_TRY(arguments(poly, kPoly, 0));
-        NOBLE_TRY(muon_product(poly, flops[kPoly], st));
+        NOBLE_TRY(product(poly, kPoly));
         if (k < 2) NOBLE_TRY(arguments(next[h], kNext, h));
-        NOBLE_TRY(muon_product(next[h], flops[kNext], st));
+        NOBLE_TRY(product(next[h], kNext));
     }
     return run(st, hbm, [&] { muon::apply_kernel<<<(unsigned)tiles, 256, 0, st>>>(b); });
 }
@@ -682,10 +722,14 @@ noble_status noble_muon_step(const noble_muon_tensor *tensors, int n_tensors, co
     }
     NOBLE_TRY(check_workspace(workspace, workspace_bytes, need));
     NOBLE_TRY(check_device());
-    if (n_tensors <= muon::kMost) return muon_run(tensors, plan, hp, static_cast<char *>(workspace), (cudaStream_t)stream);
+    auto go = [&](const MuonPlan &w) {
+        char *ws = static_cast<char *>(workspace);
+        return w.n <= 4 ? muon_run<4>(tensors, w, hp, ws, (cudaStream_t)stream) : muon_run<muon::kMost>(tensors, w, hp, ws, (cudaStream_t)stream);
+    };
+    if (n_tensors <= muon::kMost) return go(plan);
     for (next = 0; next < n_tensors;) {
         const MuonPlan w = muon_plan(tensors, n_tensors, &next, hp->flags);
-        if (w.n) NOBLE_TRY(muon_run(tensors, w, hp, static_cast<char *>(workspace), (cudaStream_t)stream));
+        if (w.n) NOBLE_TRY(go(w));
     }
     return NOBLE_OK;
 }
