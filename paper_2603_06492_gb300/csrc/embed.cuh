@@ -64,11 +64,31 @@ __global__ void __launch_bounds__(256) fwd_kernel(const FwdArgs<T> a)
 }
 
 // ---------------------------------------------------------------- gradient
+// 32 bytes a lane in one store where they are aligned: two of 16 write every sector twice.
+template <int N>
+__device__ __forceinline__ void store_scaled(float *p, const float (&f)[N], float scale, bool wide)
+{
+    if constexpr (N == 8) {
+        if (wide) {
+            asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0] * scale), "f"(f[1] * scale),
+                         "f"(f[2] * scale), "f"(f[3] * scale), "f"(f[4] * scale), "f"(f[5] * scale), "f"(f[6] * scale),
+                         "f"(f[7] * scale)
+                         : "memory");
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+        __stcs(reinterpret_cast<float4 *>(p) + i,
+               make_float4(f[4 * i] * scale, f[4 * i + 1] * scale, f[4 * i + 2] * scale, f[4 * i + 3] * scale));
+}
+
 constexpr int kFewTokens = 2048;  // at most so many: one launch
 constexpr int kFewRows = 64;      // rows of the table of a block then
 constexpr int kShort = 32;        // a list of so many tokens is one warp's
 constexpr int kPiece = 64;        // tokens of a piece of a longer list
-constexpr int kWindow = 1 << 18;  // tokens that a block's bit map covers at a time
+constexpr int kCompared = 256;    // tokens of a list that is ordered by comparing
+constexpr int kWindow = 1 << 18;  // tokens that a block's bit map covers at a time, for longer ones
 
 template <typename T>
 struct BwdArgs {
@@ -86,40 +106,54 @@ struct BwdArgs {
     uint32_t *long_at;   // their first pieces
     uint2 *piece;        // row, which piece of its list
     float *part;         // [pieces][d]
+    int rows_per_warp, piece_blocks;  // of sum_kernel
+    int wide;            // dtable is aligned to 32 bytes
 };
 
-// acc += the rows of dy that list names, first to last; the columns of vector `at`
-template <typename T>
-__device__ __forceinline__ void add_rows(const T *dy, int64_t d, const uint32_t *list, int n, int at, float (&acc)[Vec<T>::n])
+// out = scale * (the sum of the n rows of dy that list names, first to last), the columns of vectors at,
+// at + 32, ..., C of them: B tokens' loads are on their way at once.
+template <int C, int B, typename T>
+__device__ __forceinline__ void sum_vectors(const BwdArgs<T> &a, const uint32_t *list, int n, int at, float *out, float scale)
 {
-    constexpr int V = Vec<T>::n, kAhead = 8;
-    int k = 0;
-    for (; k + kAhead <= n; k += kAhead) {
-        uint4 q[kAhead];
+    constexpr int V = Vec<T>::n;
+    const int vecs = a.d / V;
+    float acc[C][V];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) q[i] = reinterpret_cast<const uint4 *>(dy + (int64_t)list[k + i] * d)[at];
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            float f[V];
-            Vec<T>::unpack(q[i], f);
+        for (int j = 0; j < V; ++j) acc[c][j] = 0.f;
+    for (int k = 0; k < n; k += B) {
+        uint4 q[B][C];
 #pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += f[j];
+        for (int i = 0; i < B; ++i) {
+            const uint4 *row = reinterpret_cast<const uint4 *>(a.dy + (k + i < n ? (int64_t)list[k + i] * a.d : 0));
+#pragma unroll
+            for (int c = 0; c < C; ++c) q[i][c] = k + i < n && at + 32 * c < vecs ? row[at + 32 * c] : make_uint4(0, 0, 0, 0);
         }
-    }
-    for (; k < n; ++k) {
-        float f[V];
-        Vec<T>::unpack(reinterpret_cast<const uint4 *>(dy + (int64_t)list[k] * d)[at], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] += f[j];
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float f[V];
+                Vec<T>::unpack(q[i][c], f);
+#pragma unroll
+                for (int j = 0; j < V; ++j) acc[c][j] += f[j];
+            }
     }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (at + 32 * c < vecs) store_scaled(out + (at + 32 * c) * V, acc[c], scale, a.wide);
 }
-template <int N>
-__device__ __forceinline__ void store_scaled(float *p, const float (&f)[N], float scale)
+// ... of all vectors from `at` on that are `step` apart, but for the steps within a warp.
+template <typename T>
+__device__ __forceinline__ void sum_row(const BwdArgs<T> &a, const uint32_t *list, int n, int at, int step, float *out, float scale)
 {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-        __stcs(reinterpret_cast<float4 *>(p) + i,
-               make_float4(f[4 * i] * scale, f[4 * i + 1] * scale, f[4 * i + 2] * scale, f[4 * i + 3] * scale));
+    const int vecs = a.d / Vec<T>::n;
+    if (n <= 4 && step == 32) {
+        for (; at < vecs; at += 4 * 32) sum_vectors<4, 2>(a, list, n, at, out, scale);
+    } else {
+        for (; at < vecs; at += step) sum_vectors<1, 8>(a, list, n, at, out, scale);
+    }
 }
 
 // Few tokens: a block has kFewRows rows of the table and 32 vectors of their columns, finds
@@ -129,7 +163,7 @@ __global__ void __launch_bounds__(256) few_kernel(const BwdArgs<T> a)
 {
     constexpr int V = Vec<T>::n;
     __shared__ uint32_t found[kFewTokens];  // row of the block << 16 | token
-    __shared__ uint32_t mine[8][kFewTokens / 4];
+    __shared__ uint32_t mine[8][kFewTokens / 8];
     __shared__ int counts[8];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int first = blockIdx.x * kFewRows, rows = min(kFewRows, a.vocab - first), n = (int)a.tokens;
@@ -152,97 +186,134 @@ __global__ void __launch_bounds__(256) few_kernel(const BwdArgs<T> a)
         if (hit) found[before + __popc(mask & ((1u << lane) - 1))] = (uint32_t)(id - first) << 16 | (uint32_t)t;
         __syncthreads();
     }
+    const int n_found = total;
     for (int r = warp; r < rows; r += 8) {
+        // this row's tokens, over the warp's part of `mine` again and again
         float acc[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = 0.f;
-        // this row's tokens, a quarter of the longest list at a time
-        int k = 0;
-        while (k < total) {
+        for (int k = 0; k < n_found;) {
             int m = 0;
-            for (; k < total && m + 32 <= kFewTokens / 4; k += 32) {
-                const uint32_t e = k + lane < total ? found[k + lane] : ~0u;
+            for (; k < n_found && m + 32 <= kFewTokens / 8; k += 32) {
+                const uint32_t e = k + lane < n_found ? found[k + lane] : ~0u;
                 const bool hit = e >> 16 == (uint32_t)r;
                 const uint32_t mask = __ballot_sync(0xffffffffu, hit);
                 if (hit) mine[warp][m + __popc(mask & ((1u << lane) - 1))] = e & 0xffffu;
                 m += __popc(mask);
             }
             __syncwarp();
-            if (in) add_rows(a.dy, a.d, mine[warp], m, at, acc);
+            for (int i0 = 0; in && i0 < m; i0 += 8) {
+                uint4 q[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    q[i] = i0 + i < m ? reinterpret_cast<const uint4 *>(a.dy + (int64_t)mine[warp][i0 + i] * a.d)[at] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float f[V];
+                    Vec<T>::unpack(q[i], f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) acc[j] += f[j];
+                }
+            }
             __syncwarp();
         }
-        if (in) store_scaled(a.dtable + (int64_t)(first + r) * a.d + at * V, acc, a.scale);
+        if (in) store_scaled(a.dtable + (int64_t)(first + r) * a.d + at * V, acc, a.scale, a.wide);
     }
 }
 
 // ---- many tokens
+// Three steps make a list of the tokens of each row, each step over everything that the one before
+// it wrote; `thread` of `threads` in whole warps.
+
 // tokens of each row, and each token's place among them (which atomics decide)
 template <typename T>
-__global__ void __launch_bounds__(256) count_kernel(const BwdArgs<T> a)
+__device__ __forceinline__ void count_tokens(const BwdArgs<T> &a, int64_t thread, int64_t threads)
 {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    int id = t < a.tokens ? a.ids[t] : -1;
-    if (id >= a.vocab) {
-        raise_status(a.status, kStatusBadIndex);
-        id = -1;
+    const int lane = threadIdx.x % 32;
+    for (int64_t t = thread; t - lane < a.tokens; t += threads) {
+        int id = t < a.tokens ? a.ids[t] : -1;
+        if (id >= a.vocab) {
+            raise_status(a.status, kStatusBadIndex);
+            id = -1;
+        }
+        // one atomic for the lanes that share a row
+        const uint32_t same = __match_any_sync(0xffffffffu, id);
+        const int lead = __ffs(same) - 1;
+        uint32_t base = 0;
+        if (id >= 0 && lane == lead) base = atomicAdd(a.count + id, (uint32_t)__popc(same));
+        base = __shfl_sync(0xffffffffu, base, lead);
+        if (t < a.tokens) a.rank[t] = id < 0 ? ~0u : base + __popc(same & ((1u << lane) - 1));
     }
-    // one atomic for the lanes that share a row
-    const uint32_t same = __match_any_sync(0xffffffffu, id);
-    const int lead = __ffs(same) - 1, lane = threadIdx.x % 32;
-    uint32_t base = 0;
-    if (id >= 0 && lane == lead) base = atomicAdd(a.count + id, (uint32_t)__popc(same));
-    base = __shfl_sync(0xffffffffu, base, lead);
-    if (t < a.tokens) a.rank[t] = id < 0 ? ~0u : base + __popc(same & ((1u << lane) - 1));
 }
 
 // where each row's list begins; long lists and their pieces
 template <typename T>
-__global__ void __launch_bounds__(256) lists_kernel(const BwdArgs<T> a)
+__device__ __forceinline__ void begin_lists(const BwdArgs<T> &a, int64_t thread, int64_t threads)
 {
-    const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int lane = threadIdx.x % 32;
-    const uint32_t n = v < a.vocab ? a.count[v] : 0;
-    uint32_t upto = n;
+    for (int64_t v = thread; v - lane < a.vocab; v += threads) {
+        const uint32_t n = v < a.vocab ? __ldcg(a.count + v) : 0;
+        uint32_t upto = n;
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += u;
-    }
-    uint32_t base = 0;
-    if (lane == 31 && upto) base = atomicAdd(a.head, upto);
-    base = __shfl_sync(0xffffffffu, base, 31);
-    if (v < a.vocab) a.begin[v] = base + upto - n;
-    if (n > kShort) {
-        const uint32_t l = atomicAdd(a.head + 1, 1u), pieces = (n + kPiece - 1) / kPiece, p = atomicAdd(a.head + 2, pieces);
-        a.long_row[l] = (uint32_t)v;
-        a.long_at[l] = p;
-        for (uint32_t k = 0; k < pieces; ++k) a.piece[p + k] = make_uint2((uint32_t)v, k);
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += u;
+        }
+        uint32_t base = 0;
+        if (lane == 31 && upto) base = atomicAdd(a.head, upto);
+        base = __shfl_sync(0xffffffffu, base, 31);
+        if (n) a.begin[v] = base + upto - n;
+        if (n > kShort) {
+            const uint32_t l = atomicAdd(a.head + 1, 1u), pieces = (n + kPiece - 1) / kPiece, p = atomicAdd(a.head + 2, pieces);
+            a.long_row[l] = (uint32_t)v;
+            a.long_at[l] = p;
+            for (uint32_t k = 0; k < pieces; ++k) a.piece[p + k] = make_uint2((uint32_t)v, k);
+        }
     }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) place_kernel(const BwdArgs<T> a)
+__device__ __forceinline__ void place_tokens(const BwdArgs<T> &a, int64_t thread, int64_t threads)
 {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= a.tokens) return;
-    const uint32_t r = a.rank[t];
-    if (r != ~0u) a.list[a.begin[a.ids[t]] + r] = (uint32_t)t;
+    for (int64_t t = thread; t < a.tokens; t += threads) {
+        const uint32_t r = __ldcg(a.rank + t);
+        if (r != ~0u) a.list[__ldcg(a.begin + a.ids[t]) + r] = (uint32_t)t;
+    }
 }
 
-// Long lists in ascending order: a bit for each token, read off again word by word.  The
-// tokens of a window are listed before those of the next; `rank`, which nothing needs any
-// more, takes the ordered list.
+// Long lists in ascending order, a list to a block at a time; `rank`, which nothing needs any more,
+// takes them.  Up to kCompared tokens each token's place is the number of smaller ones; beyond,
+// a bit is set for each token and the bits are read off again word by word, the tokens of a window
+// before those of the next.
 template <typename T>
 __global__ void __launch_bounds__(256) order_kernel(const BwdArgs<T> a)
 {
     extern __shared__ uint32_t bits[];
     __shared__ uint32_t sums[8];
+    __shared__ __align__(16) uint32_t some[kCompared];
+    ptx::griddep_launch();
+    ptx::griddep_wait();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    for (uint32_t l = blockIdx.x; l < a.head[1]; l += gridDim.x) {
+    const uint32_t lists = a.head[1];
+    for (uint32_t l = blockIdx.x; l < lists; l += gridDim.x) {
         const uint32_t row = a.long_row[l], n = a.count[row], begin = a.begin[row];
+        if (n <= kCompared) {
+            const uint32_t t = threadIdx.x < n ? a.list[begin + threadIdx.x] : ~0u;
+            __syncthreads();
+            some[threadIdx.x] = t;
+            __syncthreads();
+            uint32_t place = 0;
+            for (uint32_t k = 0; k < n; k += 4) {  // what pads the last four is not smaller
+                const uint4 q = *reinterpret_cast<const uint4 *>(some + k);
+                place += (q.x < t) + (q.y < t) + (q.z < t) + (q.w < t);
+            }
+            if (threadIdx.x < n) a.rank[begin + place] = t;
+            continue;
+        }
         uint32_t done = begin;
         for (int64_t w0 = 0; w0 < a.tokens; w0 += kWindow) {
             const int words = (int)((min((int64_t)kWindow, a.tokens - w0) + 31) / 32);
+            __syncthreads();
             for (int i = threadIdx.x; i < words; i += 256) bits[i] = 0;
             __syncthreads();
             for (uint32_t k = threadIdx.x; k < n; k += 256) {
@@ -274,62 +345,131 @@ __global__ void __launch_bounds__(256) order_kernel(const BwdArgs<T> a)
     }
 }
 
-// A warp per row with a short list, or none, and per piece of a long one: the rows come
-// first, then the pieces.  blockIdx.y: columns, 32 vectors at a time.
+// The first three by one cluster of eight blocks, which wait for each other at the cluster's barrier.
+constexpr int kIndexBlocks = 8, kIndexThreads = 1024;
+constexpr int64_t kIndexMost = 1 << 17;  // tokens, and rows of the table: beyond, a launch each
+template <typename T>
+__global__ void __cluster_dims__(kIndexBlocks, 1, 1) __launch_bounds__(kIndexThreads) index_kernel(const BwdArgs<T> a)
+{
+    ptx::griddep_launch();
+    ptx::griddep_wait();
+    const int64_t thread = blockIdx.x * kIndexThreads + threadIdx.x, threads = kIndexBlocks * kIndexThreads;
+    auto all = [] {
+        __threadfence();
+        __syncthreads();
+        cluster::sync();
+    };
+    for (int64_t v = thread; v < a.vocab; v += threads) a.count[v] = 0;
+    if (thread < 4) a.head[thread] = 0;
+    all();
+    count_tokens(a, thread, threads);
+    all();
+    begin_lists(a, thread, threads);
+    all();
+    place_tokens(a, thread, threads);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) count_kernel(const BwdArgs<T> a)
+{
+    ptx::griddep_launch();
+    ptx::griddep_wait();
+    count_tokens(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+template <typename T>
+__global__ void __launch_bounds__(256) lists_kernel(const BwdArgs<T> a)
+{
+    ptx::griddep_launch();
+    ptx::griddep_wait();
+    begin_lists(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+template <typename T>
+__global__ void __launch_bounds__(256) place_kernel(const BwdArgs<T> a)
+{
+    ptx::griddep_launch();
+    ptx::griddep_wait();
+    place_tokens(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+// A warp for rows_per_warp rows of the table with short lists, or none, and one for each piece of a
+// long list, which come first.  blockIdx.y: columns, 32 vectors at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs<T> a)
 {
     constexpr int V = Vec<T>::n;
     __shared__ uint32_t order[8][kPiece];
+    ptx::griddep_launch();
+    ptx::griddep_wait();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, vecs = a.d / V;
-    const int64_t work = (int64_t)a.vocab + a.head[2];
-    for (int64_t w = (int64_t)blockIdx.x * 8 + warp; w < work; w += (int64_t)gridDim.x * 8) {
-        int n;
-        float *out;
+    const int at0 = blockIdx.y * 32 + lane, step = gridDim.y * 32;
+    if ((int)blockIdx.x < a.piece_blocks) {
+        const uint32_t w = blockIdx.x * 8 + warp;
+        if (w >= a.head[2]) return;
+        const uint2 p = a.piece[w];
+        const uint32_t begin = a.begin[p.x] + p.y * kPiece;
+        const int n = (int)min((uint32_t)kPiece, a.count[p.x] - p.y * kPiece);
+        for (int k = lane; k < n; k += 32) order[warp][k] = a.rank[begin + k];
         __syncwarp();
-        if (w < a.vocab) {
-            n = (int)a.count[w];
-            if (n > kShort) continue;
-            out = a.dtable + w * a.d;
-            const uint32_t t = lane < n ? a.list[a.begin[w] + lane] : ~0u;
-            // a token's place: how many of the list come before it
-            int place = 0;
-            for (int k = 0; k < n; ++k) place += __shfl_sync(0xffffffffu, t, k) < t;
-            if (lane < n) order[warp][place] = t;
-        } else {
-            const uint2 p = a.piece[w - a.vocab];
-            const uint32_t begin = a.begin[p.x] + p.y * kPiece;
-            n = (int)min((uint32_t)kPiece, a.count[p.x] - p.y * kPiece);
-            out = a.part + (w - a.vocab) * a.d;
-            for (int k = lane; k < n; k += 32) order[warp][k] = a.rank[begin + k];
-        }
+        sum_row(a, order[warp], n, at0, step, a.part + (int64_t)w * a.d, 1.f);
+        return;
+    }
+    // counts of this warp's rows, a lane each
+    const int64_t first = ((int64_t)(blockIdx.x - a.piece_blocks) * 8 + warp) * a.rows_per_warp;
+    const bool mine = lane < a.rows_per_warp && first + lane < a.vocab;
+    const uint32_t count = mine ? a.count[first + lane] : ~0u;
+    const uint32_t begin = mine && count && count <= kShort ? a.begin[first + lane] : 0;
+    // rows without tokens, then the others: writing zeros waits for nothing
+    for (uint32_t none = __ballot_sync(0xffffffffu, count == 0); none; none &= none - 1) {
+        float *out = a.dtable + (first + __ffs(none) - 1) * a.d;
+        const float zero[V] = {};
+        for (int at = at0; at < vecs; at += step) store_scaled(out + at * V, zero, 1.f, a.wide);
+    }
+    for (uint32_t some = __ballot_sync(0xffffffffu, count && count <= kShort); some; some &= some - 1) {
+        const int r = __ffs(some) - 1, n = (int)__shfl_sync(0xffffffffu, count, r);
+        const uint32_t b = __shfl_sync(0xffffffffu, begin, r);
+        const uint32_t t = lane < n ? a.list[b + lane] : ~0u;
+        // a token's place: how many of the list come before it
+        int place = 0;
+        for (int k = 0; k < n; ++k) place += __shfl_sync(0xffffffffu, t, k) < t;
         __syncwarp();
-        for (int at = blockIdx.y * 32 + lane; at < vecs; at += gridDim.y * 32) {
-            float acc[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] = 0.f;
-            add_rows(a.dy, a.d, order[warp], n, at, acc);
-            store_scaled(out + at * V, acc, w < a.vocab ? a.scale : 1.f);
-        }
+        if (lane < n) order[warp][place] = t;
+        __syncwarp();
+        sum_row(a, order[warp], n, at0, step, a.dtable + (first + r) * a.d, a.scale);
     }
 }
 
-// the pieces of each long list, first to last
+// The pieces of each long list: 128 columns of a list to a block, an eighth of the pieces to a
+// warp, in order; then the eighths in order.
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const BwdArgs<T> a)
 {
-    const int quads = a.d / 4;
+    __shared__ float4 sm[8][32];
+    ptx::griddep_wait();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, quads = a.d / 4;
     for (uint32_t l = blockIdx.x; l < a.head[1]; l += gridDim.x) {
-        const uint32_t row = a.long_row[l], pieces = (a.count[row] + kPiece - 1) / kPiece;
+        const uint32_t row = a.long_row[l], pieces = (a.count[row] + kPiece - 1) / kPiece, per = (pieces + 7) / 8;
         const float *part = a.part + (int64_t)a.long_at[l] * a.d;
-        for (int at = blockIdx.y * 256 + threadIdx.x; at < quads; at += gridDim.y * 256) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int q0 = blockIdx.y * 32; q0 < quads; q0 += gridDim.y * 32) {
+            const int at = q0 + lane;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (at < quads) {
+                const uint32_t end = min(pieces, (warp + 1) * per);
 #pragma unroll 8
-            for (uint32_t k = 0; k < pieces; ++k) {
-                const float4 q = reinterpret_cast<const float4 *>(part + (int64_t)k * a.d)[at];
-                acc[0] += q.x, acc[1] += q.y, acc[2] += q.z, acc[3] += q.w;
+                for (uint32_t k = warp * per; k < end; ++k) {
+                    const float4 q = reinterpret_cast<const float4 *>(part + (int64_t)k * a.d)[at];
+                    acc.x += q.x, acc.y += q.y, acc.z += q.z, acc.w += q.w;
+                }
             }
-            store_scaled(a.dtable + (int64_t)row * a.d + 4 * at, acc, a.scale);
+            __syncthreads();
+            sm[warp][lane] = acc;
+            __syncthreads();
+            if (warp == 0 && at < quads) {
+                for (int w = 1; w < 8; ++w) {
+                    const float4 q = sm[w][lane];
+                    acc.x += q.x, acc.y += q.y, acc.z += q.z, acc.w += q.w;
+                }
+                const float f[4] = {acc.x, acc.y, acc.z, acc.w};
+                store_scaled(a.dtable + (int64_t)row * a.d + 4 * at, f, a.scale, false);
+            }
         }
     }
 }

@@ -15,8 +15,8 @@
 namespace noble {
 namespace norm {
 
-constexpr int kThreads = 256;  // of a block, unless a row takes more
-constexpr int kMaxVecs = 4;    // 16-byte pieces of a row that a thread of the forward holds
+constexpr int kWarps = 8;    // of a block of the forward, unless a row takes more
+constexpr int kMaxVecs = 4;  // 16-byte pieces of a row that a thread of the forward holds
 
 // 16 bytes of operands as floats and back
 template <typename T> struct Vec;
@@ -90,7 +90,7 @@ struct FwdArgs {
 };
 
 template <typename T, int NV, bool RES>
-__global__ void __launch_bounds__(1024) fwd_kernel(const FwdArgs<T> a)
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 1024) fwd_kernel(const FwdArgs<T> a)
 {
     constexpr int V = Vec<T>::n;
     __shared__ float sm[2][32];
@@ -169,111 +169,180 @@ struct BwdArgs {
     const float *gain;
     T *dx;
     float *part;  // [parts][2][d], or NULL: no gradients of gain and bias
+    uint32_t *status;
     int64_t rows;
-    int d, warps, rows_per_part;
+    int d, warps, groups, rows_per_part;  // warps: of a row; groups: rows at a time
+    int stages;
     float inv_d;
 };
 
-// Block p takes the rows of part p, `groups` of them at a time; a thread has the same columns
-// of every row, whose sums for dgain and dbias it keeps in registers and the block then adds
-// up in order of the groups.
-template <typename T, int NV, bool STREAM>
-__global__ void __launch_bounds__(1024) bwd_kernel(const BwdArgs<T> a)
+// warps that compute, at most, beside one that loads: 16 in all leave 128 registers to each thread
+constexpr int kBwdWarps = 15;
+constexpr uint32_t kBwdRing = 200 << 10;  // bytes of rows on their way, at most
+
+// A bulk copy of contiguous bytes (a multiple of 16) into shared memory.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
-    constexpr int V = Vec<T>::n;
-    extern __shared__ float cols[];  // [groups][2][d] for the sums over rows
-    __shared__ float sm[2][64];
-    const int per_row = a.warps * 32, lane = threadIdx.x % per_row, group = threadIdx.x / per_row,
-              groups = blockDim.x / per_row;
-    const int vecs = a.d / V;
-    float dg[NV][V], db[NV][V], g[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f, g[i][j] = 1.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (a.gain && i * per_row + lane < vecs) load_floats(a.gain, (i * per_row + lane) * V, g[i]);
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+                 "r"(bar)
+                 : "memory");
+}
+
+// Block p takes the rows of part p, `groups` of them at a time, out of a ring in shared memory
+// that the last warp keeps full by bulk copies: what bounds the pass is HBM, and rows on their way
+// in registers are too few of them.  A thread has the same columns of every row, whose sums
+// for dgain and dbias it keeps in registers and the block then adds up in order of the groups.
+// (rows of more than 8192 elements: 16 warps, and 32 columns a thread)
+template <typename T, int NV, bool STREAM>
+__global__ void __launch_bounds__(32 * (kBwdWarps + (NV * Vec<T>::n > 16 ? 2 : 1)), 1) bwd_kernel(const BwdArgs<T> a)
+{
+    constexpr int V = Vec<T>::n, kTensors = STREAM ? 3 : 2, kMostStages = 32;
+    extern __shared__ __align__(128) uint8_t ring[];  // [stages][tensors][groups][d], then the sums over rows
+    __shared__ float2 sm[2][kBwdWarps + 1];
+    __shared__ __align__(8) uint64_t bars[2 * kMostStages];
+    const int warp = threadIdx.x / 32, work_warps = a.warps * a.groups;
     const int64_t first = (int64_t)blockIdx.x * a.rows_per_part;
-    const int rows = (int)min((int64_t)a.rows_per_part, a.rows - first);
-    int turn = 0;
-    for (int k = 0; k < rows; k += groups, turn ^= 1) {
-        const bool in = k + group < rows;
-        const int64_t row = first + k + group, base = row * a.d;
-        float2 st = make_float2(0.f, 0.f);
-        if (in) st = a.stats[row];
-        uint4 qy[NV], qs[NV], qd[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = i * per_row + lane;
-            qy[i] = qs[i] = qd[i] = make_uint4(0, 0, 0, 0);
-            if (in && at < vecs) {
-                qy[i] = reinterpret_cast<const uint4 *>(a.dy + base)[at];
-                qs[i] = reinterpret_cast<const uint4 *>(a.s + base)[at];
-                if (STREAM) qd[i] = reinterpret_cast<const uint4 *>(a.dstream + base)[at];
-            }
+    const int rows = (int)min((int64_t)a.rows_per_part, a.rows - first), steps = (rows + a.groups - 1) / a.groups;
+    const uint32_t row_bytes = (uint32_t)a.d * sizeof(T), tensor_bytes = row_bytes * a.groups;
+    const uint32_t base = ptx::smem_u32(ring), full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * kMostStages;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) {
+            ptx::mbar_init(full0 + 8 * i, 1);
+            ptx::mbar_init(empty0 + 8 * i, work_warps);
         }
-        float t[2] = {0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (!in || i * per_row + lane >= vecs) continue;
-            float y[V], n[V];
-            Vec<T>::unpack(qy[i], y);
-            Vec<T>::unpack(qs[i], n);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                n[j] = (n[j] - st.x) * st.y;
-                dg[i][j] = fmaf(y[j], n[j], dg[i][j]);
-                db[i][j] += y[j];
-                const float w = y[j] * g[i][j];
-                t[0] += w;
-                t[1] = fmaf(w, n[j], t[1]);
+        ptx::fence_barrier_init();
+    }
+    __syncthreads();
+    const int vecs = a.d / V, per_row = a.warps * 32, tid = threadIdx.x;
+    const int group = tid / per_row, lane = tid - group * per_row;
+    float dg[NV][V], db[NV][V];
+    if (warp == work_warps) {
+        if (tid % 32 == 0) {
+            int s = 0;
+            uint32_t ph = 0;
+            for (int k = 0; k < steps; ++k) {
+                if (!ptx::mbar_wait(empty0 + 8 * s, ph ^ 1, a.status)) break;
+                const int64_t row = first + (int64_t)k * a.groups;
+                const uint32_t n = (uint32_t)min(a.groups, rows - k * a.groups) * row_bytes, full = full0 + 8 * s;
+                const uint32_t to = base + (uint32_t)s * kTensors * tensor_bytes;
+                ptx::mbar_arrive_expect_tx(full, n * kTensors);
+                bulk_load(to, a.dy + row * a.d, n, full);
+                bulk_load(to + tensor_bytes, a.s + row * a.d, n, full);
+                if (STREAM) bulk_load(to + 2 * tensor_bytes, a.dstream + row * a.d, n, full);
+                if (++s == a.stages) s = 0, ph ^= 1;
             }
+            // no copy may still be landing when the block ends
+            for (int k = max(0, steps - a.stages); k < steps; ++k) ptx::mbar_wait(full0 + 8 * (k % a.stages), (k / a.stages) & 1, nullptr);
         }
-        row_sums(t, a.warps, sm[turn]);
-        const float mw = t[0] * a.inv_d, mwn = t[1] * a.inv_d;
+    } else if (warp < work_warps) {
+        float g[NV][V];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = i * per_row + lane;
-            if (!in || at >= vecs) continue;
-            float y[V], n[V], e[V];
-            Vec<T>::unpack(qy[i], y);
-            Vec<T>::unpack(qs[i], n);
-            Vec<T>::unpack(qd[i], e);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                n[j] = (n[j] - st.x) * st.y;
-                y[j] = st.y * (fmaf(y[j], g[i][j], -mw) - n[j] * mwn);
-                if (STREAM) y[j] += e[j];
+            for (int j = 0; j < V; ++j) dg[i][j] = db[i][j] = 0.f, g[i][j] = 1.f;
+            if (a.gain && i * per_row + lane < vecs) load_floats(a.gain, (i * per_row + lane) * V, g[i]);
+        }
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        float2 st = group < rows ? a.stats[first + group] : make_float2(0.f, 0.f);
+        for (int k = 0; k < steps; ++k) {
+            const bool in = k * a.groups + group < rows;
+            // the next row's statistics, a step ahead
+            const int ahead = (k + 1) * a.groups + group;
+            const float2 next = ahead < rows ? a.stats[first + ahead] : make_float2(0.f, 0.f);
+            // a wait that gave up is reported; the barriers below still need every warp
+            if (ok) ok = ptx::mbar_wait(full0 + 8 * s, ph, a.status);
+            const uint8_t *at = ring + (size_t)s * kTensors * tensor_bytes + group * row_bytes;
+            uint4 qy[NV], qs[NV];
+            float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = i * per_row + lane;
+                if (!in || c >= vecs) continue;
+                qy[i] = reinterpret_cast<const uint4 *>(at)[c];
+                qs[i] = reinterpret_cast<const uint4 *>(at + tensor_bytes)[c];
+                float y[V], n[V];
+                Vec<T>::unpack(qy[i], y);
+                Vec<T>::unpack(qs[i], n);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    n[j] = (n[j] - st.x) * st.y;
+                    dg[i][j] = fmaf(y[j], n[j], dg[i][j]);
+                    db[i][j] += y[j];
+                    const float w = y[j] * g[i][j];
+                    t.x += w;
+                    t.y = fmaf(w, n[j], t.y);
+                }
             }
-            reinterpret_cast<uint4 *>(a.dx + base)[at] = Vec<T>::pack(y);
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) {
+                t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
+                t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
+            }
+            if (a.warps > 1) {
+                if (tid % 32 == 0) sm[k & 1][warp] = t;
+                ptx::named_barrier_sync(1 + group, per_row);
+                t = make_float2(0.f, 0.f);
+                for (int w = 0; w < a.warps; ++w) {
+                    const float2 p = sm[k & 1][group * a.warps + w];
+                    t.x += p.x, t.y += p.y;
+                }
+            }
+            const float mw = t.x * a.inv_d, mwn = t.y * a.inv_d;
+            T *dx = a.dx + (first + (int64_t)k * a.groups + group) * a.d;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = i * per_row + lane;
+                if (!in || c >= vecs) continue;
+                float y[V], n[V];
+                Vec<T>::unpack(qy[i], y);
+                Vec<T>::unpack(qs[i], n);
+#pragma unroll
+                for (int j = 0; j < V; ++j) y[j] = st.y * (fmaf(y[j], g[i][j], -mw) - (n[j] - st.x) * st.y * mwn);
+                if (STREAM) {
+                    float e[V];
+                    Vec<T>::unpack(reinterpret_cast<const uint4 *>(at + 2 * tensor_bytes)[c], e);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) y[j] += e[j];
+                }
+                reinterpret_cast<uint4 *>(dx)[c] = Vec<T>::pack(y);
+            }
+            __syncwarp();
+            if (tid % 32 == 0) ptx::mbar_arrive(empty0 + 8 * s);
+            st = next;
+            if (++s == a.stages) s = 0, ph ^= 1;
         }
     }
     if (!a.part) return;
     float *out = a.part + (int64_t)blockIdx.x * 2 * a.d;
-    if (groups == 1) {
+    if (a.groups == 1) {
+        if (warp < work_warps)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i * per_row + lane < vecs)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        out[(i * per_row + lane) * V + j] = dg[i][j];
+                        out[a.d + (i * per_row + lane) * V + j] = db[i][j];
+                    }
+        return;
+    }
+    __syncthreads();  // the ring is through
+    float *cols = reinterpret_cast<float *>(ring);  // [groups][2][d]
+    if (warp < work_warps)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i * per_row + lane < vecs)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    out[(i * per_row + lane) * V + j] = dg[i][j];
-                    out[a.d + (i * per_row + lane) * V + j] = db[i][j];
+                    cols[group * 2 * a.d + (i * per_row + lane) * V + j] = dg[i][j];
+                    cols[group * 2 * a.d + a.d + (i * per_row + lane) * V + j] = db[i][j];
                 }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (i * per_row + lane < vecs)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                cols[group * 2 * a.d + (i * per_row + lane) * V + j] = dg[i][j];
-                cols[group * 2 * a.d + a.d + (i * per_row + lane) * V + j] = db[i][j];
-            }
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
+    for (int c = tid; c < 2 * a.d; c += blockDim.x) {
         float v = 0.f;
-        for (int k = 0; k < groups; ++k) v += cols[k * 2 * a.d + c];
+        for (int k = 0; k < a.groups; ++k) v += cols[k * 2 * a.d + c];
         out[c] = v;
     }
 }

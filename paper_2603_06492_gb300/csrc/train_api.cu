@@ -33,6 +33,23 @@ noble_status get_status(uint32_t **p)
     return *p ? NOBLE_OK : fail(NOBLE_ERR_CUDA, "status word address");
 }
 
+// Dynamic shared memory up to an SM's for a kernel, once in each context.
+constexpr size_t kMostShared = 225 << 10;
+template <class Kern>
+noble_status allow_shared(Kern kern)
+{
+    static std::mutex mu;
+    static std::vector<std::pair<const void *, CUcontext>> done;
+    const CUcontext ctx = current_context();
+    std::lock_guard<std::mutex> g(mu);
+    for (const auto &e : done)
+        if (ctx && e.first == (const void *)kern && e.second == ctx) return NOBLE_OK;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared) != cudaSuccess)
+        return fail(NOBLE_ERR_CUDA, "shared memory: %s", cudaGetErrorString(cudaGetLastError()));
+    done.emplace_back((const void *)kern, current_context());
+    return NOBLE_OK;
+}
+
 // ---------------------------------------------------------------- layer norm
 noble_status validate(const noble_norm_desc *d)
 {
@@ -47,16 +64,6 @@ noble_status validate(const noble_norm_desc *d)
     return NOBLE_OK;
 }
 
-// f(16-byte pieces of a row per thread, warps of a row)
-template <class F>
-void norm_split(int vecs, int most, F &&f)
-{
-    if (vecs <= 32 || most == 1) f(std::integral_constant<int, 1>{}, (int)ceil_div(vecs, 32));
-    else if (vecs <= 64 || most == 2) f(std::integral_constant<int, 2>{}, (int)ceil_div(vecs, 64));
-    else f(std::integral_constant<int, 4>{}, (int)ceil_div(vecs, 128));
-}
-int norm_groups(int warps) { return std::max(1, norm::kThreads / 32 / warps); }
-
 template <typename T>
 noble_status norm_fwd(const noble_norm_desc *d, const void *x, const void *res, const float *gain, const float *bias,
                       void *sum, void *y, float *stats, cudaStream_t st)
@@ -66,46 +73,64 @@ noble_status norm_fwd(const noble_norm_desc *d, const void *x, const void *res, 
                        // eps 0: a row of equal elements gives 0 times a finite factor
                        std::max(d->eps, 1e-37f)};
     const KernelInfo ki{"norm_fwd", kBoundHbm, 0.0, (double)sizeof(T) * d->T * d->d * (res ? 4 : 2)};
-    return run(st, ki, [&] {
-        norm_split((int)(d->d / norm::Vec<T>::n), 4, [&](auto nv, int warps) {
-            a.warps = warps;
-            const int groups = norm_groups(warps);
-            const dim3 grid((unsigned)ceil_div(d->T, groups)), block(32 * warps * groups);
+    // a warp per row as far as four pieces a lane go; where there are few rows, eight warps a row
+    const int vecs = (int)(d->d / norm::Vec<T>::n), least = (int)ceil_div(vecs, 32 * norm::kMaxVecs);
+    a.warps = d->T < 4 * kSms ? std::max(least, std::min(norm::kWarps, (int)ceil_div(vecs, 32))) : least;
+    const int groups = std::max(1, norm::kWarps / a.warps);
+    const dim3 grid((unsigned)ceil_div(d->T, groups)), block(32 * a.warps * groups);
+    auto launch = [&](auto nv) {
+        return run(st, ki, [&] {
             if (res) norm::fwd_kernel<T, nv.value, true><<<grid, block, 0, st>>>(a);
             else norm::fwd_kernel<T, nv.value, false><<<grid, block, 0, st>>>(a);
         });
-    });
+    };
+    switch (ceil_div(vecs, 32 * a.warps)) {
+    case 1: return launch(std::integral_constant<int, 1>{});
+    case 2: return launch(std::integral_constant<int, 2>{});
+    case 3: return launch(std::integral_constant<int, 3>{});
+    default: return launch(std::integral_constant<int, 4>{});
+    }
 }
 
-// Rows of a part of the sums for dgain and dbias: about two blocks per SM, and at most 512, so that
-// sums of like rows stay short.
+// Rows of a part of the sums for dgain and dbias: a block per SM, and at most 512, so that sums of
+// like rows stay short.
 int norm_rows_per_part(const noble_norm_desc *d)
 {
-    return (int)std::min<int64_t>(512, std::max<int64_t>(8, ceil_div(d->T, 2 * kSms)));
+    return (int)std::min<int64_t>(512, std::max<int64_t>(4, ceil_div(d->T, kSms)));
 }
 
 template <typename T>
 noble_status norm_bwd(const noble_norm_desc *d, const void *dy, const void *s, const float *stats, const float *gain,
                       const void *dstream, void *dx, float *dgain, float *dbias, void *workspace, cudaStream_t st)
 {
-    norm::BwdArgs<T> a{static_cast<const T *>(dy), static_cast<const T *>(s), static_cast<const T *>(dstream),
-                       reinterpret_cast<const float2 *>(stats), gain, static_cast<T *>(dx),
-                       dgain || dbias ? static_cast<float *>(workspace) : nullptr, d->T, (int)d->d, 0,
-                       norm_rows_per_part(d), 1.f / (float)d->d};
+    norm::BwdArgs<T> a{};
+    a.dy = static_cast<const T *>(dy), a.s = static_cast<const T *>(s), a.dstream = static_cast<const T *>(dstream);
+    a.stats = reinterpret_cast<const float2 *>(stats), a.gain = gain, a.dx = static_cast<T *>(dx);
+    a.part = dgain || dbias ? static_cast<float *>(workspace) : nullptr;
+    NOBLE_TRY(get_status(&a.status));
+    a.rows = d->T, a.d = (int)d->d, a.rows_per_part = norm_rows_per_part(d), a.inv_d = 1.f / (float)d->d;
     const int64_t parts = ceil_div(d->T, a.rows_per_part);
     const KernelInfo ki{"norm_bwd", kBoundHbm, 0.0, (double)sizeof(T) * d->T * d->d * (dstream ? 4 : 3)};
-    NOBLE_TRY(run(st, ki, [&] {
-        norm_split((int)(d->d / norm::Vec<T>::n), 16 / norm::Vec<T>::n, [&](auto nv, int warps) {
-            a.warps = warps;
-            const int groups = norm_groups(warps);
-            const size_t smem = groups > 1 ? (size_t)groups * 2 * d->d * 4 : 0;
-            const dim3 grid((unsigned)parts), block(32 * warps * groups);
-            if constexpr (nv.value * norm::Vec<T>::n <= 16) {
-                if (dstream) norm::bwd_kernel<T, nv.value, true><<<grid, block, smem, st>>>(a);
-                else norm::bwd_kernel<T, nv.value, false><<<grid, block, smem, st>>>(a);
-            }
-        });
-    }));
+    // columns of a thread: 16, or half of it where fewer lanes then stay idle, or all that a row needs
+    const int vecs = a.d / norm::Vec<T>::n, one = 16 / norm::Vec<T>::n;
+    const int warps1 = (int)ceil_div(vecs, 32 * one / 2), warps2 = (int)ceil_div(vecs, 32 * one);
+    const int per = warps2 > norm::kBwdWarps ? 2 * one : warps1 <= norm::kBwdWarps && warps1 < 2 * warps2 ? one / 2 : one;
+    a.warps = (int)ceil_div(vecs, 32 * per);
+    a.groups = std::max(1, std::min<int>(norm::kBwdWarps / a.warps, a.rows_per_part));
+    const uint32_t stage = (uint32_t)a.groups * (uint32_t)a.d * (uint32_t)sizeof(T) * (dstream ? 3 : 2);
+    a.stages = (int)std::max<uint32_t>(1, std::min<uint32_t>({norm::kBwdRing / stage, 32u, (uint32_t)ceil_div(a.rows_per_part, a.groups)}));
+    const size_t smem = std::max<size_t>((size_t)a.stages * stage, a.groups > 1 ? (size_t)a.groups * 2 * a.d * 4 : 0);
+    auto launch = [&](auto kern) -> noble_status {
+        NOBLE_TRY(allow_shared(kern));
+        return run(st, ki, [&] { kern<<<(unsigned)parts, 32 * (a.warps * a.groups + 1), smem, st>>>(a); });
+    };
+    auto with = [&](auto nv) {
+        return dstream ? launch(norm::bwd_kernel<T, nv.value, true>) : launch(norm::bwd_kernel<T, nv.value, false>);
+    };
+    constexpr int kOne = 16 / norm::Vec<T>::n;
+    if (per == kOne / 2) NOBLE_TRY(with(std::integral_constant<int, kOne / 2>{}));
+    else if (per == kOne) NOBLE_TRY(with(std::integral_constant<int, kOne>{}));
+    else NOBLE_TRY(with(std::integral_constant<int, 2 * kOne>{}));
     if (!a.part) return NOBLE_OK;
     SplitJobs J{};
     for (float *out : {dgain, dbias}) {
@@ -185,6 +210,7 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
     embed::BwdArgs<T> a{};
     a.ids = ids, a.dy = static_cast<const T *>(dy), a.dtable = dtable;
     a.tokens = d->T, a.vocab = (int)d->vocab, a.d = (int)d->d, a.scale = d->scale;
+    a.wide = reinterpret_cast<uintptr_t>(dtable) % 32 == 0;
     NOBLE_TRY(get_status(&a.status));
     const int vecs = (int)(d->d / norm::Vec<T>::n);
     const unsigned slices = (unsigned)ceil_div(vecs, 32);
@@ -199,22 +225,32 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
     a.head = at(w.head), a.count = at(w.count), a.begin = at(w.begin), a.rank = at(w.rank), a.list = at(w.list);
     a.long_row = at(w.long_row), a.long_at = at(w.long_at);
     a.piece = reinterpret_cast<uint2 *>(ws + w.piece), a.part = reinterpret_cast<float *>(ws + w.part);
-    if (memset_async(ws, 0, w.count + 4 * (size_t)d->vocab, st) != cudaSuccess)
-        return fail(NOBLE_ERR_CUDA, "memset: %s", cudaGetErrorString(cudaGetLastError()));
-    const unsigned per_token = (unsigned)ceil_div(d->T, 256), per_row = (unsigned)ceil_div(d->vocab, 256);
-    const KernelInfo index{"embed_index", kBoundHbm, 0.0, 0.0};
-    NOBLE_TRY(run(st, index, [&] { embed::count_kernel<T><<<per_token, 256, 0, st>>>(a); }));
-    NOBLE_TRY(run(st, index, [&] { embed::lists_kernel<T><<<per_row, 256, 0, st>>>(a); }));
-    NOBLE_TRY(run(st, index, [&] { embed::place_kernel<T><<<per_token, 256, 0, st>>>(a); }));
+    const KernelInfo index{"embed_index", kBoundHbm, 0.0, 0.0}, sum{"embed_sum", kBoundHbm, 0.0, in + out};
+    const auto launch = [&](const KernelInfo &ki, auto kern, dim3 grid, size_t smem, unsigned threads = 256) {
+        const bool pdl = pdl_ok();
+        return run(st, ki, [&] { launch_maybe_pdl(kern, grid, dim3(threads), smem, st, pdl, a); });
+    };
+    const unsigned lists = (unsigned)(d->T / embed::kShort);
     const size_t bits = (size_t)std::min<int64_t>(embed::kWindow, (int64_t)align_up((size_t)d->T, 32)) / 8;
-    NOBLE_TRY(run(st, index, [&] { embed::order_kernel<T><<<4 * kSms, 256, bits, st>>>(a); }));
-    NOBLE_TRY(run(st, {"embed_sum", kBoundHbm, 0.0, in + out}, [&] {
-        const int64_t blocks = ceil_div(d->vocab + d->T / embed::kShort, 8);
-        embed::sum_kernel<T><<<dim3((unsigned)std::min<int64_t>(blocks, 1 << 16), std::min(slices, 64u)), 256, 0, st>>>(a);
-    }));
-    return run(st, {"embed_join", kBoundHbm, 0.0, 0.0}, [&] {
-        embed::join_kernel<T><<<dim3(kSms, (unsigned)std::min<int64_t>(ceil_div(d->d, 1024), 64)), 256, 0, st>>>(a);
-    });
+    if (d->T <= embed::kIndexMost && d->vocab <= embed::kIndexMost) {
+        NOBLE_TRY(launch(index, embed::index_kernel<T>, dim3(embed::kIndexBlocks), 0, embed::kIndexThreads));
+    } else {
+        if (memset_async(ws, 0, w.count + 4 * (size_t)d->vocab, st) != cudaSuccess)
+            return fail(NOBLE_ERR_CUDA, "memset: %s", cudaGetErrorString(cudaGetLastError()));
+        const unsigned per_token = (unsigned)ceil_div(d->T, 256);
+        NOBLE_TRY(launch(index, embed::count_kernel<T>, dim3(per_token), 0));
+        NOBLE_TRY(launch(index, embed::lists_kernel<T>, dim3((unsigned)ceil_div(d->vocab, 256)), 0));
+        NOBLE_TRY(launch(index, embed::place_kernel<T>, dim3(per_token), 0));
+    }
+    NOBLE_TRY(launch(index, embed::order_kernel<T>, dim3(std::min(lists, 4u * kSms)), bits));
+    // rows of a warp: as many as leave every SM 16 warps; pieces of long lists come first
+    a.rows_per_warp = (int)std::max<int64_t>(1, std::min<int64_t>(4, d->vocab / (16 * kSms)));
+    a.piece_blocks = (int)ceil_div(lists, 8);
+    const int64_t blocks = a.piece_blocks + ceil_div(d->vocab, 8 * a.rows_per_warp);
+    // columns in parts where rows alone are too few warps
+    const unsigned parts = a.rows_per_warp > 1 ? 1 : std::min(slices, 64u);
+    NOBLE_TRY(launch(sum, embed::sum_kernel<T>, dim3((unsigned)blocks, parts), 0));
+    return launch(sum, embed::join_kernel<T>, dim3(std::min(lists, 2u * kSms), (unsigned)std::min<int64_t>(ceil_div(d->d, 128), 64)), 0);
 }
 
 // ---------------------------------------------------------------- orthogonalised momentum
