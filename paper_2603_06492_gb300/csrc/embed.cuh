@@ -246,14 +246,25 @@ __device__ __forceinline__ void count_tokens(const BwdArgs<T> &a, int64_t thread
     }
 }
 
-// where each row's list begins; long lists and their pieces
+// where each row's list begins, eight rows to a thread; long lists and their pieces
 template <typename T>
 __device__ __forceinline__ void begin_lists(const BwdArgs<T> &a, int64_t thread, int64_t threads)
 {
     const int lane = threadIdx.x % 32;
-    for (int64_t v = thread; v - lane < a.vocab; v += threads) {
-        const uint32_t n = v < a.vocab ? __ldcg(a.count + v) : 0;
-        uint32_t upto = n;
+    for (int64_t v = 8 * thread; v - 8 * lane < a.vocab; v += 8 * threads) {
+        uint32_t n[8], mine = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (v + 4 * h < a.vocab) q = __ldcg(reinterpret_cast<const uint4 *>(a.count + v) + h);
+            n[4 * h] = q.x, n[4 * h + 1] = q.y, n[4 * h + 2] = q.z, n[4 * h + 3] = q.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (v + i >= a.vocab) n[i] = 0;  // behind the last row
+            mine += n[i];
+        }
+        uint32_t upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
             const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
@@ -261,13 +272,19 @@ __device__ __forceinline__ void begin_lists(const BwdArgs<T> &a, int64_t thread,
         }
         uint32_t base = 0;
         if (lane == 31 && upto) base = atomicAdd(a.head, upto);
-        base = __shfl_sync(0xffffffffu, base, 31);
-        if (n) a.begin[v] = base + upto - n;
-        if (n > kShort) {
-            const uint32_t l = atomicAdd(a.head + 1, 1u), pieces = (n + kPiece - 1) / kPiece, p = atomicAdd(a.head + 2, pieces);
-            a.long_row[l] = (uint32_t)v;
-            a.long_at[l] = p;
-            for (uint32_t k = 0; k < pieces; ++k) a.piece[p + k] = make_uint2((uint32_t)v, k);
+        base = __shfl_sync(0xffffffffu, base, 31) + upto - mine;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t c = n[i];
+            if (!c) continue;
+            a.begin[v + i] = base;
+            base += c;
+            if (c > kShort) {
+                const uint32_t l = atomicAdd(a.head + 1, 1u), pieces = (c + kPiece - 1) / kPiece, p = atomicAdd(a.head + 2, pieces);
+                a.long_row[l] = (uint32_t)(v + i);
+                a.long_at[l] = p;
+                for (uint32_t k = 0; k < pieces; ++k) a.piece[p + k] = make_uint2((uint32_t)(v + i), k);
+            }
         }
     }
 }
@@ -347,7 +364,7 @@ __global__ void __launch_bounds__(256) order_kernel(const BwdArgs<T> a)
 
 // The first three by one cluster of eight blocks, which wait for each other at the cluster's barrier.
 constexpr int kIndexBlocks = 8, kIndexThreads = 1024;
-constexpr int64_t kIndexMost = 1 << 17;  // tokens, and rows of the table: beyond, a launch each
+constexpr int64_t kIndexTokens = 1 << 14, kIndexRows = 1 << 16;  // beyond, a launch each
 template <typename T>
 __global__ void __cluster_dims__(kIndexBlocks, 1, 1) __launch_bounds__(kIndexThreads) index_kernel(const BwdArgs<T> a)
 {
@@ -359,7 +376,7 @@ __global__ void __cluster_dims__(kIndexBlocks, 1, 1) __launch_bounds__(kIndexThr
         __syncthreads();
         cluster::sync();
     };
-    for (int64_t v = thread; v < a.vocab; v += threads) a.count[v] = 0;
+    for (int64_t v = thread; 4 * v < a.vocab; v += threads) reinterpret_cast<uint4 *>(a.count)[v] = make_uint4(0, 0, 0, 0);
     if (thread < 4) a.head[thread] = 0;
     all();
     count_tokens(a, thread, threads);
@@ -402,14 +419,16 @@ __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs<T> a)
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, vecs = a.d / V;
     const int at0 = blockIdx.y * 32 + lane, step = gridDim.y * 32;
     if ((int)blockIdx.x < a.piece_blocks) {
-        const uint32_t w = blockIdx.x * 8 + warp;
-        if (w >= a.head[2]) return;
-        const uint2 p = a.piece[w];
+        if (blockIdx.y) return;
+        // 32 vectors of a piece to a warp
+        const uint32_t w = blockIdx.x * 8 + warp, slices = (vecs + 31) / 32, piece = w / slices;
+        if (piece >= a.head[2]) return;
+        const uint2 p = a.piece[piece];
         const uint32_t begin = a.begin[p.x] + p.y * kPiece;
-        const int n = (int)min((uint32_t)kPiece, a.count[p.x] - p.y * kPiece);
+        const int n = (int)min((uint32_t)kPiece, a.count[p.x] - p.y * kPiece), at = (int)(w % slices) * 32 + lane;
         for (int k = lane; k < n; k += 32) order[warp][k] = a.rank[begin + k];
         __syncwarp();
-        sum_row(a, order[warp], n, at0, step, a.part + (int64_t)w * a.d, 1.f);
+        if (at < vecs) sum_vectors<1, 8>(a, order[warp], n, at, a.part + (int64_t)piece * a.d, 1.f);
         return;
     }
     // counts of this warp's rows, a lane each

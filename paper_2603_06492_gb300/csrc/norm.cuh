@@ -15,8 +15,12 @@
 namespace noble {
 namespace norm {
 
-constexpr int kWarps = 8;    // of a block of the forward, unless a row takes more
-constexpr int kMaxVecs = 4;  // 16-byte pieces of a row that a thread of the forward holds
+// The backward's rows go through a ring in shared memory: a warp of the block keeps it full by bulk
+// copies, up to kRingWarps others compute.  What bounds the pass is HBM, and rows on their way in
+// registers are too few of them beside the sums over rows (50432 x 768 106 us without the ring).
+constexpr int kRingWarps = 15;              // 16 warps in all leave 128 registers to each thread
+constexpr uint32_t kRingBytes = 200 << 10;  // at most
+constexpr int kRingStages = 32;             // at most
 
 // 16 bytes of operands as floats and back
 template <typename T> struct Vec;
@@ -56,28 +60,6 @@ __device__ __forceinline__ void load_floats(const float *p, int64_t at, float (&
     }
 }
 
-// Sums of N values each over the threads of a row, `warps` of them from a multiple of it on:
-// every thread gets them.  sm: N floats for each warp of the block.
-template <int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], int warps, float *sm)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if (warps == 1) return;
-    const int warp = threadIdx.x / 32, first = warp / warps * warps;
-    if (threadIdx.x % 32 == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) sm[warp * N + i] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.f;
-    for (int w = 0; w < warps; ++w)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += sm[(first + w) * N + i];
-}
-
 template <typename T>
 struct FwdArgs {
     const T *x, *res;
@@ -85,81 +67,149 @@ struct FwdArgs {
     T *sum, *y;
     float2 *stats;
     int64_t rows;
-    int d, warps;  // warps: of a row
-    float inv_d, eps;
+    int d, warps, groups;  // warps: of a row; groups: rows of a block at a time
+    float eps;
 };
 
-template <typename T, int NV, bool RES>
-__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 1024) fwd_kernel(const FwdArgs<T> a)
+// What warps know of their parts of a row: elements, their mean, and the squares off it.
+struct Moments {
+    float n, mean, squares;
+};
+__device__ __forceinline__ Moments join(const Moments *p, int warps)
+{
+    Moments m{0.f, 0.f, 0.f};
+    for (int w = 0; w < warps; ++w) m.n += p[w].n, m.mean += p[w].n * p[w].mean;
+    m.mean /= m.n;
+    for (int w = 0; w < warps; ++w) {
+        const float off = p[w].mean - m.mean;
+        m.squares += fmaf(p[w].n * off, off, p[w].squares);
+    }
+    return m;
+}
+
+// Blocks of a.groups rows at a time, which take a row after another; the next one's loads are on their
+// way while a row is normed.  KEEP: gain and bias stay in registers, or they cost more of L1 than the
+// rows (50432 x 768: 33 us).
+template <typename T, int NV, bool RES, bool KEEP>
+__global__ void __launch_bounds__(512) fwd_kernel(const FwdArgs<T> a)
 {
     constexpr int V = Vec<T>::n;
-    __shared__ float sm[2][32];
-    const int per_row = a.warps * 32, lane = threadIdx.x % per_row;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / per_row) + threadIdx.x / per_row;
-    const int vecs = row < a.rows ? a.d / V : 0;
-    const int64_t base = row * a.d;
-    uint4 q[NV];
-    float f[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = i * per_row + lane;
-        q[i] = make_uint4(0, 0, 0, 0);
-        if (at < vecs) q[i] = reinterpret_cast<const uint4 *>(a.x + base)[at];
-    }
-    if constexpr (RES) {
-        uint4 p[NV];
+    __shared__ Moments sm[2][16];
+    const int step = a.warps * 32, group = threadIdx.x / step, lane = threadIdx.x - group * step, vecs = a.d / V;
+    const int64_t stride = (int64_t)gridDim.x * a.groups;
+    uint4 q[NV], p[NV];
+    auto load = [&](int64_t row) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = i * per_row + lane;
-            p[i] = make_uint4(0, 0, 0, 0);
-            if (at < vecs) p[i] = reinterpret_cast<const uint4 *>(a.res + base)[at];
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float g[V];
-            Vec<T>::unpack(q[i], f[i]);
-            Vec<T>::unpack(p[i], g);
-#pragma unroll
-            for (int j = 0; j < V; ++j) f[i][j] += g[j];
-            q[i] = Vec<T>::pack(f[i]);
-        }
-    }
-    float s[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        Vec<T>::unpack(q[i], f[i]);  // the stream as it is stored
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[0] += f[i][j];
-    }
-    row_sums(s, a.warps, sm[0]);
-    const float mean = s[0] * a.inv_d;
-    s[0] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (i * per_row + lane < vecs)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                f[i][j] -= mean;
-                s[0] = fmaf(f[i][j], f[i][j], s[0]);
+            const int at = i * step + lane;
+            q[i] = p[i] = make_uint4(0, 0, 0, 0);
+            if (row < a.rows && at < vecs) {
+                q[i] = reinterpret_cast<const uint4 *>(a.x + row * a.d)[at];
+                if (RES) p[i] = reinterpret_cast<const uint4 *>(a.res + row * a.d)[at];
             }
-    row_sums(s, a.warps, sm[1]);
-    const float r = 1.f / sqrtf(fmaf(s[0], a.inv_d, a.eps));
-    if (a.stats && vecs && lane == 0) a.stats[row] = make_float2(mean, r);
+        }
+    };
+    auto affine = [&](int i, float (&g)[V], float (&b)[V]) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = i * per_row + lane;
-        if (at < vecs) {
-            float g[V], b[V];
+        for (int j = 0; j < V; ++j) g[j] = 1.f, b[j] = 0.f;
+        const int at = i * step + lane;
+        if (at < vecs && a.gain) load_floats(a.gain, at * V, g);
+        if (at < vecs && a.bias) load_floats(a.bias, at * V, b);
+    };
+    int64_t row = (int64_t)blockIdx.x * a.groups + group;
+    load(row);
+    float g[KEEP ? NV : 1][V], b[KEEP ? NV : 1][V];
+    if constexpr (KEEP)
 #pragma unroll
-            for (int j = 0; j < V; ++j) g[j] = 1.f, b[j] = 0.f;
-            if (a.gain) load_floats(a.gain, at * V, g);
-            if (a.bias) load_floats(a.bias, at * V, b);
+        for (int i = 0; i < NV; ++i) affine(i, g[i], b[i]);
+    int turn = 0;
+    // every group of a block goes round as often: there is a barrier among its warps only
+    for (int64_t first = (int64_t)blockIdx.x * a.groups; first < a.rows; first += stride, row += stride, turn ^= 1) {
+        const bool in = row < a.rows;
+        float f[NV][V], sum = 0.f, n = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f[i][j] = fmaf(f[i][j] * r, g[j], b[j]);
-            if (RES) reinterpret_cast<uint4 *>(a.sum + base)[at] = q[i];
-            reinterpret_cast<uint4 *>(a.y + base)[at] = Vec<T>::pack(f[i]);
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * step + lane;
+            Vec<T>::unpack(q[i], f[i]);
+            if constexpr (RES) {
+                float r[V];
+                Vec<T>::unpack(p[i], r);
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[i][j] += r[j];
+                const uint4 s = Vec<T>::pack(f[i]);
+                Vec<T>::unpack(s, f[i]);  // the stream as it is stored
+                if (in && at < vecs) reinterpret_cast<uint4 *>(a.sum + row * a.d)[at] = s;
+            }
+            if (at < vecs) n += V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += f[i][j];
+        }
+        load(row + stride);
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            n += __shfl_xor_sync(0xffffffffu, n, o);
+        }
+        Moments m{n, n > 0.f ? sum / n : 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * step + lane < vecs)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float off = f[i][j] - m.mean;
+                    m.squares = fmaf(off, off, m.squares);
+                }
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) m.squares += __shfl_xor_sync(0xffffffffu, m.squares, o);
+        if (a.warps > 1) {
+            if (threadIdx.x % 32 == 0) sm[turn][threadIdx.x / 32] = m;
+            ptx::named_barrier_sync(1 + group, step);
+            m = join(sm[turn] + group * a.warps, a.warps);
+        }
+        if (!in) continue;
+        const float r = 1.f / sqrtf(m.squares / (float)a.d + a.eps);
+        if (a.stats && lane == 0) a.stats[row] = make_float2(m.mean, r);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = i * step + lane;
+            if (at >= vecs) continue;
+            if constexpr (!KEEP) affine(i, g[0], b[0]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[i][j] = fmaf((f[i][j] - m.mean) * r, g[KEEP ? i : 0][j], b[KEEP ? i : 0][j]);
+            reinterpret_cast<uint4 *>(a.y + row * a.d)[at] = Vec<T>::pack(f[i]);
         }
     }
+}
+
+// A bulk copy of contiguous bytes (a multiple of 16) into shared memory.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+                 "r"(bar)
+                 : "memory");
+}
+
+// The ring's loading thread: rows first .. first + rows of up to three tensors, `groups` of them to a
+// stage [tensors][groups][d].
+template <typename T, int N>
+__device__ __forceinline__ void feed(const T *const (&from)[N], int64_t first, int rows, int groups, int d, int stages, uint32_t base,
+                                     uint32_t full0, uint32_t empty0, uint32_t *status)
+{
+    const uint32_t row_bytes = (uint32_t)d * sizeof(T), tensor_bytes = row_bytes * groups;
+    const int steps = (rows + groups - 1) / groups;
+    int s = 0, issued = 0;
+    uint32_t ph = 0;
+    for (; issued < steps; ++issued) {
+        if (!ptx::mbar_wait(empty0 + 8 * s, ph ^ 1, status)) break;
+        const int64_t row = first + (int64_t)issued * groups;
+        const uint32_t n = (uint32_t)min(groups, rows - issued * groups) * row_bytes;
+        ptx::mbar_arrive_expect_tx(full0 + 8 * s, n * N);
+#pragma unroll
+        for (int i = 0; i < N; ++i) bulk_load(base + ((uint32_t)s * N + i) * tensor_bytes, from[i] + row * d, n, full0 + 8 * s);
+        if (++s == stages) s = 0, ph ^= 1;
+    }
+    // no copy may still be landing when the block ends
+    for (int k = max(0, issued - stages); k < issued; ++k) ptx::mbar_wait(full0 + 8 * (k % stages), (k / stages) & 1, nullptr);
 }
 
 template <typename T>
@@ -176,35 +226,22 @@ struct BwdArgs {
     float inv_d;
 };
 
-// warps that compute, at most, beside one that loads: 16 in all leave 128 registers to each thread
-constexpr int kBwdWarps = 15;
-constexpr uint32_t kBwdRing = 200 << 10;  // bytes of rows on their way, at most
-
-// A bulk copy of contiguous bytes (a multiple of 16) into shared memory.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
-                 "r"(bar)
-                 : "memory");
-}
-
-// Block p takes the rows of part p, `groups` of them at a time, out of a ring in shared memory
-// that the last warp keeps full by bulk copies: what bounds the pass is HBM, and rows on their way
-// in registers are too few of them.  A thread has the same columns of every row, whose sums
-// for dgain and dbias it keeps in registers and the block then adds up in order of the groups.
-// (rows of more than 8192 elements: 16 warps, and 32 columns a thread)
+// Block p takes the rows of part p, `groups` of them at a time.  A thread has the same columns of
+// every row, whose sums for dgain and dbias it keeps in registers and the block then adds up in
+// order of the groups.
 template <typename T, int NV, bool STREAM>
-__global__ void __launch_bounds__(32 * (kBwdWarps + (NV * Vec<T>::n > 16 ? 2 : 1)), 1) bwd_kernel(const BwdArgs<T> a)
+__global__ void __launch_bounds__(32 * (kRingWarps + (NV * Vec<T>::n > 24 ? 2 : 1)), 1) bwd_kernel(const BwdArgs<T> a)
 {
-    constexpr int V = Vec<T>::n, kTensors = STREAM ? 3 : 2, kMostStages = 32;
+    constexpr int V = Vec<T>::n, kTensors = STREAM ? 3 : 2;
     extern __shared__ __align__(128) uint8_t ring[];  // [stages][tensors][groups][d], then the sums over rows
-    __shared__ float2 sm[2][kBwdWarps + 1];
-    __shared__ __align__(8) uint64_t bars[2 * kMostStages];
+    __shared__ float2 sm[2][kRingWarps + 1];
+    __shared__ __align__(8) uint64_t bars[2 * kRingStages];
+    ptx::griddep_launch();
     const int warp = threadIdx.x / 32, work_warps = a.warps * a.groups;
     const int64_t first = (int64_t)blockIdx.x * a.rows_per_part;
     const int rows = (int)min((int64_t)a.rows_per_part, a.rows - first), steps = (rows + a.groups - 1) / a.groups;
     const uint32_t row_bytes = (uint32_t)a.d * sizeof(T), tensor_bytes = row_bytes * a.groups;
-    const uint32_t base = ptx::smem_u32(ring), full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * kMostStages;
+    const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * kRingStages;
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             ptx::mbar_init(full0 + 8 * i, 1);
@@ -218,21 +255,13 @@ __global__ void __launch_bounds__(32 * (kBwdWarps + (NV * Vec<T>::n > 16 ? 2 : 1
     float dg[NV][V], db[NV][V];
     if (warp == work_warps) {
         if (tid % 32 == 0) {
-            int s = 0;
-            uint32_t ph = 0;
-            for (int k = 0; k < steps; ++k) {
-                if (!ptx::mbar_wait(empty0 + 8 * s, ph ^ 1, a.status)) break;
-                const int64_t row = first + (int64_t)k * a.groups;
-                const uint32_t n = (uint32_t)min(a.groups, rows - k * a.groups) * row_bytes, full = full0 + 8 * s;
-                const uint32_t to = base + (uint32_t)s * kTensors * tensor_bytes;
-                ptx::mbar_arrive_expect_tx(full, n * kTensors);
-                bulk_load(to, a.dy + row * a.d, n, full);
-                bulk_load(to + tensor_bytes, a.s + row * a.d, n, full);
-                if (STREAM) bulk_load(to + 2 * tensor_bytes, a.dstream + row * a.d, n, full);
-                if (++s == a.stages) s = 0, ph ^= 1;
+            if constexpr (STREAM) {
+                const T *const from[3] = {a.dy, a.s, a.dstream};
+                feed(from, first, rows, a.groups, a.d, a.stages, ptx::smem_u32(ring), full0, empty0, a.status);
+            } else {
+                const T *const from[2] = {a.dy, a.s};
+                feed(from, first, rows, a.groups, a.d, a.stages, ptx::smem_u32(ring), full0, empty0, a.status);
             }
-            // no copy may still be landing when the block ends
-            for (int k = max(0, steps - a.stages); k < steps; ++k) ptx::mbar_wait(full0 + 8 * (k % a.stages), (k / a.stages) & 1, nullptr);
         }
     } else if (warp < work_warps) {
         float g[NV][V];
@@ -348,7 +377,11 @@ __global__ void __launch_bounds__(32 * (kBwdWarps + (NV * Vec<T>::n > 16 ? 2 : 1
 }
 
 // dgain and dbias from the parts, in order
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SplitJobs J) { sum_block(J, blockIdx.x); }
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SplitJobs J)
+{
+    ptx::griddep_wait();
+    sum_block(J, blockIdx.x);
+}
 
 }  // namespace norm
 }  // namespace noble

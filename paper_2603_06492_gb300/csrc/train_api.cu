@@ -68,27 +68,36 @@ template <typename T>
 noble_status norm_fwd(const noble_norm_desc *d, const void *x, const void *res, const float *gain, const float *bias,
                       void *sum, void *y, float *stats, cudaStream_t st)
 {
-    norm::FwdArgs<T> a{static_cast<const T *>(x), static_cast<const T *>(res), gain, bias, static_cast<T *>(sum),
-                       static_cast<T *>(y), reinterpret_cast<float2 *>(stats), d->T, (int)d->d, 0, 1.f / (float)d->d,
-                       // eps 0: a row of equal elements gives 0 times a finite factor
-                       std::max(d->eps, 1e-37f)};
+    norm::FwdArgs<T> a{};
+    a.x = static_cast<const T *>(x), a.res = static_cast<const T *>(res), a.gain = gain, a.bias = bias;
+    a.sum = static_cast<T *>(sum), a.y = static_cast<T *>(y), a.stats = reinterpret_cast<float2 *>(stats);
+    a.rows = d->T, a.d = (int)d->d;
+    // eps 0: a row of equal elements gives 0 times a finite factor
+    a.eps = std::max(d->eps, 1e-37f);
     const KernelInfo ki{"norm_fwd", kBoundHbm, 0.0, (double)sizeof(T) * d->T * d->d * (res ? 4 : 2)};
-    // a warp per row as far as four pieces a lane go; where there are few rows, eight warps a row
-    const int vecs = (int)(d->d / norm::Vec<T>::n), least = (int)ceil_div(vecs, 32 * norm::kMaxVecs);
-    a.warps = d->T < 4 * kSms ? std::max(least, std::min(norm::kWarps, (int)ceil_div(vecs, 32))) : least;
-    const int groups = std::max(1, norm::kWarps / a.warps);
-    const dim3 grid((unsigned)ceil_div(d->T, groups)), block(32 * a.warps * groups);
-    auto launch = [&](auto nv) {
+    const int vecs = (int)(d->d / norm::Vec<T>::n);
+    constexpr int kMost = 32 / norm::Vec<T>::n;  // vectors of a thread
+    // a warp per row as far as 32 elements a lane go; where there are few rows, eight warps a row
+    const int least = (int)ceil_div(vecs, 32 * kMost);
+    a.warps = d->T < 4 * kSms ? std::max(least, std::min(8, (int)ceil_div(vecs, 32))) : least;
+    a.groups = std::max(1, 8 / a.warps);
+    const int nv = (int)ceil_div(vecs, 32 * a.warps);
+    auto with = [&](auto n) {
+        constexpr bool kKeep = n.value * norm::Vec<T>::n <= 24;
+        // as many blocks as an SM's registers hold
+        constexpr int kBlocks = n.value * norm::Vec<T>::n >= 16 ? 2 : 4;
+        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(d->T, a.groups), kBlocks * kSms)), block(32 * a.warps * a.groups);
         return run(st, ki, [&] {
-            if (res) norm::fwd_kernel<T, nv.value, true><<<grid, block, 0, st>>>(a);
-            else norm::fwd_kernel<T, nv.value, false><<<grid, block, 0, st>>>(a);
+            if (res) norm::fwd_kernel<T, n.value, true, kKeep><<<grid, block, 0, st>>>(a);
+            else norm::fwd_kernel<T, n.value, false, kKeep><<<grid, block, 0, st>>>(a);
         });
     };
-    switch (ceil_div(vecs, 32 * a.warps)) {
-    case 1: return launch(std::integral_constant<int, 1>{});
-    case 2: return launch(std::integral_constant<int, 2>{});
-    case 3: return launch(std::integral_constant<int, 3>{});
-    default: return launch(std::integral_constant<int, 4>{});
+    constexpr int kStep = kMost / 4;
+    switch (ceil_div(nv, kStep)) {
+    case 1: return with(std::integral_constant<int, kStep>{});
+    case 2: return with(std::integral_constant<int, 2 * kStep>{});
+    case 3: return with(std::integral_constant<int, 3 * kStep>{});
+    default: return with(std::integral_constant<int, 4 * kStep>{});
     }
 }
 
@@ -111,14 +120,18 @@ noble_status norm_bwd(const noble_norm_desc *d, const void *dy, const void *s, c
     a.rows = d->T, a.d = (int)d->d, a.rows_per_part = norm_rows_per_part(d), a.inv_d = 1.f / (float)d->d;
     const int64_t parts = ceil_div(d->T, a.rows_per_part);
     const KernelInfo ki{"norm_bwd", kBoundHbm, 0.0, (double)sizeof(T) * d->T * d->d * (dstream ? 4 : 3)};
-    // columns of a thread: 16, or half of it where fewer lanes then stay idle, or all that a row needs
-    const int vecs = a.d / norm::Vec<T>::n, one = 16 / norm::Vec<T>::n;
-    const int warps1 = (int)ceil_div(vecs, 32 * one / 2), warps2 = (int)ceil_div(vecs, 32 * one);
-    const int per = warps2 > norm::kBwdWarps ? 2 * one : warps1 <= norm::kBwdWarps && warps1 < 2 * warps2 ? one / 2 : one;
+    // columns of a thread: 16, or 8 where fewer lanes then stay idle; 24 where a warp then has a row to
+    // itself; 32 where a block's warps reach no further
+    const int vecs = a.d / norm::Vec<T>::n;
+    constexpr int kOne = 16 / norm::Vec<T>::n;
+    const int warps1 = (int)ceil_div(vecs, 32 * kOne / 2), warps2 = (int)ceil_div(vecs, 32 * kOne);
+    const int per = warps2 > norm::kRingWarps ? 2 * kOne
+                    : warps2 == 2 && vecs <= 48 * kOne ? 3 * kOne / 2
+                    : warps1 <= norm::kRingWarps && warps1 < 2 * warps2 ? kOne / 2 : kOne;
     a.warps = (int)ceil_div(vecs, 32 * per);
-    a.groups = std::max(1, std::min<int>(norm::kBwdWarps / a.warps, a.rows_per_part));
+    a.groups = std::max(1, std::min<int>(norm::kRingWarps / a.warps, a.rows_per_part));
     const uint32_t stage = (uint32_t)a.groups * (uint32_t)a.d * (uint32_t)sizeof(T) * (dstream ? 3 : 2);
-    a.stages = (int)std::max<uint32_t>(1, std::min<uint32_t>({norm::kBwdRing / stage, 32u, (uint32_t)ceil_div(a.rows_per_part, a.groups)}));
+    a.stages = (int)std::max<uint32_t>(1, std::min<uint32_t>({norm::kRingBytes / stage, 32u, (uint32_t)ceil_div(a.rows_per_part, a.groups)}));
     const size_t smem = std::max<size_t>((size_t)a.stages * stage, a.groups > 1 ? (size_t)a.groups * 2 * a.d * 4 : 0);
     auto launch = [&](auto kern) -> noble_status {
         NOBLE_TRY(allow_shared(kern));
@@ -127,10 +140,12 @@ noble_status norm_bwd(const noble_norm_desc *d, const void *dy, const void *s, c
     auto with = [&](auto nv) {
         return dstream ? launch(norm::bwd_kernel<T, nv.value, true>) : launch(norm::bwd_kernel<T, nv.value, false>);
     };
-    constexpr int kOne = 16 / norm::Vec<T>::n;
-    if (per == kOne / 2) NOBLE_TRY(with(std::integral_constant<int, kOne / 2>{}));
-    else if (per == kOne) NOBLE_TRY(with(std::integral_constant<int, kOne>{}));
-    else NOBLE_TRY(with(std::integral_constant<int, 2 * kOne>{}));
+    switch (per) {
+    case kOne / 2: NOBLE_TRY(with(std::integral_constant<int, kOne / 2>{})); break;
+    case kOne: NOBLE_TRY(with(std::integral_constant<int, kOne>{})); break;
+    case 3 * kOne / 2: NOBLE_TRY(with(std::integral_constant<int, 3 * kOne / 2>{})); break;
+    default: NOBLE_TRY(with(std::integral_constant<int, 2 * kOne>{}));
+    }
     if (!a.part) return NOBLE_OK;
     SplitJobs J{};
     for (float *out : {dgain, dbias}) {
@@ -141,8 +156,10 @@ noble_status norm_bwd(const noble_norm_desc *d, const void *dy, const void *s, c
         J.begin[j + 1] = J.begin[j] + d->d;
     }
     J.nparts = (int)parts;
-    return run(st, {"norm_join", kBoundHbm, 0.0, 8.0 * parts * d->d},
-               [&] { norm::join_kernel<<<(unsigned)ceil_div(J.begin[J.njobs], 32), 256, 0, st>>>(J); });
+    const bool pdl = pdl_ok();
+    return run(st, {"norm_join", kBoundHbm, 0.0, 8.0 * parts * d->d}, [&] {
+        launch_maybe_pdl(norm::join_kernel, dim3((unsigned)ceil_div(J.begin[J.njobs], 32)), dim3(256), 0, st, pdl, J);
+    });
 }
 
 // ---------------------------------------------------------------- embedding
@@ -232,20 +249,20 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
     };
     const unsigned lists = (unsigned)(d->T / embed::kShort);
     const size_t bits = (size_t)std::min<int64_t>(embed::kWindow, (int64_t)align_up((size_t)d->T, 32)) / 8;
-    if (d->T <= embed::kIndexMost && d->vocab <= embed::kIndexMost) {
+    if (d->T <= embed::kIndexTokens && d->vocab <= embed::kIndexRows) {
         NOBLE_TRY(launch(index, embed::index_kernel<T>, dim3(embed::kIndexBlocks), 0, embed::kIndexThreads));
     } else {
         if (memset_async(ws, 0, w.count + 4 * (size_t)d->vocab, st) != cudaSuccess)
             return fail(NOBLE_ERR_CUDA, "memset: %s", cudaGetErrorString(cudaGetLastError()));
         const unsigned per_token = (unsigned)ceil_div(d->T, 256);
         NOBLE_TRY(launch(index, embed::count_kernel<T>, dim3(per_token), 0));
-        NOBLE_TRY(launch(index, embed::lists_kernel<T>, dim3((unsigned)ceil_div(d->vocab, 256)), 0));
+        NOBLE_TRY(launch(index, embed::lists_kernel<T>, dim3((unsigned)ceil_div(d->vocab, 8 * 256)), 0));
         NOBLE_TRY(launch(index, embed::place_kernel<T>, dim3(per_token), 0));
     }
     NOBLE_TRY(launch(index, embed::order_kernel<T>, dim3(std::min(lists, 4u * kSms)), bits));
     // rows of a warp: as many as leave every SM 16 warps; pieces of long lists come first
     a.rows_per_warp = (int)std::max<int64_t>(1, std::min<int64_t>(4, d->vocab / (16 * kSms)));
-    a.piece_blocks = (int)ceil_div(lists, 8);
+    a.piece_blocks = (int)ceil_div((int64_t)lists * slices, 8);
     const int64_t blocks = a.piece_blocks + ceil_div(d->vocab, 8 * a.rows_per_warp);
     // columns in parts where rows alone are too few warps
     const unsigned parts = a.rows_per_warp > 1 ? 1 : std::min(slices, 64u);

@@ -84,7 +84,10 @@ def _check(T, d, dtype, res=True, gain=True, bias=True, eps=1e-5, seed=0, offset
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("T,d", [(1, 8), (3, 16), (5, 64), (2, 136), (24, 256), (33, 264), (7, 512), (300, 768), (9, 1000), (64, 1024),
-                                 (17, 1032), (11, 2048), (5, 2056), (3, 4096), (2, 5504), (4, 8192), (1, 8200), (2, 16384), (3, 16376)])
+                                 (17, 1032), (11, 2048), (5, 2056), (3, 4096), (2, 5504), (4, 8192), (1, 8200), (2, 16384), (3, 16376),
+                                 # rows through the ring
+                                 (607, 8), (608, 8), (650, 136), (700, 768), (611, 776), (700, 1000), (640, 1032), (609, 2056),
+                                 (608, 4104), (700, 5504), (613, 7680), (609, 7688), (610, 8200), (608, 16384)])
 def test_sizes(T, d, dtype):
     _check(T, d, dtype)
     _check(T, d, dtype, res=False, seed=1)
@@ -102,14 +105,17 @@ def test_rows(T):
     _check(T, 64, "bf16")
 
 
-def test_large_mean():
+@pytest.mark.parametrize("T", [40, 640])
+@pytest.mark.parametrize("d", [512, 2048])
+def test_large_mean(T, d):
     # the variance is of what is left after the mean: 1000 +- 1.5 in fp32
-    _check(40, 512, "fp32", res=False, offset=1000.0)
+    _check(T, d, "fp32", res=False, offset=1000.0)
 
 
-def test_small_values():
-    _check(20, 256, "fp32", eps=1e-30)
-    _check(20, 256, "fp32", eps=0.0)
+@pytest.mark.parametrize("T", [20, 640])
+def test_small_eps(T):
+    _check(T, 256, "fp32", eps=1e-30)
+    _check(T, 256, "fp32", eps=0.0)
 
 
 def test_sums_of_like_rows():
@@ -125,9 +131,10 @@ def test_sums_of_like_rows():
     _close(b.dbias, want, 700 * U * want.abs(), "dbias")
 
 
-def test_non_finite_rows_stay_apart():
+@pytest.mark.parametrize("T", [20, 700])
+def test_non_finite_rows_stay_apart(T):
     from paper_2603_06492_gb300 import layers as L
-    T, d = 20, 256
+    d = 256
     x, r, dy, ds, ga, bi = (t.cuda() for t in _inputs(T, d, "bf16"))
     b = L.NormBuffers(T, d, "bf16", residual=True)
     y0 = L.norm_forward(b, x, ga, bi, res=r).clone()
@@ -140,10 +147,11 @@ def test_non_finite_rows_stay_apart():
     assert y1[3].isnan().all() and y1[7].isnan().all()
 
 
-def test_in_place():
+@pytest.mark.parametrize("T", [37, 1000])
+def test_in_place(T):
     # sum over x, y over res; dx over dy or over dstream
     from paper_2603_06492_gb300 import binding as B, layers as L
-    T, d = 37, 1024
+    d = 1024
     x, r, dy, ds, ga, bi = (t.cuda() for t in _inputs(T, d, "bf16"))
     b = L.NormBuffers(T, d, "bf16", residual=True)
     y0 = L.norm_forward(b, x, ga, bi, res=r).clone()
