@@ -10,15 +10,14 @@
 #pragma once
 
 #include "cluster.cuh"
-#include "sums.cuh"
+#include "common.cuh"
 
 namespace noble {
 namespace norm {
 
 // The backward's rows go through a ring in shared memory: a warp of the block keeps it full by bulk
-// copies, up to kRingWarps others compute.  What bounds the pass is HBM, and rows on their way in
+// copies, up to 15 others compute (16 leave 128 registers to each thread).  What bounds the pass is HBM, and rows on their way in
 // registers are too few of them beside the sums over rows (50432 x 768 106 us without the ring).
-constexpr int kRingWarps = 15;              // 16 warps in all leave 128 registers to each thread
 constexpr uint32_t kRingBytes = 200 << 10;  // at most
 constexpr int kRingStages = 32;             // at most
 
@@ -212,6 +211,9 @@ __device__ __forceinline__ void feed(const T *const (&from)[N], int64_t first, i
     for (int k = max(0, issued - stages); k < issued; ++k) ptx::mbar_wait(full0 + 8 * (k % stages), (k / stages) & 1, nullptr);
 }
 
+// Rows that a group of the backward has in hand, by the columns of a thread.
+__host__ __device__ constexpr int rows_side_by_side(int columns) { return columns <= 8 ? 2 : 1; }
+
 template <typename T>
 struct BwdArgs {
     const T *dy, *s, *dstream;
@@ -226,21 +228,22 @@ struct BwdArgs {
     float inv_d;
 };
 
-// Block p takes the rows of part p, `groups` of them at a time.  A thread has the same columns of
+// Block p takes the rows of part p, R groups' of them at a time.  A thread has the same columns of
 // every row, whose sums for dgain and dbias it keeps in registers and the block then adds up in
-// order of the groups.
-template <typename T, int NV, bool STREAM>
-__global__ void __launch_bounds__(32 * (kRingWarps + (NV * Vec<T>::n > 24 ? 2 : 1)), 1) bwd_kernel(const BwdArgs<T> a)
+// order of the groups.  R: rows of a group side by side, for narrow rows, whose chain of loads, sums
+// over the row and stores is longer than their work.  WARPS: 15 or, where a row takes more, 16.
+template <typename T, int NV, bool STREAM, int WARPS>
+__global__ void __launch_bounds__(32 * (WARPS + 1), 1) bwd_kernel(const BwdArgs<T> a)
 {
-    constexpr int V = Vec<T>::n, kTensors = STREAM ? 3 : 2;
-    extern __shared__ __align__(128) uint8_t ring[];  // [stages][tensors][groups][d], then the sums over rows
-    __shared__ float2 sm[2][kRingWarps + 1];
+    constexpr int V = Vec<T>::n, kTensors = STREAM ? 3 : 2, R = rows_side_by_side(NV * V);
+    extern __shared__ __align__(128) uint8_t ring[];  // [stages][tensors][R groups][d], then the sums over rows
+    __shared__ float2 sm[2][R][WARPS];
     __shared__ __align__(8) uint64_t bars[2 * kRingStages];
     ptx::griddep_launch();
-    const int warp = threadIdx.x / 32, work_warps = a.warps * a.groups;
+    const int warp = threadIdx.x / 32, work_warps = a.warps * a.groups, batch = R * a.groups;
     const int64_t first = (int64_t)blockIdx.x * a.rows_per_part;
-    const int rows = (int)min((int64_t)a.rows_per_part, a.rows - first), steps = (rows + a.groups - 1) / a.groups;
-    const uint32_t row_bytes = (uint32_t)a.d * sizeof(T), tensor_bytes = row_bytes * a.groups;
+    const int rows = (int)min((int64_t)a.rows_per_part, a.rows - first), steps = (rows + batch - 1) / batch;
+    const uint32_t row_bytes = (uint32_t)a.d * sizeof(T), tensor_bytes = row_bytes * batch;
     const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * kRingStages;
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
@@ -257,10 +260,10 @@ __global__ void __launch_bounds__(32 * (kRingWarps + (NV * Vec<T>::n > 24 ? 2 : 
         if (tid % 32 == 0) {
             if constexpr (STREAM) {
                 const T *const from[3] = {a.dy, a.s, a.dstream};
-                feed(from, first, rows, a.groups, a.d, a.stages, ptx::smem_u32(ring), full0, empty0, a.status);
+                feed(from, first, rows, batch, a.d, a.stages, ptx::smem_u32(ring), full0, empty0, a.status);
             } else {
                 const T *const from[2] = {a.dy, a.s};
-                feed(from, first, rows, a.groups, a.d, a.stages, ptx::smem_u32(ring), full0, empty0, a.status);
+                feed(from, first, rows, batch, a.d, a.stages, ptx::smem_u32(ring), full0, empty0, a.status);
             }
         }
     } else if (warp < work_warps) {
@@ -274,72 +277,95 @@ __global__ void __launch_bounds__(32 * (kRingWarps + (NV * Vec<T>::n > 24 ? 2 : 
         int s = 0;
         uint32_t ph = 0;
         bool ok = true;
-        float2 st = group < rows ? a.stats[first + group] : make_float2(0.f, 0.f);
+        auto stats = [&](int k, int h) {  // of row h of this group in step k
+            const int row = k * batch + h * a.groups + group;
+            return row < rows ? a.stats[first + row] : make_float2(0.f, 0.f);
+        };
+        float2 st[R];
+#pragma unroll
+        for (int h = 0; h < R; ++h) st[h] = stats(0, h);
         for (int k = 0; k < steps; ++k) {
-            const bool in = k * a.groups + group < rows;
-            // the next row's statistics, a step ahead
-            const int ahead = (k + 1) * a.groups + group;
-            const float2 next = ahead < rows ? a.stats[first + ahead] : make_float2(0.f, 0.f);
+            float2 next[R];  // the next rows' statistics, a step ahead
+#pragma unroll
+            for (int h = 0; h < R; ++h) next[h] = stats(k + 1, h);
             // a wait that gave up is reported; the barriers below still need every warp
             if (ok) ok = ptx::mbar_wait(full0 + 8 * s, ph, a.status);
             const uint8_t *at = ring + (size_t)s * kTensors * tensor_bytes + group * row_bytes;
-            uint4 qy[NV], qs[NV];
-            float2 t = make_float2(0.f, 0.f);
+            uint4 qy[R][NV], qs[R][NV];
+            float2 t[R];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = i * per_row + lane;
-                if (!in || c >= vecs) continue;
-                qy[i] = reinterpret_cast<const uint4 *>(at)[c];
-                qs[i] = reinterpret_cast<const uint4 *>(at + tensor_bytes)[c];
-                float y[V], n[V];
-                Vec<T>::unpack(qy[i], y);
-                Vec<T>::unpack(qs[i], n);
+            for (int h = 0; h < R; ++h) {
+                t[h] = make_float2(0.f, 0.f);
+                const bool in = k * batch + h * a.groups + group < rows;
+                const uint8_t *row = at + h * a.groups * row_bytes;
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    n[j] = (n[j] - st.x) * st.y;
-                    dg[i][j] = fmaf(y[j], n[j], dg[i][j]);
-                    db[i][j] += y[j];
-                    const float w = y[j] * g[i][j];
-                    t.x += w;
-                    t.y = fmaf(w, n[j], t.y);
+                for (int i = 0; i < NV; ++i) {
+                    const int c = i * per_row + lane;
+                    if (!in || c >= vecs) continue;
+                    qy[h][i] = reinterpret_cast<const uint4 *>(row)[c];
+                    qs[h][i] = reinterpret_cast<const uint4 *>(row + tensor_bytes)[c];
+                    float y[V], n[V];
+                    Vec<T>::unpack(qy[h][i], y);
+                    Vec<T>::unpack(qs[h][i], n);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        n[j] = (n[j] - st[h].x) * st[h].y;
+                        dg[i][j] = fmaf(y[j], n[j], dg[i][j]);
+                        db[i][j] += y[j];
+                        const float w = y[j] * g[i][j];
+                        t[h].x += w;
+                        t[h].y = fmaf(w, n[j], t[h].y);
+                    }
                 }
             }
 #pragma unroll
-            for (int o = 16; o > 0; o /= 2) {
-                t.x += __shfl_xor_sync(0xffffffffu, t.x, o);
-                t.y += __shfl_xor_sync(0xffffffffu, t.y, o);
-            }
+            for (int o = 16; o > 0; o /= 2)
+#pragma unroll
+                for (int h = 0; h < R; ++h) {
+                    t[h].x += __shfl_xor_sync(0xffffffffu, t[h].x, o);
+                    t[h].y += __shfl_xor_sync(0xffffffffu, t[h].y, o);
+                }
             if (a.warps > 1) {
-                if (tid % 32 == 0) sm[k & 1][warp] = t;
+#pragma unroll
+                for (int h = 0; h < R; ++h)
+                    if (tid % 32 == 0) sm[k & 1][h][warp] = t[h];
                 ptx::named_barrier_sync(1 + group, per_row);
-                t = make_float2(0.f, 0.f);
-                for (int w = 0; w < a.warps; ++w) {
-                    const float2 p = sm[k & 1][group * a.warps + w];
-                    t.x += p.x, t.y += p.y;
+#pragma unroll
+                for (int h = 0; h < R; ++h) {
+                    t[h] = make_float2(0.f, 0.f);
+                    for (int w = 0; w < a.warps; ++w) {
+                        const float2 p = sm[k & 1][h][group * a.warps + w];
+                        t[h].x += p.x, t[h].y += p.y;
+                    }
                 }
             }
-            const float mw = t.x * a.inv_d, mwn = t.y * a.inv_d;
-            T *dx = a.dx + (first + (int64_t)k * a.groups + group) * a.d;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = i * per_row + lane;
-                if (!in || c >= vecs) continue;
-                float y[V], n[V];
-                Vec<T>::unpack(qy[i], y);
-                Vec<T>::unpack(qs[i], n);
+            for (int h = 0; h < R; ++h) {
+                const int r = k * batch + h * a.groups + group;
+                const float mw = t[h].x * a.inv_d, mwn = t[h].y * a.inv_d;
+                T *dx = a.dx + (first + r) * a.d;
 #pragma unroll
-                for (int j = 0; j < V; ++j) y[j] = st.y * (fmaf(y[j], g[i][j], -mw) - (n[j] - st.x) * st.y * mwn);
-                if (STREAM) {
-                    float e[V];
-                    Vec<T>::unpack(reinterpret_cast<const uint4 *>(at + 2 * tensor_bytes)[c], e);
+                for (int i = 0; i < NV; ++i) {
+                    const int c = i * per_row + lane;
+                    if (r >= rows || c >= vecs) continue;
+                    float y[V], n[V];
+                    Vec<T>::unpack(qy[h][i], y);
+                    Vec<T>::unpack(qs[h][i], n);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) y[j] += e[j];
+                    for (int j = 0; j < V; ++j)
+                        y[j] = st[h].y * (fmaf(y[j], g[i][j], -mw) - (n[j] - st[h].x) * st[h].y * mwn);
+                    if (STREAM) {
+                        float e[V];
+                        Vec<T>::unpack(reinterpret_cast<const uint4 *>(at + h * a.groups * row_bytes + 2 * tensor_bytes)[c], e);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) y[j] += e[j];
+                    }
+                    reinterpret_cast<uint4 *>(dx)[c] = Vec<T>::pack(y);
                 }
-                reinterpret_cast<uint4 *>(dx)[c] = Vec<T>::pack(y);
+                st[h] = next[h];
             }
             __syncwarp();
             if (tid % 32 == 0) ptx::mbar_arrive(empty0 + 8 * s);
-            st = next;
             if (++s == a.stages) s = 0, ph ^= 1;
         }
     }
@@ -364,9 +390,10 @@ __global__ void __launch_bounds__(32 * (kRingWarps + (NV * Vec<T>::n > 24 ? 2 : 
         for (int i = 0; i < NV; ++i)
             if (i * per_row + lane < vecs)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    cols[group * 2 * a.d + (i * per_row + lane) * V + j] = dg[i][j];
-                    cols[group * 2 * a.d + a.d + (i * per_row + lane) * V + j] = db[i][j];
+                for (int j = 0; j < V; j += 4) {
+                    float *to = cols + group * 2 * a.d + (i * per_row + lane) * V + j;
+                    *reinterpret_cast<float4 *>(to) = make_float4(dg[i][j], dg[i][j + 1], dg[i][j + 2], dg[i][j + 3]);
+                    *reinterpret_cast<float4 *>(to + a.d) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
                 }
     __syncthreads();
     for (int c = tid; c < 2 * a.d; c += blockDim.x) {
@@ -376,11 +403,27 @@ __global__ void __launch_bounds__(32 * (kRingWarps + (NV * Vec<T>::n > 24 ? 2 : 
     }
 }
 
-// dgain and dbias from the parts, in order
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SplitJobs J)
+// dgain and dbias from the parts: 32 columns to a block, a range of the parts to each warp, in order;
+// then the ranges in order.  Columns 0 to d are dgain's, the others dbias's; either may be NULL.
+__global__ void __launch_bounds__(1024) join_kernel(const float *part, int parts, int d, float *dgain, float *dbias)
 {
+    __shared__ float sm[32][33];
     ptx::griddep_wait();
-    sum_block(J, blockIdx.x);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, col = blockIdx.x * 32 + lane, per = (parts + 31) / 32;
+    float v = 0.f;
+    if (col < 2 * d) {
+        const int end = min(parts, (warp + 1) * per);
+#pragma unroll 8
+        for (int p = warp * per; p < end; ++p) v += part[(int64_t)p * 2 * d + col];
+    }
+    sm[warp][lane] = v;
+    __syncthreads();
+    if (warp != 0 || col >= 2 * d) return;
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 32; ++w) v += sm[w][lane];
+    float *out = col < d ? dgain : dbias;
+    if (out) out[col < d ? col : col - d] = v;
 }
 
 }  // namespace norm

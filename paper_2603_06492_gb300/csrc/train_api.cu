@@ -105,7 +105,7 @@ noble_status norm_fwd(const noble_norm_desc *d, const void *x, const void *res, 
 // like rows stay short.
 int norm_rows_per_part(const noble_norm_desc *d)
 {
-    return (int)std::min<int64_t>(512, std::max<int64_t>(4, ceil_div(d->T, kSms)));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(512, ceil_div(d->T, kSms)));
 }
 
 template <typename T>
@@ -120,45 +120,41 @@ noble_status norm_bwd(const noble_norm_desc *d, const void *dy, const void *s, c
     a.rows = d->T, a.d = (int)d->d, a.rows_per_part = norm_rows_per_part(d), a.inv_d = 1.f / (float)d->d;
     const int64_t parts = ceil_div(d->T, a.rows_per_part);
     const KernelInfo ki{"norm_bwd", kBoundHbm, 0.0, (double)sizeof(T) * d->T * d->d * (dstream ? 4 : 3)};
-    // columns of a thread: 16, or 8 where fewer lanes then stay idle; 24 where a warp then has a row to
-    // itself; 32 where a block's warps reach no further
+    // columns of a thread: 16, or 8 where fewer lanes then stay idle; of bf16 24 where a warp then has a
+    // row to itself (50432 x 768: 46 us, with 8 columns 59); 32 where 16 warps reach no further
     const int vecs = a.d / norm::Vec<T>::n;
-    constexpr int kOne = 16 / norm::Vec<T>::n;
+    constexpr int kOne = 16 / norm::Vec<T>::n, kWide = 3 * kOne / 2;
     const int warps1 = (int)ceil_div(vecs, 32 * kOne / 2), warps2 = (int)ceil_div(vecs, 32 * kOne);
-    const int per = warps2 > norm::kRingWarps ? 2 * kOne
-                    : warps2 == 2 && vecs <= 48 * kOne ? 3 * kOne / 2
-                    : warps1 <= norm::kRingWarps && warps1 < 2 * warps2 ? kOne / 2 : kOne;
+    const int per = warps2 > 16                                            ? 2 * kOne
+                    : sizeof(T) == 2 && warps2 == 2 && vecs <= 32 * kWide ? kWide
+                    : warps1 <= 15 && warps1 < 2 * warps2                 ? kOne / 2
+                                                                          : kOne;
     a.warps = (int)ceil_div(vecs, 32 * per);
-    a.groups = std::max(1, std::min<int>(norm::kRingWarps / a.warps, a.rows_per_part));
-    const uint32_t stage = (uint32_t)a.groups * (uint32_t)a.d * (uint32_t)sizeof(T) * (dstream ? 3 : 2);
-    a.stages = (int)std::max<uint32_t>(1, std::min<uint32_t>({norm::kRingBytes / stage, 32u, (uint32_t)ceil_div(a.rows_per_part, a.groups)}));
+    const int side = norm::rows_side_by_side(per * norm::Vec<T>::n);
+    a.groups = std::max(1, std::min<int>(15 / a.warps, (int)ceil_div(a.rows_per_part, side)));
+    const uint32_t stage = (uint32_t)(side * a.groups) * (uint32_t)a.d * (uint32_t)sizeof(T) * (dstream ? 3 : 2);
+    a.stages = (int)std::max<uint32_t>(1, std::min<uint32_t>({norm::kRingBytes / stage, (uint32_t)norm::kRingStages,
+                                                              (uint32_t)ceil_div(a.rows_per_part, side * a.groups)}));
     const size_t smem = std::max<size_t>((size_t)a.stages * stage, a.groups > 1 ? (size_t)a.groups * 2 * a.d * 4 : 0);
     auto launch = [&](auto kern) -> noble_status {
         NOBLE_TRY(allow_shared(kern));
         return run(st, ki, [&] { kern<<<(unsigned)parts, 32 * (a.warps * a.groups + 1), smem, st>>>(a); });
     };
-    auto with = [&](auto nv) {
-        return dstream ? launch(norm::bwd_kernel<T, nv.value, true>) : launch(norm::bwd_kernel<T, nv.value, false>);
+    auto with = [&](auto nv, auto warps) {
+        return dstream ? launch(norm::bwd_kernel<T, nv.value, true, warps.value>) : launch(norm::bwd_kernel<T, nv.value, false, warps.value>);
     };
-    switch (per) {
-    case kOne / 2: NOBLE_TRY(with(std::integral_constant<int, kOne / 2>{})); break;
-    case kOne: NOBLE_TRY(with(std::integral_constant<int, kOne>{})); break;
-    case 3 * kOne / 2: NOBLE_TRY(with(std::integral_constant<int, 3 * kOne / 2>{})); break;
-    default: NOBLE_TRY(with(std::integral_constant<int, 2 * kOne>{}));
-    }
+    const std::integral_constant<int, 15> most{};
+    const std::integral_constant<int, 16> more{};
+    if (per == kOne / 2) NOBLE_TRY(with(std::integral_constant<int, kOne / 2>{}, most));
+    else if (per == kWide) NOBLE_TRY(with(std::integral_constant<int, sizeof(T) == 2 ? kWide : kOne>{}, most));
+    else if (per == 2 * kOne) NOBLE_TRY(with(std::integral_constant<int, 2 * kOne>{}, more));
+    else if (a.warps == 16) NOBLE_TRY(with(std::integral_constant<int, kOne>{}, more));
+    else NOBLE_TRY(with(std::integral_constant<int, kOne>{}, most));
     if (!a.part) return NOBLE_OK;
-    SplitJobs J{};
-    for (float *out : {dgain, dbias}) {
-        if (!out) continue;
-        const int j = J.njobs++;
-        J.part[j] = a.part + (out == dgain ? 0 : d->d);
-        J.out[j] = out, J.n[j] = d->d, J.stride[j] = 2 * d->d;
-        J.begin[j + 1] = J.begin[j] + d->d;
-    }
-    J.nparts = (int)parts;
     const bool pdl = pdl_ok();
     return run(st, {"norm_join", kBoundHbm, 0.0, 8.0 * parts * d->d}, [&] {
-        launch_maybe_pdl(norm::join_kernel, dim3((unsigned)ceil_div(J.begin[J.njobs], 32)), dim3(256), 0, st, pdl, J);
+        launch_maybe_pdl(norm::join_kernel, dim3((unsigned)ceil_div(2 * d->d, 32)), dim3(1024), 0, st, pdl, (const float *)a.part, (int)parts,
+                         a.d, dgain, dbias);
     });
 }
 
