@@ -85,7 +85,7 @@ __device__ __forceinline__ void store_scaled(float *p, const float (&f)[N], floa
 
 constexpr int kFewTokens = 2048;  // at most so many: one launch
 constexpr int kFewRows = 64;      // rows of the table of a block then
-constexpr int kShort = 32;        // a list of so many tokens is one warp's
+constexpr int kShort = 8;         // a list of so many tokens is one warp's
 constexpr int kPiece = 64;        // tokens of a piece of a longer list
 constexpr int kCompared = 256;    // tokens of a list that is ordered by comparing
 constexpr int kWindow = 1 << 18;  // tokens that a block's bit map covers at a time, for longer ones
@@ -101,11 +101,12 @@ struct BwdArgs {
     uint32_t *status;
     // many tokens: tokens of each row, where its list begins, each token's place in it
     uint32_t *count, *begin, *rank, *list;
-    uint32_t *head;      // [0] tokens listed, [1] long lists, [2] pieces
+    uint32_t *head;      // [0] tokens listed, [1] long lists, [2] their pieces, [3] of several, [4] lists of several
     uint32_t *long_row;  // rows with long lists
-    uint32_t *long_at;   // their first pieces
     uint2 *piece;        // row, which piece of its list
-    float *part;         // [pieces][d]
+    uint32_t *piece_part;  // where the piece's sum goes in `part`; ~0: a list of one piece, to the table
+    uint2 *joined;       // lists of several pieces: row, first of their sums
+    float *part;         // [pieces of lists of several][d]
     int rows_per_warp, piece_blocks;  // of sum_kernel
     int wide;            // dtable is aligned to 32 bytes
 };
@@ -144,15 +145,17 @@ __device__ __forceinline__ void sum_vectors(const BwdArgs<T> &a, const uint32_t 
     for (int c = 0; c < C; ++c)
         if (at + 32 * c < vecs) store_scaled(out + (at + 32 * c) * V, acc[c], scale, a.wide);
 }
-// ... of all vectors from `at` on that are `step` apart, but for the steps within a warp.
+// ... of all vectors from `at` on that are `step` apart, but for the steps within a warp; n <= kShort.
 template <typename T>
 __device__ __forceinline__ void sum_row(const BwdArgs<T> &a, const uint32_t *list, int n, int at, int step, float *out, float scale)
 {
     const int vecs = a.d / Vec<T>::n;
-    if (n <= 4 && step == 32) {
+    if (step != 32) {
+        for (; at < vecs; at += step) sum_vectors<1, 8>(a, list, n, at, out, scale);
+    } else if (n <= 2) {
         for (; at < vecs; at += 4 * 32) sum_vectors<4, 2>(a, list, n, at, out, scale);
     } else {
-        for (; at < vecs; at += step) sum_vectors<1, 8>(a, list, n, at, out, scale);
+        for (; at < vecs; at += 2 * 32) sum_vectors<2, 4>(a, list, n, at, out, scale);
     }
 }
 
@@ -264,26 +267,48 @@ __device__ __forceinline__ void begin_lists(const BwdArgs<T> &a, int64_t thread,
             if (v + i >= a.vocab) n[i] = 0;  // behind the last row
             mine += n[i];
         }
-        uint32_t upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += u;
-        }
-        uint32_t base = 0;
-        if (lane == 31 && upto) base = atomicAdd(a.head, upto);
-        base = __shfl_sync(0xffffffffu, base, 31) + upto - mine;
+        // room for this warp's tokens, lists, pieces: sums over the lanes, one atomic for each kind
+        uint32_t kinds[5] = {mine, 0, 0, 0, 0}, base[5];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t c = n[i];
+            if (n[i] <= kShort) continue;
+            const uint32_t pieces = (n[i] + kPiece - 1) / kPiece;
+            kinds[1] += 1, kinds[2] += pieces;
+            if (pieces > 1) kinds[3] += pieces, kinds[4] += 1;
+        }
+        const int live = __any_sync(0xffffffffu, kinds[1]) ? 5 : 1;
+        uint32_t total = 0;  // in lane k, of kind k
+#pragma unroll
+        for (int k = 0; k < 5; ++k) {
+            if (k >= live) break;
+            uint32_t upto = kinds[k];
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += u;
+            }
+            const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
+            if (lane == k) total = all;
+            base[k] = upto - kinds[k];
+        }
+        uint32_t room = 0;
+        if (total) room = atomicAdd(a.head + lane, total);
+#pragma unroll
+        for (int k = 0; k < 5; ++k)
+            if (k < live) base[k] += __shfl_sync(0xffffffffu, room, k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t c = n[i], row = (uint32_t)(v + i);
             if (!c) continue;
-            a.begin[v + i] = base;
-            base += c;
-            if (c > kShort) {
-                const uint32_t l = atomicAdd(a.head + 1, 1u), pieces = (c + kPiece - 1) / kPiece, p = atomicAdd(a.head + 2, pieces);
-                a.long_row[l] = (uint32_t)(v + i);
-                a.long_at[l] = p;
-                for (uint32_t k = 0; k < pieces; ++k) a.piece[p + k] = make_uint2((uint32_t)(v + i), k);
+            a.begin[v + i] = base[0];
+            base[0] += c;
+            if (c <= kShort) continue;
+            const uint32_t pieces = (c + kPiece - 1) / kPiece;
+            a.long_row[base[1]++] = row;
+            if (pieces > 1) a.joined[base[4]++] = make_uint2(row, base[3]);
+            for (uint32_t k = 0; k < pieces; ++k) {
+                a.piece[base[2]] = make_uint2(row, k);
+                a.piece_part[base[2]++] = pieces > 1 ? base[3]++ : ~0u;
             }
         }
     }
@@ -377,7 +402,7 @@ __global__ void __cluster_dims__(kIndexBlocks, 1, 1) __launch_bounds__(kIndexThr
         cluster::sync();
     };
     for (int64_t v = thread; 4 * v < a.vocab; v += threads) reinterpret_cast<uint4 *>(a.count)[v] = make_uint4(0, 0, 0, 0);
-    if (thread < 4) a.head[thread] = 0;
+    if (thread < 8) a.head[thread] = 0;
     all();
     count_tokens(a, thread, threads);
     all();
@@ -407,8 +432,8 @@ __global__ void __launch_bounds__(256) place_kernel(const BwdArgs<T> a)
     ptx::griddep_wait();
     place_tokens(a, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
 }
-// A warp for rows_per_warp rows of the table with short lists, or none, and one for each piece of a
-// long list, which come first.  blockIdx.y: columns, 32 vectors at a time.
+// A warp for rows_per_warp rows of the table with short lists, or none; the first blocks take the
+// pieces of long lists.  blockIdx.y: columns, 32 vectors at a time.
 template <typename T>
 __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs<T> a)
 {
@@ -421,14 +446,19 @@ __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs<T> a)
     if ((int)blockIdx.x < a.piece_blocks) {
         if (blockIdx.y) return;
         // 32 vectors of a piece to a warp
-        const uint32_t w = blockIdx.x * 8 + warp, slices = (vecs + 31) / 32, piece = w / slices;
-        if (piece >= a.head[2]) return;
-        const uint2 p = a.piece[piece];
-        const uint32_t begin = a.begin[p.x] + p.y * kPiece;
-        const int n = (int)min((uint32_t)kPiece, a.count[p.x] - p.y * kPiece), at = (int)(w % slices) * 32 + lane;
-        for (int k = lane; k < n; k += 32) order[warp][k] = a.rank[begin + k];
-        __syncwarp();
-        if (at < vecs) sum_vectors<1, 8>(a, order[warp], n, at, a.part + (int64_t)piece * a.d, 1.f);
+        const uint32_t slices = (vecs + 31) / 32;
+        const uint64_t work = (uint64_t)a.head[2] * slices;
+        for (uint64_t w = blockIdx.x * 8 + warp; w < work; w += (uint64_t)a.piece_blocks * 8) {
+            const uint32_t piece = (uint32_t)(w / slices), part = a.piece_part[piece];
+            const uint2 p = a.piece[piece];
+            const uint32_t begin = a.begin[p.x] + p.y * kPiece;
+            const int n = (int)min((uint32_t)kPiece, a.count[p.x] - p.y * kPiece), at = (int)(w - (uint64_t)piece * slices) * 32 + lane;
+            __syncwarp();
+            for (int k = lane; k < n; k += 32) order[warp][k] = a.rank[begin + k];
+            __syncwarp();
+            float *out = part == ~0u ? a.dtable + (int64_t)p.x * a.d : a.part + (int64_t)part * a.d;
+            if (at < vecs) sum_vectors<1, 8>(a, order[warp], n, at, out, part == ~0u ? a.scale : 1.f);
+        }
         return;
     }
     // counts of this warp's rows, a lane each
@@ -456,7 +486,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs<T> a)
     }
 }
 
-// The pieces of each long list: 128 columns of a list to a block, an eighth of the pieces to a
+// The pieces of each list of several: 128 columns of a list to a block, an eighth of the pieces to a
 // warp, in order; then the eighths in order.
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const BwdArgs<T> a)
@@ -464,9 +494,9 @@ __global__ void __launch_bounds__(256) join_kernel(const BwdArgs<T> a)
     __shared__ float4 sm[8][32];
     ptx::griddep_wait();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, quads = a.d / 4;
-    for (uint32_t l = blockIdx.x; l < a.head[1]; l += gridDim.x) {
-        const uint32_t row = a.long_row[l], pieces = (a.count[row] + kPiece - 1) / kPiece, per = (pieces + 7) / 8;
-        const float *part = a.part + (int64_t)a.long_at[l] * a.d;
+    for (uint32_t l = blockIdx.x; l < a.head[4]; l += gridDim.x) {
+        const uint32_t row = a.joined[l].x, pieces = (a.count[row] + kPiece - 1) / kPiece, per = (pieces + 7) / 8;
+        const float *part = a.part + (int64_t)a.joined[l].y * a.d;
         for (int q0 = blockIdx.y * 32; q0 < quads; q0 += gridDim.y * 32) {
             const int at = q0 + lane;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);

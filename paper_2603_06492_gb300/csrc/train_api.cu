@@ -173,7 +173,7 @@ noble_status validate(const noble_embed_desc *d)
 }
 
 struct EmbedWork {
-    size_t count, head, begin, rank, list, long_row, long_at, piece, part, total;
+    size_t count, head, begin, rank, list, long_row, piece, piece_part, joined, part, total;
 };
 EmbedWork embed_work(const noble_embed_desc *d)
 {
@@ -188,19 +188,19 @@ EmbedWork embed_work(const noble_embed_desc *d)
         at = align_up(at + bytes, 256);
         return p;
     };
-    // long lists have at least kShort + 1 tokens, so that there are at most T / kShort of them, and of
-    // pieces
-    const size_t T = (size_t)d->T, V = (size_t)d->vocab, lists = T / embed::kShort + 1;
-    static_assert(embed::kPiece >= 2 * embed::kShort, "a list of n > kShort tokens has at most n / kShort pieces");
-    w.head = take(16);
+    // a long list has more than kShort tokens, and no more pieces than a (kShort + 1)th of them; one of
+    // several pieces has more than kPiece tokens, and fewer pieces than a 32nd of them
+    const size_t T = (size_t)d->T, V = (size_t)d->vocab, lists = T / (embed::kShort + 1) + 1, parts = T / (embed::kPiece / 2) + 1;
+    w.head = take(32);
     w.count = take(4 * V);
     w.begin = take(4 * V);
     w.rank = take(4 * T);
     w.list = take(4 * T);
     w.long_row = take(4 * lists);
-    w.long_at = take(4 * lists);
     w.piece = take(8 * lists);
-    w.part = take(4 * lists * (size_t)d->d);
+    w.piece_part = take(4 * lists);
+    w.joined = take(8 * (T / embed::kPiece + 1));
+    w.part = take(4 * parts * (size_t)d->d);
     w.total = at;
     return w;
 }
@@ -236,14 +236,14 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
     char *ws = static_cast<char *>(workspace);
     auto at = [&](size_t off) { return reinterpret_cast<uint32_t *>(ws + off); };
     a.head = at(w.head), a.count = at(w.count), a.begin = at(w.begin), a.rank = at(w.rank), a.list = at(w.list);
-    a.long_row = at(w.long_row), a.long_at = at(w.long_at);
+    a.long_row = at(w.long_row), a.piece_part = at(w.piece_part), a.joined = reinterpret_cast<uint2 *>(ws + w.joined);
     a.piece = reinterpret_cast<uint2 *>(ws + w.piece), a.part = reinterpret_cast<float *>(ws + w.part);
     const KernelInfo index{"embed_index", kBoundHbm, 0.0, 0.0}, sum{"embed_sum", kBoundHbm, 0.0, in + out};
     const auto launch = [&](const KernelInfo &ki, auto kern, dim3 grid, size_t smem, unsigned threads = 256) {
         const bool pdl = pdl_ok();
         return run(st, ki, [&] { launch_maybe_pdl(kern, grid, dim3(threads), smem, st, pdl, a); });
     };
-    const unsigned lists = (unsigned)(d->T / embed::kShort);
+    const unsigned lists = (unsigned)(d->T / (embed::kShort + 1));
     const size_t bits = (size_t)std::min<int64_t>(embed::kWindow, (int64_t)align_up((size_t)d->T, 32)) / 8;
     if (d->T <= embed::kIndexTokens && d->vocab <= embed::kIndexRows) {
         NOBLE_TRY(launch(index, embed::index_kernel<T>, dim3(embed::kIndexBlocks), 0, embed::kIndexThreads));
@@ -258,12 +258,12 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
     NOBLE_TRY(launch(index, embed::order_kernel<T>, dim3(std::min(lists, 4u * kSms)), bits));
     // rows of a warp: as many as leave every SM 16 warps; pieces of long lists come first
     a.rows_per_warp = (int)std::max<int64_t>(1, std::min<int64_t>(4, d->vocab / (16 * kSms)));
-    a.piece_blocks = (int)ceil_div((int64_t)lists * slices, 8);
+    a.piece_blocks = (int)std::min<int64_t>(ceil_div((int64_t)lists * slices, 8), 2 * kSms);
     const int64_t blocks = a.piece_blocks + ceil_div(d->vocab, 8 * a.rows_per_warp);
     // columns in parts where rows alone are too few warps
     const unsigned parts = a.rows_per_warp > 1 ? 1 : std::min(slices, 64u);
     NOBLE_TRY(launch(sum, embed::sum_kernel<T>, dim3((unsigned)blocks, parts), 0));
-    return launch(sum, embed::join_kernel<T>, dim3(std::min(lists, 2u * kSms), (unsigned)std::min<int64_t>(ceil_div(d->d, 128), 64)), 0);
+    return launch(sum, embed::join_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(d->T, embed::kPiece), kSms), (unsigned)std::min<int64_t>(ceil_div(d->d, 128), 64)), 0);
 }
 
 // ---------------------------------------------------------------- orthogonalised momentum

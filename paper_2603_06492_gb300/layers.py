@@ -24,18 +24,26 @@ def _at(x, name, dtype, shape, device):
     """Address of a contiguous tensor of the given shape, type and device; None stays None."""
     if x is None:
         return None
-    if x.shape != shape or x.dtype is not dtype or x.device != device or not x.is_cuda or not x.is_contiguous():
+    if x.dtype is not dtype or x.shape != shape or x.device != device or not x.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on {device}, got {x.dtype} "
                          f"{list(x.shape)} on {x.device}")
     return x.data_ptr()
 
 
-def _stream(stream, device):
-    """Handle of the stream of a call whose tensors are on ``device``, which has to be the current one."""
+def _place(x):
+    """The device of a buffer's tensors, and its index; no tensor is on that of buffers without a GPU."""
+    return (x.device, x.device.index) if x.is_cuda else ("a GPU, which these buffers are not on", -1)
+
+
+def _stream(stream, buf):
+    """Handle of the stream of a call, whose device has to be the current one."""
     handle = _stream_handle(stream)
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the buffers are on {device}, the current device is {torch.cuda.current_device()}")
+    if buf._index != _current():
+        raise ValueError(f"the buffers are on {buf.device}, the current device is {_current()}")
     return handle
+
+
+_current = torch.cuda.current_device
 
 
 # ---------------------------------------------------------------- layer norm
@@ -49,7 +57,8 @@ class NormBuffers:
         self.dtype = _TORCH[self.desc.dtype]
         new = dict(dtype=self.dtype, device=device)
         self.y = torch.empty((T, d), **new)
-        self.device = self.y.device
+        self.device, self._index = _place(self.y)
+        self._lib = binding.load()
         self.sum = torch.empty((T, d), **new) if residual else None
         self._ref, self._rows, self._row = ctypes.byref(self.desc), (T, d), (d,)
         self._out = (self.sum.data_ptr() if residual else None, self.y.data_ptr())
@@ -73,9 +82,9 @@ def norm_forward(buf: NormBuffers, x, gain=None, bias=None, res=None, stream=Non
     ``buf.sum``."""
     if (res is not None) != buf.residual:
         raise ValueError("buffers with residual take res, others do not")
-    _check(binding.load().noble_norm_fwd(buf._ref, buf._rows_of(x, "x"), buf._rows_of(res, "res"),
-                                         buf._features(gain, "gain"), buf._features(bias, "bias"), *buf._out,
-                                         None if buf.stats is None else buf.stats.data_ptr(), _stream(stream, buf.device)))
+    _check(buf._lib.noble_norm_fwd(buf._ref, buf._rows_of(x, "x"), buf._rows_of(res, "res"),
+                                   buf._features(gain, "gain"), buf._features(bias, "bias"), *buf._out,
+                                   None if buf.stats is None else buf.stats.data_ptr(), _stream(stream, buf)))
     return buf.y
 
 
@@ -85,10 +94,10 @@ def norm_backward(buf: NormBuffers, dy, s, gain=None, dstream=None, stream=None)
     it by the residual stream."""
     if buf.stats is None:
         raise ValueError("buffers without gradients")
-    _check(binding.load().noble_norm_bwd(buf._ref, buf._rows_of(dy, "dy"), buf._rows_of(s, "s"), buf.stats.data_ptr(),
-                                         buf._features(gain, "gain"), buf._rows_of(dstream, "dstream"),
-                                         buf.dx.data_ptr(), buf.dgain.data_ptr(), buf.dbias.data_ptr(),
-                                         buf.workspace.data_ptr(), buf.workspace_bytes, _stream(stream, buf.device)))
+    _check(buf._lib.noble_norm_bwd(buf._ref, buf._rows_of(dy, "dy"), buf._rows_of(s, "s"), buf.stats.data_ptr(),
+                                   buf._features(gain, "gain"), buf._rows_of(dstream, "dstream"),
+                                   buf.dx.data_ptr(), buf.dgain.data_ptr(), buf.dbias.data_ptr(),
+                                   buf.workspace.data_ptr(), buf.workspace_bytes, _stream(stream, buf)))
     return buf.dx
 
 
@@ -102,7 +111,8 @@ class EmbedBuffers:
         self.desc = binding.EmbedDesc(T, vocab, d, scale, _code(dtype), 0)
         self.dtype = _TORCH[self.desc.dtype]
         self.y = torch.empty((T, d), dtype=self.dtype, device=device)
-        self.device = self.y.device
+        self.device, self._index = _place(self.y)
+        self._lib = binding.load()
         self._ref, self._tokens, self._rows, self._table = ctypes.byref(self.desc), (T,), (T, d), (vocab, d)
         self.dtable = None
         if with_grads:
@@ -113,9 +123,9 @@ class EmbedBuffers:
 
 def embed_forward(buf: EmbedBuffers, ids, table, stream=None):
     """Scaled rows of table [vocab, d] by ids [T] (int32; negative: padding) into ``buf.y``."""
-    _check(binding.load().noble_embed_fwd(buf._ref, _at(ids, "ids", torch.int32, buf._tokens, buf.device),
-                                          _at(table, "table", buf.dtype, buf._table, buf.device), buf.y.data_ptr(),
-                                          _stream(stream, buf.device)))
+    _check(buf._lib.noble_embed_fwd(buf._ref, _at(ids, "ids", torch.int32, buf._tokens, buf.device),
+                                    _at(table, "table", buf.dtype, buf._table, buf.device), buf.y.data_ptr(),
+                                    _stream(stream, buf)))
     return buf.y
 
 
@@ -123,7 +133,7 @@ def embed_backward(buf: EmbedBuffers, ids, dy, stream=None):
     """The table's gradient into ``buf.dtable``, every row of it."""
     if buf.dtable is None:
         raise ValueError("buffers without gradients")
-    _check(binding.load().noble_embed_bwd(buf._ref, _at(ids, "ids", torch.int32, buf._tokens, buf.device),
-                                          _at(dy, "dy", buf.dtype, buf._rows, buf.device), buf.dtable.data_ptr(),
-                                          buf.workspace.data_ptr(), buf.workspace_bytes, _stream(stream, buf.device)))
+    _check(buf._lib.noble_embed_bwd(buf._ref, _at(ids, "ids", torch.int32, buf._tokens, buf.device),
+                                    _at(dy, "dy", buf.dtype, buf._rows, buf.device), buf.dtable.data_ptr(),
+                                    buf.workspace.data_ptr(), buf.workspace_bytes, _stream(stream, buf)))
     return buf.dtable
