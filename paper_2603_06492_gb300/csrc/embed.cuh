@@ -83,8 +83,9 @@ __device__ __forceinline__ void store_scaled(float *p, const float (&f)[N], floa
                make_float4(f[4 * i] * scale, f[4 * i + 1] * scale, f[4 * i + 2] * scale, f[4 * i + 3] * scale));
 }
 
-constexpr int kFewTokens = 2048;  // at most so many: one launch
+constexpr int kFewTokens = 1024;  // at most so many: one launch
 constexpr int kFewRows = 64;      // rows of the table of a block then
+constexpr int kFewAlone = 16;     // tokens of a row that one warp adds up
 constexpr int kShort = 8;         // a list of so many tokens is one warp's
 constexpr int kPiece = 64;        // tokens of a piece of a longer list
 constexpr int kCompared = 256;    // tokens of a list that is ordered by comparing
@@ -167,7 +168,9 @@ __global__ void __launch_bounds__(256) few_kernel(const BwdArgs<T> a)
     constexpr int V = Vec<T>::n;
     __shared__ uint32_t found[kFewTokens];  // row of the block << 16 | token
     __shared__ uint32_t mine[8][kFewTokens / 8];
-    __shared__ int counts[8];
+    __shared__ int counts[8], many[kFewRows];
+    __shared__ float sums[8][V][32];
+    if (threadIdx.x < kFewRows) many[threadIdx.x] = 0;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int first = blockIdx.x * kFewRows, rows = min(kFewRows, a.vocab - first), n = (int)a.tokens;
     const int at = blockIdx.y * 32 + lane;
@@ -186,19 +189,19 @@ __global__ void __launch_bounds__(256) few_kernel(const BwdArgs<T> a)
             if (w < warp) before += counts[w];
             total += counts[w];
         }
-        if (hit) found[before + __popc(mask & ((1u << lane) - 1))] = (uint32_t)(id - first) << 16 | (uint32_t)t;
+        if (hit) {
+            found[before + __popc(mask & ((1u << lane) - 1))] = (uint32_t)(id - first) << 16 | (uint32_t)t;
+            atomicAdd(many + id - first, 1);
+        }
         __syncthreads();
     }
-    const int n_found = total;
-    for (int r = warp; r < rows; r += 8) {
-        // this row's tokens, over the warp's part of `mine` again and again
-        float acc[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
-        for (int k = 0; k < n_found;) {
+    const bool crowded = __syncthreads_or(threadIdx.x < kFewRows && many[threadIdx.x] > kFewAlone);
+    // a row's tokens among found[from .. to), over the warp's part of `mine` again and again
+    auto add = [&](int r, int from, int to, float (&acc)[V]) {
+        for (int k = from; k < to;) {
             int m = 0;
-            for (; k < n_found && m + 32 <= kFewTokens / 8; k += 32) {
-                const uint32_t e = k + lane < n_found ? found[k + lane] : ~0u;
+            for (; k < to && m + 32 <= kFewTokens / 8; k += 32) {
+                const uint32_t e = k + lane < to ? found[k + lane] : ~0u;
                 const bool hit = e >> 16 == (uint32_t)r;
                 const uint32_t mask = __ballot_sync(0xffffffffu, hit);
                 if (hit) mine[warp][m + __popc(mask & ((1u << lane) - 1))] = e & 0xffffu;
@@ -220,7 +223,28 @@ __global__ void __launch_bounds__(256) few_kernel(const BwdArgs<T> a)
             }
             __syncwarp();
         }
+    };
+    for (int r = warp; r < rows; r += 8) {
+        if (many[r] > kFewAlone) continue;
+        float acc[V] = {};
+        if (many[r]) add(r, 0, total, acc);
         if (in) store_scaled(a.dtable + (int64_t)(first + r) * a.d + at * V, acc, a.scale, a.wide);
+    }
+    // rows of more tokens: an eighth of what was found to a warp, then the eighths in order
+    for (int r = 0; crowded && r < rows; ++r) {
+        if (many[r] <= kFewAlone) continue;
+        const int per = (total + 7) / 8;
+        float acc[V] = {};
+        add(r, warp * per, min(total, (warp + 1) * per), acc);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < V; ++j) sums[warp][j][lane] = acc[j];
+        __syncthreads();
+        if (warp != 0 || !in) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            for (int w = 1; w < 8; ++w) acc[j] += sums[w][j][lane];
+        store_scaled(a.dtable + (int64_t)(first + r) * a.d + at * V, acc, a.scale, a.wide);
     }
 }
 
@@ -276,7 +300,8 @@ __device__ __forceinline__ void begin_lists(const BwdArgs<T> &a, int64_t thread,
             kinds[1] += 1, kinds[2] += pieces;
             if (pieces > 1) kinds[3] += pieces, kinds[4] += 1;
         }
-        const int live = __any_sync(0xffffffffu, kinds[1]) ? 5 : 1;
+        const bool some_long = __any_sync(0xffffffffu, kinds[1]);
+        const int live = some_long ? 5 : 1;
         uint32_t total = 0;  // in lane k, of kind k
 #pragma unroll
         for (int k = 0; k < 5; ++k) {
@@ -306,9 +331,33 @@ __device__ __forceinline__ void begin_lists(const BwdArgs<T> &a, int64_t thread,
             const uint32_t pieces = (c + kPiece - 1) / kPiece;
             a.long_row[base[1]++] = row;
             if (pieces > 1) a.joined[base[4]++] = make_uint2(row, base[3]);
-            for (uint32_t k = 0; k < pieces; ++k) {
-                a.piece[base[2]] = make_uint2(row, k);
-                a.piece_part[base[2]++] = pieces > 1 ? base[3]++ : ~0u;
+            for (uint32_t k = 0; k < min(pieces, 4u); ++k) {
+                a.piece[base[2] + k] = make_uint2(row, k);
+                a.piece_part[base[2] + k] = pieces > 1 ? base[3] + k : ~0u;
+            }
+            base[2] += pieces;
+            if (pieces > 1) base[3] += pieces;
+        }
+        // pieces after a list's fourth by the whole warp
+#pragma unroll
+        for (int i = 0; some_long && i < 8; ++i) {
+            for (uint32_t more = __ballot_sync(0xffffffffu, n[i] > 4 * kPiece); more; more &= more - 1) {
+                const int from = __ffs(more) - 1;
+                const uint32_t pieces = (__shfl_sync(0xffffffffu, n[i], from) + kPiece - 1) / kPiece;
+                // behind this list's, the lane has put those of its later rows
+                uint32_t after2 = 0, after3 = 0;
+#pragma unroll
+                for (int j = i + 1; j < 8; ++j) {
+                    const uint32_t p = n[j] > kShort ? (n[j] + kPiece - 1) / kPiece : 0;
+                    after2 += p, after3 += p > 1 ? p : 0;
+                }
+                const uint32_t at2 = __shfl_sync(0xffffffffu, base[2] - after2, from) - pieces;
+                const uint32_t at3 = __shfl_sync(0xffffffffu, base[3] - after3, from) - pieces;
+                const uint32_t row = (uint32_t)__shfl_sync(0xffffffffu, (int)v, from) + i;
+                for (uint32_t k = 4 + lane; k < pieces; k += 32) {
+                    a.piece[at2 + k] = make_uint2(row, k);
+                    a.piece_part[at2 + k] = at3 + k;
+                }
             }
         }
     }

@@ -9,7 +9,7 @@ import torch
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
-FEW = 2048  # tokens of the path with one launch
+FEW = 1024  # tokens of the path with one launch
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -67,7 +67,8 @@ def _check(T, V, d, dtype, how, scale=1.0, seed=0):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("T,V,d", [(1, 1, 8), (1, 100, 64), (7, 3, 264), (24, 1000, 2048), (100, 63, 520), (257, 65, 1000),
                                    (FEW - 1, 500, 136), (FEW, 64, 256), (FEW + 1, 64, 256), (3000, 7, 40), (5000, 1001, 264),
-                                   (4097, 20000, 128)])
+                                   (4097, 20000, 128), (64, 2, 72), (65, 2, 72), (1000, 2100, 136), (FEW, 5000, 264), (6000, 16, 64),
+                                   (16385, 70000, 16), (70000, 11, 8)])
 @pytest.mark.parametrize("how", ["even", "skewed", "padded", "one"])
 def test_sizes(T, V, d, dtype, how):
     _check(T, V, d, dtype, how, scale=0.5 if how == "even" else 1.0)
@@ -79,11 +80,12 @@ def test_scales(T, scale):
     _check(T, 300, 64, "bf16", "skewed", scale)
 
 
-@pytest.mark.parametrize("n", [31, 32, 33, 63, 64, 65, 127, 128, 129, 1000])
-def test_lengths_of_lists(n):
+@pytest.mark.parametrize("n", [1, 2, 3, 7, 8, 9, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 1000])
+@pytest.mark.parametrize("T", [1024, 3000])
+def test_lengths_of_lists(T, n):
     # one row with exactly n tokens, spread among others
     from paper_2603_06492_gb300 import layers as L
-    T, V, d = 3000, 5000, 72
+    V, d = 5000, 72
     g = torch.Generator().manual_seed(n)
     ids = torch.randint(0, V - 1, (T,), generator=g)
     ids[torch.randperm(T, generator=g)[:n]] = V - 1
