@@ -48,7 +48,7 @@ struct Matrix {
 };
 struct Batch {
     Matrix t[kMost];
-    int n;
+    int n, tiles;       // matrices; 64 x 64 tiles of all
     float momentum, eps;
     int nesterov;
     uint32_t *counts;   // of the products (muon_gemm.cuh), set to zero
@@ -184,75 +184,105 @@ __device__ __forceinline__ void add_halves(const __half *p, float (&f)[8])
     }
 }
 
-// X = u / (|u| + eps) in fp16, a 64 x 64 tile of u per block: 512 groups of eight, two per thread.
-// Rows that pad X to a multiple of eight are zero in both of its places, as the products
-// read them (times zeros).
-__global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batch b)
+// The 64 x 64 tile at (r0, c0) of a matrix whose rows are not aligned: lanes along a row.
+template <class F>
+__device__ __forceinline__ void each_element(const Matrix &M, int r0, int c0, F &&f)
 {
-    __shared__ float tile[64][65];
+#pragma unroll 4
+    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
+        const int r = i / 64, c = i % 64;
+        f(r, c, r0 + r < M.rows && c0 + c < M.cols, (int64_t)(r0 + r) * M.cols + c0 + c);
+    }
+}
+
+// kScaleX / (|u| + eps) as a power of two and the rest: fp32 need not hold it.
+__device__ __forceinline__ float2 inverse_norm(const Matrix &M, float eps)
+{
     __shared__ double sm[8];
-    __shared__ float inv[2];  // 1 / norm as a power of two and the rest: fp32 need not hold it
-    const Matrix &M = b.t[tile_matrix(b, blockIdx.x)];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int at = blockIdx.x - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
-    const bool wide = M.cols % 4 == 0;
-    float g[2][8], u[2][8];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int r = r0 + 32 * k + threadIdx.x / 8, c = c0 + threadIdx.x % 8 * 8, n = r < M.rows ? M.cols - c : 0;
-        const int64_t e = (int64_t)r * M.cols + c;
-        load8(M.mom + e, n, wide, u[k]);
-        if (b.nesterov) load8(M.grad + e, n, wide, g[k]);
-    }
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < b.ncounts; i += gridDim.x * 256) b.counts[i] = 0;
-    if (at == 0) {
-        const int pad = (M.m8 - M.m) * M.ld;
-        for (int i = threadIdx.x; i < pad; i += 256) {
-            const int64_t e = (int64_t)M.m * M.ld + i;
-            M.x[e] = M.x_other[e] = __ushort_as_half(0);
-            if (M.x_lo) M.x_lo[e] = M.x_other_lo[e] = __ushort_as_half(0);
-        }
-    }
-    // the norm, the same in every block
+    __shared__ float2 inv;
     double s = 0.0;
     for (int i = threadIdx.x; i < M.nsums; i += 256) s += M.sums[i];
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) sm[warp] = s;
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) sm[threadIdx.x / 32] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
         s = 0.0;
         for (int w = 0; w < 8; ++w) s += sm[w];
-        const double norm = sqrt(s) + (double)b.eps;
+        const double norm = sqrt(s) + (double)eps;
         const double f = norm > 0.0 || norm != norm ? (double)kScaleX / norm : 0.0;
         const int e = f > 0.0 ? max(-126, min(126, ilogb(f))) : 0;
-        inv[0] = ldexpf(1.f, e);
-        inv[1] = (float)ldexp(f, -e);
+        inv = make_float2(ldexpf(1.f, e), (float)ldexp(f, -e));
     }
     __syncthreads();
-    const float i0 = inv[0], i1 = inv[1];
+    return inv;
+}
+
+// X = u / (|u| + eps) in fp16, in tiles of 64 x 64 elements of u: 512 groups of eight, two per thread.
+// The last tiles first, of which momentum_kernel has left the most in L2.  Rows that pad X to a
+// multiple of eight are zero in both of its places, as the products read them (times zeros).
+__global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batch b)
+{
+    __shared__ float tile[64][65];
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < b.ncounts; i += gridDim.x * 256) b.counts[i] = 0;
+    int last = -1;
+    float2 inv = make_float2(0.f, 0.f);
+    for (int t = b.tiles - 1 - (int)blockIdx.x; t >= 0; t -= gridDim.x) {
+        const int j = tile_matrix(b, t);
+        const Matrix &M = b.t[j];
+        const int at = t - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
+        const bool wide = M.cols % 4 == 0;
+        float g[2][8], u[2][8];
+        if (wide) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            u[k][i] = (b.nesterov ? blend(b, g[k][i], u[k][i]) : u[k][i]) * i0 * i1;
-            if (M.tall) tile[r][c + i] = u[k][i];
+            for (int k = 0; k < 2; ++k) {
+                const int r = r0 + 32 * k + threadIdx.x / 8, c = c0 + threadIdx.x % 8 * 8, n = r < M.rows ? M.cols - c : 0;
+                const int64_t e = (int64_t)r * M.cols + c;
+                load8(M.mom + e, n, true, u[k]);
+                if (b.nesterov) load8(M.grad + e, n, true, g[k]);
+            }
         }
-    }
-    if (M.tall) __syncthreads();
+        if (at == 0) {
+            const int pad = (M.m8 - M.m) * M.ld;
+            for (int i = threadIdx.x; i < pad; i += 256) {
+                const int64_t e = (int64_t)M.m * M.ld + i;
+                M.x[e] = M.x_other[e] = __ushort_as_half(0);
+                if (M.x_lo) M.x_lo[e] = M.x_other_lo[e] = __ushort_as_half(0);
+            }
+        }
+        if (j != last) inv = inverse_norm(M, b.eps);
+        last = j;
+        if (M.tall || !wide) __syncthreads();  // the tile before this one is through
+        if (!wide) {
+            each_element(M, r0, c0, [&](int r, int c, bool in, int64_t e) {
+                tile[r][c] = in ? (b.nesterov ? blend(b, M.grad[e], M.mom[e]) : M.mom[e]) * inv.x * inv.y : 0.f;
+            });
+        } else {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        // of X: row, column within the tile
-        const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
-        if (M.tall)
+            for (int k = 0; k < 2; ++k) {
+                const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[k][i] = tile[c + i][r];
-        const int xr = (M.tall ? c0 : r0) + r, xc = (M.tall ? r0 : c0) + c;
-        if (xr >= M.m || xc >= M.k) continue;
-        const int64_t e = (int64_t)xr * M.ld + xc;
-        store_halves(M.x + e, u[k]);
-        if (M.x_lo) store_halves(M.x_lo + e, u[k]);
+                for (int i = 0; i < 8; ++i) {
+                    u[k][i] = (b.nesterov ? blend(b, g[k][i], u[k][i]) : u[k][i]) * inv.x * inv.y;
+                    if (M.tall) tile[r][c + i] = u[k][i];
+                }
+            }
+        }
+        if (M.tall || !wide) __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            // of X: row, column within the tile
+            const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+            if (M.tall || !wide)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[k][i] = M.tall ? tile[c + i][r] : tile[r][c + i];
+            const int xr = (M.tall ? c0 : r0) + r, xc = (M.tall ? r0 : c0) + c;
+            if (xr >= M.m || xc >= M.k) continue;
+            const int64_t e = (int64_t)xr * M.ld + xc;
+            store_halves(M.x + e, u[k]);
+            if (M.x_lo) store_halves(M.x_lo + e, u[k]);
+        }
     }
 }
 
@@ -262,14 +292,14 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Batc
     __shared__ float tile[64][65];
     const Matrix &M = b.t[tile_matrix(b, blockIdx.x)];
     const int at = blockIdx.x - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
-    const bool wide = M.cols % 4 == 0, wide_bf16 = M.cols % 8 == 0;
+    const bool wide = M.cols % 8 == 0;
     float o[2][8], p[2][8];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
-        if (M.param) {
+        if (M.param && wide) {
             const int n = r0 + r < M.rows ? M.cols - c0 - c : 0;
-            load8(M.param + (int64_t)(r0 + r) * M.cols + c0 + c, n, wide, p[k]);
+            load8(M.param + (int64_t)(r0 + r) * M.cols + c0 + c, n, true, p[k]);
         }
         const int xr = (M.tall ? c0 : r0) + r, xc = (M.tall ? r0 : c0) + c;
 #pragma unroll
@@ -279,11 +309,27 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Batc
             add_halves(M.o + e, o[k]);
             if (M.o_lo) add_halves(M.o_lo + e, o[k]);
         }
-        if (M.tall)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) tile[c + i][r] = o[k][i];
+        for (int i = 0; i < 8; ++i) {
+            o[k][i] *= 1.f / kScaleX;
+            if (M.tall) tile[c + i][r] = o[k][i];
+            else if (!wide) tile[r][c + i] = o[k][i];
+        }
     }
-    if (M.tall) __syncthreads();
+    if (M.tall || !wide) __syncthreads();
+    if (!wide) {
+        each_element(M, r0, c0, [&](int r, int c, bool in, int64_t e) {
+            if (!in) return;
+            const float x = tile[r][c];
+            if (M.update) M.update[e] = __float2bfloat16_rn(x);
+            if (!M.param) return;
+            float v = M.param[e];
+            v = fmaf(-M.lr, x, fmaf(-M.decay, v, v));
+            M.param[e] = v;
+            if (M.param_bf16) M.param_bf16[e] = __float2bfloat16_rn(v);
+        });
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int r = 32 * k + threadIdx.x / 8, c = threadIdx.x % 8 * 8;
@@ -291,13 +337,14 @@ __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Batc
         if (n <= 0) continue;
         const int64_t e = (int64_t)(r0 + r) * M.cols + c0 + c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[k][i] = (M.tall ? tile[r][c + i] : o[k][i]) * (1.f / kScaleX);
-        if (M.update) store8(M.update + e, n, wide_bf16, o[k]);
+        for (int i = 0; i < 8; ++i)
+            if (M.tall) o[k][i] = tile[r][c + i];
+        if (M.update) store8(M.update + e, n, true, o[k]);
         if (!M.param) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[k][i] = fmaf(-M.lr, o[k][i], fmaf(-M.decay, p[k][i], p[k][i]));
-        store8(M.param + e, n, wide, p[k]);
-        if (M.param_bf16) store8(M.param_bf16 + e, n, wide_bf16, p[k]);
+        store8(M.param + e, n, true, p[k]);
+        if (M.param_bf16) store8(M.param_bf16 + e, n, true, p[k]);
     }
 }
 

@@ -44,6 +44,10 @@ struct Problem {
     const __half *d, *d_lo;
     int ldd;           // elements between rows of D, a multiple of 8
     int pairs;         // C has low parts
+    // k-blocks that are added up in TMEM before the next ones get columns of their own: the tensor core
+    // cuts what it adds to an accumulator off to fp32, so that a long sum of like terms (the diagonal of
+    // X X^T) comes out too small, by 2^-24 for each of its adds
+    int piece_kb;
     float *part;       // [unit][256][bn] as the warps hold them
     uint32_t *count;   // [tile][2 CTAs][8 warps][4 chunks], zero before and after
 };
@@ -231,11 +235,14 @@ product_pairs(const __grid_constant__ Args<N> g)
                 const uint64_t b0 = b_mn ? ptx::smem_desc_sw128(sbase + Smem::kA, 1024, 1024 * nch)
                                          : ptx::smem_desc_sw128(sbase + Smem::kA, 16, 1024);
                 const uint32_t stepB = b_mn ? 128u * nch : 2u;
-                const int nkb = t.kb_end - t.kb_begin, b = acc & 1;
+                const int nkb = t.kb_end - t.kb_begin, b = acc & 1, piece = P.piece_kb, bn = P.bn;
                 if (!ptx::mbar_wait(tempty_bar(b), ((uint32_t)(acc >> 1) & 1u) ^ 1u, status)) break;
                 ptx::tc_fence_after();
-                const uint32_t d_tmem = tmem + b * 256;
+                uint32_t d_tmem = tmem + b * 256;
+                int next = piece;  // k-block that begins the next piece; pieces are even
+                uint32_t add = 0;
                 for (int i = 0; i < nkb; i += 2) {
+                    if (i == next) d_tmem += bn, next += piece, add = 0;
                     const bool two = i + 1 < nkb;
                     int s2 = s + 1;
                     uint32_t ph2 = ph;
@@ -245,7 +252,8 @@ product_pairs(const __grid_constant__ Args<N> g)
                         break;
                     }
                     const uint64_t so = (uint64_t)((uint32_t)s * kUnits);
-                    pair::mma2_bf16(d_tmem, a0 + so, b0 + so, idesc, i > 0 ? 1u : 0u);
+                    pair::mma2_bf16(d_tmem, a0 + so, b0 + so, idesc, add);
+                    add = 1;
 #pragma unroll
                     for (int kk = 1; kk < kBK / 16; ++kk)
                         pair::mma2_bf16(d_tmem, a0 + so + kk * 2, b0 + so + kk * stepB, idesc, 1u);
@@ -311,10 +319,21 @@ product_pairs(const __grid_constant__ Args<N> g)
             float *parts = P.part + (int64_t)t.tile * P.nsplit * split_stride + ((int)rank * 8 + w8) * chunks * 1024 + lane;
             uint32_t *count = P.count + ((t.tile * 2 + (int)rank) * 8 + w8) * 4;
             const bool split = P.nsplit > 1;
+            const int pieces = (t.kb_end - t.kb_begin + P.piece_kb - 1) / P.piece_kb;
+            // 32 columns of the accumulator: its pieces in order
+            auto load = [&](int c, float (&v)[32]) {
+                ptx::tmem_ld_32x32b_x32(lane_addr + 64 * c, v);
+                for (int k = 1; k < pieces; ++k) {
+                    float w[32];
+                    ptx::tmem_ld_32x32b_x32(lane_addr + 64 * c + k * P.bn, w);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] += w[j];
+                }
+            };
             if (split && rows_in) {
                 for (int c = 0; c < chunks && column(c) < P.n; ++c) {
                     float v[32];
-                    ptx::tmem_ld_32x32b_x32(lane_addr + 64 * c, v);
+                    load(c, v);
                     float *mine = parts + t.split * split_stride + c * 1024;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) __stcg(mine + 32 * j, v[j]);
@@ -358,7 +377,7 @@ product_pairs(const __grid_constant__ Args<N> g)
                         for (int j = 0; j < 32; ++j) v[j] = v[j] + w[0][j] + w[1][j];
                     }
                 } else {
-                    ptx::tmem_ld_32x32b_x32(lane_addr + 64 * c, v);
+                    load(c, v);
                 }
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] *= P.alpha;

@@ -339,9 +339,18 @@ int muon_tiles(const muon::mma::Problem &p, int bn)
     const int tm = (int)ceil_div(p.m, muon::mma::kRows), tn = (int)ceil_div(p.n, bn);
     return p.sym ? muon::mma::sym_tiles_before(tm, tn, muon::mma::kRows / bn) : tm * tn;
 }
-// Time of a unit in k-blocks of a tile of 256 columns: a tile of 128 takes 0.6 of one per
-// k-block, and 8 pass between a unit's last k-block and what waits for it.
-double muon_cost(int kb, int bn, int nsplit) { return kb * (bn == 256 ? 1.0 : 0.6) + (bn == 256 ? 8 : 5) + (nsplit > 1 ? 4 + nsplit : 0); }
+// Times of a unit in k-blocks of a tile of 256 columns, 0.29 us, of its main loop and of its epilogue, which
+// runs beside the next unit's main loop.  One k-block of 128 columns takes 0.27 us, as both kinds wait for
+// L2.  Parts of a split K are stored, fenced and joined, which takes longer than most main loops:
+// splits pay only while all units run at once (X X^T of 1024 x 4096, 76 pairs: 20 tiles of 128 columns whole, in 3
+// and in 4 parts 6, 0 and 5 us above the best; 2048 x 8192: 36 tiles of 256 columns whole and in 2 parts 7 and 0;
+// B X of 2048 x 8192, 256 tiles, whole and in 2 parts 0 and 70).
+double muon_main(int kb, int bn) { return kb * (bn == 256 ? 1.0 : 0.92) + 2; }
+double muon_epilogue(int bn, int nsplit)
+{
+    if (nsplit == 1) return bn == 256 ? 12 : 6;
+    return (bn == 256 ? 2 : 1) * (20 + 1.1 * nsplit);
+}
 
 // Columns of tiles and splits of K for the problems of a launch, by the time of the busiest pair.
 void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
@@ -366,20 +375,19 @@ void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
                 order[i] = i;
             }
             std::stable_sort(order, order + n, [&](int a, int b) {
-                return muon_cost(p[a].kb_per_split, p[a].bn, p[a].nsplit) > muon_cost(p[b].kb_per_split, p[b].bn, p[b].nsplit);
+                return muon_main(p[a].kb_per_split, p[a].bn) > muon_main(p[b].kb_per_split, p[b].bn);
             });
             double load[kPairs] = {}, longest = 0.0;
-            bool split = false;
             for (int k = 0; k < n; ++k) {
                 Problem &q = p[order[k]];
                 q.unit_begin = total;
-                split |= q.nsplit > 1;
                 const int count = muon_tiles(q, q.bn) * q.nsplit;
-                const double cost = muon_cost(q.kb_per_split, q.bn, q.nsplit);
+                const double loop = muon_main(q.kb_per_split, q.bn), end = muon_epilogue(q.bn, q.nsplit);
                 for (int c = 0; c < kPairs; ++c) {  // units total + c, total + c + kPairs, ...
                     double &l = load[(total + c) % kPairs];
-                    if (c < count) l += cost * ((count - c - 1) / kPairs + 1);
-                    longest = std::max(longest, l);
+                    if (c >= count) break;
+                    l += std::max(loop, end) * ((count - c - 1) / kPairs + 1);
+                    longest = std::max(longest, l + std::min(loop, end));
                 }
                 total += count;
             }
@@ -393,6 +401,12 @@ void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
     }
     std::copy(kept, kept + n, p), std::copy(kept_order, kept_order + n, order);
     *units = kept_units;
+    // pieces of the accumulation of pairs: the columns of TMEM that a unit has, all 512 where no pair takes a
+    // second one
+    for (int i = 0; i < n; ++i) {
+        const int pieces = p[i].segs > 1 ? (kept_units <= kPairs ? 512 : 256) / p[i].bn : 1;
+        p[i].piece_kb = (int)align_up((size_t)ceil_div(p[i].kb_per_split, pieces), 2);
+    }
 }
 
 // Takes the next matrices that are not empty, from *next on.
@@ -512,7 +526,7 @@ noble_status muon_product(const muon::mma::Args<N> &g, const KernelInfo &ki, cud
         allowed.store(current_context(), std::memory_order_relaxed);
     }
     // each pair takes units of its own: no pair waits for another, so that they need not all be resident
-    const int pairs = std::min({g.units, muon::mma::kPairs, std::max(1, num_sms() / 2)});
+    const int pairs = std::min(g.units, muon::mma::kPairs);
     const bool pdl = pdl_ok();
     return run(st, ki, [&] {
         launch_maybe_pdl(muon::mma::product_pairs<N, WIDE>, dim3(2 * (unsigned)pairs), dim3(tc::pair::kPairThreads), smem, st, pdl, g);
@@ -559,6 +573,7 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
         M.x = X[0][i].hi, M.x_lo = X[0][i].lo, M.x_other = X[1][i].hi, M.x_other_lo = X[1][i].lo;
         M.o = X[hp->steps % 2][i].hi, M.o_lo = X[hp->steps % 2][i].lo;
     }
+    b.tiles = tiles;
     // a product's arguments: what it multiplies, what it writes
     double flops[kPhases] = {};
     auto arguments = [&](Args &g, int phase, int half) -> noble_status {
@@ -604,7 +619,7 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
     };
     const KernelInfo hbm{"muon_elementwise", kBoundHbm, 0.0, bytes / 3};
     NOBLE_TRY(run(st, hbm, [&] { muon::momentum_kernel<<<dim3((unsigned)blocks, (unsigned)w.n), 256, 0, st>>>(b); }));
-    NOBLE_TRY(run(st, hbm, [&] { muon::scale_kernel<<<(unsigned)tiles, 256, 0, st>>>(b); }));
+    NOBLE_TRY(run(st, hbm, [&] { muon::scale_kernel<<<(unsigned)std::min(tiles, 4 * kSms), 256, 0, st>>>(b); }));
     Args gram[2] = {}, poly = {}, next[2] = {};
     auto product = [&](const Args &g, int phase) {
         static const char *const names[kPhases] = {"muon_gram", "muon_poly", "muon_next"};
