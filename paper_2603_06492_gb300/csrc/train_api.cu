@@ -352,53 +352,63 @@ double muon_epilogue(int bn, int nsplit)
     return (bn == 256 ? 2 : 1) * (20 + 1.1 * nsplit);
 }
 
-// Columns of tiles and splits of K for the problems of a launch, by the time of the busiest pair.
+// Columns of tiles and splits of K for the problems of a launch, by the time of the busiest pair: the
+// problem with the most work in 1, 2, ... parts while they all run at once, the others in parts as long
+// as its, or twice or four times that.
 void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
 {
     using namespace muon::mma;
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) tiles += muon_tiles(p[i], 256);
+    int main = 0;
+    auto work = [&](int i) { return (int64_t)muon_tiles(p[i], 256) * p[i].kb * p[i].segs; };
+    for (int i = 1; i < n; ++i)
+        if (work(i) > work(main)) main = i;
+    const int main_kb = p[main].kb * p[main].segs;
     double best = 1e300;
     Problem kept[muon::kMost];
     int kept_order[muon::kMost], kept_units = 0;
-    for (int bn : {256, 128}) {
-        for (int most = 1 << 20; most >= 4; most = most > 1024 ? 1024 : most * 3 / 4) {  // k-blocks of a unit
-            int total = 0;
-            for (int i = 0; i < n; ++i) {
-                Problem &q = p[i];
-                const int kb = q.kb * q.segs;
-                q.bn = q.n <= 128 ? 128 : bn;
-                q.tiles_m = (int)ceil_div(q.m, kRows), q.tiles_n = (int)ceil_div(q.n, q.bn);
-                const int splits = (int)std::min<int64_t>(kMostSplits, ceil_div(kb, most));
-                q.kb_per_split = (int)ceil_div(kb, splits);
-                q.nsplit = (int)ceil_div(kb, q.kb_per_split);
-                order[i] = i;
-            }
-            std::stable_sort(order, order + n, [&](int a, int b) {
-                return muon_main(p[a].kb_per_split, p[a].bn) > muon_main(p[b].kb_per_split, p[b].bn);
-            });
-            double load[kPairs] = {}, longest = 0.0;
-            for (int k = 0; k < n; ++k) {
-                Problem &q = p[order[k]];
-                q.unit_begin = total;
-                const int count = muon_tiles(q, q.bn) * q.nsplit;
-                const double loop = muon_main(q.kb_per_split, q.bn), end = muon_epilogue(q.bn, q.nsplit);
-                for (int c = 0; c < kPairs; ++c) {  // units total + c, total + c + kPairs, ...
-                    double &l = load[(total + c) % kPairs];
-                    if (c >= count) break;
-                    l += std::max(loop, end) * ((count - c - 1) / kPairs + 1);
-                    longest = std::max(longest, l + std::min(loop, end));
-                }
-                total += count;
-            }
-            if (longest < best) {
-                best = longest;
-                std::copy(p, p + n, kept), std::copy(order, order + n, kept_order);
-                kept_units = total;
-            }
-            if (tiles >= 8 * kPairs) break;  // splits gain nothing
+    auto attempt = [&](int bn, int splits, int longer) {
+        const int most = (int)ceil_div(main_kb, splits);  // k-blocks of a unit
+        for (int i = 0; i < n; ++i) {
+            Problem &q = p[i];
+            const int kb = q.kb * q.segs;
+            q.bn = q.n <= 128 ? 128 : bn;
+            q.tiles_m = (int)ceil_div(q.m, kRows), q.tiles_n = (int)ceil_div(q.n, q.bn);
+            q.kb_per_split = (int)ceil_div(kb, std::min<int64_t>(kMostSplits, ceil_div(kb, i == main ? most : longer * most)));
+            q.nsplit = (int)ceil_div(kb, q.kb_per_split);
+            order[i] = i;
         }
-    }
+        std::sort(order, order + n, [&](int a, int b) {
+            const double x = muon_main(p[a].kb_per_split, p[a].bn), y = muon_main(p[b].kb_per_split, p[b].bn);
+            return x != y ? x > y : a < b;
+        });
+        double load[kPairs] = {}, longest = 0.0;
+        int total = 0;
+        for (int k = 0; k < n; ++k) {
+            Problem &q = p[order[k]];
+            q.unit_begin = total;
+            const int count = muon_tiles(q, q.bn) * q.nsplit;
+            const double loop = muon_main(q.kb_per_split, q.bn), end = muon_epilogue(q.bn, q.nsplit);
+            for (int c = 0; c < std::min(count, kPairs); ++c) {  // units total + c, total + c + kPairs, ...
+                double &l = load[(total + c) % kPairs];
+                l += std::max(loop, end) * ((count - c - 1) / kPairs + 1);
+                longest = std::max(longest, l + std::min(loop, end));
+            }
+            total += count;
+        }
+        if (longest < best) {
+            best = longest;
+            std::copy(p, p + n, kept), std::copy(order, order + n, kept_order);
+            kept_units = total;
+        }
+    };
+    for (int bn : {256, 128})
+        for (int splits = 1; splits <= kMostSplits; ++splits) {
+            if (splits > 1 && (splits > main_kb || muon_tiles(p[main], bn) * splits > kPairs)) break;
+            for (int longer : {1, 2, 4}) {
+                if (longer > 1 && n == 1) break;
+                attempt(bn, splits, longer);
+            }
+        }
     std::copy(kept, kept + n, p), std::copy(kept_order, kept_order + n, order);
     *units = kept_units;
     // pieces of the accumulation of pairs: the columns of TMEM that a unit has, all 512 where no pair takes a
