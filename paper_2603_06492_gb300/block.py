@@ -1,14 +1,15 @@
 """The attention half of a transformer block: NOBLE QKV projection, head norms and rotation,
 attention, NOBLE output projection -- forward and backward for training on packed
-documents, and one step of generation over a paged cache.
+documents, and one step of generation over a paged cache; a stack of them between its table of
+tokens and its last norm; and the optimizer of its parameters.
 
-Nothing is computed here: the block keeps buffers and calls the operators in order.
+Nothing is computed here: these keep buffers and call the operators in order.
 """
 from __future__ import annotations
 
 import torch
 
-from . import attention as A, binding as B
+from . import attention as A, binding as B, layers as L
 
 
 class AttentionBlock:
@@ -85,3 +86,101 @@ class AttentionBlock:
 def page_slots(page_table, seq, pos, page_size):
     """Slots of tokens at ``pos`` of sequences ``seq`` (int64 tensors)."""
     return page_table[seq, pos // page_size].to(torch.int64) * page_size + pos % page_size
+
+
+class Stack:
+    """Attention halves one behind the other, from tokens to the last norm: the table's rows are the
+    residual stream, each half reads a layer norm of it and adds its output.
+
+    ``params`` of its calls: ``{"table": [vocab, d_model], "norms": [{"gain", "bias"}, ...], "blocks":
+    [...]}``, with a norm more than blocks, and the blocks' as for ``AttentionBlock``."""
+
+    def __init__(self, vocab, blocks, d_model, *heads, dtype="bf16", scale=1.0, eps=1e-5, **options):
+        self.vocab, self.d_model, self.dtype, self.scale, self.eps = vocab, d_model, dtype, scale, eps
+        self.blocks = [AttentionBlock(d_model, *heads, dtype=dtype, **options)]
+        self.blocks += [AttentionBlock(d_model, *heads, dtype=dtype, table=self.blocks[0].table, **options) for _ in range(blocks - 1)]
+
+    def _ends(self, T, with_grads):
+        norm = dict(dtype=self.dtype, eps=self.eps, with_grads=with_grads)
+        return {"embed": L.EmbedBuffers(T, self.vocab, self.d_model, self.dtype, scale=self.scale, with_grads=with_grads),
+                "norms": [L.NormBuffers(T, self.d_model, residual=i > 0, **norm) for i in range(len(self.blocks) + 1)]}
+
+    def _through(self, b, ids, params, half):
+        """The last norm's output; half(i, x): block i's on x."""
+        norms, stream = params["norms"], L.embed_forward(b["embed"], ids, params["table"])
+        x = L.norm_forward(b["norms"][0], stream, norms[0]["gain"], norms[0]["bias"])
+        for i in range(len(self.blocks)):
+            n = b["norms"][i + 1]
+            x = L.norm_forward(n, half(i, x), norms[i + 1]["gain"], norms[i + 1]["bias"], res=stream)
+            stream = n.sum
+        return x
+
+    # ---------------------------------------------------------------- training
+    def buffers(self, T, n_docs=1):
+        """Buffers of a training step on T packed tokens."""
+        return {**self._ends(T, True), "blocks": [blk.buffers(T, n_docs) for blk in self.blocks]}
+
+    def forward(self, b, ids, params, pos, doc_start, prefix=None):
+        return self._through(b, ids, params,
+                             lambda i, x: self.blocks[i].forward(b["blocks"][i], x, params["blocks"][i], pos, doc_start, prefix))
+
+    def backward(self, b, ids, dx, params, pos, doc_start, prefix=None):
+        """Gradients of every parameter, in the layout of ``params``, after ``forward`` on the same buffers."""
+        norms, blocks, dstream = [], [], None
+        for i in range(len(self.blocks), -1, -1):
+            n = b["norms"][i]
+            dstream = L.norm_backward(n, dx, n.sum if i else b["embed"].y, params["norms"][i]["gain"], dstream)
+            norms.insert(0, {"gain": n.dgain, "bias": n.dbias})
+            if i:
+                dx, g = self.blocks[i - 1].backward(b["blocks"][i - 1], b["norms"][i - 1].y, dstream, params["blocks"][i - 1], pos,
+                                                    doc_start, prefix)
+                blocks.insert(0, g)
+        return {"table": L.embed_backward(b["embed"], ids, dstream), "norms": norms, "blocks": blocks}
+
+    # ---------------------------------------------------------------- generation
+    def caches(self, pages, page_size):
+        return [blk.cache(pages, page_size) for blk in self.blocks]
+
+    def step_buffers(self, n_seq, max_len, q_len=1):
+        """Buffers of a step of n_seq sequences by q_len tokens each."""
+        return {**self._ends(n_seq * q_len, False), "blocks": [blk.step_buffers(n_seq, max_len, q_len) for blk in self.blocks]}
+
+    def step(self, b, caches, ids, params, pos, slots, page_table, kv_len):
+        """The last norm's output for the newest tokens; their keys and values join the caches first."""
+        return self._through(b, ids, params, lambda i, x: self.blocks[i].step(b["blocks"][i], caches[i], x, params["blocks"][i],
+                                                                             pos, slots, page_table, kv_len))
+
+
+class Update:
+    """Optimizer of a Stack's parameters: orthogonalised momentum for the matrices of its
+    projections, AdamW for everything else.  Keeps fp32 parameters and moments; the operands that
+    the layers read (bf16, or the parameters themselves in fp32) are written in the same pass."""
+
+    _MATRICES = {"W", "W_down", "W_up", "M"}
+    _GRADS = {"W": "dW", "bias": "dbias", "W_down": "dW_down", "W_up": "dW_up", "M": "dM", "omega1": "domega1", "phi1": "dphi1",
+              "omega2": "domega2", "phi2": "dphi2"}
+
+    def __init__(self, params, grads, precise=False):
+        self.steps, self.precise, self.muon, self.adamw = 0, precise, [], []
+        for matrix, p, g in self._leaves(params, grads):
+            fp32 = p.dtype is torch.float32
+            t = {"param": p if fp32 else p.float(), "param_bf16": None if fp32 else p, "grad": g, "decay": p.dim() == 2}
+            moments = ("momentum",) if matrix else ("exp_avg", "exp_avg_sq")
+            t.update({k: torch.zeros_like(t["param"]) for k in moments})
+            (self.muon if matrix else self.adamw).append(t)
+        self.workspace = B.muon_workspace(self.muon, precise)
+
+    def _leaves(self, params, grads):
+        yield False, params["table"], grads["table"]
+        for p, g in zip(params["norms"], grads["norms"]):
+            yield from ((False, p[k], g[k]) for k in ("gain", "bias"))
+        for p, g in zip(params["blocks"], grads["blocks"]):
+            yield from ((False, p[k], g[k]) for k in ("gain_q", "gain_k") if p.get(k) is not None and k in g)
+            for name in ("qkv", "out"):
+                yield from ((k in self._MATRICES, p[name][k], g[name][d]) for k, d in self._GRADS.items() if p[name].get(k) is not None)
+
+    def step(self, lr, lr_matrices, weight_decay=0.01):
+        """One step from the gradients that the Stack's buffers hold."""
+        self.steps += 1
+        B.noble_muon_step(self.muon, lr_matrices, weight_decay=weight_decay, precise=self.precise, workspace=self.workspace)
+        B.noble_adamw_step(self.adamw, lr, weight_decay=weight_decay, step=self.steps)
