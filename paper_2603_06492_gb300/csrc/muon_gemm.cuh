@@ -4,7 +4,8 @@
 //   C = alpha P Q^T + beta D + diag I       P [m][k], Q [n][k] or, for X <- B X, stored [k][n]
 //
 // fp16 operands, fp32 accumulation in TMEM, fp16 results.  A matrix in pairs (v = hi + lo)
-// takes three segments of K into one accumulator: hi hi, hi lo, lo hi.
+// takes three segments of K into one accumulator: lo hi, hi lo, hi hi.  The large terms come last, as every
+// add to an accumulator costs it half a bit of fp32 (64 x 64 with hi hi first: X 4e-6 off).
 //
 // CTA pairs as in tc_pair.cuh: tiles of 256 x bn, TMA -> ring of six stages -> tcgen05.mma by
 // the leader's warp 1 -> TMEM -> eight epilogue warps per CTA, two accumulators in turn.
@@ -192,6 +193,7 @@ product_pairs(const __grid_constant__ Args<N> g)
                 const int m0 = t.m0 + 128 * (int)rank, n0 = t.n0 + bh * (int)rank;
                 const uint32_t bytes = Smem::kA + (uint32_t)bh * kBK * 2;
                 int seg = t.kb_begin / kb_of_seg, kb = t.kb_begin - seg * kb_of_seg;
+                seg += 3 - P.segs;  // the last one is hi hi
                 for (int i = t.kb_begin; i < t.kb_end; ++i, ++it) {
                     if (!ptx::mbar_wait(empty_bar(s), ph ^ 1, g.status)) {
                         ok = false;
@@ -200,7 +202,7 @@ product_pairs(const __grid_constant__ Args<N> g)
                     const uint32_t fb = cluster::map_to_rank(full_bar(s), 0);
                     if (leader) ptx::mbar_arrive_expect_tx(full_bar(s), 2 * bytes);
                     const uint32_t sA = sbase + s * Smem::kStage, sB = sA + Smem::kA;
-                    const CUtensorMap *mP = &g.map[t.prob][seg == 2 ? 1 : 0], *mQ = &g.map[t.prob][seg == 1 ? 3 : 2];
+                    const CUtensorMap *mP = &g.map[t.prob][seg == 0 ? 1 : 0], *mQ = &g.map[t.prob][seg == 1 ? 3 : 2];
                     const int k = kb * kBK;
                     pair::tma_load_2d_pair(sA, mP, fb, k, m0);
                     if (b_mn)
