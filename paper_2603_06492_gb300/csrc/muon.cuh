@@ -63,6 +63,7 @@ __device__ __forceinline__ float blend(const Batch &b, float g, float m) { retur
 __global__ void __launch_bounds__(256) momentum_kernel(const __grid_constant__ Batch b)
 {
     __shared__ double sm[8];
+    ptx::griddep_launch();
     const Matrix &M = b.t[blockIdx.y];
     if ((int)blockIdx.x >= M.nsums) return;
     const int64_t n4 = M.n / 4, stride = (int64_t)M.nsums * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -225,6 +226,8 @@ __device__ __forceinline__ float2 inverse_norm(const Matrix &M, float eps)
 __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batch b)
 {
     __shared__ float tile[64][65];
+    ptx::griddep_launch();
+    ptx::griddep_wait();
     for (int i = blockIdx.x * 256 + threadIdx.x; i < b.ncounts; i += gridDim.x * 256) b.counts[i] = 0;
     int last = -1;
     float2 inv = make_float2(0.f, 0.f);
@@ -290,6 +293,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Batc
 __global__ void __launch_bounds__(256) apply_kernel(const __grid_constant__ Batch b)
 {
     __shared__ float tile[64][65];
+    ptx::griddep_wait();
     const Matrix &M = b.t[tile_matrix(b, blockIdx.x)];
     const int at = blockIdx.x - M.tile_begin, r0 = at / M.tiles_c * 64, c0 = at % M.tiles_c * 64;
     const bool wide = M.cols % 8 == 0;

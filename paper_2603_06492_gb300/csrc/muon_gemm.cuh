@@ -9,7 +9,8 @@
 //
 // CTA pairs as in tc_pair.cuh: tiles of 256 x bn, TMA -> ring of six stages -> tcgen05.mma by
 // the leader's warp 1 -> TMEM -> eight epilogue warps per CTA, two accumulators in turn.
-// Units of work are given to the pairs in turn, the longest first.
+// Units of work are given to the pairs in turn, the longest first, there and back: what a round
+// leaves over goes to the pairs that had the shortest units in the one before.
 //  - A and A A are symmetric: tiles that lie below the diagonal are not computed, the others
 //    are also stored transposed.  (2048 x 8192: 72 units in place of 128 for X X^T.)
 //  - A product of few tiles and long K is split along K.  Each warp stores its part of the
@@ -71,6 +72,10 @@ struct Smem {
     static constexpr uint32_t kBytes = kBarOff + 8 * kNumBars + 16;
     static constexpr uint32_t kDynamic = kBytes + 1024;
 };
+
+// Unit u's pair, and a pair's unit in round r.
+__host__ __device__ inline int pair_of(int u, int pairs) { return u / pairs % 2 ? pairs - 1 - u % pairs : u % pairs; }
+__device__ __forceinline__ int unit_of(int r, int pair, int pairs) { return r * pairs + (r % 2 ? pairs - 1 - pair : pair); }
 
 struct Unit {
     int prob, tile, split;
@@ -186,7 +191,7 @@ product_pairs(const __grid_constant__ Args<N> g)
             int s = 0;
             uint32_t ph = 0;
             bool ok = true;
-            for (int u = first; ok && u < g.units; u += pairs) {
+            for (int r = 0, u; ok && (u = unit_of(r, first, pairs)) < g.units; ++r) {
                 const Unit t = locate(g, u);
                 const Problem &P = g.p[t.prob];
                 const int kb_of_seg = P.kb, bh = P.bn / 2, b_mn = P.b_mn;
@@ -227,7 +232,7 @@ product_pairs(const __grid_constant__ Args<N> g)
             int s = 0, acc = 0;
             uint32_t ph = 0;
             bool ok = true;
-            for (int u = first; ok && u < g.units; u += pairs, ++acc) {
+            for (int u; ok && (u = unit_of(acc, first, pairs)) < g.units; ++acc) {
                 const Unit t = locate(g, u);
                 const Problem &P = g.p[t.prob];
                 const bool b_mn = P.b_mn != 0;
@@ -286,7 +291,7 @@ product_pairs(const __grid_constant__ Args<N> g)
         uint8_t *stg_ptr = smem + Smem::kStgOff + w8 * 4096;
         ptx::griddep_wait();  // parts, counters and D are earlier kernels'
         int acc = 0;
-        for (int u = first; u < g.units; u += pairs, ++acc) {
+        for (int u; (u = unit_of(acc, first, pairs)) < g.units; ++acc) {
             const Unit t = locate(g, u);
             const Problem &P = g.p[t.prob];
             const int b = acc & 1;

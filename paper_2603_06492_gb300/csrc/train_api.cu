@@ -259,8 +259,9 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
         NOBLE_TRY(launch(index, embed::place_kernel<T>, dim3(per_token), 0));
     }
     NOBLE_TRY(launch(index, embed::order_kernel<T>, dim3(std::min(lists, 4u * kSms)), bits));
-    // rows of a warp: as many as leave every SM 16 warps; pieces of long lists come first
-    a.rows_per_warp = (int)std::max<int64_t>(1, std::min<int64_t>(4, d->vocab / (16 * kSms)));
+    // rows of a warp: two, where there are that many for 16 warps per SM (8192 tokens, 50257 x 1024, and 65536,
+    // 131072 x 2048: one 80 and 509 us, two 67 and 302, four 68 and 309); pieces of long lists come first
+    a.rows_per_warp = (int)std::max<int64_t>(1, std::min<int64_t>(2, d->vocab / (16 * kSms)));
     a.piece_blocks = (int)std::min<int64_t>(ceil_div((int64_t)lists * slices, 8), 4 * kSms);
     const int64_t blocks = a.piece_blocks + ceil_div(d->vocab, 8 * a.rows_per_warp);
     // columns in parts where rows alone are too few warps
@@ -388,11 +389,14 @@ void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
             q.unit_begin = total;
             const int count = muon_tiles(q, q.bn) * q.nsplit;
             const double loop = muon_main(q.kb_per_split, q.bn), end = muon_epilogue(q.bn, q.nsplit);
-            for (int c = 0; c < std::min(count, kPairs); ++c) {  // units total + c, total + c + kPairs, ...
-                double &l = load[(total + c) % kPairs];
-                l += std::max(loop, end) * ((count - c - 1) / kPairs + 1);
-                longest = std::max(longest, l + std::min(loop, end));
-            }
+            auto add = [&](int pair, int units) {
+                load[pair] += std::max(loop, end) * units;
+                longest = std::max(longest, load[pair] + std::min(loop, end));
+            };
+            // whole rounds of all pairs, then the units that are left in their places
+            const int rounds = count / kPairs;
+            for (int c = 0; rounds && c < kPairs; ++c) add(c, rounds);
+            for (int c = rounds * kPairs; c < count; ++c) add(pair_of(total + c, kPairs), 1);
             total += count;
         }
         if (longest < best) {
@@ -629,7 +633,11 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
     };
     const KernelInfo hbm{"muon_elementwise", kBoundHbm, 0.0, bytes / 3};
     NOBLE_TRY(run(st, hbm, [&] { muon::momentum_kernel<<<dim3((unsigned)blocks, (unsigned)w.n), 256, 0, st>>>(b); }));
-    NOBLE_TRY(run(st, hbm, [&] { muon::scale_kernel<<<(unsigned)std::min(tiles, 4 * kSms), 256, 0, st>>>(b); }));
+    const auto dependent = [&](auto kern, int grid) {
+        const bool pdl = pdl_ok();
+        return run(st, hbm, [&] { launch_maybe_pdl(kern, dim3((unsigned)grid), dim3(256), 0, st, pdl, b); });
+    };
+    NOBLE_TRY(dependent(muon::scale_kernel, std::min(tiles, 4 * kSms)));
     Args gram[2] = {}, poly = {}, next[2] = {};
     auto product = [&](const Args &g, int phase) {
         static const char *const names[kPhases] = {"muon_gram", "muon_poly", "muon_next"};
@@ -645,7 +653,7 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
         if (k < 2) NOBLE_TRY(arguments(next[h], kNext, h));
         NOBLE_TRY(product(next[h], kNext));
     }
-    return run(st, hbm, [&] { muon::apply_kernel<<<(unsigned)tiles, 256, 0, st>>>(b); });
+    return dependent(muon::apply_kernel, tiles);
 }
 
 }  // namespace
