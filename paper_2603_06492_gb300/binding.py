@@ -365,25 +365,31 @@ def noble_adamw_step(tensors, lr, beta1=0.9, beta2=0.98, eps=1e-8, weight_decay=
     _check(load().noble_adamw_step(arr, len(tensors), ctypes.byref(hp), stream))
 
 
+_MUON_PACK = struct.Struct("=5Q2qfi").pack_into
+_MUON_SIZE = ctypes.sizeof(MuonTensor)
+assert _MUON_SIZE == struct.calcsize("=5Q2qfi")
+
+
 def _muon_array(tensors):
+    import torch
+    fp32, bf16 = torch.float32, torch.bfloat16
     arr = (MuonTensor * max(1, len(tensors)))()
     for i, t in enumerate(tensors):
         g = t["grad"]
-        if g.dim() != 2:
-            raise ValueError(f"tensor {i}: a matrix is needed, got {list(g.shape)}")
-        for name, dtype in _MUON_TYPES:
-            x = t.get(name)
-            if x is not None and (x.shape != g.shape or str(x.dtype) != dtype or x.device != g.device or not x.is_cuda or
-                                  not x.is_contiguous()):
-                raise ValueError(f"tensor {i}, {name}: expected a contiguous {dtype} CUDA tensor {list(g.shape)} on {g.device}, "
+        shape, device, at = g.shape, g.device, []
+        if len(shape) != 2:
+            raise ValueError(f"tensor {i}: a matrix is needed, got {list(shape)}")
+        for x, name, dtype in ((t.get("param"), "param", fp32), (t.get("param_bf16"), "param_bf16", bf16), (g, "grad", fp32),
+                               (t["momentum"], "momentum", fp32), (t.get("update"), "update", bf16)):
+            if x is None:
+                at.append(0)
+                continue
+            if x.dtype is not dtype or x.shape != shape or x.device != device or not x.is_cuda or not x.is_contiguous():
+                raise ValueError(f"tensor {i}, {name}: expected a contiguous {dtype} CUDA tensor {list(shape)} on {device}, "
                                  f"got {x.dtype} {list(x.shape)} on {x.device}")
-        arr[i] = MuonTensor(_p(t.get("param")), _p(t.get("param_bf16")), _p(g), _p(t["momentum"]), _p(t.get("update")),
-                            g.shape[0], g.shape[1], float(t.get("lr_mult", 1.0)), int(t.get("decay", True)))
+            at.append(x.data_ptr())
+        _MUON_PACK(arr, i * _MUON_SIZE, *at, *shape, float(t.get("lr_mult", 1.0)), int(bool(t.get("decay", True))))
     return arr
-
-
-_MUON_TYPES = (("param", "torch.float32"), ("param_bf16", "torch.bfloat16"), ("grad", "torch.float32"),
-               ("momentum", "torch.float32"), ("update", "torch.bfloat16"))
 
 
 def muon_workspace(tensors, precise=False):
@@ -401,9 +407,18 @@ def noble_muon_step(tensors, lr, momentum=0.95, weight_decay=0.0, nesterov=True,
     momentum, and param (with optional param_bf16) or update or both -- contiguous device
     matrices of one shape, fp32 but for param_bf16 and update in bf16 --, optional lr_mult
     (default 1) and decay (default True).  ``workspace``: of muon_workspace; a new one if None."""
+    import torch
     arr = _muon_array(tensors)
     if workspace is None:
         workspace = muon_workspace(tensors, precise)
+    if not workspace.is_cuda or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: expected one of muon_workspace")
+    for t in tensors[:1]:
+        if t["grad"].device != workspace.device or t["grad"].device.index != torch.cuda.current_device():
+            raise ValueError(f"the tensors are on {t['grad'].device}, the workspace on {workspace.device}, the current device is "
+                             f"{torch.cuda.current_device()}")
+    if any(t["grad"].device != workspace.device for t in tensors):
+        raise ValueError("the tensors of a call have to be on one device")
     hp = MuonHparams(lr, momentum, weight_decay, eps, steps,
                      (NOBLE_MUON_NESTEROV if nesterov else 0) | (NOBLE_MUON_PRECISE if precise else 0))
     _check(load().noble_muon_step(arr, len(tensors), ctypes.byref(hp), _p(workspace), workspace.numel(),

@@ -33,20 +33,25 @@ noble_status get_status(uint32_t **p)
     return *p ? NOBLE_OK : fail(NOBLE_ERR_CUDA, "status word address");
 }
 
-// Dynamic shared memory up to an SM's for a kernel, once in each context.
-constexpr size_t kMostShared = 225 << 10;
+// Dynamic shared memory beyond 48 KB has to be allowed for each kernel, in each context; a kernel is
+// allowed the same number of bytes every time.
 template <class Kern>
-noble_status allow_shared(Kern kern)
+noble_status allow_shared(Kern kern, size_t bytes)
 {
+    struct Done {
+        const void *kern;
+        CUcontext ctx;
+    };
     static std::mutex mu;
-    static std::vector<std::pair<const void *, CUcontext>> done;
+    static Done done[64];  // kernels of one signature
+    static int n = 0;
     const CUcontext ctx = current_context();
     std::lock_guard<std::mutex> g(mu);
-    for (const auto &e : done)
-        if (ctx && e.first == (const void *)kern && e.second == ctx) return NOBLE_OK;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared) != cudaSuccess)
+    for (int i = 0; ctx && i < n; ++i)
+        if (done[i].kern == (const void *)kern && done[i].ctx == ctx) return NOBLE_OK;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess)
         return fail(NOBLE_ERR_CUDA, "shared memory: %s", cudaGetErrorString(cudaGetLastError()));
-    done.emplace_back((const void *)kern, current_context());
+    if (n < 64) done[n++] = {(const void *)kern, current_context()};
     return NOBLE_OK;
 }
 
@@ -137,7 +142,7 @@ noble_status norm_bwd(const noble_norm_desc *d, const void *dy, const void *s, c
                                                               (uint32_t)ceil_div(a.rows_per_part, side * a.groups)}));
     const size_t smem = std::max<size_t>((size_t)a.stages * stage, a.groups > 1 ? (size_t)a.groups * 2 * a.d * 4 : 0);
     auto launch = [&](auto kern) -> noble_status {
-        NOBLE_TRY(allow_shared(kern));
+        NOBLE_TRY(allow_shared(kern, norm::kRingBytes));
         return run(st, ki, [&] { kern<<<(unsigned)parts, 32 * (a.warps * a.groups + 1), smem, st>>>(a); });
     };
     auto with = [&](auto nv, auto warps) {
@@ -532,13 +537,7 @@ template <int N, bool WIDE>
 noble_status muon_product(const muon::mma::Args<N> &g, const KernelInfo &ki, cudaStream_t st)
 {
     constexpr size_t smem = muon::mma::Smem<WIDE>::kDynamic;
-    static std::atomic<CUcontext> allowed{nullptr};
-    const CUcontext ctx = current_context();
-    if (!ctx || allowed.load(std::memory_order_relaxed) != ctx) {
-        if (cudaFuncSetAttribute(muon::mma::product_pairs<N, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-            return fail(NOBLE_ERR_CUDA, "shared memory: %s", cudaGetErrorString(cudaGetLastError()));
-        allowed.store(current_context(), std::memory_order_relaxed);
-    }
+    NOBLE_TRY(allow_shared(muon::mma::product_pairs<N, WIDE>, smem));
     // each pair takes units of its own: no pair waits for another, so that they need not all be resident
     const int pairs = std::min(g.units, muon::mma::kPairs);
     const bool pdl = pdl_ok();

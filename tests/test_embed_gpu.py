@@ -184,3 +184,26 @@ def test_workspace_stays_in_its_size():
                                           b.workspace_bytes, B._stream_handle(None)))
         torch.cuda.synchronize()
         assert bool((room[b.workspace_bytes:] == 171).all())
+
+
+@pytest.mark.parametrize("T", [60, 5000])
+def test_offsets_beyond_32_bits(T):
+    # 2.2e9 elements of the table: rows at both ends, on the device
+    from paper_2603_06492_gb300 import layers as L
+    V, d = 540001, 4096
+    g = torch.Generator(device="cuda").manual_seed(3)
+    ids = torch.randint(V - 50, V, (T,), generator=g, device="cuda").int()
+    ids[::7] = torch.randint(0, 50, (len(ids[::7]),), generator=g, device="cuda").int()
+    table = torch.empty((V, d), dtype=torch.bfloat16, device="cuda")
+    for rows in (slice(0, 50), slice(V - 50, V)):
+        table[rows] = torch.randn((50, d), generator=g, device="cuda").bfloat16()
+    dy = torch.randint(-8, 9, (T, d), generator=g, device="cuda").bfloat16()  # sums are exact
+    b = L.EmbedBuffers(T, V, d, "bf16")
+    b.dtable.fill_(7.0)
+    assert torch.equal(L.embed_forward(b, ids, table), table[ids.long()])
+    got = L.embed_backward(b, ids, dy)
+    for lo in (0, V - 50):
+        inside = (ids >= lo) & (ids < lo + 50)
+        want = torch.zeros((50, d), device="cuda").index_add_(0, ids[inside].long() - lo, dy[inside].float())
+        assert torch.equal(got[lo:lo + 50], want)
+    assert not any(bool(got[i:i + 50000].any()) for i in range(50, V - 50, 50000) if i + 50000 <= V - 50)

@@ -237,3 +237,19 @@ def test_gradients_against_differences():
         mine = sum((a.double().cpu() * q).sum() for a, q in zip((dx, b.dgain, b.dbias), v))
         # third derivatives of rows of O(1): h^2 of the sum of magnitudes; the gradients' own errors 1e-5 of it
         assert abs(mine - slope) <= 1e-5 * sum((a.double().cpu() * q).abs().sum() for a, q in zip((dx, b.dgain, b.dbias), v))
+
+
+def test_offsets_beyond_32_bits():
+    # 2.2e9 elements: the last rows come out as in a call of their own
+    from paper_2603_06492_gb300 import layers as L
+    T, d, n = 532000, 4096, 700
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, dy = (torch.empty((T, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x.fill_(1.0), dy.zero_()
+    x[:, 0] = 3.0
+    x[-n:], dy[-n:] = (torch.randn((n, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    ga, bi = torch.randn(d, generator=g, device="cuda"), torch.randn(d, generator=g, device="cuda")
+    b, few = L.NormBuffers(T, d, "bf16"), L.NormBuffers(n, d, "bf16")
+    assert torch.equal(L.norm_forward(b, x, ga, bi)[-n:], L.norm_forward(few, x[-n:], ga, bi))
+    assert torch.equal(L.norm_backward(b, dy, x, ga)[-n:], L.norm_backward(few, dy[-n:], x[-n:], ga))
+    assert torch.allclose(b.dgain, few.dgain, rtol=0, atol=1e-3) and torch.allclose(b.dbias, few.dbias, rtol=0, atol=1e-3)

@@ -2,12 +2,14 @@
 host: a wrong argument gives its status before any device is touched; a right call reaches
 the device check."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
 
 from paper_2603_06492_gb300 import binding as B
-from paper_2603_06492_gb300.build import build
+from paper_2603_06492_gb300.build import CSRC, build
 
 FAKE = 0x100000  # aligned, never dereferenced
 INVALID, MISALIGNED, UNSUPPORTED, SMALL, NO_DEVICE = 1, 2, 3, 4, 7
@@ -188,3 +190,25 @@ def test_torch_side_refuses(lib):
         L.embed_forward(e, torch.zeros(4, dtype=torch.int32), torch.zeros(6, 8))
     with pytest.raises(ValueError):
         L.embed_backward(e, torch.zeros(4, dtype=torch.int32), x)
+
+
+# kernels that start before the one before them has ended and then read what it wrote
+@pytest.mark.parametrize("name", ["embed.cuh", "muon.cuh", "muon_gemm.cuh", "norm.cuh"])
+def test_no_read_only_loads_in_programmatic_dependents(name):
+    with open(os.path.join(CSRC, name)) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    assert "griddep_wait" in text and re.findall(r"__ldg\w*|ld\.global\S*\.nc|__restrict__", text) == []
+
+
+def _body(text, head):
+    start = text.index("\n{", text.index(head))
+    return text[start:text.index("\n}", start)]
+
+
+# the shape decides how sums are cut, so that results and sizes are the same on every device
+@pytest.mark.parametrize("head", ["int norm_rows_per_part(", "EmbedWork embed_work(", "bool embed_few(", "void muon_cut(", "MuonPlan muon_plan("])
+def test_orders_of_sums_do_not_depend_on_the_device(head):
+    with open(os.path.join(CSRC, "train_api.cu")) as f:
+        text = f.read()
+    body = _body(text, head) if not head.startswith("bool") else text[text.index(head):text.index("\n", text.index(head))]
+    assert len(body) > 60 and "num_sms" not in body
