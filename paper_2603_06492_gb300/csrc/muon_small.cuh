@@ -1,0 +1,251 @@
+// The orthogonalising iteration of small matrices (muon.cuh has the mathematics) in one launch: up to
+// 128 rows by 2048 columns, a cluster of up to eight blocks per matrix.  15 launches of a few us of
+// work each would take their gaps.
+//
+// X stays in shared memory throughout, each block holding up to 256 of its columns; all matrices in
+// pairs (v = hi + lo).  One step:
+//   A   each block multiplies its columns (tcgen05, K = its columns), the partial sums go through
+//       distributed shared memory to the block that owns the columns of A, which adds them up in
+//       order of the blocks and sends A to all;
+//   B = a I + b A + c A A   in every block, in place of A;
+//   X <- B X                each block its columns, in place.
+// A tile of 128 rows by 64 columns with the 128-byte swizzle is the operand along K of the first
+// product and the operand across K of the last one: the descriptors differ, the bytes do not.
+//
+// What bounds it is the chain of its parts: 64 x 1024 takes about 7 us a step, of which the tensor core
+// works 2.
+#pragma once
+
+#include "muon_gemm.cuh"
+
+namespace noble {
+namespace muon {
+namespace small {
+
+constexpr int kRows = 128, kBlocks = 8, kCols = 256;  // rows of X; blocks of a cluster, columns of a block at most
+constexpr int kThreads = 256;
+constexpr uint32_t kTile = kRows * 128;         // 128 rows of 64 columns
+constexpr uint32_t kLow = 4 * kTile;            // X: four tiles, and as many of low parts
+constexpr uint32_t kPoly = 8 * kTile;           // A, then B: two tiles, two of low parts
+constexpr uint32_t kBarOff = kPoly + 4 * kTile;
+constexpr uint32_t kBytes = kBarOff + 16, kDynamic = kBytes + 1024;
+
+struct Args {
+    Batch b;
+    int cols[kMost];  // of a block: a multiple of 64
+    int steps;
+    uint32_t *status;
+};
+
+// A group of eight elements of a tile.
+__device__ __forceinline__ uint32_t at(int row, int col) { return (uint32_t)(col / 64) * kTile + row * 128 + ((((col % 64) / 8) ^ (row & 7)) << 4); }
+
+__device__ __forceinline__ void remote_store(uint32_t cluster_addr, const uint4 &v)
+{
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// Eight values as halves; what is left of them stays in f.
+__device__ __forceinline__ uint4 halves(float *f)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+        const float2 r = __half22float2(h);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        f[2 * i] -= r.x, f[2 * i + 1] -= r.y;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void add_eight(const uint4 &q, float scale, float *f)
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 r = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+        f[2 * i] = fmaf(scale, r.x, f[2 * i]), f[2 * i + 1] = fmaf(scale, r.y, f[2 * i + 1]);
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_constant__ Args g)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = ptx::smem_u32(smem_raw), sbase = (raw + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (sbase - raw);
+    const uint32_t bar = sbase + kBarOff;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + kBarOff + 8);
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quarter = warp % 4, half = warp / 4;
+    const uint32_t rank = cluster::ctarank();
+    const int blocks = (int)cluster::nctarank(), own = kRows / blocks;  // columns of A that a block owns
+    const Matrix &M = g.b.t[blockIdx.x / blocks];
+    const int cols = g.cols[blockIdx.x / blocks], c0 = (int)rank * cols;
+
+    ptx::griddep_launch();
+    if (tid == 0) {
+        ptx::mbar_init(bar, 1);
+        ptx::fence_barrier_init();
+    }
+    if (warp == 0) {
+        ptx::tmem_alloc(ptx::smem_u32(tmem_slot), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = *tmem_slot, lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    const int row = quarter * 32 + lane;  // of a thread in every epilogue
+
+    ptx::griddep_wait();
+    // X: groups of eight columns that have elements, zeros elsewhere
+    for (int i = tid; i < kRows * cols / 8; i += kThreads) {
+        const int r = i / (cols / 8), c = i % (cols / 8) * 8;
+        const bool in = r < M.m && c0 + c < M.k;
+        const int64_t e = (int64_t)r * M.ld + c0 + c;
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(smem + at(r, c)) = in ? *reinterpret_cast<const uint4 *>(M.x + e) : none;
+        *reinterpret_cast<uint4 *>(smem + kLow + at(r, c)) = in ? *reinterpret_cast<const uint4 *>(M.x_lo + e) : none;
+    }
+
+    uint32_t phase = 0;
+    bool ok = true;
+    // D = P Q^T over `chunks` tiles along K, by one thread: lo hi, hi lo, hi hi; the operands are in
+    // place once all threads are here, and D is complete when they are through
+    auto multiply = [&](uint32_t d, uint32_t p, uint32_t p_lo, uint32_t q, uint32_t q_lo, int chunks, int n, bool across) {
+        ptx::fence_proxy_async_smem();
+        ptx::tc_fence_before();
+        __syncthreads();
+        if (tid == 0 && ok) {
+            ptx::tc_fence_after();
+            const uint32_t idesc = mma::idesc_f16(kRows, n, across);
+            for (int seg = 0; seg < 3; ++seg) {
+                const uint32_t a = sbase + (seg == 0 ? p_lo : p), b = sbase + (seg == 1 ? q_lo : q);
+                for (int k = 0; k < 4 * chunks; ++k) {
+                    const uint64_t ad = ptx::smem_desc_sw128(a + k / 4 * kTile + k % 4 * 32, 16, 1024);
+                    const uint64_t bd = across ? ptx::smem_desc_sw128(b + k * 2048, kTile, 1024)
+                                               : ptx::smem_desc_sw128(b + k / 4 * kTile + k % 4 * 32, 16, 1024);
+                    ptx::mma_bf16(d, ad, bd, idesc, seg + k > 0 ? 1u : 0u);
+                }
+            }
+            ptx::mma_commit(bar);
+        }
+        // a wait that gave up is reported, and given once more for what is in flight; the barriers still
+        // need every thread
+        if (ok && !ptx::mbar_wait(bar, phase, g.status)) {
+            ptx::mbar_wait(bar, phase, nullptr);
+            ok = false;
+        }
+        phase ^= 1;
+        __syncwarp();
+        ptx::tc_fence_after();
+    };
+
+    for (int step = 0; step < g.steps; ++step) {
+        // ---- A
+        multiply(tmem, 0, kLow, 0, kLow, cols / 64, kRows, false);
+        cluster::sync();  // no block needs its B any more: parts of A go there, [block][row][own]
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float v[32];
+            ptx::tmem_ld_32x32b_x32(lanes + 64 * half + 32 * c, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int col = 64 * half + 32 * c + 4 * j, to = col / own;
+                const uint32_t off = kPoly + ((rank * kRows + row) * own + col % own) * 4;
+                remote_store(cluster::map_to_rank(sbase + off, to), make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]),
+                                                                               __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+            }
+        }
+        cluster::sync();
+        // the columns that this block owns: two threads to a row, groups of eight (one, but for fewer blocks)
+        const int r = tid / 2, groups = own / 16;
+        uint4 hi[8], lo[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k >= groups) break;
+            const int col = 8 * (tid % 2 * groups + k);
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = 0.f;
+            for (int p = 0; p < blocks; ++p) {
+                const float4 *from = reinterpret_cast<const float4 *>(smem + kPoly + ((p * kRows + r) * own + col) * 4);
+                const float4 u = from[0], w = from[1];
+                f[0] += u.x, f[1] += u.y, f[2] += u.z, f[3] += u.w, f[4] += w.x, f[5] += w.y, f[6] += w.z, f[7] += w.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= kScaleA / (kScaleX * kScaleX);
+            hi[k] = halves(f), lo[k] = halves(f);
+        }
+        cluster::sync();  // all parts are read
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k >= groups) break;
+            const uint32_t off = kPoly + at(r, (int)rank * own + 8 * (tid % 2 * groups + k));
+            for (int p = 0; p < blocks; ++p) {
+                const uint32_t to = cluster::map_to_rank(sbase + off, p);
+                remote_store(to, hi[k]);
+                remote_store(to + 2 * kTile, lo[k]);
+            }
+        }
+        // the tensor core of each block reads what all of them wrote: writes, fence, barrier, fence
+        ptx::fence_proxy_async_smem_cluster();
+        cluster::sync();
+        // ---- B
+        multiply(tmem, kPoly, kPoly + 2 * kTile, kPoly, kPoly + 2 * kTile, 2, kRows, false);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float v[32];
+            const int col0 = 64 * half + 32 * c;
+            ptx::tmem_ld_32x32b_x32(lanes + col0, v);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float *f = v + 8 * q;
+                uint4 *h = reinterpret_cast<uint4 *>(smem + kPoly + at(row, col0 + 8 * q));
+                uint4 *l = reinterpret_cast<uint4 *>(smem + kPoly + 2 * kTile + at(row, col0 + 8 * q));
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    f[j] *= muon::kC * kScaleB / (kScaleA * kScaleA);
+                    if (row == col0 + 8 * q + j) f[j] += muon::kA * kScaleB;
+                }
+                add_eight(*h, muon::kB * kScaleB / kScaleA, f);
+                add_eight(*l, muon::kB * kScaleB / kScaleA, f);
+                *h = halves(f);
+                *l = halves(f);
+            }
+        }
+        // ---- X
+        multiply(tmem + 128, kPoly, kPoly + 2 * kTile, 0, kLow, 2, cols, true);
+        for (int col0 = cols / 2 * half; col0 < cols / 2 * (half + 1); col0 += 32) {
+            float v[32];
+            ptx::tmem_ld_32x32b_x32(lanes + 128 + col0, v);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float *f = v + 8 * q;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] *= 1.f / kScaleB;
+                *reinterpret_cast<uint4 *>(smem + at(row, col0 + 8 * q)) = halves(f);
+                *reinterpret_cast<uint4 *>(smem + kLow + at(row, col0 + 8 * q)) = halves(f);
+            }
+        }
+    }
+    __syncthreads();
+    __half *o = const_cast<__half *>(M.o), *o_lo = const_cast<__half *>(M.o_lo);
+    for (int i = tid; i < M.m * (cols / 8); i += kThreads) {
+        const int r = i / (cols / 8), c = i % (cols / 8) * 8;
+        if (c0 + c >= M.k) continue;
+        const int64_t e = (int64_t)r * M.ld + c0 + c;
+        *reinterpret_cast<uint4 *>(o + e) = *reinterpret_cast<const uint4 *>(smem + at(r, c));
+        *reinterpret_cast<uint4 *>(o_lo + e) = *reinterpret_cast<const uint4 *>(smem + kLow + at(r, c));
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    cluster::sync();  // no block leaves while others may still write to it
+    if (warp == 0) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace small
+}  // namespace muon
+}  // namespace noble

@@ -7,7 +7,7 @@
 
 #include "host.cuh"
 #include "embed.cuh"
-#include "muon_gemm.cuh"
+#include "muon_small.cuh"
 #include "norm.cuh"
 
 namespace noble {
@@ -334,6 +334,7 @@ struct MuonPlan {
     } at[muon::kMost];
     size_t counts, part, total;
     int ncounts;
+    int small;  // blocks of a matrix if all iterate in one launch, else 0
     muon::mma::Problem p[kPhases][muon::kMost];  // sizes only
     int order[kPhases][muon::kMost];             // place in the launch -> matrix
     int units[kPhases];
@@ -428,6 +429,22 @@ void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
     }
 }
 
+// Blocks per matrix of a group whose matrices all iterate in one launch (muon_small.cuh), or 0: up to 128
+// columns each, as the products of a block take as long as its columns, and more where eight blocks
+// are not enough.
+int muon_small(const noble_muon_tensor *t, const int *pick, int n)
+{
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        if (std::min(t[pick[i]].rows, t[pick[i]].cols) > muon::small::kRows) return 0;
+        most = std::max({most, t[pick[i]].rows, t[pick[i]].cols});
+    }
+    if (most > muon::small::kBlocks * muon::small::kCols) return 0;
+    int blocks = 1;
+    while (blocks < muon::small::kBlocks && blocks * 128 < most) blocks *= 2;
+    return n ? blocks : 0;
+}
+
 // Takes the next matrices that are not empty, from *next on.
 MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
 {
@@ -439,14 +456,17 @@ MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
         w.total = align_up(w.total + bytes, 256);
         return p;
     };
+    w.small = muon_small(t, w.pick, w.n);
     for (int i = 0; i < w.n; ++i) {
         const noble_muon_tensor &s = t[w.pick[i]];
         const bool precise = muon_precise(s, flags);
         const int m = (int)std::min(s.rows, s.cols), k = (int)std::max(s.rows, s.cols);
         const size_t e = precise ? 4 : 2;
         for (size_t &x : w.at[i].x) x = take(align_up((size_t)m, 8) * (size_t)muon_ld(k) * e);
-        w.at[i].a = take((size_t)m * (size_t)muon_ld(m) * e);
-        w.at[i].b = take((size_t)m * (size_t)muon_ld(m) * e);
+        if (!w.small) {
+            w.at[i].a = take((size_t)m * (size_t)muon_ld(m) * e);
+            w.at[i].b = take((size_t)m * (size_t)muon_ld(m) * e);
+        }
         w.at[i].sums = take(muon::kMomentBlocks * sizeof(double));
         for (int j = 0; j < kPhases; ++j) {
             muon::mma::Problem &p = w.p[j][i];
@@ -456,6 +476,7 @@ MuonPlan muon_plan(const noble_muon_tensor *t, int n, int *next, uint32_t flags)
             p.sym = j != kNext, p.b_mn = j == kNext;
         }
     }
+    if (w.small) return w;
     size_t part = 0;
     for (int j = 0; j < kPhases; ++j) {
         muon_cut(w.p[j], w.order[j], w.n, &w.units[j]);
@@ -543,6 +564,24 @@ noble_status muon_product(const muon::mma::Args<N> &g, const KernelInfo &ki, cud
     const bool pdl = pdl_ok();
     return run(st, ki, [&] {
         launch_maybe_pdl(muon::mma::product_pairs<N, WIDE>, dim3(2 * (unsigned)pairs), dim3(tc::pair::kPairThreads), smem, st, pdl, g);
+    });
+}
+
+noble_status muon_iterate(const muon::Batch &b, const MuonPlan &w, int steps, cudaStream_t st)
+{
+    using namespace muon::small;
+    Args g{};
+    g.b = b, g.steps = steps;
+    NOBLE_TRY(get_status(&g.status));
+    double flops = 0.0;
+    for (int i = 0; i < b.n; ++i) {
+        g.cols[i] = (int)align_up((size_t)ceil_div(b.t[i].k, w.small), 64);
+        flops += steps * (double)b.t[i].m * b.t[i].m * (3.0 * b.t[i].k + b.t[i].m);
+    }
+    NOBLE_TRY(allow_shared(iterate_kernel, kDynamic));
+    const bool pdl = pdl_ok();
+    return run(st, {"muon_iterate", kBoundTensor, flops, 0.0}, [&] {
+        launch_cluster(iterate_kernel, dim3((unsigned)(b.n * w.small)), w.small, dim3(kThreads), kDynamic, st, pdl, g);
     });
 }
 
@@ -637,6 +676,10 @@ noble_status muon_run(const noble_muon_tensor *t, const MuonPlan &w, const noble
         return run(st, hbm, [&] { launch_maybe_pdl(kern, dim3((unsigned)grid), dim3(256), 0, st, pdl, b); });
     };
     NOBLE_TRY(dependent(muon::scale_kernel, std::min(tiles, 4 * kSms)));
+    if (w.small) {
+        if (hp->steps > 0) NOBLE_TRY(muon_iterate(b, w, hp->steps, st));
+        return dependent(muon::apply_kernel, tiles);
+    }
     Args gram[2] = {}, poly = {}, next[2] = {};
     auto product = [&](const Args &g, int phase) {
         static const char *const names[kPhases] = {"muon_gram", "muon_poly", "muon_next"};

@@ -122,15 +122,34 @@ def test_sizes(shape, precise):
 
 
 @pytest.mark.parametrize("steps", [0, 1, 2, 3, 4, 7])
-@pytest.mark.parametrize("shape", [(300, 600), (90, 33)])
+@pytest.mark.parametrize("shape", [(300, 600), (90, 33), (700, 100)])
 def test_steps(shape, steps):
     _check(_inputs([shape], 1), steps=steps)
+
+
+@pytest.mark.parametrize("shapes", [
+    [(128, 2048)], [(129, 2048)], [(128, 2049)], [(2041, 127)], [(1, 2048)], [(128, 129), (128, 127)],
+    [(64, 1024), (1024, 64), (64, 64)], [(5, 1500), (1, 1), (100, 260), (77, 640)], [(128, 128)] * 16,
+    [(33 + 5 * i, 2000 - 100 * i) for i in range(18)], [(100, 300), (140, 300)]])
+def test_small_groups(shapes):
+    # all iterate in one launch up to 128 rows and 2048 columns, on one to eight blocks each
+    _check(_inputs(shapes, 11))
+
+
+def test_small_alone_and_in_company():
+    # blocks of another count add up in another order, and larger matrices take all along to their launches
+    t = _inputs([(100, 260), (70, 2000), (300, 300)], 12)
+    for n in (1, 2, 3):
+        dev = _check(t[:n])
+        again = _run(t[:n], lr=0.5, weight_decay=0.1, momentum=0.95, eps=1e-7)
+        assert all(torch.equal(a[k], b[k]) for a, b in zip(dev, again) for k in ("param", "momentum", "update"))
 
 
 @pytest.mark.parametrize("precise", [False, True])
 def test_spectra(precise):
     # rows of very different sizes, and a matrix of few directions with little noise
     _check(_inputs([(320, 500)], 2, spread=1.5), precise=precise)
+    _check(_inputs([(120, 500)], 2, spread=1.5), precise=precise)
     g = torch.Generator().manual_seed(4)
     t = _inputs([(400, 400)], 3)
     t[0]["momentum"] = torch.randn((400, 5), generator=g) @ torch.randn((5, 400), generator=g) + 0.05 * torch.randn((400, 400), generator=g)
@@ -180,6 +199,15 @@ def test_zero_and_empty_and_non_finite():
     _near(good[0]["update"], _iterate(u, 5, 1e-7), 0.02, "alone")
 
 
+def test_small_non_finite_stays_alone():
+    t = _inputs([(100, 700), (64, 64), (90, 20)], 13)
+    good = _run(t, lr=0.1)
+    t[1]["grad"][3, 4] = float("nan")
+    dev = _run(t, lr=0.1)
+    assert all(torch.equal(dev[i][k], good[i][k]) for i in (0, 2) for k in ("param", "update"))
+    assert not dev[1]["update"].isfinite().any()
+
+
 def test_result_is_orthogonal():
     # a spectrum within a factor of 100: five steps bring every singular value into [0.3, 1.25]
     g = torch.Generator().manual_seed(10)
@@ -194,9 +222,10 @@ def test_result_is_orthogonal():
 
 
 @pytest.mark.parametrize("precise", [False, True])
-def test_repeats_streams_and_graphs(precise):
+@pytest.mark.parametrize("shapes", [[(300, 900), (512, 64), (64, 64), (1100, 300)], [(100, 900), (513, 61), (64, 64)]])
+def test_repeats_streams_and_graphs(precise, shapes):
     from paper_2603_06492_gb300 import binding as B
-    t = _inputs([(300, 900), (512, 64), (64, 64), (1100, 300)], 11)
+    t = _inputs(shapes, 11)
     want = _run(t, lr=0.1, precise=precise)
     again = _run(t, lr=0.1, precise=precise)
     keys = ("param", "param_bf16", "momentum", "update")
