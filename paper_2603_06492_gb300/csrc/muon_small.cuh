@@ -4,16 +4,17 @@
 //
 // X stays in shared memory throughout, each block holding up to 256 of its columns; all matrices in
 // pairs (v = hi + lo).  One step:
-//   A   each block multiplies its columns (tcgen05, K = its columns), the partial sums go through
-//       distributed shared memory to the block that owns the columns of A, which adds them up in
-//       order of the blocks and sends A to all;
+//   A   each block multiplies its columns (tcgen05, K = its columns) and leaves its part of the sum in
+//       shared memory, where the block that owns the rows reads it (distributed shared memory).
+//       That one adds the parts up in order of the blocks and sends its rows of A to all;
 //   B = a I + b A + c A A   in every block, in place of A;
 //   X <- B X                each block its columns, in place.
 // A tile of 128 rows by 64 columns with the 128-byte swizzle is the operand along K of the first
 // product and the operand across K of the last one: the descriptors differ, the bytes do not.
+// Up to 64 rows, A and B have 64 rows and columns.
 //
-// What bounds it is the chain of its parts: 64 x 1024 takes about 7 us a step, of which the tensor core
-// works 2.
+// What bounds it is the chain of its parts.  Lanes next to each other exchange bytes next to each other: 16
+// bytes of one row per lane take three cycles a lane (sent as columns, 23000 of a step's 36000 cycles).
 #pragma once
 
 #include "muon_gemm.cuh"
@@ -23,10 +24,10 @@ namespace muon {
 namespace small {
 
 constexpr int kRows = 128, kBlocks = 8, kCols = 256;  // rows of X; blocks of a cluster, columns of a block at most
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr uint32_t kTile = kRows * 128;         // 128 rows of 64 columns
 constexpr uint32_t kLow = 4 * kTile;            // X: four tiles, and as many of low parts
-constexpr uint32_t kPoly = 8 * kTile;           // A, then B: two tiles, two of low parts
+constexpr uint32_t kPoly = 8 * kTile;           // parts of A in fp32, A, then B: two tiles, two of low parts
 constexpr uint32_t kBarOff = kPoly + 4 * kTile;
 constexpr uint32_t kBytes = kBarOff + 16, kDynamic = kBytes + 1024;
 
@@ -75,11 +76,14 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     uint8_t *smem = smem_raw + (sbase - raw);
     const uint32_t bar = sbase + kBarOff;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + kBarOff + 8);
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quarter = warp % 4, half = warp / 4;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quarter = warp % 4, group = warp / 4;
     const uint32_t rank = cluster::ctarank();
-    const int blocks = (int)cluster::nctarank(), own = kRows / blocks;  // columns of A that a block owns
+    const int blocks = (int)cluster::nctarank();
     const Matrix &M = g.b.t[blockIdx.x / blocks];
     const int cols = g.cols[blockIdx.x / blocks], c0 = (int)rank * cols;
+    const int side = M.m <= 64 ? 64 : 128, own = side / blocks;  // of A; rows that a block adds up
+    const int holders = (M.k + cols - 1) / cols;                 // blocks that have columns
+    const bool holds = (int)rank < holders;
 
     ptx::griddep_launch();
     if (tid == 0) {
@@ -94,7 +98,9 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = *tmem_slot, lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    const int row = quarter * 32 + lane;  // of a thread in every epilogue
+    // in every epilogue: a thread has this row and every fourth 32 columns
+    const int row = quarter * 32 + lane;
+    const bool rows = quarter * 32 < side;
 
     ptx::griddep_wait();
     // X: groups of eight columns that have elements, zeros elsewhere
@@ -141,36 +147,43 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     };
 
     for (int step = 0; step < g.steps; ++step) {
-        // ---- A
-        multiply(tmem, 0, kLow, 0, kLow, cols / 64, kRows, false);
-        cluster::sync();  // no block needs its B any more: parts of A go there, [block][row][own]
+        // ---- A: parts, a row's groups of four elements in an order that keeps lanes of one column on
+        // different banks
+        auto part = [&](int r, int four) { return kPoly + (uint32_t)(r * side + (four ^ (r & (side / 4 - 1))) * 4) * 4; };
+        if (holds) {
+            multiply(tmem, 0, kLow, 0, kLow, cols / 64, side, false);
+            if (rows && group < side / 32) {
+                float v[32];
+                ptx::tmem_ld_32x32b_x32(lanes + 32 * group, v);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            float v[32];
-            ptx::tmem_ld_32x32b_x32(lanes + 64 * half + 32 * c, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int col = 64 * half + 32 * c + 4 * j, to = col / own;
-                const uint32_t off = kPoly + ((rank * kRows + row) * own + col % own) * 4;
-                remote_store(cluster::map_to_rank(sbase + off, to), make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]),
-                                                                               __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3])));
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<float4 *>(smem + part(row, 8 * group + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
             }
         }
         cluster::sync();
-        // the columns that this block owns: two threads to a row, groups of eight (one, but for fewer blocks)
-        const int r = tid / 2, groups = own / 16;
-        uint4 hi[8], lo[8];
+        // own rows, in groups of eight elements
+        constexpr int kGroups = kRows * kRows / 8 / kThreads;
+        const int per_row = side / 8;
+        uint4 hi[kGroups], lo[kGroups];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (k >= groups) break;
-            const int col = 8 * (tid % 2 * groups + k);
+        for (int k = 0; k < kGroups; ++k) {
+            const int i = tid + kThreads * k, r = (int)rank * own + i / per_row, four = i % per_row * 2;
+            if (i >= own * per_row) break;
             float f[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[j] = 0.f;
-            for (int p = 0; p < blocks; ++p) {
-                const float4 *from = reinterpret_cast<const float4 *>(smem + kPoly + ((p * kRows + r) * own + col) * 4);
-                const float4 u = from[0], w = from[1];
-                f[0] += u.x, f[1] += u.y, f[2] += u.z, f[3] += u.w, f[4] += w.x, f[5] += w.y, f[6] += w.z, f[7] += w.w;
+            for (int p = 0; p < holders; p += 4) {
+                float4 u[4], w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    u[q] = w[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (p + q >= holders) continue;
+                    u[q] = cluster::ld4(cluster::map_to_rank(sbase + part(r, four), p + q));
+                    w[q] = cluster::ld4(cluster::map_to_rank(sbase + part(r, four + 1), p + q));
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    f[0] += u[q].x, f[1] += u[q].y, f[2] += u[q].z, f[3] += u[q].w, f[4] += w[q].x, f[5] += w[q].y, f[6] += w[q].z, f[7] += w[q].w;
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[j] *= kScaleA / (kScaleX * kScaleX);
@@ -178,10 +191,11 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         }
         cluster::sync();  // all parts are read
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (k >= groups) break;
-            const uint32_t off = kPoly + at(r, (int)rank * own + 8 * (tid % 2 * groups + k));
-            for (int p = 0; p < blocks; ++p) {
+        for (int k = 0; k < kGroups; ++k) {
+            const int i = tid + kThreads * k, r = (int)rank * own + i / per_row;
+            if (i >= own * per_row) break;
+            const uint32_t off = kPoly + at(r, i % per_row * 8);
+            for (int p = 0; p < holders; ++p) {
                 const uint32_t to = cluster::map_to_rank(sbase + off, p);
                 remote_store(to, hi[k]);
                 remote_store(to + 2 * kTile, lo[k]);
@@ -190,12 +204,12 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         // the tensor core of each block reads what all of them wrote: writes, fence, barrier, fence
         ptx::fence_proxy_async_smem_cluster();
         cluster::sync();
+        if (!holds) continue;
         // ---- B
-        multiply(tmem, kPoly, kPoly + 2 * kTile, kPoly, kPoly + 2 * kTile, 2, kRows, false);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        multiply(tmem, kPoly, kPoly + 2 * kTile, kPoly, kPoly + 2 * kTile, side / 64, side, false);
+        if (rows && group < side / 32) {
             float v[32];
-            const int col0 = 64 * half + 32 * c;
+            const int col0 = 32 * group;
             ptx::tmem_ld_32x32b_x32(lanes + col0, v);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -214,8 +228,8 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
             }
         }
         // ---- X
-        multiply(tmem + 128, kPoly, kPoly + 2 * kTile, 0, kLow, 2, cols, true);
-        for (int col0 = cols / 2 * half; col0 < cols / 2 * (half + 1); col0 += 32) {
+        multiply(tmem + 128, kPoly, kPoly + 2 * kTile, 0, kLow, side / 64, cols, true);
+        for (int col0 = 32 * group; rows && col0 < cols; col0 += 128) {
             float v[32];
             ptx::tmem_ld_32x32b_x32(lanes + 128 + col0, v);
 #pragma unroll
