@@ -6,7 +6,7 @@
 // pairs (v = hi + lo).  One step:
 //   A   each block multiplies its columns (tcgen05, K = its columns) and leaves its part of the sum in
 //       shared memory, where the block that owns the rows reads it (distributed shared memory).
-//       That one adds the parts up in order of the blocks and sends its rows of A to all;
+//       That one adds the parts up, its own first, in a fixed order and sends its rows of A to all;
 //   B = a I + b A + c A A   in every block, in place of A;
 //   X <- B X                each block its columns, in place.
 // A tile of 128 rows by 64 columns with the 128-byte swizzle is the operand along K of the first
@@ -41,9 +41,9 @@ struct Args {
 // A group of eight elements of a tile.
 __device__ __forceinline__ uint32_t at(int row, int col) { return (uint32_t)(col / 64) * kTile + row * 128 + ((((col % 64) / 8) ^ (row & 7)) << 4); }
 
-__device__ __forceinline__ void remote_store(uint32_t cluster_addr, const uint4 &v)
+__device__ __forceinline__ void remote_store(uint32_t cluster_addr, const uint2 &v)
 {
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y) : "memory");
 }
 
 // Eight values as halves; what is left of them stays in f.
@@ -58,6 +58,14 @@ __device__ __forceinline__ uint4 halves(float *f)
         f[2 * i] -= r.x, f[2 * i + 1] -= r.y;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Four values in pairs.
+__device__ __forceinline__ uint2 halves(float a, float b, float c, float d, uint2 *lo)
+{
+    const __half2 h = __floats2half2_rn(a, b), i = __floats2half2_rn(c, d);
+    const float2 r = __half22float2(h), s = __half22float2(i);
+    *lo = make_uint2(mma::pack_half(a - r.x, b - r.y), mma::pack_half(c - s.x, d - s.y));
+    return make_uint2(*reinterpret_cast<const uint32_t *>(&h), *reinterpret_cast<const uint32_t *>(&i));
 }
 __device__ __forceinline__ void add_eight(const uint4 &q, float scale, float *f)
 {
@@ -98,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = *tmem_slot, lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    // in every epilogue: a thread has this row and every fourth 32 columns
+    // in every epilogue: a thread has this row and a quarter of the columns
     const int row = quarter * 32 + lane;
     const bool rows = quarter * 32 < side;
 
@@ -124,13 +132,18 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         if (tid == 0 && ok) {
             ptx::tc_fence_after();
             const uint32_t idesc = mma::idesc_f16(kRows, n, across);
+            const uint64_t first = ptx::smem_desc_sw128(sbase, across ? kTile : 16, 1024), a_first = ptx::smem_desc_sw128(sbase, 16, 1024);
+            const uint32_t b_next = across ? 128 : 2, b_tile = across ? 512 : kTile / 16;  // descriptors count 16 bytes
+            uint32_t add = 0;
+#pragma unroll 1
             for (int seg = 0; seg < 3; ++seg) {
-                const uint32_t a = sbase + (seg == 0 ? p_lo : p), b = sbase + (seg == 1 ? q_lo : q);
-                for (int k = 0; k < 4 * chunks; ++k) {
-                    const uint64_t ad = ptx::smem_desc_sw128(a + k / 4 * kTile + k % 4 * 32, 16, 1024);
-                    const uint64_t bd = across ? ptx::smem_desc_sw128(b + k * 2048, kTile, 1024)
-                                               : ptx::smem_desc_sw128(b + k / 4 * kTile + k % 4 * 32, 16, 1024);
-                    ptx::mma_bf16(d, ad, bd, idesc, seg + k > 0 ? 1u : 0u);
+                uint64_t a = a_first + (seg == 0 ? p_lo : p) / 16, b = first + (seg == 1 ? q_lo : q) / 16;
+#pragma unroll 1
+                for (int i = 0; i < chunks; ++i, a += kTile / 16, b += b_tile) {
+                    ptx::mma_bf16(d, a, b, idesc, add);
+                    add = 1;
+#pragma unroll
+                    for (int k = 1; k < 4; ++k) ptx::mma_bf16(d, a + 2 * k, b + b_next * k, idesc, 1u);
                 }
             }
             ptx::mma_commit(bar);
@@ -152,53 +165,48 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         auto part = [&](int r, int four) { return kPoly + (uint32_t)(r * side + (four ^ (r & (side / 4 - 1))) * 4) * 4; };
         if (holds) {
             multiply(tmem, 0, kLow, 0, kLow, cols / 64, side, false);
-            if (rows && group < side / 32) {
-                float v[32];
-                ptx::tmem_ld_32x32b_x32(lanes + 32 * group, v);
+            for (int col0 = side / 4 * group; rows && col0 < side / 4 * (group + 1); col0 += 16) {
+                float v[16];
+                ptx::tmem_ld_32x32b_x16(lanes + col0, v);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<float4 *>(smem + part(row, 8 * group + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<float4 *>(smem + part(row, col0 / 4 + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
             }
         }
         cluster::sync();
-        // own rows, in groups of eight elements
-        constexpr int kGroups = kRows * kRows / 8 / kThreads;
-        const int per_row = side / 8;
-        uint4 hi[kGroups], lo[kGroups];
+        // own rows, in groups of four elements; each block begins with itself, so that not one is asked by all
+        constexpr int kGroups = kRows * kRows / 4 / kThreads;
+        const int per_row = side / 4;
+        uint2 hi[kGroups], lo[kGroups];
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
-            const int i = tid + kThreads * k, r = (int)rank * own + i / per_row, four = i % per_row * 2;
+            const int i = tid + kThreads * k;
             if (i >= own * per_row) break;
-            float f[8];
+            const uint32_t from = sbase + part((int)rank * own + i / per_row, i % per_row);
+            float4 u[kBlocks];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = 0.f;
-            for (int p = 0; p < holders; p += 4) {
-                float4 u[4], w[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    u[q] = w[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (p + q >= holders) continue;
-                    u[q] = cluster::ld4(cluster::map_to_rank(sbase + part(r, four), p + q));
-                    w[q] = cluster::ld4(cluster::map_to_rank(sbase + part(r, four + 1), p + q));
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    f[0] += u[q].x, f[1] += u[q].y, f[2] += u[q].z, f[3] += u[q].w, f[4] += w[q].x, f[5] += w[q].y, f[6] += w[q].z, f[7] += w[q].w;
+            for (int q = 0; q < kBlocks; ++q) {
+                const int p = ((int)rank + q) & (blocks - 1);
+                u[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (q < blocks && p < holders) u[q] = cluster::ld4(cluster::map_to_rank(from, p));
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] *= kScaleA / (kScaleX * kScaleX);
-            hi[k] = halves(f), lo[k] = halves(f);
+            for (int q = 1; q < kBlocks; ++q) u[0].x += u[q].x, u[0].y += u[q].y, u[0].z += u[q].z, u[0].w += u[q].w;
+            constexpr float f = kScaleA / (kScaleX * kScaleX);
+            hi[k] = halves(u[0].x * f, u[0].y * f, u[0].z * f, u[0].w * f, &lo[k]);
         }
         cluster::sync();  // all parts are read
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
-            const int i = tid + kThreads * k, r = (int)rank * own + i / per_row;
+            const int i = tid + kThreads * k, r = (int)rank * own + i / per_row, col = i % per_row * 4;
             if (i >= own * per_row) break;
-            const uint32_t off = kPoly + at(r, i % per_row * 8);
-            for (int p = 0; p < holders; ++p) {
-                const uint32_t to = cluster::map_to_rank(sbase + off, p);
-                remote_store(to, hi[k]);
-                remote_store(to + 2 * kTile, lo[k]);
+            const uint32_t to = sbase + kPoly + at(r, col) + col % 8 * 2;
+#pragma unroll
+            for (int q = 0; q < kBlocks; ++q) {
+                const int p = ((int)rank + q) & (blocks - 1);
+                if (q >= blocks || p >= holders) continue;
+                remote_store(cluster::map_to_rank(to, p), hi[k]);
+                remote_store(cluster::map_to_rank(to + 2 * kTile, p), lo[k]);
             }
         }
         // the tensor core of each block reads what all of them wrote: writes, fence, barrier, fence
@@ -207,12 +215,11 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         if (!holds) continue;
         // ---- B
         multiply(tmem, kPoly, kPoly + 2 * kTile, kPoly, kPoly + 2 * kTile, side / 64, side, false);
-        if (rows && group < side / 32) {
-            float v[32];
-            const int col0 = 32 * group;
-            ptx::tmem_ld_32x32b_x32(lanes + col0, v);
+        for (int col0 = side / 4 * group; rows && col0 < side / 4 * (group + 1); col0 += 16) {
+            float v[16];
+            ptx::tmem_ld_32x32b_x16(lanes + col0, v);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 2; ++q) {
                 float *f = v + 8 * q;
                 uint4 *h = reinterpret_cast<uint4 *>(smem + kPoly + at(row, col0 + 8 * q));
                 uint4 *l = reinterpret_cast<uint4 *>(smem + kPoly + 2 * kTile + at(row, col0 + 8 * q));
@@ -229,11 +236,11 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         }
         // ---- X
         multiply(tmem + 128, kPoly, kPoly + 2 * kTile, 0, kLow, side / 64, cols, true);
-        for (int col0 = 32 * group; rows && col0 < cols; col0 += 128) {
-            float v[32];
-            ptx::tmem_ld_32x32b_x32(lanes + 128 + col0, v);
+        for (int col0 = cols / 4 * group; rows && col0 < cols / 4 * (group + 1); col0 += 16) {
+            float v[16];
+            ptx::tmem_ld_32x32b_x16(lanes + 128 + col0, v);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 2; ++q) {
                 float *f = v + 8 * q;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] *= 1.f / kScaleB;
