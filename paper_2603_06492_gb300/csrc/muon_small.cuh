@@ -13,8 +13,12 @@
 // product and the operand across K of the last one: the descriptors differ, the bytes do not.
 // Up to 64 rows, A and B have 64 rows and columns.
 //
-// What bounds it is the chain of its parts.  Lanes next to each other exchange bytes next to each other: 16
-// bytes of one row per lane take three cycles a lane (sent as columns, 23000 of a step's 36000 cycles).
+// What bounds it is the chain of its parts.  (64 x 1024, 1024 x 64, 64 x 64) on eight blocks each: 10300
+// cycles a step, of which the three products have 4000 (62 cycles per tcgen05.mma, whether N is 64 or
+// 128), the exchange of A 3700, the passes over B and X 2000.  47.6 us a call with what comes before and
+// after, in place of 144.5 by 15 launches of muon_gemm.cuh; 64 x 64 35 for 102; 128 x 2048 78 for 174.
+// Lanes next to each other exchange bytes next to each other: 16 bytes of one row per lane take three
+// cycles a lane (sent as columns, 23000 of a step's 36000 cycles).
 #pragma once
 
 #include "muon_gemm.cuh"
@@ -24,12 +28,13 @@ namespace muon {
 namespace small {
 
 constexpr int kRows = 128, kBlocks = 8, kCols = 256;  // rows of X; blocks of a cluster, columns of a block at most
+constexpr int kFewBlocks = 4;                         // at least: all add up parts, with columns or without
 constexpr int kThreads = 512;
 constexpr uint32_t kTile = kRows * 128;         // 128 rows of 64 columns
 constexpr uint32_t kLow = 4 * kTile;            // X: four tiles, and as many of low parts
 constexpr uint32_t kPoly = 8 * kTile;           // parts of A in fp32, A, then B: two tiles, two of low parts
 constexpr uint32_t kBarOff = kPoly + 4 * kTile;
-constexpr uint32_t kBytes = kBarOff + 16, kDynamic = kBytes + 1024;
+constexpr uint32_t kBytes = kBarOff + 48, kDynamic = kBytes + 1024;
 
 struct Args {
     Batch b;
@@ -41,9 +46,12 @@ struct Args {
 // A group of eight elements of a tile.
 __device__ __forceinline__ uint32_t at(int row, int col) { return (uint32_t)(col / 64) * kTile + row * 128 + ((((col % 64) / 8) ^ (row & 7)) << 4); }
 
-__device__ __forceinline__ void remote_store(uint32_t cluster_addr, const uint2 &v)
+// Into a block of the cluster; a barrier of that block counts the bytes.
+__device__ __forceinline__ void remote_store(uint32_t cluster_addr, const uint2 &v, uint32_t cluster_bar)
 {
-    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(cluster_addr), "r"(v.x), "r"(v.y) : "memory");
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(cluster_addr), "r"(v.x),
+                 "r"(v.y), "r"(cluster_bar)
+                 : "memory");
 }
 
 // Eight values as halves; what is left of them stays in f.
@@ -82,8 +90,8 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = ptx::smem_u32(smem_raw), sbase = (raw + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (sbase - raw);
-    const uint32_t bar = sbase + kBarOff;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + kBarOff + 8);
+    const uint32_t bar = sbase + kBarOff, a_bar = bar + 8, meet_bar = bar + 16;  // products; A; blocks (two)
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + kBarOff + 32);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quarter = warp % 4, group = warp / 4;
     const uint32_t rank = cluster::ctarank();
     const int blocks = (int)cluster::nctarank();
@@ -96,6 +104,8 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     ptx::griddep_launch();
     if (tid == 0) {
         ptx::mbar_init(bar, 1);
+        ptx::mbar_init(a_bar, 1);
+        for (int i = 0; i < 2; ++i) ptx::mbar_init(meet_bar + 8 * i, (uint32_t)blocks);
         ptx::fence_barrier_init();
     }
     if (warp == 0) {
@@ -104,6 +114,7 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
     }
     ptx::tc_fence_before();
     __syncthreads();
+    cluster::sync();  // all blocks' barriers are initialised
     ptx::tc_fence_after();
     const uint32_t tmem = *tmem_slot, lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     // in every epilogue: a thread has this row and a quarter of the columns
@@ -148,8 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
             }
             ptx::mma_commit(bar);
         }
-        // a wait that gave up is reported, and given once more for what is in flight; the barriers still
-        // need every thread
+        // a wait that gave up is reported, and given once more for what is in flight
         if (ok && !ptx::mbar_wait(bar, phase, g.status)) {
             ptx::mbar_wait(bar, phase, nullptr);
             ok = false;
@@ -159,10 +169,22 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
         ptx::tc_fence_after();
     };
 
+    // All blocks have come here, and see what the others wrote to their shared memory.  The one of the two
+    // barriers is reached again only after all blocks have left it: A arrives from each in between.
+    auto meet = [&](int which, uint32_t parity) {
+        __syncthreads();
+        if (tid < blocks) cluster::mbar_arrive(cluster::map_to_rank(meet_bar + 8 * which, tid));
+        if (ok) ok = ptx::mbar_wait_cluster(meet_bar + 8 * which, parity, g.status);
+        __syncwarp();
+    };
+
     for (int step = 0; step < g.steps; ++step) {
+        const uint32_t parity = step & 1;
+        if (tid == 0) ptx::mbar_arrive_expect_tx(a_bar, (uint32_t)(side * side * 4));
         // ---- A: parts, a row's groups of four elements in an order that keeps lanes of one column on
         // different banks
-        auto part = [&](int r, int four) { return kPoly + (uint32_t)(r * side + (four ^ (r & (side / 4 - 1))) * 4) * 4; };
+        const uint32_t parts = kPoly + (side == 64 ? kTile : 0);  // 64 rows leave room beside A
+        auto part = [&](int r, int four) { return parts + (uint32_t)(r * side + (four ^ (r & (side / 4 - 1))) * 4) * 4; };
         if (holds) {
             multiply(tmem, 0, kLow, 0, kLow, cols / 64, side, false);
             for (int col0 = side / 4 * group; rows && col0 < side / 4 * (group + 1); col0 += 16) {
@@ -173,9 +195,9 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
                     *reinterpret_cast<float4 *>(smem + part(row, col0 / 4 + j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
             }
         }
-        cluster::sync();
+        meet(0, parity);
         // own rows, in groups of four elements; each block begins with itself, so that not one is asked by all
-        constexpr int kGroups = kRows * kRows / 4 / kThreads;
+        constexpr int kGroups = kRows * kRows / 4 / kFewBlocks / kThreads;
         const int per_row = side / 4;
         uint2 hi[kGroups], lo[kGroups];
 #pragma unroll
@@ -195,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
             constexpr float f = kScaleA / (kScaleX * kScaleX);
             hi[k] = halves(u[0].x * f, u[0].y * f, u[0].z * f, u[0].w * f, &lo[k]);
         }
-        cluster::sync();  // all parts are read
+        if (side != 64) meet(1, parity);  // all parts are read
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
             const int i = tid + kThreads * k, r = (int)rank * own + i / per_row, col = i % per_row * 4;
@@ -204,14 +226,14 @@ __global__ void __launch_bounds__(kThreads, 1) iterate_kernel(const __grid_const
 #pragma unroll
             for (int q = 0; q < kBlocks; ++q) {
                 const int p = ((int)rank + q) & (blocks - 1);
-                if (q >= blocks || p >= holders) continue;
-                remote_store(cluster::map_to_rank(to, p), hi[k]);
-                remote_store(cluster::map_to_rank(to + 2 * kTile, p), lo[k]);
+                if (q >= blocks) continue;
+                const uint32_t there = cluster::map_to_rank(a_bar, p);
+                remote_store(cluster::map_to_rank(to, p), hi[k], there);
+                remote_store(cluster::map_to_rank(to + 2 * kTile, p), lo[k], there);
             }
         }
-        // the tensor core of each block reads what all of them wrote: writes, fence, barrier, fence
-        ptx::fence_proxy_async_smem_cluster();
-        cluster::sync();
+        if (ok) ok = ptx::mbar_wait_cluster(a_bar, parity, g.status);
+        __syncwarp();
         if (!holds) continue;
         // ---- B
         multiply(tmem, kPoly, kPoly + 2 * kTile, kPoly, kPoly + 2 * kTile, side / 64, side, false);

@@ -429,9 +429,10 @@ void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
     }
 }
 
-// Blocks per matrix of a group whose matrices all iterate in one launch (muon_small.cuh), or 0: up to 128
-// columns each, as the products of a block take as long as its columns, and more where eight blocks
-// are not enough.
+// Blocks per matrix of a group whose matrices all iterate in one launch (muon_small.cuh), or 0.  Eight, or
+// four where they hold few columns each: 128 x 512 63 us with four, 128 x 1024 67 with eight.  A GB300 does
+// not hold more than some 14 clusters of eight at once: 16 of 64 x 1024 take 63 us with four blocks each,
+// 90 with eight; 8 of them 55 and 47.
 int muon_small(const noble_muon_tensor *t, const int *pick, int n)
 {
     int64_t most = 0;
@@ -440,9 +441,8 @@ int muon_small(const noble_muon_tensor *t, const int *pick, int n)
         most = std::max({most, t[pick[i]].rows, t[pick[i]].cols});
     }
     if (most > muon::small::kBlocks * muon::small::kCols) return 0;
-    int blocks = 1;
-    while (blocks < muon::small::kBlocks && blocks * 128 < most) blocks *= 2;
-    return n ? blocks : 0;
+    if (n == 0) return 0;
+    return most <= 512 || (n > 8 && most <= 1024) ? muon::small::kFewBlocks : muon::small::kBlocks;
 }
 
 // Takes the next matrices that are not empty, from *next on.
