@@ -347,8 +347,8 @@ int muon_tiles(const muon::mma::Problem &p, int bn)
     return p.sym ? muon::mma::sym_tiles_before(tm, tn, muon::mma::kRows / bn) : tm * tn;
 }
 // Times of a unit in k-blocks of a tile of 256 columns, 0.29 us, of its main loop and of its epilogue, which
-// runs beside the next unit's main loop.  One k-block of 128 columns takes 0.27 us, as both kinds wait for
-// L2.  Parts of a split K are stored, fenced and joined, which takes longer than most main loops:
+// runs beside the next unit's main loop.  That is the tensor pipe's rate; one k-block of 128 columns takes 0.27 us
+// all the same, for three quarters of the operands.  Parts of a split K are stored, fenced and joined, which takes longer than most main loops:
 // splits pay only while all units run at once (X X^T of 1024 x 4096, 76 pairs: 20 tiles of 128 columns whole, in 3
 // and in 4 parts 6, 0 and 5 us above the best; 2048 x 8192: 36 tiles of 256 columns whole and in 2 parts 7 and 0;
 // B X of 2048 x 8192, 256 tiles, whole and in 2 parts 0 and 70).
