@@ -109,13 +109,13 @@ struct BwdArgs {
     uint2 *joined;       // lists of several pieces: row, first of their sums
     float *part;         // [pieces of lists of several][d]
     int rows_per_warp, piece_blocks;  // of sum_kernel
-    int wide;            // dtable is aligned to 32 bytes
+    int wide, part_wide;  // dtable, part are aligned to 32 bytes: the interface asks for 16
 };
 
 // out = scale * (the sum of the n rows of dy that list names, first to last), the columns of vectors at,
-// at + 32, ..., C of them: B tokens' loads are on their way at once.
+// at + 32, ..., C of them: B tokens' loads are on their way at once.  wide: `out` is aligned to 32 bytes.
 template <int C, int B, typename T>
-__device__ __forceinline__ void sum_vectors(const BwdArgs<T> &a, const uint32_t *list, int n, int at, float *out, float scale)
+__device__ __forceinline__ void sum_vectors(const BwdArgs<T> &a, const uint32_t *list, int n, int at, float *out, float scale, bool wide)
 {
     constexpr int V = Vec<T>::n;
     const int vecs = a.d / V;
@@ -144,19 +144,20 @@ __device__ __forceinline__ void sum_vectors(const BwdArgs<T> &a, const uint32_t 
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (at + 32 * c < vecs) store_scaled(out + (at + 32 * c) * V, acc[c], scale, a.wide);
+        if (at + 32 * c < vecs) store_scaled(out + (at + 32 * c) * V, acc[c], scale, wide);
 }
-// ... of all vectors from `at` on that are `step` apart, but for the steps within a warp; n <= kShort.
+// ... of all vectors of a row of the table from `at` on that are `step` apart, but for the steps within a
+// warp; n <= kShort.
 template <typename T>
 __device__ __forceinline__ void sum_row(const BwdArgs<T> &a, const uint32_t *list, int n, int at, int step, float *out, float scale)
 {
     const int vecs = a.d / Vec<T>::n;
     if (step != 32) {
-        for (; at < vecs; at += step) sum_vectors<1, 8>(a, list, n, at, out, scale);
+        for (; at < vecs; at += step) sum_vectors<1, 8>(a, list, n, at, out, scale, a.wide);
     } else if (n <= 2) {
-        for (; at < vecs; at += 4 * 32) sum_vectors<4, 2>(a, list, n, at, out, scale);
+        for (; at < vecs; at += 4 * 32) sum_vectors<4, 2>(a, list, n, at, out, scale, a.wide);
     } else {
-        for (; at < vecs; at += 2 * 32) sum_vectors<2, 4>(a, list, n, at, out, scale);
+        for (; at < vecs; at += 2 * 32) sum_vectors<2, 4>(a, list, n, at, out, scale, a.wide);
     }
 }
 
@@ -505,8 +506,9 @@ __global__ void __launch_bounds__(256) sum_kernel(const BwdArgs<T> a)
             __syncwarp();
             for (int k = lane; k < n; k += 32) order[warp][k] = a.rank[begin + k];
             __syncwarp();
-            float *out = part == ~0u ? a.dtable + (int64_t)p.x * a.d : a.part + (int64_t)part * a.d;
-            if (at < vecs) sum_vectors<1, 8>(a, order[warp], n, at, out, part == ~0u ? a.scale : 1.f);
+            const bool whole = part == ~0u;
+            float *out = whole ? a.dtable + (int64_t)p.x * a.d : a.part + (int64_t)part * a.d;
+            if (at < vecs) sum_vectors<1, 8>(a, order[warp], n, at, out, whole ? a.scale : 1.f, whole ? a.wide : a.part_wide);
         }
         return;
     }

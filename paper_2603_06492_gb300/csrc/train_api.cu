@@ -246,6 +246,7 @@ noble_status embed_bwd(const noble_embed_desc *d, const int32_t *ids, const void
     a.head = at(w.head), a.count = at(w.count), a.begin = at(w.begin), a.rank = at(w.rank), a.list = at(w.list);
     a.long_row = at(w.long_row), a.piece_part = at(w.piece_part), a.joined = reinterpret_cast<uint2 *>(ws + w.joined);
     a.piece = reinterpret_cast<uint2 *>(ws + w.piece), a.part = reinterpret_cast<float *>(ws + w.part);
+    a.part_wide = reinterpret_cast<uintptr_t>(a.part) % 32 == 0;
     const KernelInfo index{"embed_index", kBoundHbm, 0.0, 0.0}, sum{"embed_sum", kBoundHbm, 0.0, in + out};
     const auto launch = [&](const KernelInfo &ki, auto kern, dim3 grid, size_t smem, unsigned threads = 256) {
         const bool pdl = pdl_ok();
