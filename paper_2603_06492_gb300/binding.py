@@ -406,11 +406,14 @@ def noble_muon_step(tensors, lr, momentum=0.95, weight_decay=0.0, nesterov=True,
     """One optimizer step by orthogonalised momentum.  ``tensors``: dicts with grad and
     momentum, and param (with optional param_bf16) or update or both -- contiguous device
     matrices of one shape, fp32 but for param_bf16 and update in bf16 --, optional lr_mult
-    (default 1) and decay (default True).  ``workspace``: of muon_workspace; a new one if None."""
+    (default 1) and decay (default True).  ``workspace``: of muon_workspace; a new one of ``stream``'s if None."""
     import torch
     arr = _muon_array(tensors)
     if workspace is None:
-        workspace = muon_workspace(tensors, precise)
+        # of the memory of the stream that uses it: it is given back on return, and memory of another
+        # stream could be that stream's again before the step has run, or be its own still
+        with torch.cuda.stream(stream):
+            workspace = muon_workspace(tensors, precise)
     if not workspace.is_cuda or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace: expected one of muon_workspace")
     for t in tensors[:1]:
