@@ -197,7 +197,8 @@ __device__ __forceinline__ void each_element(const Matrix &M, int r0, int c0, F 
     }
 }
 
-// kScaleX / (|u| + eps) as a power of two and the rest: fp32 need not hold it.
+// kScaleX / (|u| + eps) as a power of two and the rest: fp32 need not hold it.  NaN where u is not finite,
+// an infinite norm among them: times 0 the finite elements would look like a result.
 __device__ __forceinline__ float2 inverse_norm(const Matrix &M, float eps)
 {
     __shared__ double sm[8];
@@ -213,7 +214,7 @@ __device__ __forceinline__ float2 inverse_norm(const Matrix &M, float eps)
         s = 0.0;
         for (int w = 0; w < 8; ++w) s += sm[w];
         const double norm = sqrt(s) + (double)eps;
-        const double f = norm > 0.0 || norm != norm ? (double)kScaleX / norm : 0.0;
+        const double f = !isfinite(norm) ? (double)NAN : norm > 0.0 ? (double)kScaleX / norm : 0.0;
         const int e = f > 0.0 ? max(-126, min(126, ilogb(f))) : 0;
         inv = make_float2(ldexpf(1.f, e), (float)ldexp(f, -e));
     }
