@@ -93,12 +93,17 @@ class Stack:
     residual stream, each half reads a layer norm of it and adds its output.
 
     ``params`` of its calls: ``{"table": [vocab, d_model], "norms": [{"gain", "bias"}, ...], "blocks":
-    [...]}``, with a norm more than blocks, and the blocks' as for ``AttentionBlock``."""
+    [...]}``, with a norm more than blocks, and the blocks' as for ``AttentionBlock``.  Its options go to
+    every half; all of them share one table of rotations, ``table`` if given."""
 
     def __init__(self, vocab, blocks, d_model, *heads, dtype="bf16", scale=1.0, eps=1e-5, **options):
         self.vocab, self.d_model, self.dtype, self.scale, self.eps = vocab, d_model, dtype, scale, eps
-        self.blocks = [AttentionBlock(d_model, *heads, dtype=dtype, **options)]
-        self.blocks += [AttentionBlock(d_model, *heads, dtype=dtype, table=self.blocks[0].table, **options) for _ in range(blocks - 1)]
+        if blocks < 0:
+            raise ValueError(f"{blocks} blocks")
+        self.blocks = []
+        for _ in range(blocks):
+            self.blocks.append(AttentionBlock(d_model, *heads, dtype=dtype, **options))
+            options["table"] = self.blocks[0].table
 
     def _ends(self, T, with_grads):
         norm = dict(dtype=self.dtype, eps=self.eps, with_grads=with_grads)
