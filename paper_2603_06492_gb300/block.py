@@ -159,30 +159,51 @@ class Stack:
 class Update:
     """Optimizer of a Stack's parameters: orthogonalised momentum for the matrices of its
     projections, AdamW for everything else.  Keeps fp32 parameters and moments; the operands that
-    the layers read (bf16, or the parameters themselves in fp32) are written in the same pass."""
+    the layers read (bf16, or the parameters themselves in fp32) are written in the same pass.
+
+    ``multipliers``: arguments of ``binding.noble_linear_lr_multipliers``, whose rule then sets the
+    learning rates of each projection's groups beside ``lr`` and ``lr_matrices``; ``{}`` are the paper's
+    values (W_up, M, omega and phi train faster).  The paper has them for AdamW alone: ``gamma=0, gamma_M=0``
+    leave W_up and M, whose steps are orthogonal here, at 1.  None: every multiplier is 1.
+
+    ``precise``: 22 bits in the products of large matrices; without, their changes are about 1e-3 of
+    their norm off, in fp32 parameters too (noble_muon_step)."""
 
     _MATRICES = {"W", "W_down", "W_up", "M"}
     _GRADS = {"W": "dW", "bias": "dbias", "W_down": "dW_down", "W_up": "dW_up", "M": "dM", "omega1": "domega1", "phi1": "dphi1",
               "omega2": "domega2", "phi2": "dphi2"}
 
-    def __init__(self, params, grads, precise=False):
+    def __init__(self, params, grads, precise=False, multipliers=None):
         self.steps, self.precise, self.muon, self.adamw = 0, precise, [], []
-        for matrix, p, g in self._leaves(params, grads):
+        for matrix, p, g, mult in self._leaves(params, grads, multipliers):
             fp32 = p.dtype is torch.float32
-            t = {"param": p if fp32 else p.float(), "param_bf16": None if fp32 else p, "grad": g, "decay": p.dim() == 2}
+            t = {"param": p if fp32 else p.float(), "param_bf16": None if fp32 else p, "grad": g, "decay": p.dim() == 2,
+                 "lr_mult": mult}
             moments = ("momentum",) if matrix else ("exp_avg", "exp_avg_sq")
             t.update({k: torch.zeros_like(t["param"]) for k in moments})
             (self.muon if matrix else self.adamw).append(t)
         self.workspace = B.muon_workspace(self.muon, precise)
 
-    def _leaves(self, params, grads):
-        yield False, params["table"], grads["table"]
+    @staticmethod
+    def _rates(p, multipliers):
+        """Learning-rate multipliers of a projection's parameters that are not 1."""
+        if multipliers is None or p.get("W_down") is None:
+            return {}
+        (d_out, d_in), r = p["W"].shape, len(p["W_down"])
+        dtype = "fp32" if p["W"].dtype is torch.float32 else "bf16"
+        _, up, m, omega, phi = B.noble_linear_lr_multipliers(B.make_desc(1, d_in, d_out, r, dtype), **multipliers)
+        return {"W_up": up, "M": m, "omega1": omega, "omega2": omega, "phi1": phi, "phi2": phi}
+
+    def _leaves(self, params, grads, multipliers):
+        yield False, params["table"], grads["table"], 1.0
         for p, g in zip(params["norms"], grads["norms"]):
-            yield from ((False, p[k], g[k]) for k in ("gain", "bias"))
+            yield from ((False, p[k], g[k], 1.0) for k in ("gain", "bias"))
         for p, g in zip(params["blocks"], grads["blocks"]):
-            yield from ((False, p[k], g[k]) for k in ("gain_q", "gain_k") if p.get(k) is not None and k in g)
+            yield from ((False, p[k], g[k], 1.0) for k in ("gain_q", "gain_k") if p.get(k) is not None and k in g)
             for name in ("qkv", "out"):
-                yield from ((k in self._MATRICES, p[name][k], g[name][d]) for k, d in self._GRADS.items() if p[name].get(k) is not None)
+                rates = self._rates(p[name], multipliers)
+                yield from ((k in self._MATRICES, p[name][k], g[name][d], rates.get(k, 1.0)) for k, d in self._GRADS.items()
+                            if p[name].get(k) is not None)
 
     def step(self, lr, lr_matrices, weight_decay=0.01):
         """One step from the gradients that the Stack's buffers hold."""
