@@ -159,3 +159,37 @@ def test_update_of_a_stack():
     for t, want, room in zip(u.muon, p, off):
         assert (t["param"].double() - want).norm() <= room
         assert torch.equal(t["param_bf16"], t["param"].bfloat16())
+
+
+@pytest.mark.parametrize("precise", [False, True])
+@pytest.mark.parametrize("shape", [(1, 65536), (65536, 3), (200, 65536), (65536, 257)])
+def test_longest_sums(shape, precise):
+    from paper_2603_06492_gb300 import binding as B
+    t = _tensors([shape], 8)[0]
+    want = _iterate(t["grad"].double() + 0.95 * (0.95 * t["momentum"].double() + t["grad"].double()))
+    rel = _tolerance(t["grad"].double() + 0.95 * (0.95 * t["momentum"].double() + t["grad"].double()), want, precise)
+    t["param"].zero_()
+    B.noble_muon_step([t], lr=1.0, precise=precise)
+    torch.cuda.synchronize()
+    B.noble_get_device_status(None)
+    off = -t["param"].double() / math.sqrt(max(1.0, shape[0] / shape[1])) - want
+    assert off.norm() <= rel * want.norm() and off.abs().max() <= 16 * rel * want.abs().max(), (off.norm() / want.norm(), rel)
+
+
+def test_two_calls_at_once():
+    # on streams and workspaces of their own: what one holds of the device, the other waits for
+    from paper_2603_06492_gb300 import binding as B
+    groups = [_tensors(s, 9) for s in ([(64, 1024), (100, 90)], [(1024, 2048), (64, 1024)], [(1500, 1600)])]
+    copies = lambda: [[{k: v.clone() for k, v in t.items()} for t in g] for g in groups]  # noqa: E731
+    want = copies()
+    for g in want:
+        B.noble_muon_step(g, 0.1)
+    streams, work = [torch.cuda.Stream() for _ in groups], [B.muon_workspace(g) for g in groups]
+    for _ in range(10):
+        got = copies()
+        torch.cuda.synchronize()
+        for g, s, w in zip(got, streams, work):
+            B.noble_muon_step(g, 0.1, workspace=w, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[k], b[k]) for x, y in zip(got, want) for a, b in zip(x, y) for k in a)
+    B.noble_get_device_status(None)
