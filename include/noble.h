@@ -664,7 +664,7 @@ noble_status noble_embed_bwd(const noble_embed_desc *desc, const int32_t *ids, c
  * Products take fp16 operands, scaled, with fp32 sums: X is off by about 1e-3 of its norm
  * when u's singular values are of one order, more when they decay fast (1e-2 over six orders).
  * With NOBLE_MUON_PRECISE operands have 22 bits, in pairs of fp16: three times the
- * products, and 3e-5 of the norm in place of 1e-3.  Matrices of up to 256 rows or columns
+ * products, and up to 4e-5 of the norm in place of 1e-3.  Matrices of up to 256 rows or columns
  * always have them.  Everything else is fp32, the norm fp64.
  *
  * `param_bf16` (optional) receives the new parameters and `update` (optional) X, in bf16.  With

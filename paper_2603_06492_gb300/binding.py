@@ -406,7 +406,8 @@ def noble_muon_step(tensors, lr, momentum=0.95, weight_decay=0.0, nesterov=True,
     """One optimizer step by orthogonalised momentum.  ``tensors``: dicts with grad and
     momentum, and param (with optional param_bf16) or update or both -- contiguous device
     matrices of one shape, fp32 but for param_bf16 and update in bf16 --, optional lr_mult
-    (default 1) and decay (default True).  ``workspace``: of muon_workspace; a new one of ``stream``'s if None."""
+    (default 1) and decay (default True).  ``precise``: products of 22 bits; without, those of
+    matrices above 256 have 11 and the update is about 1e-3 of its norm off.  ``workspace``: of muon_workspace; a new one of ``stream``'s if None."""
     import torch
     arr = _muon_array(tensors)
     if workspace is None:

@@ -376,7 +376,8 @@ __device__ __forceinline__ void place_tokens(const BwdArgs<T> &a, int64_t thread
 // Long lists in ascending order, a list to a block at a time; `rank`, which nothing needs any more,
 // takes them.  Up to kCompared tokens each token's place is the number of smaller ones; beyond,
 // a bit is set for each token and the bits are read off again word by word, the tokens of a window
-// before those of the next.
+// before those of the next.  Each window goes over the whole list: one row with all of 2^20 tokens takes 2.2 ms, with
+// 2^24 225; 2^24 tokens spread over 100 rows 9 ms.
 template <typename T>
 __global__ void __launch_bounds__(256) order_kernel(const BwdArgs<T> a)
 {

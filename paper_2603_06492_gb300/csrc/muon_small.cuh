@@ -15,8 +15,8 @@
 //
 // What bounds it is the chain of its parts.  (64 x 1024, 1024 x 64, 64 x 64) on eight blocks each: 10300
 // cycles a step, of which the three products have 4000 (62 cycles per tcgen05.mma, whether N is 64 or
-// 128), the exchange of A 3700, the passes over B and X 2000.  47.6 us a call with what comes before and
-// after, in place of 144.5 by 15 launches of muon_gemm.cuh; 64 x 64 35 for 102; 128 x 2048 78 for 174.
+// 128), the exchange of A 3700, the passes over B and X 2000.  A whole call in a captured graph takes 40 us
+// in place of 120 by 15 launches of muon_gemm.cuh; 64 x 64 33 for 86; 128 x 2048 74 for 158.
 // Lanes next to each other exchange bytes next to each other: 16 bytes of one row per lane take three
 // cycles a lane (sent as columns, 23000 of a step's 36000 cycles).
 #pragma once

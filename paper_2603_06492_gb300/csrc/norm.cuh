@@ -231,7 +231,9 @@ struct BwdArgs {
 // Block p takes the rows of part p, R groups' of them at a time.  A thread has the same columns of
 // every row, whose sums for dgain and dbias it keeps in registers and the block then adds up in
 // order of the groups.  R: rows of a group side by side, for narrow rows, whose chain of loads, sums
-// over the row and stores is longer than their work.  WARPS: 15 or, where a row takes more, 16.
+// over the row and stores is longer than their work.  WARPS: 15 or, where a row takes more, 16, which leave 96
+// registers to a thread: wide rows spill, most of them beyond 8192 columns (4096 rows of bf16: 7680 columns 59 us, 8192
+// 64, 8200 166; 2048 of 16384 132).
 template <typename T, int NV, bool STREAM, int WARPS>
 __global__ void __launch_bounds__(32 * (WARPS + 1), 1) bwd_kernel(const BwdArgs<T> a)
 {

@@ -107,7 +107,8 @@ noble_status norm_fwd(const noble_norm_desc *d, const void *x, const void *res, 
 }
 
 // Rows of a part of the sums for dgain and dbias: a block per SM, and at most 512, so that sums of
-// like rows stay short.
+// like rows stay short.  Beyond 77824 rows the blocks are more than the SMs, and a last round that is not full costs
+// as much as a full one (rows of 768: 77824 in 68 us, 5.3 TB/s; 98304 in 122, 131072 in 123, 160000 in 176).
 int norm_rows_per_part(const noble_norm_desc *d)
 {
     return (int)std::max<int64_t>(1, std::min<int64_t>(512, ceil_div(d->T, kSms)));
@@ -314,7 +315,10 @@ noble_status check_apart(const noble_muon_tensor *t, int n)
     return NOBLE_OK;
 }
 
-// Small matrices cost launches, not products, and the error of a small X is not averaged.
+// Small matrices cost launches, not products, and the error of a small X is not averaged: pairs without being
+// asked.  That costs nothing up to 128 rows and 2048 columns, which iterate in one launch (128 x 2048 78 us, without
+// pairs by launches 129), and most from there on: 129 x 2048 182 us (without 136), 256 x 1024 183 (129); 300 x 1024,
+// not in pairs, takes 130.
 bool muon_precise(const noble_muon_tensor &t, uint32_t flags)
 {
     return (flags & NOBLE_MUON_PRECISE) != 0 || std::min(t.rows, t.cols) <= 256;
@@ -431,9 +435,9 @@ void muon_cut(muon::mma::Problem *p, int *order, int n, int *units)
 }
 
 // Blocks per matrix of a group whose matrices all iterate in one launch (muon_small.cuh), or 0.  Eight, or
-// four where they hold few columns each: 128 x 512 63 us with four, 128 x 1024 67 with eight.  A GB300 does
-// not hold more than some 14 clusters of eight at once: 16 of 64 x 1024 take 63 us with four blocks each,
-// 90 with eight; 8 of them 55 and 47.
+// four where they hold few columns each: 128 x 1024 62 us a call in a graph with eight and 72 with four, 128 x 512
+// 58 and 60, 64 x 64 35 and 33.  A GB300 does not hold more than some 14 clusters of eight at once: 16 of 64 x 1024
+// take 54 us with four blocks each, 73 with eight; 8 of them 52 and 43.
 int muon_small(const noble_muon_tensor *t, const int *pick, int n)
 {
     int64_t most = 0;
