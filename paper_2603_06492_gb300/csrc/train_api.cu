@@ -107,8 +107,9 @@ noble_status norm_fwd(const noble_norm_desc *d, const void *x, const void *res, 
 }
 
 // Rows of a part of the sums for dgain and dbias: a block per SM, and at most 512, so that sums of
-// like rows stay short.  Beyond 77824 rows the blocks are more than the SMs, and a last round that is not full costs
-// as much as a full one (rows of 768: 77824 in 68 us, 5.3 TB/s; 98304 in 122, 131072 in 123, 160000 in 176).
+// like rows stay short.  Beyond 77824 rows the blocks are more than the SMs, and whole parts in a last round that they do
+// not fill cost as much as a full one (rows of 768: 77824, and one more, in 68 us, 5.3 TB/s; 98304 in 122, 131072 in 123,
+// 160000 in 176).
 int norm_rows_per_part(const noble_norm_desc *d)
 {
     return (int)std::max<int64_t>(1, std::min<int64_t>(512, ceil_div(d->T, kSms)));
